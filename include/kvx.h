@@ -389,6 +389,127 @@ KVX_API int64_t kvx_fit_tokens(const kvx_fitter* f);
 /* Free the fitter.  Synchronises the device first.  NULL is accepted. */
 KVX_API kvx_status kvx_fit_destroy(kvx_fitter* f);
 
+/* ------------------------------------------------------------------------------------------
+ * Going on from a cache.  In the paper's handoff (Section 6.1) the frozen target model decodes
+ * from the translated state.  These entry points are the steps of that decoding that touch the
+ * cache, one target layer at a time: the new tokens' queries and keys are rotated and their keys
+ * and values written into the cache (kvx_append), the new tokens attend to everything cached
+ * (kvx_attend, which can also sum the attention weight that each cached token receives), and a
+ * cache that has grown too long is cut down to the tokens that received the most (kvx_evict).
+ * Caches are described as for kvx_translate: contiguous, or paged pools with a page table. */
+typedef struct kvx_decoder kvx_decoder;
+
+typedef struct {
+    kvx_model_geom model;       /* the model whose cache this is: KV heads, head_dim, RoPE schedule */
+    int32_t num_q_heads;        /* query heads: a multiple of model.num_kv_heads, at most 64 for each; query
+                                   head g reads KV head g / (num_q_heads / num_kv_heads) */
+    int32_t dtype;              /* kvx_dtype of queries, keys, values, caches and outputs */
+    int32_t max_position;       /* as in kvx_translator_desc */
+    double  scale;              /* factor of q.k; 0 = 1 / sqrt(head_dim); else finite and > 0 */
+    double  score_cap;          /* c > 0: a scaled score s becomes c * tanh(s / c); 0 = no cap */
+} kvx_decoder_desc;
+
+/* Checks the description and allocates what the calls below need on the current device: rotation
+ * frequencies, a status word and the workspace of split attention (a few tens of MB whatever the
+ * lengths).  Synchronous.  On success *out owns device memory until kvx_decoder_destroy. */
+KVX_API kvx_status kvx_decoder_create(const kvx_decoder_desc* desc, kvx_decoder** out);
+
+/* Free the decoder's device memory.  Synchronises the device first.  NULL is accepted. */
+KVX_API kvx_status kvx_decoder_destroy(kvx_decoder* dec);
+
+/* Rows of a token's heads: element (t, head, c) at t*stride_t + head*stride_h + c, channels
+ * contiguous; 16-byte aligned, strides in elements, multiples of 8 (bf16) / 4 (fp32).  A slice of
+ * a fused projection's output is such a view. */
+typedef struct {
+    void* ptr;
+    int64_t stride_t, stride_h;
+} kvx_rows;
+
+/* The new tokens of a call, packed: sequence b owns packed indices [seq_off[b], seq_off[b+1]), n_b
+ * of them (0 is allowed).  kv_len[b] counts the cached tokens of sequence b with its new ones
+ * among them: new token i takes slot kv_len[b] - n_b + i. */
+typedef struct {
+    int32_t batch;
+    int32_t total_tokens;       /* seq_off[batch] (host copy, sizes the launch) */
+    const int32_t* seq_off;     /* device int32[batch+1], seq_off[0] = 0, non-decreasing */
+    const int32_t* kv_len;      /* device int32[batch], at most the cache's capacity per sequence (longer
+                                   lengths are clamped and flagged KVX_DEV_SEQ_CLAMPED) */
+    const int32_t* pos;         /* kvx_append: device int32[total_tokens], RoPE position of each new token,
+                                   or NULL for its slot */
+} kvx_new_tokens;
+
+/* Write the new tokens into layer `layer` of the cache: K rows k rotated at their positions, V rows v
+ * as they are; q_out receives the queries rotated alike (q_out may be q: in place).
+ * q, q_out: num_q_heads rows a token; k, v: model.num_kv_heads.  Rows whose slot lies outside the
+ * cache or in an unlisted page are skipped and flagged; q is rotated for every token.
+ * Asynchronous on stream; allocates nothing. */
+KVX_API kvx_status kvx_append(kvx_decoder* dec, const kvx_new_tokens* tok, const kvx_rows* q, const kvx_rows* k,
+                              const kvx_rows* v, const kvx_rows* q_out, const kvx_dst_kv* cache, int32_t layer,
+                              void* stream);
+
+/* Options of one kvx_attend call; all zero is plain causal attention. */
+typedef struct {
+    int32_t window;             /* 0 = none; w > 0: the new token in slot i sees slots i-w+1 .. i */
+    const int32_t* prefix_len;  /* device int32[batch] or NULL: the first prefix_len[b] slots are seen by every
+                                   new token of sequence b, whatever the window and the causal order */
+    float* lse;                 /* device float[total_tokens][num_q_heads] or NULL: log of the sum of
+                                   exponentials of the seen scores, -infinity where none is seen */
+    float* key_weight;          /* device float[batch][num_kv_heads][weight_stride] or NULL: element (b, h, j) has
+                                   added to it the attention weights slot j receives in this call, summed over
+                                   sequence b's new tokens and KV head h's query heads.  Needs lse. */
+    int64_t weight_stride;      /* slots a row of key_weight holds, at least every kv_len (slots past it are
+                                   not summed) */
+} kvx_attend_opts;
+
+/* Attention of the new tokens over the cache (their own rows included: append first).  For new
+ * token i of sequence b in slot s_i, query head g and its KV head h:
+ *   x_j = cap(scale * q_{i,g} . K_h[j]),  out_{i,g} = sum_j softmax_j(x) V_h[j]
+ * over the seen slots j < kv_len[b]: j <= s_i and (no window or s_i - j < window), or
+ * j < prefix_len[b].  A token that sees no slot (s_i < 0 and no prefix) gets a zero row.  Scores, sums and
+ * the output's accumulation are fp32 (bf16 caches: attention weights are rounded to bf16 before
+ * they multiply V, 8 bits as V has); rows no new token sees are never part of a result, whatever
+ * they hold.  Page-table entries outside the pool read as zero rows and are flagged.
+ * The sums behind every output are taken in an order that depends on sizes alone: equal calls
+ * give equal bits.  At most 1024 sequences a call (KVX_ERR_UNSUPPORTED).
+ * Asynchronous on stream; allocates nothing.  Calls on one decoder share its workspace: issue them on
+ * one stream, or order them (events). */
+KVX_API kvx_status kvx_attend(kvx_decoder* dec, const kvx_new_tokens* tok, const kvx_rows* q, const kvx_dst_kv* cache,
+                              int32_t layer, const kvx_attend_opts* opts, const kvx_rows* out, void* stream);
+
+/* What kvx_evict keeps, and where it says so.  L = num_layers, H = model.num_kv_heads. */
+typedef struct {
+    int32_t batch;
+    int32_t num_layers;         /* layers cut down in this call: cache layers 0 .. num_layers-1, at most
+                                   KVX_MAX_TARGET_LAYERS */
+    const int32_t* kv_len;      /* device int32[batch]: cached tokens of each sequence */
+    const float* key_weight;    /* device float[L][batch][H][weight_stride]: weight of each slot */
+    int64_t weight_stride;      /* at least every kv_len (longer lengths are clamped and flagged) */
+    int32_t keep;               /* slots a sequence may keep, >= 1; shorter sequences keep every slot */
+    int32_t sinks, recent;      /* of them the first `sinks` and the last `recent` in any case; sinks + recent <= keep */
+    int32_t* kept;              /* device int32[L][batch][H][keep]: the slots kept, ascending, then -1 */
+    int32_t* new_len;           /* device int32[batch]: min(kv_len, keep) */
+    float* kept_weight;         /* device float[L][batch][H][kept_weight_stride] or NULL: the kept slots'
+                                   weights, then zeros up to the stride */
+    int64_t kept_weight_stride; /* >= keep */
+} kvx_evict_plan;
+
+/* Cut a cache down by accumulated attention weight.  Per layer, sequence and KV head the first
+ * `sinks` slots, the last `recent` and, of the others, those of the largest key_weight (ties go to
+ * the lowest slot; NaN ranks lowest) keep their K and V rows: row kept[r] of src becomes row r of
+ * dst.  The order of the tokens stays, so slots still ascend by position, but heads keep different
+ * tokens: give kvx_append the true positions from then on, and use windows only on caches that
+ * were not cut.  dst must not overlap src (pages shared with other sequences stay intact); both
+ * have the same pool or contiguous layout rules as above, each its own page table.
+ * Asynchronous on stream; allocates nothing. */
+KVX_API kvx_status kvx_evict(kvx_decoder* dec, const kvx_evict_plan* plan, const kvx_dst_kv* src,
+                             const kvx_dst_kv* dst, void* stream);
+
+/* As kvx_get_device_status, for a decoder (KVX_DEV_* bits of its calls). */
+KVX_API kvx_status kvx_decoder_status(kvx_decoder* dec, void* stream, uint32_t* bits, int32_t clear);
+
+/* Kernel launches the most recent kvx_append, kvx_attend or kvx_evict on this decoder made. */
+KVX_API int32_t kvx_decoder_launches(const kvx_decoder* dec);
+
 /* Size of the device scratch array kvx_translate_static works in (8 MiB). */
 #define KVX_STATIC_SCRATCH_BYTES (8u << 20)
 

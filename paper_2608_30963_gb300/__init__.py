@@ -85,6 +85,32 @@ class kvx_dst_kv(ctypes.Structure):
                 ("num_pages", ctypes.c_int32)]
 
 
+class kvx_decoder_desc(ctypes.Structure):
+    _fields_ = [("model", kvx_model_geom), ("num_q_heads", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("max_position", ctypes.c_int32), ("scale", ctypes.c_double), ("score_cap", ctypes.c_double)]
+
+
+class kvx_rows(ctypes.Structure):
+    _fields_ = [("ptr", VP), ("stride_t", ctypes.c_int64), ("stride_h", ctypes.c_int64)]
+
+
+class kvx_new_tokens(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("total_tokens", ctypes.c_int32), ("seq_off", VP), ("kv_len", VP),
+                ("pos", VP)]
+
+
+class kvx_attend_opts(ctypes.Structure):
+    _fields_ = [("window", ctypes.c_int32), ("prefix_len", VP), ("lse", VP), ("key_weight", VP),
+                ("weight_stride", ctypes.c_int64)]
+
+
+class kvx_evict_plan(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("num_layers", ctypes.c_int32), ("kv_len", VP), ("key_weight", VP),
+                ("weight_stride", ctypes.c_int64), ("keep", ctypes.c_int32), ("sinks", ctypes.c_int32),
+                ("recent", ctypes.c_int32), ("kept", VP), ("new_len", VP), ("kept_weight", VP),
+                ("kept_weight_stride", ctypes.c_int64)]
+
+
 class kvx_translator_info(ctypes.Structure):
     _fields_ = [("path", ctypes.c_int32), ("group_in", ctypes.c_int32), ("n_tile", ctypes.c_int32),
                 ("smem_bytes", ctypes.c_int32), ("threads", ctypes.c_int32), ("num_sms", ctypes.c_int32),
@@ -95,7 +121,8 @@ EXPORTS = ["kvx_translator_create", "kvx_translator_create_low_rank", "kvx_trans
            "kvx_fit_accumulate", "kvx_fit_solve", "kvx_fit_reset", "kvx_fit_tokens", "kvx_fit_destroy", "kvx_build_alignment", "kvx_layer_map_nearest",
            "kvx_get_device_status", "kvx_get_info", "kvx_launches_per_translate", "kvx_last_error",
            "kvx_destroy", "kvx_translate_static", "kvx_static_last_error", "kvx_span_plan_stats",
-           "kvx_enable_peer", "kvx_translate_to_device", "kvx_debug_stall_next_translate"]
+           "kvx_enable_peer", "kvx_translate_to_device", "kvx_debug_stall_next_translate", "kvx_decoder_create",
+           "kvx_decoder_destroy", "kvx_append", "kvx_attend", "kvx_evict", "kvx_decoder_status", "kvx_decoder_launches"]
 KVX_PEER_STORES, KVX_PEER_STAGED = 0, 1
 KVX_STATIC_SCRATCH_BYTES = 8 << 20
 
@@ -158,9 +185,19 @@ def lib():
         L.kvx_translate_to_device.argtypes = [VP, ctypes.POINTER(kvx_src_kv), ctypes.POINTER(kvx_tgt_tokens),
                                               ctypes.POINTER(kvx_dst_kv), ctypes.c_int32, ctypes.c_int32,
                                               ctypes.POINTER(kvx_dst_kv), VP]
+        L.kvx_decoder_create.argtypes = [ctypes.POINTER(kvx_decoder_desc), ctypes.POINTER(VP)]
+        L.kvx_decoder_destroy.argtypes = [VP]
+        rows, cache = ctypes.POINTER(kvx_rows), ctypes.POINTER(kvx_dst_kv)
+        L.kvx_append.argtypes = [VP, ctypes.POINTER(kvx_new_tokens), rows, rows, rows, rows, cache, ctypes.c_int32, VP]
+        L.kvx_attend.argtypes = [VP, ctypes.POINTER(kvx_new_tokens), rows, cache, ctypes.c_int32,
+                                 ctypes.POINTER(kvx_attend_opts), rows, VP]
+        L.kvx_evict.argtypes = [VP, ctypes.POINTER(kvx_evict_plan), cache, cache, VP]
+        L.kvx_decoder_status.argtypes = [VP, VP, ctypes.POINTER(ctypes.c_uint32), ctypes.c_int32]
+        L.kvx_decoder_launches.argtypes = [VP]
+        L.kvx_decoder_launches.restype = ctypes.c_int32
         for name in EXPORTS:
             if name not in ("kvx_last_error", "kvx_launches_per_translate", "kvx_static_last_error",
-                            "kvx_fit_tokens"):
+                            "kvx_fit_tokens", "kvx_decoder_launches"):
                 getattr(L, name).restype = ctypes.c_int
         _lib = L
     return _lib
@@ -451,3 +488,118 @@ def build_alignment(src_seq_off, src_end, tgt_seq_off, tgt_end, span_lo, span_hi
     kvx_build_alignment(batch, src_end.shape[0], tgt_end.shape[0], _ptr(src_seq_off), _ptr(src_end),
                         _ptr(tgt_seq_off), _ptr(tgt_end), _ptr(span_lo), _ptr(span_hi), _ptr(dev_status),
                         _stream(stream))
+
+
+def _rows(t) -> kvx_rows:
+    """A [tokens, heads, head_dim] tensor (strided; channels contiguous) as kvx_rows."""
+    if t.dim() != 3 or t.stride(2) != 1:
+        raise ValueError("rows must be [tokens, heads, head_dim] with contiguous channels")
+    return kvx_rows(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def _cache(k: Sequence, v: Sequence, page_table, page_size: int, num_pages: int) -> kvx_dst_kv:
+    """Layers of a cache (contiguous [B, H, S, d], or pools [pages, page_size, H, d] with a page table) as kvx_dst_kv."""
+    k0 = k[0]
+    if page_table is None:
+        return kvx_dst_kv(_ptr_array(k), _ptr_array(v), 0, k0.shape[2], k0.stride(0), k0.stride(1), k0.stride(2), None, 0, 0, 0)
+    return kvx_dst_kv(_ptr_array(k), _ptr_array(v), 1, 0, 0, 0, 0, page_table.data_ptr(), page_table.shape[1], page_size,
+                      num_pages or k0.shape[0])
+
+
+class Decoder:
+    """Owns one kvx_decoder: the steps of a target model's decoding that touch its cache.
+
+    geom: the target model (as for Translator); num_q_heads query heads, consecutive groups of them
+    reading one KV head.  scale: factor of q.k (0 = 1 / sqrt(head_dim)).  score_cap: c > 0 caps a
+    scaled score s as c * tanh(s / c).  Calls are asynchronous on `stream` (None: torch's current
+    stream) and allocate nothing; cache_k / cache_v are one layer's tensors, contiguous
+    [B, H, S, d], or pools [num_pages, page_size, H, d] with an int32 page_table [B, max_pages]."""
+
+    def __init__(self, geom, num_q_heads: int, dtype: int = KVX_BF16, scale: float = 0.0, score_cap: float = 0.0,
+                 max_position: int = 0):
+        self.desc = kvx_decoder_desc(model_geom(geom), int(num_q_heads), dtype, max_position, float(scale), float(score_cap))
+        self.geom = geom
+        h = VP()
+        _check(lib().kvx_decoder_create(ctypes.byref(self.desc), ctypes.byref(h)))
+        self.handle = h.value
+
+    def _fits(self, tokens: int, *rows):
+        """Rows of one token count, of this decoder's heads, width and element size."""
+        d, size = self.desc.model.head_dim, 2 if self.desc.dtype == KVX_BF16 else 4
+        for t, heads in rows:
+            if tuple(t.shape) != (tokens, heads, d) or t.element_size() != size:
+                raise ValueError(f"rows must be [{tokens}, {heads}, {d}] of {size}-byte elements, got {tuple(t.shape)}")
+
+    def append(self, q, k, v, seq_off, kv_len, cache_k, cache_v, q_out, *, pos=None, page_table=None, page_size: int = 16,
+               num_pages: int = 0, stream=None):
+        """Rotate the new tokens' q [T, Hq, d] into q_out (q itself: in place) and k [T, H, d] into the cache, and
+        write v into the cache.  seq_off int32[B+1]: packed tokens of each sequence; kv_len int32[B]: its
+        cached tokens with the new ones; pos int32[T]: RoPE positions (None: the slots)."""
+        T, H, Hq = q.shape[0], self.desc.model.num_kv_heads, self.desc.num_q_heads
+        self._fits(T, (q, Hq), (k, H), (v, H), (q_out, Hq))
+        tok = kvx_new_tokens(seq_off.shape[0] - 1, T, seq_off.data_ptr(), kv_len.data_ptr(), _ptr(pos))
+        cache = _cache((cache_k,), (cache_v,), page_table, page_size, num_pages)
+        _check(lib().kvx_append(self.handle, tok, _rows(q), _rows(k), _rows(v), _rows(q_out), cache, 0, _stream(stream)))
+
+    def attend(self, q, seq_off, kv_len, cache_k, cache_v, out, *, window: int = 0, prefix_len=None, lse=None, key_weight=None,
+               page_table=None, page_size: int = 16, num_pages: int = 0, stream=None):
+        """Attention of the rotated queries q [T, Hq, d] over the cache (their own rows appended before), into out.
+        window: slots a token sees up to its own (0: all); prefix_len int32[B]: slots every token sees;
+        lse float32[T, Hq]: log-sum-exp of each row; key_weight float32[B, H, S]: has the attention weights
+        each slot receives added to it (needs lse)."""
+        T, Hq = q.shape[0], self.desc.num_q_heads
+        self._fits(T, (q, Hq), (out, Hq))
+        if lse is not None and not (lse.shape == (T, Hq) and lse.is_contiguous() and lse.element_size() == 4):
+            raise ValueError("lse must be contiguous float32 [tokens, query heads]")
+        B = seq_off.shape[0] - 1
+        if key_weight is not None and not (key_weight.shape[:2] == (B, self.desc.model.num_kv_heads) and key_weight.is_contiguous()
+                                           and key_weight.element_size() == 4):
+            raise ValueError("key_weight must be contiguous float32 [sequences, KV heads, slots]")
+        tok = kvx_new_tokens(B, T, seq_off.data_ptr(), kv_len.data_ptr(), None)
+        opts = kvx_attend_opts(window, _ptr(prefix_len), _ptr(lse), _ptr(key_weight), 0 if key_weight is None else key_weight.shape[2])
+        cache = _cache((cache_k,), (cache_v,), page_table, page_size, num_pages)
+        _check(lib().kvx_attend(self.handle, tok, _rows(q), cache, 0, opts, _rows(out), _stream(stream)))
+
+    def evict(self, kv_len, key_weight, keep: int, src_k: Sequence, src_v: Sequence, dst_k: Sequence, dst_v: Sequence, kept, new_len, *,
+              sinks: int = 0, recent: int = 0, kept_weight=None, page_table=None, dst_page_table=None, page_size: int = 16,
+              num_pages: int = 0, dst_num_pages: int = 0, stream=None):
+        """Cut the cache (lists of layers) down to `keep` slots per sequence, KV head and layer, by key_weight float32[L, B, H, S]:
+        rows into dst_k / dst_v, their slots into kept int32[L, B, H, keep] (-1 past the end), the lengths
+        into new_len int32[B], the weights into kept_weight float32[L, B, H, >= keep]."""
+        L, B, H = len(src_k), kv_len.shape[0], self.desc.model.num_kv_heads
+        if not (tuple(key_weight.shape[:3]) == (L, B, H) and key_weight.is_contiguous() and key_weight.element_size() == 4):
+            raise ValueError(f"key_weight must be contiguous float32 [{L}, {B}, {H}, slots]")
+        if not (tuple(kept.shape) == (L, B, H, keep) and kept.is_contiguous() and kept.element_size() == 4):
+            raise ValueError(f"kept must be contiguous int32 [{L}, {B}, {H}, {keep}]")
+        if kept_weight is not None and not (tuple(kept_weight.shape[:3]) == (L, B, H) and kept_weight.is_contiguous()
+                                            and kept_weight.element_size() == 4):
+            raise ValueError(f"kept_weight must be contiguous float32 [{L}, {B}, {H}, slots]")
+        if not len(src_v) == len(dst_k) == len(dst_v) == L:
+            raise ValueError("src_k, src_v, dst_k and dst_v must have as many layers as one another")
+        plan = kvx_evict_plan(B, L, kv_len.data_ptr(), key_weight.data_ptr(), key_weight.shape[3], keep, sinks, recent, kept.data_ptr(),
+                              new_len.data_ptr(), _ptr(kept_weight), 0 if kept_weight is None else kept_weight.shape[3])
+        src = _cache(src_k, src_v, page_table, page_size, num_pages)
+        dst = _cache(dst_k, dst_v, dst_page_table, page_size, dst_num_pages)
+        _check(lib().kvx_evict(self.handle, plan, src, dst, _stream(stream)))
+
+    def device_status(self, stream=None, clear: bool = True) -> int:
+        bits = ctypes.c_uint32(0)
+        st = lib().kvx_decoder_status(self.handle, _stream(stream), ctypes.byref(bits), int(clear))
+        if st not in (KVX_OK, KVX_ERR_DEVICE_STATUS):
+            _check(st)
+        return bits.value
+
+    def launches(self) -> int:
+        """Kernel launches of the most recent call."""
+        return lib().kvx_decoder_launches(self.handle)
+
+    def close(self):
+        if getattr(self, "handle", None):
+            _check(lib().kvx_decoder_destroy(self.handle))
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass

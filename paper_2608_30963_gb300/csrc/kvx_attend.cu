@@ -1,0 +1,400 @@
+// kvx_attend.cu -- attention of new tokens over a cache on the CUDA cores, and the launch of the
+// attention kernels.
+//
+//   o_i = sum_j p_ij v_j / sum_j p_ij,  p_ij = exp(x_ij - m_i),  x_ij = cap(scale q_i . k_j)
+// in one pass over the slots j with the running maximum m_i and sum (kept in units of log2).
+#include <atomic>
+
+#include "kvx_attend_rows.cuh"
+#include "kvx_kernels.h"
+#include "kvx_tc_common.cuh"
+
+namespace kvx {
+namespace {
+
+// Two packed fp32 products added to a packed sum.
+__device__ __forceinline__ float2 ffma2(float2 a, float2 b, float2 c)
+{
+    unsigned long long r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;"
+        : "=l"(r)
+        : "l"(reinterpret_cast<unsigned long long&>(a)), "l"(reinterpret_cast<unsigned long long&>(b)),
+          "l"(reinterpret_cast<unsigned long long&>(c)));
+    return reinterpret_cast<float2&>(r);
+}
+
+// A tile of R rows (BM queries or kBN slots) of D channels as fp32 in shared memory, rows D + 4 floats
+// apart (float4 reads of neighbouring rows fall into different banks).  off(r) gives a row's element
+// offset, or -1 for a row of zeros.  fp32 rows are copied asynchronously, bf16 rows widened here.
+template <typename T, int D, int R, int THREADS, typename Off>
+__device__ __forceinline__ void load_tile(float* dst, const T* src, Off off)
+{
+    constexpr int V = 16 / (int)sizeof(T), PER = D / V;
+    for (int i = threadIdx.x; i < R * PER; i += THREADS) {
+        const int r = i / PER, c = (i - r * PER) * V;
+        const long long at = off(r);
+        float* d = dst + r * (D + 4) + c;
+        if (at < 0) {
+#pragma unroll
+            for (int e = 0; e < V; e += 4) *reinterpret_cast<float4*>(d + e) = make_float4(0.f, 0.f, 0.f, 0.f);
+        } else if constexpr (sizeof(T) == 4) {
+            cp_async16(smem_u32(d), src + at + c);
+        } else {
+            const uint4 w = *reinterpret_cast<const uint4*>(src + at + c);
+            *reinterpret_cast<float4*>(d) = make_float4(bf_lo(w.x), bf_hi(w.x), bf_lo(w.y), bf_hi(w.y));
+            *reinterpret_cast<float4*>(d + 4) = make_float4(bf_lo(w.z), bf_hi(w.z), bf_lo(w.w), bf_hi(w.w));
+        }
+    }
+}
+__device__ __forceinline__ void async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+constexpr int kBN = 32;          // slots a tile
+constexpr int kThreads = 128;    // 16 row groups (tr) x 8 slot groups (tc)
+constexpr int kTR = 16, kTC = 8, kKN = kBN / kTC;
+
+// Scores of rows tr + 16 i and slots tc + 8 j of the tile: each thread RM x kKN of them.
+template <int D, int RM>
+__device__ __forceinline__ void scores(const float* sQ, const float* sK, int tr, int tc, float (&x)[RM][kKN])
+{
+    float2 acc[RM][kKN];
+#pragma unroll
+    for (int i = 0; i < RM; ++i)
+#pragma unroll
+        for (int j = 0; j < kKN; ++j) acc[i][j] = make_float2(0.f, 0.f);
+#pragma unroll 4
+    for (int c = 0; c < D; c += 4) {
+        float4 q[RM], k[kKN];
+#pragma unroll
+        for (int i = 0; i < RM; ++i) q[i] = *reinterpret_cast<const float4*>(sQ + (tr + kTR * i) * (D + 4) + c);
+#pragma unroll
+        for (int j = 0; j < kKN; ++j) k[j] = *reinterpret_cast<const float4*>(sK + (tc + kTC * j) * (D + 4) + c);
+#pragma unroll
+        for (int i = 0; i < RM; ++i)
+#pragma unroll
+            for (int j = 0; j < kKN; ++j) {
+                acc[i][j] = ffma2(make_float2(q[i].x, q[i].y), make_float2(k[j].x, k[j].y), acc[i][j]);
+                acc[i][j] = ffma2(make_float2(q[i].z, q[i].w), make_float2(k[j].z, k[j].w), acc[i][j]);
+            }
+    }
+#pragma unroll
+    for (int i = 0; i < RM; ++i)
+#pragma unroll
+        for (int j = 0; j < kKN; ++j) x[i][j] = acc[i][j].x + acc[i][j].y;
+}
+
+// A raw score in log2 units, capped.
+__device__ __forceinline__ float score2(const AttendParams& P, float dot, float inv_cap)
+{
+    float v = dot * P.scale;
+    if (P.cap > 0.0f) v = capped(v, P.cap, inv_cap);
+    return v * kLog2e;
+}
+
+template <int D, int BM> constexpr int simt_smem()
+{
+    return ((BM + 2 * kBN) * (D + 4) + BM * (kBN + 4)) * 4 + (kMaxAttendBatch + 2) * 8;
+}
+
+// 128 threads on a tile of BM rows and 32 slots; K of the next tile is copied while V is multiplied, V
+// while the scores are.
+template <typename T, int D, int BM>
+__global__ void __launch_bounds__(kThreads) attend_simt_kernel(const __grid_constant__ AttendParams P)
+{
+    constexpr int RM = BM / kTR, CN = D / 32;   // rows of a thread; its float4 column groups 4 tc + 32 n
+    extern __shared__ __align__(16) float sm[];
+    float* sQ = sm;
+    float* sK = sQ + BM * (D + 4);
+    float* sV = sK + kBN * (D + 4);
+    float* sP = sV + kBN * (D + 4);             // [BM][kBN + 4]
+    long long* sums = reinterpret_cast<long long*>(sP + BM * (kBN + 4));
+    int* flag = reinterpret_cast<int*>(sums + kMaxAttendBatch + 1);
+    const int tid = threadIdx.x, tc = tid & 7, tr = tid >> 3, lane = tid & 31, warp = tid >> 5;
+    const float inv_cap = P.cap > 0.0f ? 1.0f / P.cap : 0.0f;
+    const Plan plan = make_plan<BM, kBN, kThreads>(P, sums);
+    SegmentWalk<BM, kBN> walk(P, plan);
+    Segment g;
+    while (walk.next(g)) {
+        const int rows = min(BM, g.s.n * P.G - g.rt * BM);
+        const long long head = cache_head(P.cache) * g.h;
+        auto slot_row = [&](int tile, int r) {
+            const int j = tile * kBN + r;
+            long long at = -1;
+            if (j < g.s.L) {
+                at = cache_row(P.cache, g.b, j);
+                if (at < 0) set_status(P.status, KVX_DEV_PAGE_INVALID);
+                else at += head;
+            }
+            return at;
+        };
+        auto load_slots = [&](float* dst, const void* src, int tile) {
+            load_tile<T, D, kBN, kThreads>(dst, (const T*)src, [&](int r) { return slot_row(tile, r); });
+            async_commit();
+        };
+        load_tile<T, D, BM, kThreads>(sQ, (const T*)P.q, [&](int r) {
+            if (r >= rows) return -1ll;
+            const RowId id = row_id(P, g.s, g.h, g.rt * BM + r);
+            return (long long)(g.s.t0 + id.t) * P.q_t + (long long)id.head * P.q_h;
+        });
+        load_slots(sK, P.ck, g.kv.at(g.i0));
+        int slot_i[RM];                          // the rows' own slots
+        float m[RM], l[RM];
+        float2 o[RM][2 * CN];
+#pragma unroll
+        for (int i = 0; i < RM; ++i) {
+            slot_i[i] = g.s.slot((g.rt * BM + tr + kTR * i) / P.G);
+            m[i] = -INFINITY;
+            l[i] = 0.0f;
+#pragma unroll
+            for (int c = 0; c < 2 * CN; ++c) o[i][c] = make_float2(0.f, 0.f);
+        }
+        for (int it = 0; it < g.n; ++it) {
+            const int tile = g.kv.at(g.i0 + it);
+            load_slots(sV, P.cv, tile);
+            async_wait<1>();
+            __syncthreads();
+            float x[RM][kKN];
+            scores<D, RM>(sQ, sK, tr, tc, x);
+            __syncthreads();
+            if (it + 1 < g.n) load_slots(sK, P.ck, g.kv.at(g.i0 + it + 1));
+            else async_commit();
+#pragma unroll
+            for (int i = 0; i < RM; ++i) {
+                float top = -INFINITY;
+#pragma unroll
+                for (int j = 0; j < kKN; ++j) {
+                    x[i][j] = sees(P, g.s, slot_i[i], tile * kBN + tc + kTC * j) ? score2(P, x[i][j], inv_cap) : -INFINITY;
+                    top = fmaxf(top, x[i][j]);
+                }
+#pragma unroll
+                for (int k = 4; k; k >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
+                const float next = fmaxf(m[i], top), base = next == -INFINITY ? 0.0f : next;
+                const float w = exp2_hw(m[i] - base);
+                m[i] = next;
+                float sum = 0.0f;
+#pragma unroll
+                for (int j = 0; j < kKN; ++j) {
+                    const float p = exp2_hw(x[i][j] - base);
+                    sum += p;
+                    sP[(tr + kTR * i) * (kBN + 4) + tc + kTC * j] = p;
+                }
+#pragma unroll
+                for (int k = 4; k; k >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, k);
+                l[i] = fmaf(l[i], w, sum);
+#pragma unroll
+                for (int c = 0; c < 2 * CN; ++c) {
+                    o[i][c].x *= w;
+                    o[i][c].y *= w;
+                }
+            }
+            async_wait<1>();
+            __syncthreads();
+#pragma unroll 2
+            for (int j = 0; j < kBN; j += 4) {
+                float4 p[RM];
+#pragma unroll
+                for (int i = 0; i < RM; ++i) p[i] = *reinterpret_cast<const float4*>(sP + (tr + kTR * i) * (kBN + 4) + j);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+#pragma unroll
+                    for (int c = 0; c < CN; ++c) {
+                        const float4 v = *reinterpret_cast<const float4*>(sV + (j + e) * (D + 4) + 4 * tc + 32 * c);
+#pragma unroll
+                        for (int i = 0; i < RM; ++i) {
+                            const float pe = e == 0 ? p[i].x : e == 1 ? p[i].y : e == 2 ? p[i].z : p[i].w;
+                            o[i][2 * c] = ffma2(make_float2(pe, pe), make_float2(v.x, v.y), o[i][2 * c]);
+                            o[i][2 * c + 1] = ffma2(make_float2(pe, pe), make_float2(v.z, v.w), o[i][2 * c + 1]);
+                        }
+                    }
+            }
+            __syncthreads();
+        }
+        async_wait<0>();
+        if (g.whole()) {
+            // through shared memory (the queries' place), so that a warp has a whole row
+#pragma unroll
+            for (int i = 0; i < RM; ++i) {
+                const int r = tr + kTR * i;
+#pragma unroll
+                for (int c = 0; c < CN; ++c)
+                    *reinterpret_cast<float4*>(sQ + r * (D + 4) + 4 * tc + 32 * c) =
+                        make_float4(o[i][2 * c].x, o[i][2 * c].y, o[i][2 * c + 1].x, o[i][2 * c + 1].y);
+                if (tc == 0) {
+                    sP[r * (kBN + 4)] = m[i];
+                    sP[r * (kBN + 4) + 1] = l[i];
+                }
+            }
+            __syncthreads();
+            for (int r = warp; r < rows; r += kThreads / 32) {
+                float y[D / 32];
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c) y[c] = sQ[r * (D + 4) + lane * (D / 32) + c];
+                finish_row<T, D>(P, g.s, g.b, g.h, g.rt * BM + r, sP[r * (kBN + 4)], sP[r * (kBN + 4) + 1], y);
+            }
+        } else {
+            const Parts parts = item_parts(plan, g);
+            const size_t at = (size_t)(2 * blockIdx.x + (g.first ? 0 : 1)) * BM;
+#pragma unroll
+            for (int i = 0; i < RM; ++i) {
+                const int r = tr + kTR * i;
+                if (r >= rows) continue;
+#pragma unroll
+                for (int c = 0; c < CN; ++c)
+                    __stcg(reinterpret_cast<float4*>(P.part_o + (at + r) * D + 4 * tc + 32 * c),
+                           make_float4(o[i][2 * c].x, o[i][2 * c].y, o[i][2 * c + 1].x, o[i][2 * c + 1].y));
+                if (tc == 0) __stcg(P.part_ml + at + r, make_float2(m[i], l[i]));
+            }
+            if (last_to_arrive(P, parts, flag)) join_parts<T, D, BM, kThreads / 32>(P, g, parts, rows);
+        }
+        __syncthreads();
+    }
+}
+
+// key_weight[b, h, j] += sum over the rows i of (b, h) of exp(x_ij - lse_i): the scores are formed again, now
+// that every row's sum is known, one CTA to a tile of 32 slots, which no other CTA adds to.
+template <typename T, int D> constexpr int weight_smem()
+{
+    return ((64 + kBN) * (D + 4) + 64 + kTR * kBN) * 4 + (kMaxAttendBatch + 2) * 8;
+}
+template <typename T, int D>
+__global__ void __launch_bounds__(kThreads) key_weight_simt_kernel(const __grid_constant__ AttendParams P)
+{
+    constexpr int BM = 64, RM = BM / kTR;
+    extern __shared__ __align__(16) float sm[];
+    float* sQ = sm;
+    float* sK = sQ + BM * (D + 4);
+    float* sL = sK + kBN * (D + 4);             // the rows' lse in log2 units, +infinity past the end
+    float* sW = sL + BM;                        // [kTR][kBN]
+    long long* first = reinterpret_cast<long long*>(sW + kTR * kBN);   // slot tiles before each sequence's
+    const int tid = threadIdx.x, tc = tid & 7, tr = tid >> 3;
+    const float inv_cap = P.cap > 0.0f ? 1.0f / P.cap : 0.0f;
+    for (int b = tid; b < P.batch; b += kThreads) first[b + 1] = (load_seq(P, b).L + kBN - 1) / kBN;
+    if (tid == 0) first[0] = 0;
+    __syncthreads();
+    if (tid == 0)
+        for (int b = 0; b < P.batch; ++b) first[b + 1] += first[b];
+    __syncthreads();
+    const long long units = first[P.batch] * P.H;
+    for (long long u = blockIdx.x; u < units; u += gridDim.x) {
+        const long long ut = u / P.H;
+        const int h = (int)(u - ut * P.H);
+        int lo = 0, hi = P.batch - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (first[mid] <= ut) lo = mid; else hi = mid - 1;
+        }
+        const int b = lo, j0 = (int)(ut - first[b]) * kBN;
+        const Seq s = load_seq(P, b);
+        __syncthreads();
+        load_tile<T, D, kBN, kThreads>(sK, (const T*)P.ck, [&](int r) {
+            const long long at = j0 + r < s.L ? cache_row(P.cache, b, j0 + r) : -1;
+            return at < 0 ? -1ll : at + cache_head(P.cache) * h;
+        });
+        float w[kKN];
+#pragma unroll
+        for (int j = 0; j < kKN; ++j) w[j] = 0.0f;
+        // rows of tokens before the first that sees the tile need not be formed
+        const int t_first = j0 < s.pre ? 0 : max(0, j0 - (s.L - s.n));
+        const int t_end = (j0 < s.pre || P.window == 0) ? s.n : (int)min((long long)s.n, (long long)j0 + kBN - 1 + P.window - (s.L - s.n));
+        for (int r0 = t_first * P.G; r0 < t_end * P.G; r0 += BM) {
+            const int rows = min(BM, t_end * P.G - r0);
+            load_tile<T, D, BM, kThreads>(sQ, (const T*)P.q, [&](int r) {
+                if (r >= rows) return -1ll;
+                const RowId id = row_id(P, s, h, r0 + r);
+                return (long long)(s.t0 + id.t) * P.q_t + (long long)id.head * P.q_h;
+            });
+            async_commit();
+            for (int r = tid; r < BM; r += kThreads) {
+                float z = INFINITY;
+                if (r < rows) {
+                    const RowId id = row_id(P, s, h, r0 + r);
+                    z = P.lse[(long long)(s.t0 + id.t) * P.Hq + id.head] * kLog2e;
+                }
+                sL[r] = z;
+            }
+            async_wait<0>();
+            __syncthreads();
+            float x[RM][kKN];
+            scores<D, RM>(sQ, sK, tr, tc, x);
+#pragma unroll
+            for (int i = 0; i < RM; ++i) {
+                const int r = tr + kTR * i;
+                const int own = s.slot((r0 + r) / P.G);
+#pragma unroll
+                for (int j = 0; j < kKN; ++j)
+                    if (r < rows && sees(P, s, own, j0 + tc + kTC * j)) w[j] += exp2_hw(score2(P, x[i][j], inv_cap) - sL[r]);
+            }
+            __syncthreads();
+        }
+        async_wait<0>();
+#pragma unroll
+        for (int j = 0; j < kKN; ++j) sW[tr * kBN + tc + kTC * j] = w[j];
+        __syncthreads();
+        if (tid < kBN && j0 + tid < s.L && j0 + tid < P.weight_stride) {
+            float sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kTR; ++i) sum += sW[i * kBN + tid];
+            P.key_weight[((long long)b * P.H + h) * P.weight_stride + j0 + tid] += sum;
+        }
+        __syncthreads();
+    }
+}
+
+template <auto Kernel> int ctas_per_sm(int smem, int threads)
+{
+    static std::atomic<int> known{0};
+    int n = known.load();
+    if (n == 0) {
+        if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, Kernel, threads, smem) != cudaSuccess || n < 1) n = 1;
+        known.store(n);
+    }
+    return n;
+}
+
+template <typename T, int D, int BM>
+cudaError_t run_simt(const AttendParams& P, int num_sms, cudaStream_t stream)
+{
+    constexpr int smem = simt_smem<D, BM>();
+    if (cudaError_t e = smem_opt_in<attend_simt_kernel<T, D, BM>>(smem); e != cudaSuccess) return e;
+    const int grid = min(num_sms * ctas_per_sm<attend_simt_kernel<T, D, BM>>(smem, kThreads), kAttendMaxRows / BM / 2);
+    attend_simt_kernel<T, D, BM><<<grid, kThreads, smem, stream>>>(P);
+    return cudaGetLastError();
+}
+template <typename T, int D> cudaError_t run_weight_simt(const AttendParams& P, int num_sms, cudaStream_t stream)
+{
+    constexpr int smem = weight_smem<T, D>();
+    if (cudaError_t e = smem_opt_in<key_weight_simt_kernel<T, D>>(smem); e != cudaSuccess) return e;
+    key_weight_simt_kernel<T, D><<<num_sms * ctas_per_sm<key_weight_simt_kernel<T, D>>(smem, kThreads), kThreads, smem, stream>>>(P);
+    return cudaGetLastError();
+}
+
+template <typename T, int D> cudaError_t run_any(const AttendParams& P, int num_sms, cudaStream_t stream, int* launches)
+{
+    // few rows for each sequence and head: 16-row tiles waste less of the arithmetic
+    const bool few = (long long)P.T * P.G <= 16ll * P.batch;
+    cudaError_t e = few ? run_simt<T, D, 16>(P, num_sms, stream) : run_simt<T, D, D == 256 ? 32 : 64>(P, num_sms, stream);
+    ++*launches;
+    if (e == cudaSuccess && P.key_weight) {
+        e = run_weight_simt<T, D>(P, num_sms, stream);
+        ++*launches;
+    }
+    return e;
+}
+
+}  // namespace
+
+cudaError_t launch_attend(const AttendParams& P, int dtype, int num_sms, cudaStream_t stream, int* launches)
+{
+    *launches = 0;
+    if (P.T == 0) return cudaSuccess;
+    if (dtype == KVX_BF16) {
+        if (P.d == 64) return run_any<__nv_bfloat16, 64>(P, num_sms, stream, launches);
+        if (P.d == 128) return run_any<__nv_bfloat16, 128>(P, num_sms, stream, launches);
+        return run_any<__nv_bfloat16, 256>(P, num_sms, stream, launches);
+    }
+    if (P.d == 64) return run_any<float, 64>(P, num_sms, stream, launches);
+    if (P.d == 128) return run_any<float, 128>(P, num_sms, stream, launches);
+    return run_any<float, 256>(P, num_sms, stream, launches);
+}
+
+}  // namespace kvx
