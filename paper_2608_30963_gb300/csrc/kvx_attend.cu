@@ -244,7 +244,7 @@ __global__ void __launch_bounds__(kThreads) attend_simt_kernel(const __grid_cons
                            make_float4(o[i][2 * c].x, o[i][2 * c].y, o[i][2 * c + 1].x, o[i][2 * c + 1].y));
                 if (tc == 0) __stcg(P.part_ml + at + r, make_float2(m[i], l[i]));
             }
-            if (last_to_arrive(P, parts, flag)) join_parts<T, D, BM, kThreads / 32>(P, g, parts, rows);
+            if (last_to_arrive(P, parts, flag)) join_parts<T, D, BM, kThreads / 32>(P, g, parts, rows, warp);
         }
         __syncthreads();
     }
@@ -388,6 +388,16 @@ cudaError_t launch_attend(const AttendParams& P, int dtype, int num_sms, cudaStr
     *launches = 0;
     if (P.T == 0) return cudaSuccess;
     if (dtype == KVX_BF16) {
+        if ((long long)P.T * P.G > 16ll * P.batch) {
+            cudaError_t e = launch_attend_tc(P, num_sms, stream);
+            ++*launches;
+            if (e == cudaSuccess && P.key_weight) {
+                e = P.d == 64 ? run_weight_simt<__nv_bfloat16, 64>(P, num_sms, stream)
+                  : P.d == 128 ? run_weight_simt<__nv_bfloat16, 128>(P, num_sms, stream) : run_weight_simt<__nv_bfloat16, 256>(P, num_sms, stream);
+                ++*launches;
+            }
+            return e;
+        }
         if (P.d == 64) return run_any<__nv_bfloat16, 64>(P, num_sms, stream, launches);
         if (P.d == 128) return run_any<__nv_bfloat16, 128>(P, num_sms, stream, launches);
         return run_any<__nv_bfloat16, 256>(P, num_sms, stream, launches);

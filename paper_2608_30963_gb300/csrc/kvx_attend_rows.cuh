@@ -111,12 +111,12 @@ __device__ __forceinline__ void finish_row(const AttendParams& P, const Seq& s, 
     if (P.lse && lane == 0) P.lse[(long long)(s.t0 + id.t) * P.Hq + id.head] = lse2 * kLn2;
 }
 
-// Join the partial results of a split item, rows [0, rows) of its tile; every warp of the CTA calls it.
+// Join the partial results of a split item, rows [0, rows) of its tile; WARPS warps call it, numbered from 0.
 template <typename T, int D, int BM, int WARPS>
-__device__ __forceinline__ void join_parts(const AttendParams& P, const Segment& g, const Parts& parts, int rows)
+__device__ __forceinline__ void join_parts(const AttendParams& P, const Segment& g, const Parts& parts, int rows, int warp)
 {
     constexpr int C = D / 32;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int lane = threadIdx.x & 31;
     for (int r = warp; r < rows; r += WARPS) {
         float m = -INFINITY;
         for (int i = lane; i < parts.parts; i += 32) m = fmaxf(m, __ldcg(&P.part_ml[(size_t)parts.slot(i) * BM + r]).x);
