@@ -388,7 +388,7 @@ cudaError_t launch_attend(const AttendParams& P, int dtype, int num_sms, cudaStr
     *launches = 0;
     if (P.T == 0) return cudaSuccess;
     if (dtype == KVX_BF16) {
-        if ((long long)P.T * P.G > 16ll * P.batch) {
+        if (true) {
             cudaError_t e = launch_attend_tc(P, num_sms, stream);
             ++*launches;
             if (e == cudaSuccess && P.key_weight) {

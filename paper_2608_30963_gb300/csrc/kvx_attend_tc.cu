@@ -3,9 +3,11 @@
 //   S = Q K^T (fp32, TMEM),  P = exp2(c S - m),  O += P V (P bf16 from TMEM, O fp32 in TMEM)
 // in one pass over the slots, with the running maximum m and sum l of a row in the registers of the thread
 // that owns the row.  A CTA holds NT tiles of 128 rows and walks slot tiles of BN.
-//   producer warps (3)  copy Q, K and V rows into 128-byte-swizzled tiles with 16-byte cp.async, through
-//                       the page table where there is one; rows past a sequence's end become zeros.  A
-//                       K tile is read as a K-major operand, a V tile, laid out alike, as an MN-major one.
+//   producer warps (3)  copy Q, K and V rows into 128-byte-swizzled tiles.  Q: 16-byte cp.async.  K and V: one
+//                       tensor copy (TMA) for each page, or for a whole tile of a contiguous cache, by one
+//                       warp, a box a lane; caches that boxes of 8 or more rows cannot describe (odd page
+//                       sizes) take cp.async too.  A K tile is read as a K-major operand, a V tile, laid
+//                       out alike, as an MN-major one.
 //   MMA thread          unit u = (slot tile, row tile): S(u) into score buffer u mod 2, then, when P(u)
 //                       is there, O += P(u) V; S(u + 2) is issued right behind it, so that the scores of
 //                       one unit are formed while the other's softmax runs.
@@ -15,6 +17,8 @@
 // P is rounded to bf16 for the MMA, as V is.  Where a row sees few slots the roundings of its few weights do
 // not average out, and the error comes near 2^-8 |v|; there, and where the copies bound the kernel
 // anyway (one row tile), P goes in as two bf16 terms, high and low, at the price of a second product.
+#include <cuda.h>
+
 #include <atomic>
 
 #include "kvx_attend_rows.cuh"
@@ -113,14 +117,29 @@ template <int BM, int NT> __device__ __forceinline__ bool two_terms(const Attend
     return own < kFewSlots || (P.window > 0 && P.window < kFewSlots);
 }
 
+// Tensor maps of K and V, and the rows of a box: a paged cache as (channel, head, slot in page, page), a
+// contiguous one as (channel, slot, head, sequence); boxes of 64 channels of one head.
+struct TileMaps {
+    CUtensorMap k, v;
+    int box_rows;
+};
+__device__ __forceinline__ void tma_box4(uint32_t dst, const CUtensorMap* map, int x, int y, int z, int w, uint32_t mbar)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(dst),
+        "l"(map), "r"(mbar), "r"(x), "r"(y), "r"(z), "r"(w)
+        : "memory");
+}
+
 // Barriers (8 bytes each) in the control block.
 template <int STAGES> struct Bars {
     static constexpr int full = 0, empty = STAGES, sfull = 2 * STAGES, pfull = sfull + 2, ofull = pfull + 2, qfull = ofull + 2,
                          qempty = qfull + 1, done = qempty + 1;
 };
 
-template <int D, int NT>
-__global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1) attend_tc_kernel(const __grid_constant__ AttendParams P)
+template <int D, int NT, bool TMA>
+__global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
+    attend_tc_kernel(const __grid_constant__ AttendParams P, const __grid_constant__ TileMaps maps)
 {
     using C = TcShape<D, NT>;
     using B = Bars<C::STAGES>;
@@ -137,7 +156,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1) attend_tc_kernel(c
     if (warp == kMmaWarp) tmem_alloc(smem_u32(tmem_slot), C::TMEM);
     if (threadIdx.x == 0) {
         for (int i = 0; i < C::STAGES; ++i) {
-            mbar_init(bar(B::full + i), kProdWarps);
+            mbar_init(bar(B::full + i), TMA ? 1 : kProdWarps);
             mbar_init(bar(B::empty + i), 1);
         }
         for (int i = 0; i < 2; ++i) {
@@ -220,6 +239,51 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1) attend_tc_kernel(c
             ++items;
             const long long head = cache_head(P.cache) * g.h;
             // tile i as K, tile i - NB + 1 as V, and at the end the V tiles left
+            if constexpr (TMA) {
+                if (warp > 0) {
+                    flush();
+                    continue;
+                }
+                // lanes take the boxes of a tile: box e is rows [r, r + box_rows) of channel block e mod D/64
+                const int boxes = BN / maps.box_rows * (D / 64);
+                for (int i = 0; i < g.n + C::NB - 1; ++i) {
+#pragma unroll
+                    for (int kv = 0; kv < 2; ++kv) {
+                        const int t = kv ? i - (C::NB - 1) : i;
+                        if (t < 0 || t >= g.n) continue;
+                        const int j0 = g.kv.at(g.i0 + t) * BN;
+                        const uint32_t st = pos % C::STAGES, ph = (pos / C::STAGES) & 1;
+                        ok = ok && W.wait(bar(B::empty + st), ph ^ 1);
+                        ok = __all_sync(0xffffffffu, ok);
+                        ++pos;
+                        if (!ok) continue;
+                        if (lane == 0) mbar_arrive_expect_tx(bar(B::full + st), C::TILE);
+                        __syncwarp();
+                        for (int e = lane; e < boxes; e += 32) {
+                            const int cb = e % (D / 64), r = e / (D / 64) * maps.box_rows, j = j0 + r;
+                            const uint32_t dst = sT + st * C::TILE + (uint32_t)(cb * (BN * 128) + r * 128);
+                            const CUtensorMap* map = kv ? &maps.v : &maps.k;
+                            if (P.cache.paged) {
+                                int page = -1;           // outside the pool: the box is filled with zeros
+                                if (j < g.s.L) {
+                                    const int pi = j >> P.cache.page_shift;
+                                    if (pi < P.cache.max_pages) page = __ldg(&P.cache.page_table[(size_t)g.b * P.cache.max_pages + pi]);
+                                    if (page < 0 || page >= P.cache.num_pages) {
+                                        page = -1;
+                                        set_status(P.status, KVX_DEV_PAGE_INVALID);
+                                    }
+                                }
+                                tma_box4(dst, map, cb * 64, g.h, j & (P.cache.page_size - 1), page, bar(B::full + st));
+                            } else {
+                                tma_box4(dst, map, cb * 64, j, g.h, g.b, bar(B::full + st));
+                            }
+                        }
+                        __syncwarp();
+                    }
+                    if (i == 0) flush();                 // the queries, behind the first tiles' copies
+                }
+                continue;
+            }
             for (int i = 0; i < g.n + C::NB - 1; ++i) {
 #pragma unroll
                 for (int kv = 0; kv < 2; ++kv) {
@@ -319,7 +383,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1) attend_tc_kernel(c
         const uint32_t lanes = tmem + ((uint32_t)(quad * 32) << 16);
         const float inv_cap = P.cap > 0.0f ? 1.0f / P.cap : 0.0f;
         const float c = P.cap > 0.0f ? 1.0f : P.scale * kLog2e;   // factor of the (capped) scores in log2 units
-        uint32_t units = 0, items = 0;
+        uint32_t units = 0, items = 0, base_tile = 0;
         bool ok = true;                                  // the same in the lanes of a warp
         auto wait = [&](int b, uint32_t parity) { ok = __all_sync(0xffffffffu, ok && W.wait(bar(b), parity)); };
         while (walk.next(g)) {
@@ -358,6 +422,19 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1) attend_tc_kernel(c
                     }
                 }
                 const int j0 = g.kv.at(g.i0 + i) * BN;
+                if (TMA && j0 + BN > g.s.L && t == 0) {
+                    // the boxes brought what the cache holds past the sequence's end: zeros in V's place, before
+                    // any P is announced for it
+                    const uint32_t p = base_tile + (uint32_t)(C::NB == 1 ? 2 * i + 1 : i == g.n - 1 ? 2 * i + 1 : 2 * i + 2), st = p % C::STAGES;
+                    wait(B::full + (int)st, (p / C::STAGES) & 1);
+                    if (!ok) break;
+                    const int from = max(g.s.L - j0, 0);
+                    uint8_t* tile = smem + C::CTRL + C::QB + st * C::TILE;
+                    for (int e = (int)threadIdx.x - 128 + from * 8; e < BN * 8; e += 128)
+#pragma unroll
+                        for (int cb = 0; cb < D / 64; ++cb) *reinterpret_cast<uint4*>(tile + cb * (BN * 128) + e * 16) = make_uint4(0, 0, 0, 0);
+                    fence_proxy_async();
+                }
                 const bool all = (j0 >= lo && j0 + BN <= hi) || j0 + BN <= pre;
                 if (!__all_sync(0xffffffffu, all)) {
 #pragma unroll
@@ -426,6 +503,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1) attend_tc_kernel(c
                 if (lane == 0) mbar_arrive(bar(B::pfull + (gu & 1)));
             }
             units += (uint32_t)(g.n * NT);
+            base_tile += 2 * (uint32_t)g.n;
             if (ok) wait(B::ofull + t, items & 1);
             ++items;
             tc_fence_after();
@@ -502,13 +580,57 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1) attend_tc_kernel(c
     }
 }
 
-template <int D, int NT> cudaError_t run_tc(const AttendParams& P, int num_sms, cudaStream_t stream)
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiled tiled_encoder()
+{
+    static const EncodeTiled fn = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) != cudaSuccess ||
+            q != cudaDriverEntryPointSuccess)
+            p = nullptr;
+        return (EncodeTiled)p;
+    }();
+    return fn;
+}
+
+// The maps of a call's cache, tiles of bn slots; false where boxes cannot describe it.
+bool make_maps(const AttendParams& P, int bn, TileMaps& m)
+{
+    const CacheView& c = P.cache;
+    const EncodeTiled enc = tiled_encoder();
+    if (!enc || c.capacity < 1 || (c.paged && (c.page_shift < 3))) return false;
+    m.box_rows = c.paged && c.page_size < bn ? c.page_size : bn;
+    const cuuint64_t H = (cuuint64_t)c.H, d = (cuuint64_t)c.d;
+    const cuuint64_t dims_p[4] = {d, H, (cuuint64_t)c.page_size, (cuuint64_t)c.num_pages};
+    const cuuint64_t str_p[3] = {d * 2, H * d * 2, (cuuint64_t)c.page_size * H * d * 2};
+    const cuuint64_t dims_c[4] = {d, (cuuint64_t)c.capacity, H, (cuuint64_t)P.batch};
+    const cuuint64_t str_c[3] = {(cuuint64_t)c.st * 2, (cuuint64_t)c.sh * 2, (cuuint64_t)c.sb * 2};
+    const cuuint32_t box_p[4] = {64, 1, (cuuint32_t)m.box_rows, 1}, box_c[4] = {64, (cuuint32_t)m.box_rows, 1, 1};
+    const cuuint32_t one[4] = {1, 1, 1, 1};
+    for (int i = 0; i < 2; ++i)
+        if (enc(i ? &m.v : &m.k, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(i ? P.cv : P.ck), c.paged ? dims_p : dims_c,
+                c.paged ? str_p : str_c, c.paged ? box_p : box_c, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+            return false;
+    return true;
+}
+
+template <int D, int NT, bool TMA> cudaError_t start_tc(const AttendParams& P, const TileMaps& maps, int num_sms, cudaStream_t stream)
 {
     using C = TcShape<D, NT>;
-    if (cudaError_t e = smem_opt_in<attend_tc_kernel<D, NT>>(C::SMEM); e != cudaSuccess) return e;
+    if (cudaError_t e = smem_opt_in<attend_tc_kernel<D, NT, TMA>>(C::SMEM); e != cudaSuccess) return e;
     const int grid = min(num_sms, kAttendMaxRows / C::BM / 2);
-    attend_tc_kernel<D, NT><<<grid, C::THREADS, C::SMEM, stream>>>(P);
+    attend_tc_kernel<D, NT, TMA><<<grid, C::THREADS, C::SMEM, stream>>>(P, maps);
     return cudaGetLastError();
+}
+template <int D, int NT> cudaError_t run_tc(const AttendParams& P, int num_sms, cudaStream_t stream)
+{
+    TileMaps maps;
+    if (make_maps(P, TcShape<D, NT>::BN, maps)) return start_tc<D, NT, true>(P, maps, num_sms, stream);
+    return start_tc<D, NT, false>(P, maps, num_sms, stream);
 }
 
 }  // namespace
