@@ -108,13 +108,14 @@ __global__ void __launch_bounds__(kThreads) attend_simt_kernel(const __grid_cons
     float* sV = sK + kBN * (D + 4);
     float* sP = sV + kBN * (D + 4);             // [BM][kBN + 4]
     long long* sums = reinterpret_cast<long long*>(sP + BM * (kBN + 4));
-    int* flag = reinterpret_cast<int*>(sums + kMaxAttendBatch + 1);
     const int tid = threadIdx.x, tc = tid & 7, tr = tid >> 3, lane = tid & 31, warp = tid >> 5;
     const float inv_cap = P.cap > 0.0f ? 1.0f / P.cap : 0.0f;
     const Plan plan = make_plan<BM, kBN, kThreads>(P, sums);
     SegmentWalk<BM, kBN> walk(P, plan);
     Segment g;
+    bool have = false;
     while (walk.next(g)) {
+        have = true;
         const int rows = min(BM, g.s.n * P.G - g.rt * BM);
         const long long head = cache_head(P.cache) * g.h;
         auto slot_row = [&](int tile, int r) {
@@ -232,7 +233,6 @@ __global__ void __launch_bounds__(kThreads) attend_simt_kernel(const __grid_cons
                 finish_row<T, D>(P, g.s, g.b, g.h, g.rt * BM + r, sP[r * (kBN + 4)], sP[r * (kBN + 4) + 1], y);
             }
         } else {
-            const Parts parts = item_parts(plan, g);
             const size_t at = (size_t)(2 * blockIdx.x + (g.first ? 0 : 1)) * BM;
 #pragma unroll
             for (int i = 0; i < RM; ++i) {
@@ -244,10 +244,10 @@ __global__ void __launch_bounds__(kThreads) attend_simt_kernel(const __grid_cons
                            make_float4(o[i][2 * c].x, o[i][2 * c].y, o[i][2 * c + 1].x, o[i][2 * c + 1].y));
                 if (tc == 0) __stcg(P.part_ml + at + r, make_float2(m[i], l[i]));
             }
-            if (last_to_arrive(P, parts, flag)) join_parts<T, D, BM, kThreads / 32>(P, g, parts, rows, warp);
         }
         __syncthreads();
     }
+    if (tid == 0) leave_split(P, plan, g, have);
 }
 
 // key_weight[b, h, j] += sum over the rows i of (b, h) of exp(x_ij - lse_i): the scores are formed again, now
@@ -358,7 +358,8 @@ cudaError_t run_simt(const AttendParams& P, int num_sms, cudaStream_t stream)
     if (cudaError_t e = smem_opt_in<attend_simt_kernel<T, D, BM>>(smem); e != cudaSuccess) return e;
     const int grid = min(num_sms * ctas_per_sm<attend_simt_kernel<T, D, BM>>(smem, kThreads), kAttendMaxRows / BM / 2);
     attend_simt_kernel<T, D, BM><<<grid, kThreads, smem, stream>>>(P);
-    return cudaGetLastError();
+    if (cudaError_t e = cudaGetLastError(); e != cudaSuccess) return e;
+    return run_join<T, D, BM>(P, grid, stream);
 }
 template <typename T, int D> cudaError_t run_weight_simt(const AttendParams& P, int num_sms, cudaStream_t stream)
 {
@@ -368,17 +369,11 @@ template <typename T, int D> cudaError_t run_weight_simt(const AttendParams& P, 
     return cudaGetLastError();
 }
 
-template <typename T, int D> cudaError_t run_any(const AttendParams& P, int num_sms, cudaStream_t stream, int* launches)
+template <int D> cudaError_t run_fp32(const AttendParams& P, int num_sms, cudaStream_t stream)
 {
     // few rows for each sequence and head: 16-row tiles waste less of the arithmetic
     const bool few = (long long)P.T * P.G <= 16ll * P.batch;
-    cudaError_t e = few ? run_simt<T, D, 16>(P, num_sms, stream) : run_simt<T, D, D == 256 ? 32 : 64>(P, num_sms, stream);
-    ++*launches;
-    if (e == cudaSuccess && P.key_weight) {
-        e = run_weight_simt<T, D>(P, num_sms, stream);
-        ++*launches;
-    }
-    return e;
+    return few ? run_simt<float, D, 16>(P, num_sms, stream) : run_simt<float, D, D == 256 ? 32 : 64>(P, num_sms, stream);
 }
 
 }  // namespace
@@ -387,24 +382,17 @@ cudaError_t launch_attend(const AttendParams& P, int dtype, int num_sms, cudaStr
 {
     *launches = 0;
     if (P.T == 0) return cudaSuccess;
-    if (dtype == KVX_BF16) {
-        if (true) {
-            cudaError_t e = launch_attend_tc(P, num_sms, stream);
-            ++*launches;
-            if (e == cudaSuccess && P.key_weight) {
-                e = P.d == 64 ? run_weight_simt<__nv_bfloat16, 64>(P, num_sms, stream)
-                  : P.d == 128 ? run_weight_simt<__nv_bfloat16, 128>(P, num_sms, stream) : run_weight_simt<__nv_bfloat16, 256>(P, num_sms, stream);
-                ++*launches;
-            }
-            return e;
-        }
-        if (P.d == 64) return run_any<__nv_bfloat16, 64>(P, num_sms, stream, launches);
-        if (P.d == 128) return run_any<__nv_bfloat16, 128>(P, num_sms, stream, launches);
-        return run_any<__nv_bfloat16, 256>(P, num_sms, stream, launches);
-    }
-    if (P.d == 64) return run_any<float, 64>(P, num_sms, stream, launches);
-    if (P.d == 128) return run_any<float, 128>(P, num_sms, stream, launches);
-    return run_any<float, 256>(P, num_sms, stream, launches);
+    const bool bf16 = dtype == KVX_BF16;
+    cudaError_t e = bf16 ? launch_attend_tc(P, num_sms, stream)
+                         : P.d == 64 ? run_fp32<64>(P, num_sms, stream) : P.d == 128 ? run_fp32<128>(P, num_sms, stream) : run_fp32<256>(P, num_sms, stream);
+    *launches = 2;
+    if (e != cudaSuccess || !P.key_weight) return e;
+    *launches = 3;
+    if (bf16)
+        return P.d == 64 ? run_weight_simt<__nv_bfloat16, 64>(P, num_sms, stream) : P.d == 128 ? run_weight_simt<__nv_bfloat16, 128>(P, num_sms, stream)
+                                                                                  : run_weight_simt<__nv_bfloat16, 256>(P, num_sms, stream);
+    return P.d == 64 ? run_weight_simt<float, 64>(P, num_sms, stream) : P.d == 128 ? run_weight_simt<float, 128>(P, num_sms, stream)
+                                                                              : run_weight_simt<float, 256>(P, num_sms, stream);
 }
 
 }  // namespace kvx

@@ -4,6 +4,7 @@
 #pragma once
 
 #include "kvx_decode.cuh"
+#include "kvx_tc_common.cuh"
 
 namespace kvx {
 namespace {
@@ -111,61 +112,111 @@ __device__ __forceinline__ void finish_row(const AttendParams& P, const Seq& s, 
     if (P.lse && lane == 0) P.lse[(long long)(s.t0 + id.t) * P.Hq + id.head] = lse2 * kLn2;
 }
 
-// Join the partial results of a split item, rows [0, rows) of its tile; WARPS warps call it, numbered from 0.
-template <typename T, int D, int BM, int WARPS>
-__device__ __forceinline__ void join_parts(const AttendParams& P, const Segment& g, const Parts& parts, int rows, int warp)
+// C floats of a partial result.
+template <int C> __device__ __forceinline__ void load_part(const float* src, float (&v)[C])
 {
-    constexpr int C = D / 32;
-    const int lane = threadIdx.x & 31;
-    for (int r = warp; r < rows; r += WARPS) {
-        float m = -INFINITY;
-        for (int i = lane; i < parts.parts; i += 32) m = fmaxf(m, __ldcg(&P.part_ml[(size_t)parts.slot(i) * BM + r]).x);
+    if constexpr (C == 2) {
+        const float2 x = __ldcg((const float2*)src);
+        v[0] = x.x;
+        v[1] = x.y;
+    } else {
 #pragma unroll
-        for (int k = 16; k; k >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, k));
-        const float base = m == -INFINITY ? 0.0f : m;
-        float l = 0.0f, o[C];
-#pragma unroll
-        for (int c = 0; c < C; ++c) o[c] = 0.0f;
-#pragma unroll 4
-        for (int i = 0; i < parts.parts; ++i) {
-            const size_t at = (size_t)parts.slot(i) * BM + r;
-            const float2 ml = __ldcg(&P.part_ml[at]);
-            const float w = exp2_hw(ml.x - base);
-            l = fmaf(ml.y, w, l);
-            const float* src = P.part_o + at * D + lane * C;
-            if constexpr (C == 2) {
-                const float2 v = __ldcg((const float2*)src);
-                o[0] = fmaf(v.x, w, o[0]);
-                o[1] = fmaf(v.y, w, o[1]);
-            } else {
-#pragma unroll
-                for (int c = 0; c < C; c += 4) {
-                    const float4 v = __ldcg((const float4*)(src + c));
-                    o[c] = fmaf(v.x, w, o[c]);
-                    o[c + 1] = fmaf(v.y, w, o[c + 1]);
-                    o[c + 2] = fmaf(v.z, w, o[c + 2]);
-                    o[c + 3] = fmaf(v.w, w, o[c + 3]);
-                }
-            }
+        for (int c = 0; c < C; c += 4) {
+            const float4 x = __ldcg((const float4*)(src + c));
+            v[c] = x.x;
+            v[c + 1] = x.y;
+            v[c + 2] = x.z;
+            v[c + 3] = x.w;
         }
-        finish_row<T, D>(P, g.s, g.b, g.h, g.rt * BM + r, m, l, o);
     }
 }
 
-// After a CTA has written its partial result: whether it is the last of the item's CTAs (all threads get the
-// answer).  The counter goes back to zero for the next launch.
-__device__ __forceinline__ bool last_to_arrive(const AttendParams& P, const Parts& parts, int* flag)
+// The last segment of a CTA's range: where an item begins that other CTAs go on with, this CTA leaves its
+// description for the join, else an empty one.
+__device__ __forceinline__ void leave_split(const AttendParams& P, const Plan& plan, const Segment& g, bool have)
 {
-    __threadfence();
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        const unsigned before = atomicAdd(&P.arrived[parts.c0], 1u);
-        *flag = before == (unsigned)parts.parts - 1;
-        if (*flag) P.arrived[parts.c0] = 0;
-        __threadfence();
+    SplitItem it = {};
+    if (have && g.i0 == 0 && !g.whole()) {
+        const Parts parts = item_parts(plan, g);
+        it = {g.b, g.rt, g.h, parts.parts, parts.slot0};
     }
-    __syncthreads();
-    return *flag;
+    P.split[blockIdx.x] = it;
+}
+
+// Joins the partial results of split items: CTA (c, y) takes rows [y * RPC, ...) of the item that CTA c of the
+// attention kernel left, WPR warps a row, each with every WPR-th part, their sums added in order.  The
+// reads come from L2, eight parts in flight a warp.
+template <typename T, int D, int BM, int WPR>
+__global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ AttendParams P)
+{
+    constexpr int C = D / 32, RPC = 8 / WPR, U = C == 8 ? 4 : 8;
+    __shared__ float sh[8][D + 2];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    grid_dependency_wait();
+    const SplitItem it = P.split[blockIdx.x];
+    if (it.parts == 0) return;
+    const Seq s = load_seq(P, it.b);
+    const int r = blockIdx.y * RPC + warp / WPR, w0 = warp % WPR;
+    const bool real = r < min(BM, s.n * P.G - it.rt * BM);
+    const Parts parts = {(int)blockIdx.x, it.parts, it.slot0};
+    float m = -INFINITY, l = 0.0f, o[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) o[c] = 0.0f;
+    if (real) {
+        for (int i = lane; i < parts.parts; i += 32) m = fmaxf(m, __ldcg(&P.part_ml[(size_t)parts.slot(i) * BM + r]).x);
+#pragma unroll
+        for (int e = 16; e; e >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, e));
+        const float base = m == -INFINITY ? 0.0f : m;
+        for (int i0 = w0; i0 < parts.parts; i0 += U * WPR) {
+            float2 ml[U];
+            float v[U][C];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (i0 + u * WPR < parts.parts) {
+                    const size_t at = (size_t)parts.slot(i0 + u * WPR) * BM + r;
+                    ml[u] = __ldcg(&P.part_ml[at]);
+                    load_part<C>(P.part_o + at * D + lane * C, v[u]);
+                }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (i0 + u * WPR < parts.parts) {
+                    const float w = exp2_hw(ml[u].x - base);
+                    l = fmaf(ml[u].y, w, l);
+#pragma unroll
+                    for (int c = 0; c < C; ++c) o[c] = fmaf(v[u][c], w, o[c]);
+                }
+        }
+    }
+    if constexpr (WPR > 1) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) sh[warp][lane * C + c] = o[c];
+        if (lane == 0) sh[warp][D] = l;
+        __syncthreads();
+        if (w0 != 0) return;
+#pragma unroll
+        for (int k = 1; k < WPR; ++k) {
+#pragma unroll
+            for (int c = 0; c < C; ++c) o[c] += sh[warp + k][lane * C + c];
+            l += sh[warp + k][D];
+        }
+    }
+    if (real) finish_row<T, D>(P, s, it.b, it.h, it.rt * BM + r, m, l, o);
+}
+template <typename T, int D, int BM> cudaError_t run_join(const AttendParams& P, int grid, cudaStream_t stream)
+{
+    // an item has at most min(BM, T G) rows; few of them: four warps a row, as there may be many parts
+    const long long rows = min((long long)BM, (long long)P.T * P.G);
+    const bool few = rows <= 64;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid, (unsigned)(few ? (rows + 1) / 2 : (rows + 7) / 8));
+    cfg.blockDim = dim3(256);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return few ? cudaLaunchKernelEx(&cfg, join_kernel<T, D, BM, 4>, P) : cudaLaunchKernelEx(&cfg, join_kernel<T, D, BM, 1>, P);
 }
 
 }  // namespace

@@ -49,7 +49,6 @@ __device__ __forceinline__ void cp_async16_or_zero(uint32_t dst, const void* src
 }
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-__device__ __forceinline__ void group_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 
 // D[tmem] (+)= A[tmem] . B[smem], bf16 inputs, fp32 accumulate
 __device__ __forceinline__ void umma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accumulate)
@@ -149,7 +148,6 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
     auto bar = [&](int i) { return s0 + (uint32_t)i * 8; };
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + 512);
     int* abort = reinterpret_cast<int*>(smem + 516);
-    int* flag = reinterpret_cast<int*>(smem + 520);
     const uint32_t sQ = s0 + C::CTRL, sT = sQ + C::QB;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
@@ -282,8 +280,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
                     }
                     if (i == 0) flush();                 // the queries, behind the first tiles' copies
                 }
-                continue;
-            }
+            } else
             for (int i = 0; i < g.n + C::NB - 1; ++i) {
 #pragma unroll
                 for (int kv = 0; kv < 2; ++kv) {
@@ -329,12 +326,11 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
                     if (!ok) return;
                     tc_fence_after();
                     const uint32_t d = tmem + ((units + u) & 1) * C::S_COL;
+                    // descriptors count 16-byte units in their low bits: steps along an operand are added
+                    const uint64_t qd = sw128_desc(sQ + t * (128 * D * 2)), kd = sw128_desc(sT + st * C::TILE);
 #pragma unroll
-                    for (int k = 0; k < D / 16; ++k) {
-                        const uint32_t in = (uint32_t)(k & 3) * 32;
-                        umma_bf16(d, sw128_desc(sQ + t * (128 * D * 2) + (k >> 2) * (128 * 128) + in),
-                                  sw128_desc(sT + st * C::TILE + (k >> 2) * (BN * 128) + in), idesc_s, k > 0);
-                    }
+                    for (int k = 0; k < D / 16; ++k)
+                        umma_bf16(d, qd + (k >> 2) * (128 * 128 / 16) + (k & 3) * 2, kd + (k >> 2) * (BN * 128 / 16) + (k & 3) * 2, idesc_s, k > 0);
                     issued = true;
                     if (t == NT - 1) umma_commit(bar(B::empty + st));
                     if (u == U - 1) umma_commit(bar(B::qempty));
@@ -350,15 +346,13 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
                     if (t == 0) ok = ok && W.wait(bar(B::full + st), (p / C::STAGES) & 1);
                     if (!ok) break;
                     tc_fence_after();
+                    const uint64_t vd = mn_desc(sT + st * C::TILE, BN * 128);
+                    const uint32_t od = tmem + C::O_COL + t * D, pd = tmem + (gu & 1) * C::S_COL;
 #pragma unroll
-                    for (int k = 0; k < BN / 16; ++k)
-                        umma_bf16_ts(tmem + C::O_COL + t * D, tmem + (gu & 1) * C::S_COL + k * 8,
-                                     mn_desc(sT + st * C::TILE + k * 2048, BN * 128), idesc_o, i > 0 || k > 0);
+                    for (int k = 0; k < BN / 16; ++k) umma_bf16_ts(od, pd + k * 8, vd + k * (2048 / 16), idesc_o, i > 0 || k > 0);
                     if (two)
 #pragma unroll
-                        for (int k = 0; k < BN / 16; ++k)
-                            umma_bf16_ts(tmem + C::O_COL + t * D, tmem + (gu & 1) * C::S_COL + BN / 2 + k * 8,
-                                         mn_desc(sT + st * C::TILE + k * 2048, BN * 128), idesc_o, 1);
+                        for (int k = 0; k < BN / 16; ++k) umma_bf16_ts(od, pd + BN / 2 + k * 8, vd + k * (2048 / 16), idesc_o, 1);
                     if (t == NT - 1) umma_commit(bar(B::empty + st));
                     if (i == g.n - 1) umma_commit(bar(B::ofull + t));
                     if (u + 2 < U) scores(u + 2);
@@ -386,7 +380,9 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
         uint32_t units = 0, items = 0, base_tile = 0;
         bool ok = true;                                  // the same in the lanes of a warp
         auto wait = [&](int b, uint32_t parity) { ok = __all_sync(0xffffffffu, ok && W.wait(bar(b), parity)); };
+        bool have = false;
         while (walk.next(g)) {
+            have = true;
             const int row = g.rt * BM + t * 128 + quad * 32 + lane;
             const bool real = row < g.s.n * P.G;
             const int own = real ? g.s.slot(row / P.G) : -1;     // rows past the end see nothing
@@ -555,22 +551,9 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
                 }
             } else {
                 if (real) __stcg(P.part_ml + part, make_float2(m, l));
-                const Parts parts = item_parts(plan, g);
-                __threadfence();
-                __syncwarp();
-                group_sync(1, NT * 128);
-                if (threadIdx.x == 128) {
-                    *flag = atomicAdd(&P.arrived[parts.c0], 1u) == (unsigned)parts.parts - 1;
-                    if (*flag) P.arrived[parts.c0] = 0;
-                    __threadfence();
-                }
-                __syncwarp();
-                group_sync(1, NT * 128);
-                const bool last = *flag;
-                if (last) join_parts<__nv_bfloat16, D, BM, NT * 4>(P, g, parts, min(BM, g.s.n * P.G - g.rt * BM), warp - 4);
-                group_sync(1, NT * 128);
             }
         }
+        if (threadIdx.x == 128) leave_split(P, plan, g, have);
     }
     tc_fence_before();
     __syncthreads();
@@ -624,7 +607,8 @@ template <int D, int NT, bool TMA> cudaError_t start_tc(const AttendParams& P, c
     if (cudaError_t e = smem_opt_in<attend_tc_kernel<D, NT, TMA>>(C::SMEM); e != cudaSuccess) return e;
     const int grid = min(num_sms, kAttendMaxRows / C::BM / 2);
     attend_tc_kernel<D, NT, TMA><<<grid, C::THREADS, C::SMEM, stream>>>(P, maps);
-    return cudaGetLastError();
+    if (cudaError_t e = cudaGetLastError(); e != cudaSuccess) return e;
+    return run_join<__nv_bfloat16, D, C::BM>(P, grid, stream);
 }
 template <int D, int NT> cudaError_t run_tc(const AttendParams& P, int num_sms, cudaStream_t stream)
 {

@@ -18,7 +18,7 @@ struct kvx_decoder {
     unsigned* status = nullptr;
     float* part_o = nullptr;               // partial results of split attention rows (kvx_decode.cuh)
     float2* part_ml = nullptr;
-    unsigned* arrived = nullptr;
+    SplitItem* split = nullptr;
 };
 
 namespace {
@@ -41,7 +41,7 @@ void free_decoder(kvx_decoder* d)
     if (d->status) cudaFree(d->status);
     if (d->part_o) cudaFree(d->part_o);
     if (d->part_ml) cudaFree(d->part_ml);
-    if (d->arrived) cudaFree(d->arrived);
+    if (d->split) cudaFree(d->split);
     delete d;
 }
 
@@ -153,7 +153,7 @@ extern "C" KVX_API kvx_status kvx_decoder_create(const kvx_decoder_desc* desc, k
     if (cudaMalloc(&d->turns, sizeof turns) != cudaSuccess || cudaMalloc(&d->status, sizeof(unsigned)) != cudaSuccess ||
         cudaMalloc(&d->part_o, rows * g.head_dim * sizeof(float)) != cudaSuccess ||
         cudaMalloc(&d->part_ml, rows * sizeof(float2)) != cudaSuccess ||
-        cudaMalloc(&d->arrived, kAttendMaxCtas * sizeof(unsigned)) != cudaSuccess) {
+        cudaMalloc(&d->split, kAttendMaxCtas * sizeof(SplitItem)) != cudaSuccess) {
         cudaGetLastError();
         free_decoder(d);
         return fail(KVX_ERR_OOM, "decoder_create: device allocation");
@@ -161,7 +161,6 @@ extern "C" KVX_API kvx_status kvx_decoder_create(const kvx_decoder_desc* desc, k
     cudaError_t e;
     if ((e = cudaMemcpy(d->turns, turns, sizeof turns, cudaMemcpyHostToDevice)) != cudaSuccess ||
         (e = cudaMemset(d->status, 0, sizeof(unsigned))) != cudaSuccess ||
-        (e = cudaMemset(d->arrived, 0, kAttendMaxCtas * sizeof(unsigned))) != cudaSuccess ||
         (e = cudaDeviceSynchronize()) != cudaSuccess) {
         free_decoder(d);
         return fail(KVX_ERR_CUDA, "decoder_create: %s", cudaGetErrorString(e));
@@ -241,7 +240,7 @@ extern "C" KVX_API kvx_status kvx_attend(kvx_decoder* dec, const kvx_new_tokens*
     P.window = opts->window; P.prefix_len = opts->prefix_len;
     P.lse = opts->lse; P.key_weight = opts->key_weight; P.weight_stride = opts->weight_stride;
     P.status = dec->status;
-    P.part_o = dec->part_o; P.part_ml = dec->part_ml; P.arrived = dec->arrived;
+    P.part_o = dec->part_o; P.part_ml = dec->part_ml; P.split = dec->split;
     const cudaError_t e = launch_attend(P, dec->desc.dtype, dec->num_sms, (cudaStream_t)stream, &dec->last_launches);
     if (e != cudaSuccess) return fail(KVX_ERR_CUDA, "attend: launch failed: %s", cudaGetErrorString(e));
     return KVX_OK;

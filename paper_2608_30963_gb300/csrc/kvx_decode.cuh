@@ -45,6 +45,11 @@ struct AppendParams {
 };
 cudaError_t launch_append(const AppendParams& P, int dtype, cudaStream_t stream);
 
+// A row tile and KV head whose tiles several CTAs have, as the CTA where it begins leaves it; parts = 0: none.
+struct SplitItem {
+    int b, rt, h, parts, slot0;
+};
+
 struct AttendParams {
     int T, batch, Hq, H, G, d;
     const int* seq_off;
@@ -62,10 +67,10 @@ struct AttendParams {
     float* key_weight;
     long long weight_stride;
     unsigned* status;
-    // workspace of split rows: two partial results a CTA and one arrival counter
+    // workspace of split rows: two partial results a CTA, and the item that begins in it and goes on in the next
     float* part_o;        // [2 * grid][BM][d]
     float2* part_ml;      // [2 * grid][BM]: running maximum (log2 units) and sum
-    unsigned* arrived;    // [grid], zero between launches
+    SplitItem* split;     // [grid]
 };
 
 struct EvictParams {
@@ -85,7 +90,7 @@ struct EvictParams {
 };
 cudaError_t launch_evict(const EvictParams& P, int dtype, int num_sms, cudaStream_t stream, int* launches);
 
-// Workspace of split rows: rows of partial results (2 x grid x BM, so grids stay within it) and arrival counters.
+// Workspace of split rows: rows of partial results (2 x grid x BM, so grids stay within it) and split items.
 constexpr int kAttendMaxRows = 2 * 152 * 4 * 64;
 constexpr int kAttendMaxCtas = kAttendMaxRows / 2 / 16;
 cudaError_t launch_attend_tc(const AttendParams& P, int num_sms, cudaStream_t stream);
@@ -153,8 +158,8 @@ template <int BM> __device__ __forceinline__ void row_tile_tokens(const AttendPa
 // ------------------------------------------------------------------ the split of the work
 // The work is a line of slot tiles: for each sequence, each row tile, each KV head its tiles in order.
 // CTA c of N takes [c W / N, (c + 1) W / N) of the W tiles, so every CTA has the same number, whatever the
-// lengths; a range may begin and end inside a row's tiles, whose partial results the CTA that
-// arrives last joins in order.  Every CTA finds its range itself: a warp per sequence sums the tiles
+// lengths; a range may begin and end inside a row's tiles, whose partial results a second launch joins
+// in order.  Every CTA finds its range itself: a warp per sequence sums the tiles
 // of its row tiles.
 struct Plan {
     long long W, lo, hi;      // all tiles; this CTA's range
