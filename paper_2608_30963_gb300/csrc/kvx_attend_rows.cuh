@@ -138,7 +138,7 @@ __device__ __forceinline__ void leave_split(const AttendParams& P, const Plan& p
     SplitItem it = {};
     if (have && g.i0 == 0 && !g.whole()) {
         const Parts parts = item_parts(plan, g);
-        it = {g.b, g.rt, g.h, parts.parts, parts.slot0};
+        it = {g.b, g.rt, g.h, parts.parts, parts.slot0, parts.lines};
     }
     P.split[blockIdx.x] = it;
 }
@@ -158,7 +158,7 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Atten
     const Seq s = load_seq(P, it.b);
     const int r = blockIdx.y * RPC + warp / WPR, w0 = warp % WPR;
     const bool real = r < min(BM, s.n * P.G - it.rt * BM);
-    const Parts parts = {(int)blockIdx.x, it.parts, it.slot0};
+    const Parts parts = {(int)blockIdx.x, it.lines, it.parts, it.slot0};
     float m = -INFINITY, l = 0.0f, o[C];
 #pragma unroll
     for (int c = 0; c < C; ++c) o[c] = 0.0f;

@@ -47,7 +47,7 @@ cudaError_t launch_append(const AppendParams& P, int dtype, cudaStream_t stream)
 
 // A row tile and KV head whose tiles several CTAs have, as the CTA where it begins leaves it; parts = 0: none.
 struct SplitItem {
-    int b, rt, h, parts, slot0;
+    int b, rt, h, parts, slot0, lines;
 };
 
 struct AttendParams {
@@ -156,22 +156,32 @@ template <int BM> __device__ __forceinline__ void row_tile_tokens(const AttendPa
 }
 
 // ------------------------------------------------------------------ the split of the work
-// The work is a line of slot tiles: for each sequence, each row tile, each KV head its tiles in order.
-// CTA c of N takes [c W / N, (c + 1) W / N) of the W tiles, so every CTA has the same number, whatever the
-// lengths; a range may begin and end inside a row's tiles, whose partial results a second launch joins
-// in order.  Every CTA finds its range itself: a warp per sequence sums the tiles
-// of its row tiles.
+// The work is a line of slot tiles: for each sequence, each row tile its tiles in order.  A line for each KV head,
+// H CTAs side by side on the same tiles of the H lines (their rows of K and V lie next to one another in
+// memory), so CTA c = k H + h of N H takes [k W / N, (k + 1) W / N) of the W tiles of head h's line; where H does
+// not divide the grid well, one line with the heads of a row tile one after the other.  Every CTA has the
+// same number of tiles, whatever the lengths; a range may begin and end inside a row's tiles, whose partial
+// results a second launch joins in order.  Every CTA finds its range itself: a warp per sequence
+// sums the tiles of its row tiles.
 struct Plan {
-    long long W, lo, hi;      // all tiles; this CTA's range
-    int N;                    // CTAs that have a range: no more than there are tiles
+    long long W, lo, hi;      // tiles of a line; this CTA's range
+    int N;                    // CTAs a line that have a range: no more than there are tiles
+    int lines, line, cta;     // lines; this CTA's line and place on it
     int b, rt;                // row tile of the first one
-    long long at;             // first tile of (b, rt), head 0
+    long long at;             // first tile of (b, rt) on the line
+    __device__ __forceinline__ int heads(int H) const { return lines == 1 ? H : 1; }   // heads one after the other
 };
+__host__ __device__ inline int plan_lines(int grid, int H) { return grid / H * H * 10 >= grid * 9 ? H : 1; }
 
 // sums: shared long long[batch + 1].  All threads call it; returns the same in each.
 template <int BM, int BN, int THREADS>
 __device__ Plan make_plan(const AttendParams& P, long long* sums)
 {
+    Plan p;
+    p.lines = plan_lines(gridDim.x, P.H);
+    p.line = blockIdx.x % p.lines;
+    p.cta = blockIdx.x / p.lines;
+    const int heads = p.heads(P.H);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     for (int b = warp; b < P.batch; b += THREADS / 32) {
         const Seq s = load_seq(P, b);
@@ -184,7 +194,7 @@ __device__ Plan make_plan(const AttendParams& P, long long* sums)
         }
 #pragma unroll
         for (int o = 16; o; o >>= 1) w += __shfl_xor_sync(0xffffffffu, w, o);
-        if (lane == 0) sums[b + 1] = w * P.H;
+        if (lane == 0) sums[b + 1] = w * heads;
     }
     if (threadIdx.x == 0) sums[0] = 0;
     __syncthreads();
@@ -203,13 +213,12 @@ __device__ Plan make_plan(const AttendParams& P, long long* sums)
         }
     }
     __syncthreads();
-    Plan p;
     p.W = sums[P.batch];
-    p.N = (int)min((long long)gridDim.x, p.W);
+    p.N = (int)min((long long)(gridDim.x / p.lines), p.W);
     p.b = 0; p.rt = 0; p.at = 0;
-    if ((int)blockIdx.x >= p.N) { p.lo = p.hi = 0; return p; }
-    p.lo = p.W * blockIdx.x / p.N;
-    p.hi = p.W * (blockIdx.x + 1) / p.N;
+    if (p.cta >= p.N) { p.lo = p.hi = 0; return p; }
+    p.lo = p.W * p.cta / p.N;
+    p.hi = p.W * (p.cta + 1) / p.N;
     int l = 0, h = P.batch - 1;                  // the sequence that holds tile lo
     while (l < h) {
         const int m = (l + h + 1) >> 1;
@@ -224,7 +233,7 @@ __device__ Plan make_plan(const AttendParams& P, long long* sums)
         if (r0 + lane < rts) {
             int ta, tb;
             row_tile_tokens<BM>(P, s, r0 + lane, ta, tb);
-            w = (long long)kv_tiles<BN>(P, s, ta, tb).count * P.H;
+            w = (long long)kv_tiles<BN>(P, s, ta, tb).count * heads;
         }
         long long v = w;
 #pragma unroll
@@ -244,7 +253,7 @@ __device__ Plan make_plan(const AttendParams& P, long long* sums)
     return p;
 }
 
-// CTA that holds tile x of W split over N.
+// CTA of a line that holds tile x of W split over N.
 __device__ __forceinline__ int tile_cta(long long x, long long W, int N)
 {
     int c = (int)((x * N) / W);                  // c W / N <= x up to rounding down
@@ -281,13 +290,14 @@ template <int BM, int BN> struct SegmentWalk {
         g.kv = kv_tiles<BN>(P, g.s, ta, tb);
         g.b = p.b;
         g.rt = p.rt;
-        g.h = (int)((x - p.at) / g.kv.count);
-        g.start = p.at + (long long)g.h * g.kv.count;
+        const int k = (int)((x - p.at) / g.kv.count);
+        g.h = p.lines == 1 ? k : p.line;
+        g.start = p.at + (long long)k * g.kv.count;
         g.i0 = (int)(x - g.start);
         g.n = (int)min((long long)(g.kv.count - g.i0), p.hi - x);
         g.first = x == p.lo;
         x += g.n;
-        if (x == p.at + (long long)g.kv.count * P.H) {
+        if (x == p.at + (long long)g.kv.count * p.heads(P.H)) {
             p.at = x;
             ++p.rt;
         }
@@ -295,18 +305,20 @@ template <int BM, int BN> struct SegmentWalk {
     }
 };
 
-// The partial results of a split item: CTAs c0 .. c0 + parts - 1 hold them, c0's in slot 2 c0 + slot0 and the
-// others' in slot 2 c.
+// The partial results of a split item: the CTAs of places c0 .. c0 + parts - 1 on a line hold them, the first in
+// its slot slot0, the others in their slot 0; CTA c has slots 2 c and 2 c + 1.
 struct Parts {
-    int c0, parts, slot0;
-    __device__ __forceinline__ int slot(int i) const { return i == 0 ? 2 * c0 + slot0 : 2 * (c0 + i); }
+    int cta0, lines, parts, slot0;
+    __device__ __forceinline__ int slot(int i) const { return 2 * (cta0 + i * lines) + (i == 0 ? slot0 : 0); }
 };
 __device__ __forceinline__ Parts item_parts(const Plan& p, const Segment& g)
 {
     Parts r;
-    r.c0 = tile_cta(g.start, p.W, p.N);
-    r.parts = tile_cta(g.start + g.kv.count - 1, p.W, p.N) - r.c0 + 1;
-    r.slot0 = g.start > p.W * r.c0 / p.N;
+    const int c0 = tile_cta(g.start, p.W, p.N);
+    r.lines = p.lines;
+    r.cta0 = c0 * p.lines + p.line;
+    r.parts = tile_cta(g.start + g.kv.count - 1, p.W, p.N) - c0 + 1;
+    r.slot0 = g.start > p.W * c0 / p.N;
     return r;
 }
 
