@@ -388,9 +388,7 @@ cudaError_t launch_attend(const AttendParams& P, int dtype, int num_sms, cudaStr
     *launches = 2;
     if (e != cudaSuccess || !P.key_weight) return e;
     *launches = 3;
-    if (bf16)
-        return P.d == 64 ? run_weight_simt<__nv_bfloat16, 64>(P, num_sms, stream) : P.d == 128 ? run_weight_simt<__nv_bfloat16, 128>(P, num_sms, stream)
-                                                                                  : run_weight_simt<__nv_bfloat16, 256>(P, num_sms, stream);
+    if (bf16) return launch_key_weight(P, num_sms, stream);
     return P.d == 64 ? run_weight_simt<float, 64>(P, num_sms, stream) : P.d == 128 ? run_weight_simt<float, 128>(P, num_sms, stream)
                                                                               : run_weight_simt<float, 256>(P, num_sms, stream);
 }

@@ -19,14 +19,12 @@
 // P is rounded to bf16 for the MMA, as V is.  Where a row sees few slots the roundings of its few weights do
 // not average out, and the error comes near 2^-8 |v|; there, and where the copies bound the kernel
 // anyway (one row tile), P goes in as two bf16 terms, high and low, at the price of a second product.
-#include <cuda.h>
-
 #include <atomic>
 #include <type_traits>
 
 #include "kvx_attend_rows.cuh"
 #include "kvx_kernels.h"
-#include "kvx_tc_common.cuh"
+#include "kvx_umma.cuh"
 
 namespace kvx {
 namespace {
@@ -47,76 +45,6 @@ template <int D, int NT> struct TcShape {
 
 constexpr int kProdWarps = 3, kMmaWarp = 3;
 
-__device__ __forceinline__ void cp_async16_or_zero(uint32_t dst, const void* src, bool real)
-{
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
-}
-// An arrival on the barrier once the thread's copies so far are complete (counted by the barrier as any other).
-__device__ __forceinline__ void cp_async_arrive(uint32_t mbar)
-{
-    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(mbar) : "memory");
-}
-
-// D[tmem] (+)= A[tmem] . B[smem], bf16 inputs, fp32 accumulate
-__device__ __forceinline__ void umma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accumulate)
-{
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
-        "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
-        : "memory");
-}
-// MN-major 128-byte-swizzled operand: lbo between 64-channel blocks, 1024 bytes between 8-row groups.
-__device__ __forceinline__ uint64_t mn_desc(uint32_t saddr, uint32_t lbo)
-{
-    return (uint64_t)((saddr & 0x3FFFFu) >> 4) | (uint64_t)((lbo >> 4) & 0x3FFFu) << 16 | (uint64_t)(1024u >> 4) << 32 |
-           (uint64_t)1 << 46 | (uint64_t)2 << 61;
-}
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* r)
-{
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
-        "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(taddr),
-        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
-        "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]),
-        "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
-        : "memory");
-}
-__device__ __forceinline__ float max3(float a, float b, float c)
-{
-    float r;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
-    return r;
-}
-__device__ __forceinline__ bool elect_one()
-{
-    uint32_t one;
-    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
-    return one != 0;
-}
-// Values a completed load has written: what uses them stays behind this point.
-__device__ __forceinline__ void pin32(uint32_t* r)
-{
-#pragma unroll
-    for (int i = 0; i < 32; i += 8)
-        asm volatile("" : "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3]), "+r"(r[i + 4]), "+r"(r[i + 5]), "+r"(r[i + 6]), "+r"(r[i + 7]));
-}
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
-{
-    unsigned long long r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;"
-        : "=l"(r)
-        : "l"(reinterpret_cast<unsigned long long&>(a)), "l"(reinterpret_cast<unsigned long long&>(b)),
-          "l"(reinterpret_cast<unsigned long long&>(c)));
-    return reinterpret_cast<float2&>(r);
-}
-__device__ __forceinline__ float2 add2(float2 a, float2 b)
-{
-    unsigned long long r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(reinterpret_cast<unsigned long long&>(a)), "l"(reinterpret_cast<unsigned long long&>(b)));
-    return reinterpret_cast<float2&>(r);
-}
 // Bits [a, b) of the 32 columns from `base` on (a, b relative to column 0 of the tile).
 __device__ __forceinline__ uint32_t range_bits(int a, int b, int base)
 {
@@ -152,25 +80,11 @@ struct TileMaps {
     CUtensorMap k, v;
     int box_rows;
 };
-__device__ __forceinline__ void tma_box4(uint32_t dst, const CUtensorMap* map, int x, int y, int z, int w, uint32_t mbar)
-{
-    asm volatile(
-        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(dst),
-        "l"(map), "r"(mbar), "r"(x), "r"(y), "r"(z), "r"(w)
-        : "memory");
-}
-
-// Barriers (8 bytes each) in the control block.
-template <int STAGES> struct Bars {
-    static constexpr int full = 0, empty = STAGES, sfull = 2 * STAGES, pfull = sfull + 2, ofull = pfull + 2, qfull = ofull + 2,
-                         qempty = qfull + 1, done = qempty + 1, mlfull = done + 1, mlempty = mlfull + 1;
-};
-
 // How K and V tiles are brought: row by row (any page size), in groups of 8 rows a fixed stride apart (page sizes that
 // are multiples of 8), or by tensor copies.
 enum Source { kRows, kGroups, kBoxes };
 
-template <int D, int NT, Source SRC>
+template <int D, int NT, Source SRC, bool CAP>
 __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
     attend_tc_kernel(const __grid_constant__ AttendParams P, const __grid_constant__ TileMaps maps)
 {
@@ -500,8 +414,8 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
         if constexpr (C::WG == 2) regs_take<208>();
         const int wg = (warp - 4) >> 2, t = NT == 2 ? wg : 0, quad = warp & 3;
         const uint32_t lanes = tmem + ((uint32_t)(quad * 32) << 16);
-        const float inv_cap = P.cap > 0.0f ? 1.0f / P.cap : 0.0f;
-        const float c = P.cap > 0.0f ? 1.0f : P.scale * kLog2e;   // factor of the (capped) scores in log2 units
+        const float inv_cap = CAP ? 1.0f / P.cap : 0.0f;
+        const float c = CAP ? 1.0f : P.scale * kLog2e;   // factor of the (capped) scores in log2 units
         constexpr bool JOIN = NT == 1 && C::WG == 2;     // two warpgroups on one row tile
         float2* ml = reinterpret_cast<float2*>(smem + 1024) + quad * 32 + lane;
         uint32_t units = 0, items = 0, base_tile = 0, filled[2] = {0, 0};   // filled: times each O has been completed
@@ -544,11 +458,11 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
                 uint32_t x[BN];
                 auto xf = [&](int k) -> float { return __uint_as_float(x[k]); };
 #pragma unroll
-                for (int k = 0; k < BN; k += 32) tmem_ld32(at + k, *reinterpret_cast<uint32_t(*)[32]>(x + k));
+                for (int k = 0; k < BN; k += 32) tmem_ld32_to(x + k, at + k);
                 tmem_ld_wait();
 #pragma unroll
                 for (int k = 0; k < BN; k += 32) pin32(x + k);
-                if (P.cap > 0.0f) {
+                if constexpr (CAP) {
                     bool near = true;                    // all scores where the series holds: no branch per score
 #pragma unroll
                     for (int k = 0; k < BN; ++k) {
@@ -742,22 +656,6 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
     }
 }
 
-using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-EncodeTiled tiled_encoder()
-{
-    static const EncodeTiled fn = [] {
-        void* p = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) != cudaSuccess ||
-            q != cudaDriverEntryPointSuccess)
-            p = nullptr;
-        return (EncodeTiled)p;
-    }();
-    return fn;
-}
-
 // The maps of a call's cache, tiles of bn slots; false where boxes cannot describe it.
 bool make_maps(const AttendParams& P, int bn, TileMaps& m)
 {
@@ -783,9 +681,15 @@ bool make_maps(const AttendParams& P, int bn, TileMaps& m)
 template <int D, int NT, Source SRC> cudaError_t start_tc(const AttendParams& P, const TileMaps& maps, int num_sms, cudaStream_t stream)
 {
     using C = TcShape<D, NT>;
-    if (cudaError_t e = smem_opt_in<attend_tc_kernel<D, NT, SRC>>(C::SMEM); e != cudaSuccess) return e;
     const int grid = min(num_sms, kAttendMaxRows / C::BM / 2);
-    attend_tc_kernel<D, NT, SRC><<<grid, C::THREADS, C::SMEM, stream>>>(P, maps);
+    // the capped scores' code apart: with it the plain kernels would be twice as long
+    if (P.cap > 0.0f) {
+        if (cudaError_t e = smem_opt_in<attend_tc_kernel<D, NT, SRC, true>>(C::SMEM); e != cudaSuccess) return e;
+        attend_tc_kernel<D, NT, SRC, true><<<grid, C::THREADS, C::SMEM, stream>>>(P, maps);
+    } else {
+        if (cudaError_t e = smem_opt_in<attend_tc_kernel<D, NT, SRC, false>>(C::SMEM); e != cudaSuccess) return e;
+        attend_tc_kernel<D, NT, SRC, false><<<grid, C::THREADS, C::SMEM, stream>>>(P, maps);
+    }
     if (cudaError_t e = cudaGetLastError(); e != cudaSuccess) return e;
     return run_join<__nv_bfloat16, D, C::BM>(P, grid, stream);
 }

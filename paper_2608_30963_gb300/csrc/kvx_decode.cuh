@@ -93,6 +93,7 @@ cudaError_t launch_evict(const EvictParams& P, int dtype, int num_sms, cudaStrea
 // Workspace of split rows: rows of partial results (2 x grid x BM, so grids stay within it) and split items.
 constexpr int kAttendMaxRows = 2 * 152 * 4 * 64;
 constexpr int kAttendMaxCtas = kAttendMaxRows / 2 / 16;
+cudaError_t launch_key_weight(const AttendParams& P, int num_sms, cudaStream_t stream);
 cudaError_t launch_attend_tc(const AttendParams& P, int num_sms, cudaStream_t stream);
 cudaError_t launch_attend(const AttendParams& P, int dtype, int num_sms, cudaStream_t stream, int* launches);
 
