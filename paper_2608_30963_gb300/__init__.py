@@ -15,6 +15,7 @@ from __future__ import annotations
 import array
 import ctypes
 import os
+import struct
 import types
 from typing import Optional, Sequence
 
@@ -187,11 +188,10 @@ def lib():
                                               ctypes.POINTER(kvx_dst_kv), VP]
         L.kvx_decoder_create.argtypes = [ctypes.POINTER(kvx_decoder_desc), ctypes.POINTER(VP)]
         L.kvx_decoder_destroy.argtypes = [VP]
-        rows, cache = ctypes.POINTER(kvx_rows), ctypes.POINTER(kvx_dst_kv)
-        L.kvx_append.argtypes = [VP, ctypes.POINTER(kvx_new_tokens), rows, rows, rows, rows, cache, ctypes.c_int32, VP]
-        L.kvx_attend.argtypes = [VP, ctypes.POINTER(kvx_new_tokens), rows, cache, ctypes.c_int32,
-                                 ctypes.POINTER(kvx_attend_opts), rows, VP]
-        L.kvx_evict.argtypes = [VP, ctypes.POINTER(kvx_evict_plan), cache, cache, VP]
+        # struct pointers as void*: ctypes structures by reference, or their bytes
+        L.kvx_append.argtypes = [VP, VP, VP, VP, VP, VP, VP, ctypes.c_int32, VP]
+        L.kvx_attend.argtypes = [VP, VP, VP, VP, ctypes.c_int32, VP, VP, VP]
+        L.kvx_evict.argtypes = [VP, VP, VP, VP, VP]
         L.kvx_decoder_status.argtypes = [VP, VP, ctypes.POINTER(ctypes.c_uint32), ctypes.c_int32]
         L.kvx_decoder_launches.argtypes = [VP]
         L.kvx_decoder_launches.restype = ctypes.c_int32
@@ -490,20 +490,52 @@ def build_alignment(src_seq_off, src_end, tgt_seq_off, tgt_end, span_lo, span_hi
                         _stream(stream))
 
 
-def _rows(t) -> kvx_rows:
+# A decoding step makes a call or two a layer, so their marshalling counts: the C structs are packed as bytes (field
+# by field into ctypes structures they cost 12 us a call more).
+_PACK_ROWS = struct.Struct("@Pqq").pack              # kvx_rows
+_PACK_TOKENS = struct.Struct("@iiPPP").pack          # kvx_new_tokens
+_PACK_OPTS = struct.Struct("@iPPPq").pack            # kvx_attend_opts
+_PACK_CACHE = struct.Struct("@PPiiqqqPiii4x").pack   # kvx_dst_kv
+
+
+def _rows(t) -> bytes:
     """A [tokens, heads, head_dim] tensor (strided; channels contiguous) as kvx_rows."""
-    if t.dim() != 3 or t.stride(2) != 1:
+    st, sh, sc = t.stride()
+    if sc != 1:
         raise ValueError("rows must be [tokens, heads, head_dim] with contiguous channels")
-    return kvx_rows(t.data_ptr(), t.stride(0), t.stride(1))
+    return _PACK_ROWS(t.data_ptr(), st, sh)
 
 
-def _cache(k: Sequence, v: Sequence, page_table, page_size: int, num_pages: int) -> kvx_dst_kv:
-    """Layers of a cache (contiguous [B, H, S, d], or pools [pages, page_size, H, d] with a page table) as kvx_dst_kv."""
-    k0 = k[0]
+def _cache(k: Sequence, v: Sequence, page_table, page_size: int, num_pages: int):
+    """Layers of a cache (contiguous [B, H, S, d], or pools [pages, page_size, H, d] with a page table) as kvx_dst_kv, and
+    what has to live as long."""
+    ptrs = array.array("Q", [t.data_ptr() for t in k])
+    ptrs.extend([t.data_ptr() for t in v])
+    at, k0 = ptrs.buffer_info()[0], k[0]
     if page_table is None:
-        return kvx_dst_kv(_ptr_array(k), _ptr_array(v), 0, k0.shape[2], k0.stride(0), k0.stride(1), k0.stride(2), None, 0, 0, 0)
-    return kvx_dst_kv(_ptr_array(k), _ptr_array(v), 1, 0, 0, 0, 0, page_table.data_ptr(), page_table.shape[1], page_size,
-                      num_pages or k0.shape[0])
+        sb, sh, ss, _ = k0.stride()
+        return _PACK_CACHE(at, at + 8 * len(k), 0, k0.shape[2], sb, sh, ss, 0, 0, 0, 0), ptrs
+    return _PACK_CACHE(at, at + 8 * len(k), 1, 0, 0, 0, 0, page_table.data_ptr(), page_table.shape[1], page_size,
+                       num_pages or k0.shape[0]), ptrs
+
+
+def _raw_stream(stream) -> int:
+    """As _stream; the current stream without a Stream object where torch offers it."""
+    if stream is None and _current_raw_stream:
+        return _current_raw_stream()
+    return _stream(stream)
+
+
+def _find_raw_stream():
+    try:
+        import torch
+        get, device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+        return lambda: get(device())
+    except (ImportError, AttributeError):
+        return None
+
+
+_current_raw_stream = None
 
 
 class Decoder:
@@ -519,27 +551,34 @@ class Decoder:
                  max_position: int = 0):
         self.desc = kvx_decoder_desc(model_geom(geom), int(num_q_heads), dtype, max_position, float(scale), float(score_cap))
         self.geom = geom
+        self._heads, self._dim, self._q_heads = self.desc.model.num_kv_heads, self.desc.model.head_dim, int(num_q_heads)
+        self._size = 2 if dtype == KVX_BF16 else 4
+        global _current_raw_stream
+        _current_raw_stream = _current_raw_stream or _find_raw_stream()
         h = VP()
         _check(lib().kvx_decoder_create(ctypes.byref(self.desc), ctypes.byref(h)))
         self.handle = h.value
 
-    def _fits(self, tokens: int, *rows):
+    def _fits(self, t, tokens: int, heads: int):
         """Rows of one token count, of this decoder's heads, width and element size."""
-        d, size = self.desc.model.head_dim, 2 if self.desc.dtype == KVX_BF16 else 4
-        for t, heads in rows:
-            if tuple(t.shape) != (tokens, heads, d) or t.element_size() != size:
-                raise ValueError(f"rows must be [{tokens}, {heads}, {d}] of {size}-byte elements, got {tuple(t.shape)}")
+        if t.shape != (tokens, heads, self._dim) or t.element_size() != self._size:
+            raise ValueError(f"rows must be [{tokens}, {heads}, {self._dim}] of {self._size}-byte elements, got {tuple(t.shape)}")
 
     def append(self, q, k, v, seq_off, kv_len, cache_k, cache_v, q_out, *, pos=None, page_table=None, page_size: int = 16,
                num_pages: int = 0, stream=None):
         """Rotate the new tokens' q [T, Hq, d] into q_out (q itself: in place) and k [T, H, d] into the cache, and
         write v into the cache.  seq_off int32[B+1]: packed tokens of each sequence; kv_len int32[B]: its
         cached tokens with the new ones; pos int32[T]: RoPE positions (None: the slots)."""
-        T, H, Hq = q.shape[0], self.desc.model.num_kv_heads, self.desc.num_q_heads
-        self._fits(T, (q, Hq), (k, H), (v, H), (q_out, Hq))
-        tok = kvx_new_tokens(seq_off.shape[0] - 1, T, seq_off.data_ptr(), kv_len.data_ptr(), _ptr(pos))
-        cache = _cache((cache_k,), (cache_v,), page_table, page_size, num_pages)
-        _check(lib().kvx_append(self.handle, tok, _rows(q), _rows(k), _rows(v), _rows(q_out), cache, 0, _stream(stream)))
+        T, H, Hq = q.shape[0], self._heads, self._q_heads
+        self._fits(q, T, Hq)
+        self._fits(k, T, H)
+        self._fits(v, T, H)
+        self._fits(q_out, T, Hq)
+        tok = _PACK_TOKENS(seq_off.shape[0] - 1, T, seq_off.data_ptr(), kv_len.data_ptr(), 0 if pos is None else pos.data_ptr())
+        cache, _keep = _cache((cache_k,), (cache_v,), page_table, page_size, num_pages)
+        st = lib().kvx_append(self.handle, tok, _rows(q), _rows(k), _rows(v), _rows(q_out), cache, 0, _raw_stream(stream))
+        if st:
+            _check(st)
 
     def attend(self, q, seq_off, kv_len, cache_k, cache_v, out, *, window: int = 0, prefix_len=None, lse=None, key_weight=None,
                page_table=None, page_size: int = 16, num_pages: int = 0, stream=None):
@@ -547,18 +586,21 @@ class Decoder:
         window: slots a token sees up to its own (0: all); prefix_len int32[B]: slots every token sees;
         lse float32[T, Hq]: log-sum-exp of each row; key_weight float32[B, H, S]: has the attention weights
         each slot receives added to it (needs lse)."""
-        T, Hq = q.shape[0], self.desc.num_q_heads
-        self._fits(T, (q, Hq), (out, Hq))
+        T, Hq, B = q.shape[0], self._q_heads, seq_off.shape[0] - 1
+        self._fits(q, T, Hq)
+        self._fits(out, T, Hq)
         if lse is not None and not (lse.shape == (T, Hq) and lse.is_contiguous() and lse.element_size() == 4):
             raise ValueError("lse must be contiguous float32 [tokens, query heads]")
-        B = seq_off.shape[0] - 1
-        if key_weight is not None and not (key_weight.shape[:2] == (B, self.desc.model.num_kv_heads) and key_weight.is_contiguous()
+        if key_weight is not None and not (key_weight.shape[:2] == (B, self._heads) and key_weight.is_contiguous()
                                            and key_weight.element_size() == 4):
             raise ValueError("key_weight must be contiguous float32 [sequences, KV heads, slots]")
-        tok = kvx_new_tokens(B, T, seq_off.data_ptr(), kv_len.data_ptr(), None)
-        opts = kvx_attend_opts(window, _ptr(prefix_len), _ptr(lse), _ptr(key_weight), 0 if key_weight is None else key_weight.shape[2])
-        cache = _cache((cache_k,), (cache_v,), page_table, page_size, num_pages)
-        _check(lib().kvx_attend(self.handle, tok, _rows(q), cache, 0, opts, _rows(out), _stream(stream)))
+        tok = _PACK_TOKENS(B, T, seq_off.data_ptr(), kv_len.data_ptr(), 0)
+        opts = _PACK_OPTS(window, 0 if prefix_len is None else prefix_len.data_ptr(), 0 if lse is None else lse.data_ptr(),
+                          0 if key_weight is None else key_weight.data_ptr(), 0 if key_weight is None else key_weight.shape[2])
+        cache, _keep = _cache((cache_k,), (cache_v,), page_table, page_size, num_pages)
+        st = lib().kvx_attend(self.handle, tok, _rows(q), cache, 0, opts, _rows(out), _raw_stream(stream))
+        if st:
+            _check(st)
 
     def evict(self, kv_len, key_weight, keep: int, src_k: Sequence, src_v: Sequence, dst_k: Sequence, dst_v: Sequence, kept, new_len, *,
               sinks: int = 0, recent: int = 0, kept_weight=None, page_table=None, dst_page_table=None, page_size: int = 16,
@@ -566,7 +608,7 @@ class Decoder:
         """Cut the cache (lists of layers) down to `keep` slots per sequence, KV head and layer, by key_weight float32[L, B, H, S]:
         rows into dst_k / dst_v, their slots into kept int32[L, B, H, keep] (-1 past the end), the lengths
         into new_len int32[B], the weights into kept_weight float32[L, B, H, >= keep]."""
-        L, B, H = len(src_k), kv_len.shape[0], self.desc.model.num_kv_heads
+        L, B, H = len(src_k), kv_len.shape[0], self._heads
         if not (tuple(key_weight.shape[:3]) == (L, B, H) and key_weight.is_contiguous() and key_weight.element_size() == 4):
             raise ValueError(f"key_weight must be contiguous float32 [{L}, {B}, {H}, slots]")
         if not (tuple(kept.shape) == (L, B, H, keep) and kept.is_contiguous() and kept.element_size() == 4):
@@ -578,9 +620,9 @@ class Decoder:
             raise ValueError("src_k, src_v, dst_k and dst_v must have as many layers as one another")
         plan = kvx_evict_plan(B, L, kv_len.data_ptr(), key_weight.data_ptr(), key_weight.shape[3], keep, sinks, recent, kept.data_ptr(),
                               new_len.data_ptr(), _ptr(kept_weight), 0 if kept_weight is None else kept_weight.shape[3])
-        src = _cache(src_k, src_v, page_table, page_size, num_pages)
-        dst = _cache(dst_k, dst_v, dst_page_table, page_size, dst_num_pages)
-        _check(lib().kvx_evict(self.handle, plan, src, dst, _stream(stream)))
+        src, _keep_src = _cache(src_k, src_v, page_table, page_size, num_pages)
+        dst, _keep_dst = _cache(dst_k, dst_v, dst_page_table, page_size, dst_num_pages)
+        _check(lib().kvx_evict(self.handle, ctypes.byref(plan), src, dst, _raw_stream(stream)))
 
     def device_status(self, stream=None, clear: bool = True) -> int:
         bits = ctypes.c_uint32(0)

@@ -378,16 +378,23 @@ template <int D> cudaError_t run_fp32(const AttendParams& P, int num_sms, cudaSt
 
 }  // namespace
 
-cudaError_t launch_attend(const AttendParams& P, int dtype, int num_sms, cudaStream_t stream, int* launches)
+cudaError_t launch_attend(const AttendParams& call, int dtype, int num_sms, cudaStream_t stream, int* launches)
 {
     *launches = 0;
-    if (P.T == 0) return cudaSuccess;
+    if (call.T == 0) return cudaSuccess;
+    AttendParams P = call;
     const bool bf16 = dtype == KVX_BF16;
+    // Weight sums of few rows (16 a sequence and KV head) add up the scores that the attention leaves, where they fit
+    // the workspace: 8 bytes a score are less than a slot's K.  Else the scores are formed again.
+    P.scores_stride = (P.weight_stride + 63) / 64 * 64;
+    const bool keep = bf16 && P.key_weight && (long long)P.T * P.G <= 16ll * P.batch && (long long)P.T * P.Hq * P.scores_stride <= kAttendScores;
+    if (!keep) P.scores = nullptr;
     cudaError_t e = bf16 ? launch_attend_tc(P, num_sms, stream)
                          : P.d == 64 ? run_fp32<64>(P, num_sms, stream) : P.d == 128 ? run_fp32<128>(P, num_sms, stream) : run_fp32<256>(P, num_sms, stream);
     *launches = 2;
     if (e != cudaSuccess || !P.key_weight) return e;
     *launches = 3;
+    if (keep) return launch_sum_scores(P, stream);
     if (bf16) return launch_key_weight(P, num_sms, stream);
     return P.d == 64 ? run_weight_simt<float, 64>(P, num_sms, stream) : P.d == 128 ? run_weight_simt<float, 128>(P, num_sms, stream)
                                                                               : run_weight_simt<float, 256>(P, num_sms, stream);

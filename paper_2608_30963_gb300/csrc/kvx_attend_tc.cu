@@ -1,714 +1,11 @@
-// kvx_attend_tc.cu -- attention of new tokens over a bf16 cache on the tensor cores (tcgen05).
-//
-//   S = Q K^T (fp32, TMEM),  P = exp2(c S - m),  O += P V (P bf16 from TMEM, O fp32 in TMEM)
-// in one pass over the slots, with the running maximum m and sum l of a row in the registers of the thread
-// that owns the row.  A CTA holds NT tiles of 128 rows and walks slot tiles of BN.
-//   producer warps (3)  copy Q, K and V rows into 128-byte-swizzled tiles.  Q: 16-byte cp.async.  K and V: one
-//                       tensor copy (TMA) for each page, or for a whole tile of a contiguous cache, by one
-//                       warp, a box a lane; caches that boxes of 8 or more rows cannot describe (odd page
-//                       sizes) take cp.async too.  A K tile is read as a K-major operand, a V tile, laid
-//                       out alike, as an MN-major one.
-//   MMA thread          unit u = (slot tile, row tile): S(u) into score buffer u mod 2, then, when P(u)
-//                       is there, O += P(u) V; S(u + 2) is issued right behind it, so that the scores of
-//                       one unit are formed while the other's softmax runs.
-//   softmax warps       two warpgroups, for units of even and odd u: a row tile each (NT = 2), or every other
-//                       slot tile of the one row tile (NT = 1), each with its own maximum, sum and O,
-//                       which the first joins at the end (heads of 256, whose two O would not fit
-//                       TMEM: one warpgroup).  P takes the place of S.  O is rescaled only when a row's maximum has grown by more than
-//                       2^8 since the last time.
-// P is rounded to bf16 for the MMA, as V is.  Where a row sees few slots the roundings of its few weights do
-// not average out, and the error comes near 2^-8 |v|; there, and where the copies bound the kernel
-// anyway (one row tile), P goes in as two bf16 terms, high and low, at the price of a second product.
-#include <atomic>
-#include <type_traits>
-
-#include "kvx_attend_rows.cuh"
-#include "kvx_kernels.h"
-#include "kvx_umma.cuh"
+// kvx_attend_tc.cu -- the attention kernels on the tensor cores, plain scores.
+#include "kvx_attend_tc.cuh"
 
 namespace kvx {
-namespace {
-
-template <int D, int NT> struct TcShape {
-    static constexpr int BM = 128 * NT, BN = NT == 1 ? 64 : 128, NB = 2 / NT;
-    static constexpr int WG = D == 256 ? 1 : 2;            // softmax warpgroups
-    static constexpr int TILE = BN * D * 2, QB = BM * D * 2;
-    static constexpr int CTRL = 2048;                      // barriers and flags; (m, l) of the second warpgroup's rows
-    static constexpr int STAGES = (kSmemMax - CTRL - QB) / TILE < 12 ? (kSmemMax - CTRL - QB) / TILE : 12;
-    static constexpr int THREADS = 128 + 128 * WG;
-    static constexpr int S_COL = BN, O_COL = 2 * BN;       // TMEM columns: scores u mod 2, then the O tiles
-    static constexpr int TMEM = 512;
-    static constexpr int SMEM = CTRL + QB + STAGES * TILE;
-    static_assert(SMEM <= kSmemMax && O_COL + WG * D <= TMEM);
-    static_assert((kMaxAttendBatch + 2) * 8 <= STAGES * TILE);   // the plan's sums lie where the tiles come later
-};
-
-constexpr int kProdWarps = 3, kMmaWarp = 3;
-
-// Bits [a, b) of the 32 columns from `base` on (a, b relative to column 0 of the tile).
-__device__ __forceinline__ uint32_t range_bits(int a, int b, int base)
-{
-    const int lo = max(a - base, 0), hi = min(b - base, 32);
-    if (hi <= lo) return 0u;
-    return (hi == 32 ? 0xffffffffu : (1u << hi) - 1u) & ~((1u << lo) - 1u);
-}
-
-// Registers of a thread once the warps have taken their parts (two softmax warpgroups: 384 threads launched with 168):
-// 128 x 88 + 256 x 208 = 384 x 168.
-template <int N> __device__ __forceinline__ void regs_give() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
-template <int N> __device__ __forceinline__ void regs_take() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
-
-constexpr int kFewSlots = 512;   // rows that see fewer slots get their weights in two terms
-
-// Sequences of up to 128 rows a KV head: one row tile, bound by the copies.
-__host__ __device__ __forceinline__ bool one_tile(const AttendParams& P) { return (long long)P.T * P.G <= 128ll * P.batch; }
-
-// Whether an item's weights are multiplied in two terms: its first token sees fewest slots.
-template <int D, int BM, int NT> __device__ __forceinline__ bool two_terms(const AttendParams& P, const Segment& g)
-{
-    if constexpr (NT == 1 && D < 256) return true;
-    if (NT == 1 && one_tile(P)) return true;
-    int ta, tb;
-    row_tile_tokens<BM>(P, g.s, g.rt, ta, tb);
-    const int own = g.s.slot(ta);
-    return own < kFewSlots || (P.window > 0 && P.window < kFewSlots);
-}
-
-// Tensor maps of K and V, and the rows of a box: a paged cache as (channel, head, slot in page, page), a
-// contiguous one as (channel, slot, head, sequence); boxes of 64 channels of one head.
-struct TileMaps {
-    CUtensorMap k, v;
-    int box_rows;
-};
-// How K and V tiles are brought: row by row (any page size), in groups of 8 rows a fixed stride apart (page sizes that
-// are multiples of 8), or by tensor copies.
-enum Source { kRows, kGroups, kBoxes };
-
-template <int D, int NT, Source SRC, bool CAP>
-__global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
-    attend_tc_kernel(const __grid_constant__ AttendParams P, const __grid_constant__ TileMaps maps)
-{
-    using C = TcShape<D, NT>;
-    using B = Bars<C::STAGES>;
-    constexpr bool TMA = SRC == kBoxes;
-    constexpr int BM = C::BM, BN = C::BN;
-    extern __shared__ __align__(1024) uint8_t smem[];
-    const uint32_t s0 = smem_u32(smem);
-    auto bar = [&](int i) { return s0 + (uint32_t)i * 8; };
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + 512);
-    int* abort = reinterpret_cast<int*>(smem + 516);
-    const uint32_t sQ = s0 + C::CTRL, sT = sQ + C::QB;
-    const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
-
-    if (warp == kMmaWarp) tmem_alloc(smem_u32(tmem_slot), C::TMEM);
-    if (threadIdx.x == 0) {
-        for (int i = 0; i < C::STAGES; ++i) {
-            mbar_init(bar(B::full + i), TMA ? 1 : NT == 2 ? kProdWarps * 32 : 32);
-            mbar_init(bar(B::empty + i), 1);
-        }
-        for (int i = 0; i < 2; ++i) {
-            mbar_init(bar(B::sfull + i), 1);
-            mbar_init(bar(B::pfull + i), 4);
-            mbar_init(bar(B::ofull + i), 1);
-        }
-        mbar_init(bar(B::qfull), kProdWarps * 32);
-        mbar_init(bar(B::qempty), 1);
-        mbar_init(bar(B::done), 1);
-        mbar_init(bar(B::mlfull), 4);
-        mbar_init(bar(B::mlempty), 4);
-        fence_mbar_init();
-        *abort = 0;
-    }
-    const Plan plan = make_plan<BM, BN, C::THREADS>(P, reinterpret_cast<long long*>(smem + C::CTRL + C::QB));
-    __syncthreads();
-    tc_fence_after();
-    const uint32_t tmem = *tmem_slot;
-    const Waiter W{abort, P.status};
-    SegmentWalk<BM, BN> walk(P, plan);
-    Segment g;
-
-    if (warp < 4) {
-    if constexpr (C::WG == 2) regs_give<88>();
-    if (warp < kProdWarps) {
-        // ---------------------------------------------------------------- producers
-        constexpr int CPR = D / 8;                       // 16-byte chunks of a row
-        constexpr int RPI = CPR < 32 ? 32 / CPR : 1;     // rows a warp copies with one instruction
-        const int sub = lane / CPR;
-        const uint32_t place = (uint32_t)((lane % CPR >> 3)), c0 = (uint32_t)(((lane % CPR & 7) ^ sub) << 4);
-        uint32_t pos = 0, items = 0;                     // tiles issued; items begun
-        bool ok = true;
-        auto wait = [&](int b, uint32_t parity) { ok = __all_sync(0xffffffffu, ok && W.wait(bar(b), parity)); };
-        // The copies of a batch announce themselves: each thread's arrival follows its own copies.  The MMA warp
-        // orders them before its reads (fence_proxy_async after the wait).
-        // The warps share a tile of R rows as 3/8, 3/8 and 2/8 of them; lane l has its warp's rows l and 32 + l.
-        struct Rows {
-            long long a, b;                              // element offsets, -1: a row of zeros
-        };
-        auto find_rows = [&](auto R, auto off) {
-            constexpr int SHARE = decltype(R)::value * 3 / 8;
-            const int r0 = warp * SHARE;
-            Rows x;
-            x.a = r0 + lane < decltype(R)::value ? off(r0 + lane) : -1ll;
-            x.b = SHARE > 32 && r0 + 32 + lane < decltype(R)::value ? off(r0 + 32 + lane) : -1ll;
-            return x;
-        };
-        auto copy_rows = [&](auto R, uint32_t base, const __nv_bfloat16* src, const Rows& x, int colblk) {
-            constexpr int SHARE = decltype(R)::value * 3 / 8;
-            const uint32_t d0 = base + place * colblk + (uint32_t)(warp * SHARE + sub) * 128;
-            const __nv_bfloat16* s1 = src + lane % CPR * 8;
-#pragma unroll
-            for (int r = 0; r < SHARE; r += RPI) {
-                if (warp == 2 && r >= decltype(R)::value / 4) break;
-                const long long at = __shfl_sync(0xffffffffu, r < 32 ? x.a : x.b, (r & 31) + sub);
-                cp_async16_or_zero(d0 + (uint32_t)r * 128 + (c0 ^ (uint32_t)((r & 7) << 4)), s1 + (at < 0 ? 0 : at), at >= 0);
-            }
-        };
-        using Int128 = std::integral_constant<int, 128>;
-        while (walk.next(g)) {
-            const int rows = min(BM, g.s.n * P.G - g.rt * BM);
-            if (items > 0) wait(B::qempty, (items - 1) & 1);
-            for (int part = 0; part < NT; ++part) {
-                const Rows x = find_rows(Int128{}, [&](int r) {
-                    if (part * 128 + r >= rows) return -1ll;
-                    const RowId id = row_id(P, g.s, g.h, g.rt * BM + part * 128 + r);
-                    return (long long)(g.s.t0 + id.t) * P.q_t + (long long)id.head * P.q_h;
-                });
-                if (ok) copy_rows(Int128{}, sQ + part * (128 * D * 2), (const __nv_bfloat16*)P.q, x, 128 * 128);
-            }
-            cp_async_arrive(bar(B::qfull));
-            ++items;
-            const long long head = cache_head(P.cache) * g.h;
-            // tile i as K, tile i - NB + 1 as V, and at the end the V tiles left
-            if constexpr (TMA) {
-                if (warp > 0) continue;
-                // Lane r looks up the page of box r of the next tile while this one is issued; the issue itself is
-                // uniform (a lane of its own would take each copy's operands through uniform registers).
-                const int n = __shfl_sync(0xffffffffu, g.n, 0), b = __shfl_sync(0xffffffffu, g.b, 0), h = __shfl_sync(0xffffffffu, g.h, 0);
-                auto tile_slot = [&](int t) { return __shfl_sync(0xffffffffu, g.kv.at(g.i0 + t) * BN, 0); };
-                auto pages = [&](int t) {
-                    int page = -1;                       // outside the pool: the box is filled with zeros
-                    const int j = tile_slot(t) + lane * maps.box_rows;
-                    if (P.cache.paged && lane * maps.box_rows < BN && j < g.s.L) {
-                        const int pi = j >> P.cache.page_shift;
-                        if (pi < P.cache.max_pages) page = __ldg(&P.cache.page_table[(size_t)b * P.cache.max_pages + pi]);
-                        if (page < 0 || page >= P.cache.num_pages) {
-                            page = -1;
-                            set_status(P.status, KVX_DEV_PAGE_INVALID);
-                        }
-                    }
-                    return page;
-                };
-                int page_k = pages(0), page_v = page_k;  // of the tiles to be issued next as K and as V
-                for (int i = 0; i < n + C::NB - 1; ++i) {
-                    const int ahead = i + 1 < n ? pages(i + 1) : -1;
-#pragma unroll
-                    for (int kv = 0; kv < 2; ++kv) {
-                        const int t = kv ? i - (C::NB - 1) : i;
-                        if (t < 0 || t >= n) continue;
-                        const int j0 = tile_slot(t), page = kv ? (C::NB == 1 ? page_k : page_v) : page_k;
-                        const uint32_t st = pos % C::STAGES, ph = (pos / C::STAGES) & 1;
-                        ok = __all_sync(0xffffffffu, ok && W.wait(bar(B::empty + st), ph ^ 1));
-                        ++pos;
-                        if (!ok) continue;
-                        const uint32_t dst = sT + st * C::TILE, full = bar(B::full + st);
-                        const CUtensorMap* map = kv ? &maps.v : &maps.k;
-                        if (elect_one()) mbar_arrive_expect_tx(full, C::TILE);
-                        for (int r = 0; r < BN; r += maps.box_rows) {
-                            const int pg = __shfl_sync(0xffffffffu, page, r / maps.box_rows);
-                            const int in = (j0 + r) & (P.cache.page_size - 1);
-                            if (elect_one()) {
-#pragma unroll
-                                for (int cb = 0; cb < D / 64; ++cb) {
-                                    const uint32_t to = dst + (uint32_t)(cb * (BN * 128) + r * 128);
-                                    if (P.cache.paged) tma_box4(to, map, cb * 64, h, in, pg, full);
-                                    else tma_box4(to, map, cb * 64, j0 + r, h, b, full);
-                                }
-                            }
-                        }
-                        __syncwarp();
-                    }
-                    page_v = page_k;
-                    page_k = ahead;
-                }
-            } else {
-                // One row tile: each warp takes every third tile (a part of every tile each would spend most of its time on
-                // what a tile costs anyway: 32768 slots x 8, heads of 128: 160 us, 132 so).  Two row tiles, whose
-                // larger tiles leave few in the ring: the warps share each, so that it is there sooner (4096
-                // tokens over 32768 slots: 1.75 ms, 1.48 so).  The next tile's pages are read while this one's copies
-                // are issued, and looked at only then.
-                constexpr bool SHARED = NT == 2;
-                constexpr int PER = SRC == kGroups ? 8 : 1;      // rows a stride apart: a lane finds the first of them
-                constexpr int PART = SHARED ? BN * 3 / 8 : BN;   // rows of a tile a warp copies at most
-                constexpr int FIND = PART / PER;
-                constexpr int LOOK = (FIND + 31) / 32;
-                // a warp's part of a shared tile: 3/8, 3/8 and 2/8 of its groups of 8 rows
-                const int q0 = SHARED ? warp * (PART / 8) : 0;
-                const long long stride = P.cache.paged ? (long long)P.cache.H * D : P.cache.st;
-                const long long mine = head + (PER > 1 ? sub * stride : 0) + lane % CPR * 8;
-                const int total = 2 * g.n;
-                // tile r of the item in the order of the ring: K or V, and the slot tile
-                auto tile_of = [&](int r, int& kv) {
-                    if (C::NB == 1) {
-                        kv = r & 1;
-                        return r >> 1;
-                    }
-                    kv = r == total - 1 || (r > 0 && !(r & 1));
-                    return r == total - 1 ? g.n - 1 : kv ? (r >> 1) - 1 : (r + 1) >> 1;
-                };
-                auto pages_of = [&](int r, int (&x)[LOOK]) {
-                    int kv;
-                    const int j0 = r < total ? g.kv.at(g.i0 + tile_of(r, kv)) * BN + q0 * 8 : g.s.L;
-#pragma unroll
-                    for (int k = 0; k < LOOK; ++k) {
-                        const int j = j0 + (k * 32 + lane) * PER;
-                        x[k] = -2;                               // past the end
-                        if (k * 32 + lane < FIND && j < g.s.L) {
-                            x[k] = 0;
-                            if (P.cache.paged) {
-                                const int pi = P.cache.page_shift >= 0 ? j >> P.cache.page_shift : j / P.cache.page_size;
-                                x[k] = pi < P.cache.max_pages ? __ldg(&P.cache.page_table[(size_t)g.b * P.cache.max_pages + pi]) : -1;
-                            }
-                        }
-                    }
-                };
-                auto row_at = [&](int j, int page) -> long long {
-                    if (page == -2) return -1;
-                    if (!P.cache.paged) return (long long)g.b * P.cache.sb + (long long)j * P.cache.st;
-                    if (page < 0 || page >= P.cache.num_pages) {
-                        set_status(P.status, KVX_DEV_PAGE_INVALID);
-                        return -1;
-                    }
-                    const int in = P.cache.page_shift >= 0 ? j & (P.cache.page_size - 1) : j % P.cache.page_size;
-                    return ((long long)page * P.cache.page_size + in) * stride;
-                };
-                int next[LOOK];
-                constexpr int STEP = SHARED ? 1 : kProdWarps;
-                int r = SHARED ? 0 : (int)((kProdWarps + (uint32_t)warp - pos % kProdWarps) % kProdWarps);
-                pages_of(r, next);
-                for (; r < total; r += STEP) {
-                    int kv;
-                    const int j0 = g.kv.at(g.i0 + tile_of(r, kv)) * BN;
-                    const __nv_bfloat16* src = (const __nv_bfloat16*)(kv ? P.cv : P.ck);
-                    const uint32_t p = pos + (uint32_t)r, st = p % C::STAGES, ph = (p / C::STAGES) & 1;
-                    long long at[LOOK];
-#pragma unroll
-                    for (int k = 0; k < LOOK; ++k) at[k] = row_at(j0 + q0 * 8 + (k * 32 + lane) * PER, next[k]);
-                    pages_of(r + STEP, next);
-                    wait(B::empty + (int)st, ph ^ 1);
-                    if (ok) {
-                        const uint32_t d0 = sT + st * C::TILE + place * (BN * 128) + (uint32_t)(q0 * 1024 + sub * 128);
-                        if constexpr (SRC == kGroups) {
-#pragma unroll
-                            for (int q = 0; q < PART / 8; ++q) {
-                                if (SHARED && warp == 2 && q >= BN / 32) break;
-                                const long long first = __shfl_sync(0xffffffffu, at[0], q);
-                                const int left = g.s.L - (j0 + (q0 + q) * 8);   // rows of the sequence from here on
-                                const __nv_bfloat16* s1 = src + first + mine;
-                                if (first >= 0 && left >= 8) {
-#pragma unroll
-                                    for (int k = 0; k < 8; k += RPI)
-                                        cp_async16(d0 + (uint32_t)(q * 1024 + k * 128) + (c0 ^ (uint32_t)(k << 4)), s1 + k * stride);
-                                } else {
-#pragma unroll
-                                    for (int k = 0; k < 8; k += RPI) {
-                                        const bool real = first >= 0 && k + sub < left;
-                                        cp_async16_or_zero(d0 + (uint32_t)(q * 1024 + k * 128) + (c0 ^ (uint32_t)(k << 4)), real ? s1 + k * stride : src,
-                                                           real);
-                                    }
-                                }
-                            }
-                        } else {
-#pragma unroll
-                            for (int k = 0; k < PART; k += RPI) {
-                                if (SHARED && warp == 2 && k >= BN / 4) break;
-                                const long long row = __shfl_sync(0xffffffffu, at[k / 32], (k & 31) + sub);
-                                cp_async16_or_zero(d0 + (uint32_t)k * 128 + (c0 ^ (uint32_t)((k & 7) << 4)), row < 0 ? src : src + row + mine, row >= 0);
-                            }
-                        }
-                    }
-                    cp_async_arrive(bar(B::full + (int)st));
-                }
-                pos += (uint32_t)total;
-            }
-        }
-    } else {
-        // ---------------------------------------------------------------- MMA
-        // The whole warp walks and waits, so that stages and descriptors stay in uniform registers (a lane of its own
-        // moves every operand there first: 120 clocks an MMA instead of 64); one lane issues.
-        constexpr uint32_t idesc_s = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
-        constexpr uint32_t idesc_o = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
-        // Two row tiles and asynchronous thread copies: a slot tile's V and the next one's K are waited for, and fenced,
-        // while the first unit's softmax runs (behind it the fences stood in the MMAs' way: 150 clocks each).
-        constexpr bool EARLY = !TMA && NT == 2;
-        const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
-        uint32_t base = 0, units = 0, items = 0;         // tiles and units of the items before; items begun
-        bool ok = true;
-        auto wait = [&](int b, uint32_t parity) { ok = __all_sync(0xffffffffu, ok && W.wait(bar(b), parity)); };
-        while (ok && walk.next(g)) {
-            const int n = __shfl_sync(0xffffffffu, g.n, 0), U = n * NT;
-            const bool two = __shfl_sync(0xffffffffu, (int)two_terms<D, BM, NT>(P, g), 0);
-            auto scores = [&](int u) {
-                const int i = u / NT, t = u - i * NT;
-                const uint32_t p = base + (uint32_t)(C::NB == 1 ? 2 * i : i == 0 ? 0 : 2 * i - 1), st = p % C::STAGES;
-                if (u == 0) wait(B::qfull, items & 1);
-                if (t == 0 && !(EARLY && u > 0)) wait(B::full + (int)st, (p / C::STAGES) & 1);
-                if (!ok) return;
-                if (u == 0 || (!TMA && !EARLY && t == 0)) fence_proxy_async();
-                tc_fence_after();
-                const uint32_t d = tm + ((units + u) & 1) * C::S_COL;
-                // descriptors count 16-byte units in their low bits: steps along an operand are added
-                const uint64_t qd = sw128_desc(sQ + t * (128 * D * 2)), kd = sw128_desc(sT + st * C::TILE);
-                if (elect_one()) {
-#pragma unroll
-                    for (int k = 0; k < D / 16; ++k)
-                        umma_bf16(d, qd + (k >> 2) * (128 * 128 / 16) + (k & 3) * 2, kd + (k >> 2) * (BN * 128 / 16) + (k & 3) * 2, idesc_s, k > 0);
-                    if (t == NT - 1) umma_commit(bar(B::empty + st));
-                    if (u == U - 1) umma_commit(bar(B::qempty));
-                    umma_commit(bar(B::sfull + ((units + u) & 1)));
-                }
-                __syncwarp();
-            };
-            scores(0);
-            if (U > 1) scores(1);
-            for (int u = 0; u < U && ok; ++u) {
-                const int i = u / NT, t = u - i * NT;
-                const uint32_t gu = units + u;
-                const uint32_t p = base + (uint32_t)(C::NB == 1 || i == n - 1 ? 2 * i + 1 : 2 * i + 2), st = p % C::STAGES;
-                if (EARLY && t == 0) {
-                    wait(B::full + (int)st, (p / C::STAGES) & 1);
-                    if (i + 1 < n) wait(B::full + (int)((p + 1) % C::STAGES), ((p + 1) / C::STAGES) & 1);
-                    fence_proxy_async();
-                }
-                wait(B::pfull + (int)(gu & 1), (gu >> 1) & 1);
-                if (!EARLY && t == 0) wait(B::full + (int)st, (p / C::STAGES) & 1);
-                if (!ok) break;
-                if (!TMA && !EARLY && t == 0) fence_proxy_async();
-                tc_fence_after();
-                const uint64_t vd = mn_desc(sT + st * C::TILE, BN * 128);
-                const uint32_t wg = C::WG == 2 ? gu & 1 : 0;
-                const uint32_t od = tm + C::O_COL + wg * D, pd = tm + (gu & 1) * C::S_COL;
-                if (elect_one()) {
-#pragma unroll
-                    for (int k = 0; k < BN / 16; ++k) umma_bf16_ts(od, pd + k * 8, vd + k * (2048 / 16), idesc_o, u >= C::WG || k > 0);
-                    if (two)
-#pragma unroll
-                        for (int k = 0; k < BN / 16; ++k) umma_bf16_ts(od, pd + BN / 2 + k * 8, vd + k * (2048 / 16), idesc_o, 1);
-                    if (t == NT - 1) umma_commit(bar(B::empty + st));
-                    if (u >= U - C::WG) umma_commit(bar(B::ofull + wg));
-                }
-                __syncwarp();
-                if (u + 2 < U) scores(u + 2);
-            }
-            base += 2 * (uint32_t)n;
-            units += (uint32_t)U;
-            ++items;
-        }
-        // every MMA issued has completed before TMEM is freed
-        if (elect_one()) umma_commit(bar(B::done));
-        const unsigned long long t0 = globaltimer();
-        while (!mbar_try_wait(bar(B::done), 0) && globaltimer() - t0 < kWaitNs) {}
-        __syncwarp();
-    }
-    } else {
-        // ---------------------------------------------------------------- softmax
-        if constexpr (C::WG == 2) regs_take<208>();
-        const int wg = (warp - 4) >> 2, t = NT == 2 ? wg : 0, quad = warp & 3;
-        const uint32_t lanes = tmem + ((uint32_t)(quad * 32) << 16);
-        const float inv_cap = CAP ? 1.0f / P.cap : 0.0f;
-        const float c = CAP ? 1.0f : P.scale * kLog2e;   // factor of the (capped) scores in log2 units
-        constexpr bool JOIN = NT == 1 && C::WG == 2;     // two warpgroups on one row tile
-        float2* ml = reinterpret_cast<float2*>(smem + 1024) + quad * 32 + lane;
-        uint32_t units = 0, items = 0, base_tile = 0, filled[2] = {0, 0};   // filled: times each O has been completed
-        bool ok = true;                                  // the same in the lanes of a warp
-        auto wait = [&](int b, uint32_t parity) { ok = __all_sync(0xffffffffu, ok && W.wait(bar(b), parity)); };
-        bool have = false;
-        while (walk.next(g)) {
-            have = true;
-            const int row = g.rt * BM + t * 128 + quad * 32 + lane;
-            const bool real = row < g.s.n * P.G;
-            const int own = real ? g.s.slot(row / P.G) : -1;     // rows past the end see nothing
-            const int hi = min(own + 1, g.s.L), lo = max(window_lo(P, own), 0), pre = real ? g.s.pre : 0;
-            const bool two = two_terms<D, BM, NT>(P, g);
-            const int U = g.n * NT;
-            const int u0 = C::WG == 1 ? 0 : NT == 2 ? t : (int)((units + (uint32_t)wg) & 1);   // this warpgroup's first unit
-            float m = -INFINITY, l = 0.0f;
-            if (JOIN && wg == 1 && items > 0) wait(B::mlempty, (items - 1) & 1);   // its sums of the last item are read
-            for (int u = u0; u < U; u += C::WG) {
-                const int i = u / NT;
-                const uint32_t gu = units + (uint32_t)u;
-                wait(B::sfull + (gu & 1), (gu >> 1) & 1);
-                if (!ok) break;
-                tc_fence_after();
-                const uint32_t at = lanes + (gu & 1) * C::S_COL;
-                const int j0 = g.kv.at(g.i0 + i) * BN;
-                if (TMA && j0 + BN > g.s.L && (NT == 1 || t == 0)) {
-                    // the boxes brought what the cache holds past the sequence's end: zeros in V's place, before
-                    // any P is announced for it
-                    const uint32_t p = base_tile + (uint32_t)(C::NB == 1 ? 2 * i + 1 : i == g.n - 1 ? 2 * i + 1 : 2 * i + 2), st = p % C::STAGES;
-                    wait(B::full + (int)st, (p / C::STAGES) & 1);
-                    if (!ok) break;
-                    const int from = max(g.s.L - j0, 0);
-                    uint8_t* tile = smem + C::CTRL + C::QB + st * C::TILE;
-                    for (int e = (int)(threadIdx.x & 127) + from * 8; e < BN * 8; e += 128)
-#pragma unroll
-                        for (int cb = 0; cb < D / 64; ++cb) *reinterpret_cast<uint4*>(tile + cb * (BN * 128) + e * 16) = make_uint4(0, 0, 0, 0);
-                    fence_proxy_async();
-                }
-                const bool all = __all_sync(0xffffffffu, (j0 >= lo && j0 + BN <= hi) || j0 + BN <= pre);
-                uint32_t x[BN];
-                auto xf = [&](int k) -> float { return __uint_as_float(x[k]); };
-#pragma unroll
-                for (int k = 0; k < BN; k += 32) tmem_ld32_to(x + k, at + k);
-                tmem_ld_wait();
-#pragma unroll
-                for (int k = 0; k < BN; k += 32) pin32(x + k);
-                if constexpr (CAP) {
-                    bool near = true;                    // all scores where the series holds: no branch per score
-#pragma unroll
-                    for (int k = 0; k < BN; ++k) {
-                        const float y = xf(k) * (P.scale * inv_cap);
-                        near = near && fabsf(y) < 0.5f;
-                        x[k] = __float_as_uint(y);
-                    }
-                    if (__all_sync(0xffffffffu, near)) {
-#pragma unroll
-                        for (int k = 0; k < BN; ++k) x[k] = __float_as_uint(P.cap * kLog2e * tanh_series(xf(k)));
-                    } else {
-#pragma unroll
-                        for (int k = 0; k < BN; ++k)
-                            x[k] = __float_as_uint(P.cap * kLog2e * (fabsf(xf(k)) < 0.5f ? tanh_series(xf(k)) : tanh_far(xf(k))));
-                    }
-                }
-                if (!all) {
-#pragma unroll
-                    for (int k0 = 0; k0 < BN; k0 += 32) {
-                        const uint32_t seen = range_bits(lo, hi, j0 + k0) | range_bits(0, pre, j0 + k0);
-#pragma unroll
-                        for (int k = 0; k < 32; ++k)
-                            if (!(seen >> k & 1u)) x[k0 + k] = 0xff800000u;
-                    }
-                }
-                float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-                for (int k = 0; k < BN; k += 2) top[k >> 1 & 3] = max3(top[k >> 1 & 3], xf(k), xf(k + 1));
-                const float next = fmaxf(m, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * c);
-                // a row that grew by more than 2^8 (or had seen nothing) takes its new maximum, and its warp with it
-                if (__any_sync(0xffffffffu, next > m + 8.0f || (m == -INFINITY && next > m))) {
-                    const float w = next == -INFINITY ? 1.0f : exp2_hw(m - next);
-                    m = next;
-                    l *= w;
-                    if (u >= C::WG) {                    // S(u) complete: so is the MMA that last added to O
-#pragma unroll
-                        for (int k = 0; k < D; k += 16) {
-                            uint32_t o[16];
-                            tmem_ld16(lanes + C::O_COL + wg * D + k, o);
-                            tmem_ld_wait();
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * w);
-                            tmem_st16(lanes + C::O_COL + wg * D + k, o);
-                        }
-                    }
-                }
-                const float base = m == -INFINITY ? 0.0f : m;
-                const float2 c2 = make_float2(c, c), b2 = make_float2(-base, -base);
-                float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-                // S is in registers by now, so P can begin to take its place
-                auto weights = [&](int k) {
-                    float2 y = fma2(make_float2(xf(k), xf(k + 1)), c2, b2);
-                    y.x = exp2_hw(y.x);
-                    y.y = exp2_hw(y.y);
-                    sum[k >> 1 & 1] = add2(sum[k >> 1 & 1], y);
-                    return y;
-                };
-                if (two) {
-#pragma unroll
-                    for (int k0 = 0; k0 < BN; k0 += 64) {
-                        uint32_t low[32];
-#pragma unroll
-                        for (int k = 0; k < 64; k += 2) {
-                            const float2 y = weights(k0 + k);
-                            const uint32_t w = pack_bf16(y.x, y.y);
-                            x[(k0 + k) >> 1] = w;
-                            low[k >> 1] = pack_bf16(y.x - bf_lo(w), y.y - bf_hi(w));
-                        }
-                        tmem_st32(at + k0 / 2, x + k0 / 2);
-                        tmem_st32(at + BN / 2 + k0 / 2, low);
-                    }
-                } else {
-#pragma unroll
-                    for (int k0 = 0; k0 < BN; k0 += 64) {
-#pragma unroll
-                        for (int k = 0; k < 64; k += 2) {
-                            const float2 y = weights(k0 + k);
-                            x[(k0 + k) >> 1] = pack_bf16(y.x, y.y);
-                        }
-                        tmem_st32(at + k0 / 2, x + k0 / 2);
-                    }
-                }
-                const float2 s2 = add2(sum[0], sum[1]);
-                l += s2.x + s2.y;
-                tmem_st_wait();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar(B::pfull + (gu & 1)));
-            }
-            const int u1 = C::WG == 1 ? 1 : u0 ^ 1;          // the other warpgroup's first unit
-            units += (uint32_t)U;
-            base_tile += 2 * (uint32_t)g.n;
-            if (ok && u0 < U) wait(B::ofull + wg, filled[0] & 1);
-            filled[0] += u0 < U;
-            bool other = false;                              // join: the other warpgroup has sums, too
-            float w0 = 1.0f, w1 = 0.0f;
-            if constexpr (JOIN) {
-                if (wg == 1) {
-                    *ml = make_float2(m, l);
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(bar(B::mlfull));
-                    ++items;
-                    continue;
-                }
-                if (ok) wait(B::mlfull, items & 1);
-                other = u1 < U;
-                if (ok && other) wait(B::ofull + 1, filled[1] & 1);
-                filled[1] += other;
-                const float2 x = *ml;
-                const float top = fmaxf(m, x.x), base = top == -INFINITY ? 0.0f : top;
-                w0 = exp2_hw(m - base);
-                w1 = exp2_hw(x.x - base);
-                l = l * w0 + x.y * w1;
-                m = top;
-            }
-            ++items;
-            tc_fence_after();
-            const bool whole = g.whole();
-            const float inv = whole ? (l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : l)) : 1.0f;
-            const float lse2 = l == 0.0f ? -INFINITY : m + log2f(l);
-            const RowId id = row_id(P, g.s, g.h, row);
-            __nv_bfloat16* out = (__nv_bfloat16*)P.out + (long long)(g.s.t0 + id.t) * P.o_t + (long long)id.head * P.o_h;
-            const size_t part = (size_t)(2 * blockIdx.x + (g.first ? 0 : 1)) * BM + (row - g.rt * BM);
-            bool fine = true;
-            if (ok) {
-#pragma unroll
-                for (int k = 0; k < D; k += 32) {
-                    uint32_t o[32];
-                    if (!JOIN || u0 < U) {
-                        tmem_ld32(lanes + C::O_COL + wg * D + k, o);
-                        tmem_ld_wait();
-                    }
-                    if constexpr (JOIN) {
-                        uint32_t o1[32];
-                        if (other) {
-                            tmem_ld32(lanes + C::O_COL + D + k, o1);
-                            tmem_ld_wait();
-                        }
-#pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            o[e] = __float_as_uint((u0 < U ? __uint_as_float(o[e]) * w0 : 0.0f) + (other ? __uint_as_float(o1[e]) * w1 : 0.0f));
-                    }
-                    if (whole && real) {
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) {
-                            const float v = l == 0.0f ? 0.0f : __uint_as_float(o[e]) * inv;
-                            fine = fine && fabsf(v) <= 3.0e38f;
-                            o[e] = __float_as_uint(v);
-                        }
-#pragma unroll
-                        for (int e = 0; e < 32; e += 8)
-                            *reinterpret_cast<uint4*>(out + k + e) =
-                                make_uint4(pack_bf16(__uint_as_float(o[e]), __uint_as_float(o[e + 1])),
-                                           pack_bf16(__uint_as_float(o[e + 2]), __uint_as_float(o[e + 3])),
-                                           pack_bf16(__uint_as_float(o[e + 4]), __uint_as_float(o[e + 5])),
-                                           pack_bf16(__uint_as_float(o[e + 6]), __uint_as_float(o[e + 7])));
-                    } else if (real) {
-#pragma unroll
-                        for (int e = 0; e < 32; e += 4)
-                            __stcg(reinterpret_cast<uint4*>(P.part_o + part * D + k + e), make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]));
-                    }
-                    __syncwarp();
-                }
-            }
-            tc_fence_before();
-            if constexpr (JOIN) {
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar(B::mlempty));
-            }
-            if (whole) {
-                if (real && P.lse) P.lse[(long long)(g.s.t0 + id.t) * P.Hq + id.head] = lse2 * kLn2;
-                for (uint32_t bad = __ballot_sync(0xffffffffu, real && !fine); bad; bad &= bad - 1) {
-                    const int who = __ffs(bad) - 1;
-                    float o[D / 32];
-                    resum_row<__nv_bfloat16, D>(P, g.s, g.b, g.h, row - lane + who, __shfl_sync(0xffffffffu, lse2, who), o);
-                    const RowId bid = row_id(P, g.s, g.h, row - lane + who);
-                    store_f32<__nv_bfloat16, D / 32>((__nv_bfloat16*)P.out + (long long)(g.s.t0 + bid.t) * P.o_t + (long long)bid.head * P.o_h +
-                                                         lane * (D / 32), o);
-                }
-            } else {
-                if (real) __stcg(P.part_ml + part, make_float2(m, l));
-            }
-        }
-        if (threadIdx.x == 128) leave_split(P, plan, g, have);
-    }
-    tc_fence_before();
-    __syncthreads();
-    if (warp == kMmaWarp) {
-        tmem_relinquish();
-        tmem_dealloc(tmem, C::TMEM);
-    }
-}
-
-// The maps of a call's cache, tiles of bn slots; false where boxes cannot describe it.
-bool make_maps(const AttendParams& P, int bn, TileMaps& m)
-{
-    const CacheView& c = P.cache;
-    const EncodeTiled enc = tiled_encoder();
-    m.box_rows = c.paged && c.page_size < bn ? c.page_size : bn;
-    if (!enc || c.capacity < 1 || (c.paged && c.page_shift < 0) || m.box_rows < 32) return false;
-    const cuuint64_t H = (cuuint64_t)c.H, d = (cuuint64_t)c.d;
-    const cuuint64_t dims_p[4] = {d, H, (cuuint64_t)c.page_size, (cuuint64_t)c.num_pages};
-    const cuuint64_t str_p[3] = {d * 2, H * d * 2, (cuuint64_t)c.page_size * H * d * 2};
-    const cuuint64_t dims_c[4] = {d, (cuuint64_t)c.capacity, H, (cuuint64_t)P.batch};
-    const cuuint64_t str_c[3] = {(cuuint64_t)c.st * 2, (cuuint64_t)c.sh * 2, (cuuint64_t)c.sb * 2};
-    const cuuint32_t box_p[4] = {64, 1, (cuuint32_t)m.box_rows, 1}, box_c[4] = {64, (cuuint32_t)m.box_rows, 1, 1};
-    const cuuint32_t one[4] = {1, 1, 1, 1};
-    for (int i = 0; i < 2; ++i)
-        if (enc(i ? &m.v : &m.k, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(i ? P.cv : P.ck), c.paged ? dims_p : dims_c,
-                c.paged ? str_p : str_c, c.paged ? box_p : box_c, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
-            return false;
-    return true;
-}
-
-template <int D, int NT, Source SRC> cudaError_t start_tc(const AttendParams& P, const TileMaps& maps, int num_sms, cudaStream_t stream)
-{
-    using C = TcShape<D, NT>;
-    const int grid = min(num_sms, kAttendMaxRows / C::BM / 2);
-    // the capped scores' code apart: with it the plain kernels would be twice as long
-    if (P.cap > 0.0f) {
-        if (cudaError_t e = smem_opt_in<attend_tc_kernel<D, NT, SRC, true>>(C::SMEM); e != cudaSuccess) return e;
-        attend_tc_kernel<D, NT, SRC, true><<<grid, C::THREADS, C::SMEM, stream>>>(P, maps);
-    } else {
-        if (cudaError_t e = smem_opt_in<attend_tc_kernel<D, NT, SRC, false>>(C::SMEM); e != cudaSuccess) return e;
-        attend_tc_kernel<D, NT, SRC, false><<<grid, C::THREADS, C::SMEM, stream>>>(P, maps);
-    }
-    if (cudaError_t e = cudaGetLastError(); e != cudaSuccess) return e;
-    return run_join<__nv_bfloat16, D, C::BM>(P, grid, stream);
-}
-template <int D, int NT> cudaError_t run_tc(const AttendParams& P, int num_sms, cudaStream_t stream)
-{
-    TileMaps maps;
-    if (make_maps(P, TcShape<D, NT>::BN, maps)) return start_tc<D, NT, kBoxes>(P, maps, num_sms, stream);
-    if (!P.cache.paged || P.cache.page_size % 8 == 0) return start_tc<D, NT, kGroups>(P, maps, num_sms, stream);
-    return start_tc<D, NT, kRows>(P, maps, num_sms, stream);
-}
-
-}  // namespace
 
 cudaError_t launch_attend_tc(const AttendParams& P, int num_sms, cudaStream_t stream)
 {
-    const bool one = one_tile(P);
-    if (P.d == 64) return one ? run_tc<64, 1>(P, num_sms, stream) : run_tc<64, 2>(P, num_sms, stream);
-    if (P.d == 128) return one ? run_tc<128, 1>(P, num_sms, stream) : run_tc<128, 2>(P, num_sms, stream);
-    return run_tc<256, 1>(P, num_sms, stream);
+    return P.cap > 0.0f ? launch_attend_tc_capped(P, num_sms, stream) : run_attend_tc<false>(P, num_sms, stream);
 }
 
 }  // namespace kvx

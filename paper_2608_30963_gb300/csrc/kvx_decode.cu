@@ -19,6 +19,7 @@ struct kvx_decoder {
     float* part_o = nullptr;               // partial results of split attention rows (kvx_decode.cuh)
     float2* part_ml = nullptr;
     SplitItem* split = nullptr;
+    float* scores = nullptr;               // scores kept for the weight sums
 };
 
 namespace {
@@ -42,6 +43,7 @@ void free_decoder(kvx_decoder* d)
     if (d->part_o) cudaFree(d->part_o);
     if (d->part_ml) cudaFree(d->part_ml);
     if (d->split) cudaFree(d->split);
+    if (d->scores) cudaFree(d->scores);
     delete d;
 }
 
@@ -153,7 +155,8 @@ extern "C" KVX_API kvx_status kvx_decoder_create(const kvx_decoder_desc* desc, k
     if (cudaMalloc(&d->turns, sizeof turns) != cudaSuccess || cudaMalloc(&d->status, sizeof(unsigned)) != cudaSuccess ||
         cudaMalloc(&d->part_o, rows * g.head_dim * sizeof(float)) != cudaSuccess ||
         cudaMalloc(&d->part_ml, rows * sizeof(float2)) != cudaSuccess ||
-        cudaMalloc(&d->split, kAttendMaxCtas * sizeof(SplitItem)) != cudaSuccess) {
+        cudaMalloc(&d->split, kAttendMaxCtas * sizeof(SplitItem)) != cudaSuccess ||
+        (desc->dtype == KVX_BF16 && cudaMalloc(&d->scores, kAttendScores * sizeof(float)) != cudaSuccess)) {
         cudaGetLastError();
         free_decoder(d);
         return fail(KVX_ERR_OOM, "decoder_create: device allocation");
@@ -186,12 +189,12 @@ extern "C" KVX_API kvx_status kvx_append(kvx_decoder* dec, const kvx_new_tokens*
     kvx_status st;
     AppendParams P;
     memset(&P, 0, sizeof P);
-    if ((st = check_tokens(dec, "append", tok)) || (st = check_layer(dec, "append", layer)) ||
-        (st = check_rows(dec, "append", "q", q)) || (st = check_rows(dec, "append", "k", k)) ||
+    if ((st = check_tokens(dec, "append", tok)) || (st = check_layer(dec, "append", layer))) return st;
+    if (tok->total_tokens == 0) return KVX_OK;
+    if ((st = check_rows(dec, "append", "q", q)) || (st = check_rows(dec, "append", "k", k)) ||
         (st = check_rows(dec, "append", "v", v)) || (st = check_rows(dec, "append", "q_out", q_out)) ||
         (st = make_view(dec, "append", "the cache", cache, layer, 1, P.cache)))
         return st;
-    if (tok->total_tokens == 0) return KVX_OK;
     const kvx_model_geom& g = dec->desc.model;
     P.T = tok->total_tokens; P.batch = tok->batch;
     P.Hq = dec->desc.num_q_heads; P.H = g.num_kv_heads; P.d = g.head_dim;
@@ -220,15 +223,15 @@ extern "C" KVX_API kvx_status kvx_attend(kvx_decoder* dec, const kvx_new_tokens*
     kvx_status st;
     AttendParams P;
     memset(&P, 0, sizeof P);
-    if ((st = check_tokens(dec, "attend", tok)) || (st = check_layer(dec, "attend", layer)) ||
-        (st = check_rows(dec, "attend", "q", q)) || (st = check_rows(dec, "attend", "out", out)) ||
+    if ((st = check_tokens(dec, "attend", tok)) || (st = check_layer(dec, "attend", layer))) return st;
+    if (tok->total_tokens == 0) return KVX_OK;
+    if ((st = check_rows(dec, "attend", "q", q)) || (st = check_rows(dec, "attend", "out", out)) ||
         (st = make_view(dec, "attend", "the cache", cache, layer, 1, P.cache)))
         return st;
     if (tok->batch > kMaxAttendBatch) return fail(KVX_ERR_UNSUPPORTED, "attend: at most %d sequences a call", kMaxAttendBatch);
     if (opts->window < 0) return fail(KVX_ERR_INVALID_ARG, "attend: window must not be negative");
     if (opts->key_weight && (!opts->lse || opts->weight_stride < 1))
         return fail(KVX_ERR_INVALID_ARG, "attend: key_weight needs lse and weight_stride >= 1");
-    if (tok->total_tokens == 0) return KVX_OK;
     const kvx_model_geom& g = dec->desc.model;
     P.T = tok->total_tokens; P.batch = tok->batch;
     P.Hq = dec->desc.num_q_heads; P.H = g.num_kv_heads; P.G = P.Hq / P.H; P.d = g.head_dim;
@@ -241,6 +244,7 @@ extern "C" KVX_API kvx_status kvx_attend(kvx_decoder* dec, const kvx_new_tokens*
     P.lse = opts->lse; P.key_weight = opts->key_weight; P.weight_stride = opts->weight_stride;
     P.status = dec->status;
     P.part_o = dec->part_o; P.part_ml = dec->part_ml; P.split = dec->split;
+    P.scores = dec->scores;
     const cudaError_t e = launch_attend(P, dec->desc.dtype, dec->num_sms, (cudaStream_t)stream, &dec->last_launches);
     if (e != cudaSuccess) return fail(KVX_ERR_CUDA, "attend: launch failed: %s", cudaGetErrorString(e));
     return KVX_OK;

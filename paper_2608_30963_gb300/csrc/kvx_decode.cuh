@@ -71,6 +71,9 @@ struct AttendParams {
     float* part_o;        // [2 * grid][BM][d]
     float2* part_ml;      // [2 * grid][BM]: running maximum (log2 units) and sum
     SplitItem* split;     // [grid]
+    // scores of few rows, kept for the weight sums (log2 units): [T][Hq][scores_stride], or NULL
+    float* scores;
+    long long scores_stride;
 };
 
 struct EvictParams {
@@ -92,8 +95,11 @@ cudaError_t launch_evict(const EvictParams& P, int dtype, int num_sms, cudaStrea
 
 // Workspace of split rows: rows of partial results (2 x grid x BM, so grids stay within it) and split items.
 constexpr int kAttendMaxRows = 2 * 152 * 4 * 64;
+constexpr long long kAttendScores = 16ll << 20;   // floats of kept scores: eight sequences of 64K, 32 query heads
 constexpr int kAttendMaxCtas = kAttendMaxRows / 2 / 16;
+cudaError_t launch_sum_scores(const AttendParams& P, cudaStream_t stream);
 cudaError_t launch_key_weight(const AttendParams& P, int num_sms, cudaStream_t stream);
+cudaError_t launch_attend_tc_capped(const AttendParams& P, int num_sms, cudaStream_t stream);
 cudaError_t launch_attend_tc(const AttendParams& P, int num_sms, cudaStream_t stream);
 cudaError_t launch_attend(const AttendParams& P, int dtype, int num_sms, cudaStream_t stream, int* launches);
 

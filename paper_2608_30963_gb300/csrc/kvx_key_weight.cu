@@ -337,6 +337,34 @@ __global__ void __launch_bounds__(KwShape<D>::THREADS, 1) key_weight_kernel(cons
     }
 }
 
+// The same sums from scores that the attention has left (few rows): a thread a slot.
+__global__ void __launch_bounds__(128) sum_scores_kernel(const __grid_constant__ AttendParams P)
+{
+    __shared__ float lse[64];
+    const int b = blockIdx.z, h = blockIdx.y, j = blockIdx.x * 128 + threadIdx.x;
+    grid_dependency_wait();
+    const Seq s = load_seq(P, b);
+    const int rows = s.n * P.G;
+    if (blockIdx.x * 128 >= s.L) return;
+    float w = 0.0f;
+    for (int r0 = 0; r0 < rows; r0 += 64) {
+        __syncthreads();
+        if (threadIdx.x < 64 && r0 + (int)threadIdx.x < rows) {
+            const RowId id = row_id(P, s, h, r0 + threadIdx.x);
+            lse[threadIdx.x] = P.lse[(long long)(s.t0 + id.t) * P.Hq + id.head] * kLog2e;
+        }
+        __syncthreads();
+        const int n = min(64, rows - r0);
+#pragma unroll 8
+        for (int r = 0; r < n; ++r) {
+            const RowId id = row_id(P, s, h, r0 + r);
+            if (j < s.L && j < P.weight_stride && sees(P, s, s.slot(id.t), j))
+                w += exp2_hw(__ldcg(&P.scores[((long long)(s.t0 + id.t) * P.Hq + id.head) * P.scores_stride + j]) - lse[r]);
+        }
+    }
+    if (j < s.L && j < P.weight_stride) P.key_weight[((long long)b * P.H + h) * P.weight_stride + j] += w;
+}
+
 template <int D, bool CAP> cudaError_t run_key_weight(const AttendParams& P, int num_sms, cudaStream_t stream)
 {
     using C = KwShape<D>;
@@ -367,6 +395,20 @@ cudaError_t launch_key_weight(const AttendParams& P, int num_sms, cudaStream_t s
                                                                                        : run_key_weight<256, true>(P, num_sms, stream);
     return P.d == 64 ? run_key_weight<64, false>(P, num_sms, stream) : P.d == 128 ? run_key_weight<128, false>(P, num_sms, stream)
                                                                                     : run_key_weight<256, false>(P, num_sms, stream);
+}
+
+cudaError_t launch_sum_scores(const AttendParams& P, cudaStream_t stream)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((P.weight_stride + 127) / 128), P.H, P.batch);
+    cfg.blockDim = dim3(128);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, sum_scores_kernel, P);
 }
 
 }  // namespace kvx
