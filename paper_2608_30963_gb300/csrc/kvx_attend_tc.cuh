@@ -301,7 +301,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
                     if (ok) {
                         const uint32_t d0 = sT + st * C::TILE + place * (BN * 128) + (uint32_t)(q0 * 1024 + sub * 128);
                         if constexpr (SRC == kGroups) {
-#pragma unroll
+#pragma unroll 1
                             for (int q = 0; q < PART / 8; ++q) {
                                 if (SHARED && warp == 2 && q >= BN / 32) break;
                                 const long long first = __shfl_sync(0xffffffffu, at[0], q);
@@ -511,7 +511,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
                     m = next;
                     l *= w;
                     if (u >= C::WG) {                    // S(u) complete: so is the MMA that last added to O
-#pragma unroll
+#pragma unroll 1
                         for (int k = 0; k < D; k += 16) {
                             uint32_t o[16];
                             tmem_ld16(lanes + C::O_COL + wg * D + k, o);
@@ -601,7 +601,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
             const size_t part = (size_t)(2 * blockIdx.x + (g.first ? 0 : 1)) * BM + (row - g.rt * BM);
             bool fine = true;
             if (ok) {
-#pragma unroll
+#pragma unroll 1                                             // short code: a cold instruction cache costs small calls most
                 for (int k = 0; k < D; k += 32) {
                     uint32_t o[32];
                     if (!JOIN || u0 < U) {
