@@ -110,8 +110,8 @@ __global__ void __launch_bounds__(kThreads) attend_simt_kernel(const __grid_cons
     long long* sums = reinterpret_cast<long long*>(sP + BM * (kBN + 4));
     const int tid = threadIdx.x, tc = tid & 7, tr = tid >> 3, lane = tid & 31, warp = tid >> 5;
     const float inv_cap = P.cap > 0.0f ? 1.0f / P.cap : 0.0f;
-    const Plan plan = make_plan<BM, kBN, kThreads>(P, sums);
-    SegmentWalk<BM, kBN> walk(P, plan);
+    const Plan plan = make_plan<kBN, kThreads>(P, sums);
+    SegmentWalk<kBN> walk(P, plan);
     Segment g;
     bool have = false;
     while (walk.next(g)) {
@@ -352,8 +352,10 @@ template <auto Kernel> int ctas_per_sm(int smem, int threads)
 }
 
 template <typename T, int D, int BM>
-cudaError_t run_simt(const AttendParams& P, int num_sms, cudaStream_t stream)
+cudaError_t run_simt(const AttendParams& call, int num_sms, cudaStream_t stream)
 {
+    AttendParams P = call;
+    P.tile_rows = BM;
     constexpr int smem = simt_smem<D, BM>();
     if (cudaError_t e = smem_opt_in<attend_simt_kernel<T, D, BM>>(smem); e != cudaSuccess) return e;
     const int grid = min(num_sms * ctas_per_sm<attend_simt_kernel<T, D, BM>>(smem, kThreads), kAttendMaxRows / BM / 2);

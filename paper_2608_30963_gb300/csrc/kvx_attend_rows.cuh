@@ -152,12 +152,13 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Atten
     constexpr int C = D / 32, RPC = 8 / WPR, U = C == 8 ? 4 : 8;
     __shared__ float sh[8][D + 2];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    grid_launch_dependents();
     grid_dependency_wait();
     const SplitItem it = P.split[blockIdx.x];
     if (it.parts == 0) return;
     const Seq s = load_seq(P, it.b);
     const int r = blockIdx.y * RPC + warp / WPR, w0 = warp % WPR;
-    const bool real = r < min(BM, s.n * P.G - it.rt * BM);
+    const bool real = r < min(P.tile_rows, s.n * P.G - it.rt * P.tile_rows);
     const Parts parts = {(int)blockIdx.x, it.lines, it.parts, it.slot0};
     float m = -INFINITY, l = 0.0f, o[C];
 #pragma unroll
@@ -200,12 +201,12 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Atten
             l += sh[warp + k][D];
         }
     }
-    if (real) finish_row<T, D>(P, s, it.b, it.h, it.rt * BM + r, m, l, o);
+    if (real) finish_row<T, D>(P, s, it.b, it.h, it.rt * P.tile_rows + r, m, l, o);
 }
 template <typename T, int D, int BM> cudaError_t run_join(const AttendParams& P, int grid, cudaStream_t stream)
 {
-    // an item has at most min(BM, T G) rows; few of them: four warps a row, as there may be many parts
-    const long long rows = min((long long)BM, (long long)P.T * P.G);
+    // an item has at most min(tile_rows, T G) rows; few of them: four warps a row, as there may be many parts
+    const long long rows = min((long long)P.tile_rows, (long long)P.T * P.G);
     const bool few = rows <= 64;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(grid, (unsigned)(few ? (rows + 1) / 2 : (rows + 7) / 8));

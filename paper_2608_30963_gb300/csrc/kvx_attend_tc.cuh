@@ -4,7 +4,7 @@
 //   S = Q K^T (fp32, TMEM),  P = exp2(c S - m),  O += P V (P bf16 from TMEM, O fp32 in TMEM)
 // in one pass over the slots, with the running maximum m and sum l of a row in the registers of the thread
 // that owns the row.  A CTA holds NT tiles of 128 rows and walks slot tiles of BN.
-//   producer warps (3)  copy Q, K and V rows into 128-byte-swizzled tiles.  Q: 16-byte cp.async.  K and V: one
+//   producer warps (3)  copy Q, K and V rows into 128-byte-swizzled tiles.  Q: tensor copies.  K and V: one
 //                       tensor copy (TMA) for each page, or for a whole tile of a contiguous cache, by one
 //                       warp, a box a lane; caches that boxes of 8 or more rows cannot describe (odd page
 //                       sizes) take cp.async too.  A K tile is read as a K-major operand, a V tile, laid
@@ -67,12 +67,12 @@ constexpr int kFewSlots = 512;   // rows that see fewer slots get their weights 
 __host__ __device__ __forceinline__ bool one_tile(const AttendParams& P) { return (long long)P.T * P.G <= 128ll * P.batch; }
 
 // Whether an item's weights are multiplied in two terms: its first token sees fewest slots.
-template <int D, int BM, int NT> __device__ __forceinline__ bool two_terms(const AttendParams& P, const Segment& g)
+template <int D, int NT> __device__ __forceinline__ bool two_terms(const AttendParams& P, const Segment& g)
 {
     if constexpr (NT == 1 && D < 256) return true;
     if (NT == 1 && one_tile(P)) return true;
     int ta, tb;
-    row_tile_tokens<BM>(P, g.s, g.rt, ta, tb);
+    row_tile_tokens(P, g.s, g.rt, ta, tb);
     const int own = g.s.slot(ta);
     return own < kFewSlots || (P.window > 0 && P.window < kFewSlots);
 }
@@ -80,7 +80,7 @@ template <int D, int BM, int NT> __device__ __forceinline__ bool two_terms(const
 // Tensor maps of K and V, and the rows of a box: a paged cache as (channel, head, slot in page, page), a
 // contiguous one as (channel, slot, head, sequence); boxes of 64 channels of one head.
 struct TileMaps {
-    CUtensorMap k, v;
+    CUtensorMap k, v, q;      // q: (channel, head, token), boxes of 64 channels of a row tile
     int box_rows;
 };
 // How K and V tiles are brought: row by row (any page size), in groups of 8 rows a fixed stride apart (page sizes that
@@ -114,7 +114,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
             mbar_init(bar(B::pfull + i), 4);
             mbar_init(bar(B::ofull + i), 1);
         }
-        mbar_init(bar(B::qfull), kProdWarps * 32);
+        mbar_init(bar(B::qfull), 1);
         mbar_init(bar(B::qempty), 1);
         mbar_init(bar(B::done), 1);
         mbar_init(bar(B::mlfull), 4);
@@ -122,12 +122,15 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
         fence_mbar_init();
         *abort = 0;
     }
-    const Plan plan = make_plan<BM, BN, C::THREADS>(P, reinterpret_cast<long long*>(smem + C::CTRL + C::QB));
+    // the kernel before this one may still be ending: what it wrote is read from here on
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const Plan plan = make_plan<BN, C::THREADS>(P, reinterpret_cast<long long*>(smem + C::CTRL + C::QB));
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
     const Waiter W{abort, P.status};
-    SegmentWalk<BM, BN> walk(P, plan);
+    SegmentWalk<BN> walk(P, plan);
     Segment g;
 
     if (warp < 4) {
@@ -143,42 +146,19 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
         auto wait = [&](int b, uint32_t parity) { ok = __all_sync(0xffffffffu, ok && W.wait(bar(b), parity)); };
         // The copies of a batch announce themselves: each thread's arrival follows its own copies.  The MMA warp
         // orders them before its reads (fence_proxy_async after the wait).
-        // The warps share a tile of R rows as 3/8, 3/8 and 2/8 of them; lane l has its warp's rows l and 32 + l.
-        struct Rows {
-            long long a, b;                              // element offsets, -1: a row of zeros
-        };
-        auto find_rows = [&](auto R, auto off) {
-            constexpr int SHARE = decltype(R)::value * 3 / 8;
-            const int r0 = warp * SHARE;
-            Rows x;
-            x.a = r0 + lane < decltype(R)::value ? off(r0 + lane) : -1ll;
-            x.b = SHARE > 32 && r0 + 32 + lane < decltype(R)::value ? off(r0 + 32 + lane) : -1ll;
-            return x;
-        };
-        auto copy_rows = [&](auto R, uint32_t base, const __nv_bfloat16* src, const Rows& x, int colblk) {
-            constexpr int SHARE = decltype(R)::value * 3 / 8;
-            const uint32_t d0 = base + place * colblk + (uint32_t)(warp * SHARE + sub) * 128;
-            const __nv_bfloat16* s1 = src + lane % CPR * 8;
-#pragma unroll
-            for (int r = 0; r < SHARE; r += RPI) {
-                if (warp == 2 && r >= decltype(R)::value / 4) break;
-                const long long at = __shfl_sync(0xffffffffu, r < 32 ? x.a : x.b, (r & 31) + sub);
-                cp_async16_or_zero(d0 + (uint32_t)r * 128 + (c0 ^ (uint32_t)((r & 7) << 4)), s1 + (at < 0 ? 0 : at), at >= 0);
-            }
-        };
-        using Int128 = std::integral_constant<int, 128>;
         while (walk.next(g)) {
-            const int rows = min(BM, g.s.n * P.G - g.rt * BM);
-            if (items > 0) wait(B::qempty, (items - 1) & 1);
-            for (int part = 0; part < NT; ++part) {
-                const Rows x = find_rows(Int128{}, [&](int r) {
-                    if (part * 128 + r >= rows) return -1ll;
-                    const RowId id = row_id(P, g.s, g.h, g.rt * BM + part * 128 + r);
-                    return (long long)(g.s.t0 + id.t) * P.q_t + (long long)id.head * P.q_h;
-                });
-                if (ok) copy_rows(Int128{}, sQ + part * (128 * D * 2), (const __nv_bfloat16*)P.q, x, 128 * 128);
+            if (warp == 0) {
+                // Q: the G query heads of tile_rows / G tokens, a box for each 64 channels; what it brings past the
+                // sequence's tokens is in rows that nothing is read from
+                if (items > 0) wait(B::qempty, (items - 1) & 1);
+                if (ok && elect_one()) {
+                    mbar_arrive_expect_tx(bar(B::qfull), (uint32_t)P.tile_rows * D * 2);
+#pragma unroll
+                    for (int cb = 0; cb < D / 64; ++cb)
+                        tma_box3(sQ + cb * (BM * 128), &maps.q, cb * 64, g.h * P.G, g.s.t0 + g.rt * (P.tile_rows / P.G), bar(B::qfull));
+                }
+                __syncwarp();
             }
-            cp_async_arrive(bar(B::qfull));
             ++items;
             const long long head = cache_head(P.cache) * g.h;
             // tile i as K, tile i - NB + 1 as V, and at the end the V tiles left
@@ -349,22 +329,22 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
         auto wait = [&](int b, uint32_t parity) { ok = __all_sync(0xffffffffu, ok && W.wait(bar(b), parity)); };
         while (ok && walk.next(g)) {
             const int n = __shfl_sync(0xffffffffu, g.n, 0), U = n * NT;
-            const bool two = __shfl_sync(0xffffffffu, (int)two_terms<D, BM, NT>(P, g), 0);
+            const bool two = __shfl_sync(0xffffffffu, (int)two_terms<D, NT>(P, g), 0);
             auto scores = [&](int u) {
                 const int i = u / NT, t = u - i * NT;
                 const uint32_t p = base + (uint32_t)(C::NB == 1 ? 2 * i : i == 0 ? 0 : 2 * i - 1), st = p % C::STAGES;
                 if (u == 0) wait(B::qfull, items & 1);
                 if (t == 0 && !(EARLY && u > 0)) wait(B::full + (int)st, (p / C::STAGES) & 1);
                 if (!ok) return;
-                if (u == 0 || (!TMA && !EARLY && t == 0)) fence_proxy_async();
+                if (!TMA && t == 0 && !(EARLY && u > 0)) fence_proxy_async();
                 tc_fence_after();
                 const uint32_t d = tm + ((units + u) & 1) * C::S_COL;
                 // descriptors count 16-byte units in their low bits: steps along an operand are added
-                const uint64_t qd = sw128_desc(sQ + t * (128 * D * 2)), kd = sw128_desc(sT + st * C::TILE);
+                const uint64_t qd = sw128_desc(sQ + t * (128 * 128)), kd = sw128_desc(sT + st * C::TILE);
                 if (elect_one()) {
 #pragma unroll
                     for (int k = 0; k < D / 16; ++k)
-                        umma_bf16(d, qd + (k >> 2) * (128 * 128 / 16) + (k & 3) * 2, kd + (k >> 2) * (BN * 128 / 16) + (k & 3) * 2, idesc_s, k > 0);
+                        umma_bf16(d, qd + (k >> 2) * (BM * 128 / 16) + (k & 3) * 2, kd + (k >> 2) * (BN * 128 / 16) + (k & 3) * 2, idesc_s, k > 0);
                     if (t == NT - 1) umma_commit(bar(B::empty + st));
                     if (u == U - 1) umma_commit(bar(B::qempty));
                     umma_commit(bar(B::sfull + ((units + u) & 1)));
@@ -421,20 +401,24 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
         const float c = CAP ? 1.0f : P.scale * kLog2e;   // factor of the (capped) scores in log2 units
         constexpr bool JOIN = NT == 1 && C::WG == 2;     // two warpgroups on one row tile
         float2* ml = reinterpret_cast<float2*>(smem + 1024) + quad * 32 + lane;
+        const int my_r = t * 128 + quad * 32 + lane, my_tok = my_r / P.G, my_head = my_r - my_tok * P.G;   // this thread's row of a tile
         uint32_t units = 0, items = 0, base_tile = 0, filled[2] = {0, 0};   // filled: times each O has been completed
         bool ok = true;                                  // the same in the lanes of a warp
         auto wait = [&](int b, uint32_t parity) { ok = __all_sync(0xffffffffu, ok && W.wait(bar(b), parity)); };
         bool have = false;
         while (walk.next(g)) {
             have = true;
-            const int row = g.rt * BM + t * 128 + quad * 32 + lane;
-            const bool real = row < g.s.n * P.G;
-            const int own = real ? g.s.slot(row / P.G) : -1;     // rows past the end see nothing
-            const int hi = min(own + 1, g.s.L), lo = max(window_lo(P, own), 0), pre = real ? g.s.pre : 0;
-            const bool two = two_terms<D, BM, NT>(P, g);
+            const int ta = g.rt * (P.tile_rows / P.G);            // the tile's first token
+            const int rows = min(P.tile_rows, (g.s.n - ta) * P.G);
+            const bool real = my_r < rows;
+            // rows without a token see what the last one sees, so that they send no tile the way of masks; nothing is read from them
+            const int own = g.s.slot(real ? ta + my_tok : g.s.n - 1 < ta + P.tile_rows / P.G - 1 ? g.s.n - 1 : ta + P.tile_rows / P.G - 1);
+            const int hi = min(own + 1, g.s.L), lo = max(window_lo(P, own), 0), pre = g.s.pre;
+            const RowId id = {ta + my_tok, g.h * P.G + my_head};
+            const int row = g.rt * P.tile_rows + my_r;
+            const bool two = two_terms<D, NT>(P, g);
             float* my_scores = nullptr;
             if (NT == 1 && P.scores && real) {
-                const RowId id = row_id(P, g.s, g.h, row);
                 my_scores = P.scores + ((long long)(g.s.t0 + id.t) * P.Hq + id.head) * P.scores_stride;
             }
             const int U = g.n * NT;
@@ -596,9 +580,8 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
             const bool whole = g.whole();
             const float inv = whole ? (l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : l)) : 1.0f;
             const float lse2 = l == 0.0f ? -INFINITY : m + log2f(l);
-            const RowId id = row_id(P, g.s, g.h, row);
             __nv_bfloat16* out = (__nv_bfloat16*)P.out + (long long)(g.s.t0 + id.t) * P.o_t + (long long)id.head * P.o_h;
-            const size_t part = (size_t)(2 * blockIdx.x + (g.first ? 0 : 1)) * BM + (row - g.rt * BM);
+            const size_t part = (size_t)(2 * blockIdx.x + (g.first ? 0 : 1)) * BM + my_r;
             bool fine = true;
             if (ok) {
 #pragma unroll 1                                             // short code: a cold instruction cache costs small calls most
@@ -696,18 +679,36 @@ template <int D, int NT, Source SRC, bool CAP> cudaError_t start_tc(const Attend
     using C = TcShape<D, NT>;
     const int grid = min(num_sms, kAttendMaxRows / C::BM / 2);
     if (cudaError_t e = smem_opt_in<attend_tc_kernel<D, NT, SRC, CAP>>(C::SMEM); e != cudaSuccess) return e;
-    attend_tc_kernel<D, NT, SRC, CAP><<<grid, C::THREADS, C::SMEM, stream>>>(P, maps);
-    if (cudaError_t e = cudaGetLastError(); e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(C::THREADS);
+    cfg.dynamicSmemBytes = C::SMEM;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaError_t e = cudaLaunchKernelEx(&cfg, attend_tc_kernel<D, NT, SRC, CAP>, P, maps); e != cudaSuccess) return e;
     return run_join<__nv_bfloat16, D, C::BM>(P, grid, stream);
 }
-template <int D, int NT, bool CAP> cudaError_t run_tc(const AttendParams& P, int num_sms, cudaStream_t stream)
+template <int D, int NT, bool CAP> cudaError_t run_tc(const AttendParams& call, int num_sms, cudaStream_t stream)
 {
+    using C = TcShape<D, NT>;
+    AttendParams P = call;
+    P.tile_rows = C::BM / P.G * P.G;               // whole tokens: with 7 query heads a KV head 126 or 252 rows
     TileMaps maps;
-    if (make_maps(P, TcShape<D, NT>::BN, maps)) return start_tc<D, NT, kBoxes, CAP>(P, maps, num_sms, stream);
+    const EncodeTiled enc = tiled_encoder();
+    const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)P.Hq, (cuuint64_t)P.T};
+    const cuuint64_t strides[2] = {(cuuint64_t)P.q_h * 2, (cuuint64_t)P.q_t * 2};
+    const cuuint32_t box[3] = {64, (cuuint32_t)P.G, (cuuint32_t)(C::BM / P.G)}, one[3] = {1, 1, 1};
+    if (!enc || enc(&maps.q, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(P.q), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                    CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+        return cudaErrorInvalidValue;
+    if (make_maps(P, C::BN, maps)) return start_tc<D, NT, kBoxes, CAP>(P, maps, num_sms, stream);
     if (!P.cache.paged || P.cache.page_size % 8 == 0) return start_tc<D, NT, kGroups, CAP>(P, maps, num_sms, stream);
     return start_tc<D, NT, kRows, CAP>(P, maps, num_sms, stream);
 }
-
 template <bool CAP> cudaError_t run_attend_tc(const AttendParams& P, int num_sms, cudaStream_t stream)
 {
     const bool one = one_tile(P);

@@ -52,6 +52,7 @@ struct SplitItem {
 
 struct AttendParams {
     int T, batch, Hq, H, G, d;
+    int tile_rows;        // rows of a row tile: of the kernel's, those it uses
     const int* seq_off;
     const int* kv_len;
     const void* q;
@@ -155,11 +156,12 @@ template <int BN> __device__ __forceinline__ KvTiles kv_tiles(const AttendParams
     return k;
 }
 
-// A row tile: BM consecutive (token, query head) rows of one (sequence, KV head), row r = t * G + g.
-template <int BM> __device__ __forceinline__ void row_tile_tokens(const AttendParams& P, const Seq& s, int rt, int& ta, int& tb)
+// A row tile: tile_rows consecutive (token, query head) rows of one (sequence, KV head), row r = t * G + g.
+__device__ __forceinline__ int row_tiles(const AttendParams& P, const Seq& s) { return (s.n * P.G + P.tile_rows - 1) / P.tile_rows; }
+__device__ __forceinline__ void row_tile_tokens(const AttendParams& P, const Seq& s, int rt, int& ta, int& tb)
 {
-    ta = rt * BM / P.G;
-    tb = min(s.n, (rt * BM + BM - 1) / P.G + 1) - 1;
+    ta = rt * P.tile_rows / P.G;
+    tb = min(s.n, (rt * P.tile_rows + P.tile_rows - 1) / P.G + 1) - 1;
 }
 
 // ------------------------------------------------------------------ the split of the work
@@ -181,7 +183,7 @@ struct Plan {
 __host__ __device__ inline int plan_lines(int grid, int H) { return grid / H * H * 10 >= grid * 9 ? H : 1; }
 
 // sums: shared long long[batch + 1].  All threads call it; returns the same in each.
-template <int BM, int BN, int THREADS>
+template <int BN, int THREADS>
 __device__ Plan make_plan(const AttendParams& P, long long* sums)
 {
     Plan p;
@@ -192,11 +194,11 @@ __device__ Plan make_plan(const AttendParams& P, long long* sums)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     for (int b = warp; b < P.batch; b += THREADS / 32) {
         const Seq s = load_seq(P, b);
-        const int rts = (s.n * P.G + BM - 1) / BM;
+        const int rts = row_tiles(P, s);
         long long w = 0;
         for (int rt = lane; rt < rts; rt += 32) {
             int ta, tb;
-            row_tile_tokens<BM>(P, s, rt, ta, tb);
+            row_tile_tokens(P, s, rt, ta, tb);
             w += kv_tiles<BN>(P, s, ta, tb).count;
         }
 #pragma unroll
@@ -234,12 +236,12 @@ __device__ Plan make_plan(const AttendParams& P, long long* sums)
     p.b = l;
     p.at = sums[l];
     const Seq s = load_seq(P, l);
-    const int rts = (s.n * P.G + BM - 1) / BM;
+    const int rts = row_tiles(P, s);
     for (int r0 = 0; r0 < rts; r0 += 32) {       // and its row tile (each warp alike)
         long long w = 0;
         if (r0 + lane < rts) {
             int ta, tb;
-            row_tile_tokens<BM>(P, s, r0 + lane, ta, tb);
+            row_tile_tokens(P, s, r0 + lane, ta, tb);
             w = (long long)kv_tiles<BN>(P, s, ta, tb).count * heads;
         }
         long long v = w;
@@ -278,7 +280,7 @@ struct Segment {
     bool first;               // the CTA's first segment (its partial result goes to the CTA's slot 0, else 1)
     __device__ __forceinline__ bool whole() const { return n == kv.count; }
 };
-template <int BM, int BN> struct SegmentWalk {
+template <int BN> struct SegmentWalk {
     const AttendParams& P;
     Plan p;
     long long x;
@@ -288,12 +290,12 @@ template <int BM, int BN> struct SegmentWalk {
         if (x >= p.hi) return false;
         while (true) {
             g.s = load_seq(P, p.b);
-            if (p.rt < (g.s.n * P.G + BM - 1) / BM) break;
+            if (p.rt < row_tiles(P, g.s)) break;
             ++p.b;                               // a sequence without new tokens, or past its last row tile
             p.rt = 0;
         }
         int ta, tb;
-        row_tile_tokens<BM>(P, g.s, p.rt, ta, tb);
+        row_tile_tokens(P, g.s, p.rt, ta, tb);
         g.kv = kv_tiles<BN>(P, g.s, ta, tb);
         g.b = p.b;
         g.rt = p.rt;
