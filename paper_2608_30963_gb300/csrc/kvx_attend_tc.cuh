@@ -14,8 +14,8 @@
 //                       one unit are formed while the other's softmax runs.
 //   softmax warps       two warpgroups, for units of even and odd u: a row tile each (NT = 2), or every other
 //                       slot tile of the one row tile (NT = 1), each with its own maximum, sum and O,
-//                       which the first joins at the end (heads of 256, whose two O would not fit
-//                       TMEM: one warpgroup).  P takes the place of S.  O is rescaled only when a row's maximum has grown by more than
+//                       which the first joins at the end.  Heads of 256, whose two O would not fit TMEM: both
+//                       on every unit, half the columns each.  P takes the place of S.  O is rescaled only when a row's maximum has grown by more than
 //                       2^8 since the last time.
 // P is rounded to bf16 for the MMA, as V is.  Where a row sees few slots the roundings of its few weights do
 // not average out, and the error comes near 2^-8 |v|; there, and where the copies bound the kernel
@@ -34,15 +34,17 @@ namespace {
 
 template <int D, int NT> struct TcShape {
     static constexpr int BM = 128 * NT, BN = NT == 1 ? 64 : 128, NB = 2 / NT;
-    static constexpr int WG = D == 256 ? 1 : 2;            // softmax warpgroups
+    static constexpr bool COLS = D == 256;                 // the softmax warpgroups share every unit's columns
+    static constexpr int STEP = COLS ? 1 : 2;              // a warpgroup's units: every, or every second
+    static constexpr int OS = COLS ? 1 : 2;                // O accumulators
     static constexpr int TILE = BN * D * 2, QB = BM * D * 2;
-    static constexpr int CTRL = 2048;                      // barriers and flags; (m, l) of the second warpgroup's rows
+    static constexpr int CTRL = 3072;                      // barriers and flags; what the warpgroups tell each other of rows
     static constexpr int STAGES = (kSmemMax - CTRL - QB) / TILE < 12 ? (kSmemMax - CTRL - QB) / TILE : 12;
-    static constexpr int THREADS = 128 + 128 * WG;
+    static constexpr int THREADS = 384;
     static constexpr int S_COL = BN, O_COL = 2 * BN;       // TMEM columns: scores u mod 2, then the O tiles
     static constexpr int TMEM = 512;
     static constexpr int SMEM = CTRL + QB + STAGES * TILE;
-    static_assert(SMEM <= kSmemMax && O_COL + WG * D <= TMEM);
+    static_assert(SMEM <= kSmemMax && O_COL + OS * D <= TMEM);
     static_assert((kMaxAttendBatch + 2) * 8 <= STAGES * TILE);   // the plan's sums lie where the tiles come later
 };
 
@@ -111,7 +113,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(bar(B::sfull + i), 1);
-            mbar_init(bar(B::pfull + i), 4);
+            mbar_init(bar(B::pfull + i), C::COLS ? 8 : 4);
             mbar_init(bar(B::ofull + i), 1);
         }
         mbar_init(bar(B::qfull), 1);
@@ -134,7 +136,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
     Segment g;
 
     if (warp < 4) {
-    if constexpr (C::WG == 2) regs_give<88>();
+    regs_give<88>();
     if (warp < kProdWarps) {
         // ---------------------------------------------------------------- producers
         constexpr int CPR = D / 8;                       // 16-byte chunks of a row
@@ -368,16 +370,16 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
                 if (!TMA && !EARLY && t == 0) fence_proxy_async();
                 tc_fence_after();
                 const uint64_t vd = mn_desc(sT + st * C::TILE, BN * 128);
-                const uint32_t wg = C::WG == 2 ? gu & 1 : 0;
+                const uint32_t wg = C::COLS ? 0 : gu & 1;
                 const uint32_t od = tm + C::O_COL + wg * D, pd = tm + (gu & 1) * C::S_COL;
                 if (elect_one()) {
 #pragma unroll
-                    for (int k = 0; k < BN / 16; ++k) umma_bf16_ts(od, pd + k * 8, vd + k * (2048 / 16), idesc_o, u >= C::WG || k > 0);
+                    for (int k = 0; k < BN / 16; ++k) umma_bf16_ts(od, pd + k * 8, vd + k * (2048 / 16), idesc_o, u >= C::OS || k > 0);
                     if (two)
 #pragma unroll
                         for (int k = 0; k < BN / 16; ++k) umma_bf16_ts(od, pd + BN / 2 + k * 8, vd + k * (2048 / 16), idesc_o, 1);
                     if (t == NT - 1) umma_commit(bar(B::empty + st));
-                    if (u >= U - C::WG) umma_commit(bar(B::ofull + wg));
+                    if (u >= U - C::OS) umma_commit(bar(B::ofull + wg));
                 }
                 __syncwarp();
                 if (u + 2 < U) scores(u + 2);
@@ -394,13 +396,17 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
     }
     } else {
         // ---------------------------------------------------------------- softmax
-        if constexpr (C::WG == 2) regs_take<208>();
+        regs_take<208>();
         const int wg = (warp - 4) >> 2, t = NT == 2 ? wg : 0, quad = warp & 3;
         const uint32_t lanes = tmem + ((uint32_t)(quad * 32) << 16);
         const float inv_cap = CAP ? 1.0f / P.cap : 0.0f;
         const float c = CAP ? 1.0f : P.scale * kLog2e;   // factor of the (capped) scores in log2 units
-        constexpr bool JOIN = NT == 1 && C::WG == 2;     // two warpgroups on one row tile
+        constexpr bool JOIN = NT == 1 && !C::COLS;       // two warpgroups on one row tile, each with its own slot tiles
+        constexpr int CW = C::COLS ? BN / 2 : BN;        // columns of a unit that this thread takes, from c0 on
+        const int c0 = C::COLS ? wg * CW : 0, o_col = C::O_COL + (C::COLS ? 0 : wg * D);
         float2* ml = reinterpret_cast<float2*>(smem + 1024) + quad * 32 + lane;
+        float* shared_max = reinterpret_cast<float*>(smem + 1024) + quad * 32 + lane;   // [2][128]
+        float* shared_sum = reinterpret_cast<float*>(smem + 2048) + quad * 32 + lane;   // [2][128]
         const int my_r = t * 128 + quad * 32 + lane, my_tok = my_r / P.G, my_head = my_r - my_tok * P.G;   // this thread's row of a tile
         uint32_t units = 0, items = 0, base_tile = 0, filled[2] = {0, 0};   // filled: times each O has been completed
         bool ok = true;                                  // the same in the lanes of a warp
@@ -422,87 +428,98 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
                 my_scores = P.scores + ((long long)(g.s.t0 + id.t) * P.Hq + id.head) * P.scores_stride;
             }
             const int U = g.n * NT;
-            const int u0 = C::WG == 1 ? 0 : NT == 2 ? t : (int)((units + (uint32_t)wg) & 1);   // this warpgroup's first unit
+            const int u0 = C::COLS ? 0 : NT == 2 ? t : (int)((units + (uint32_t)wg) & 1);   // this warpgroup's first unit
             float m = -INFINITY, l = 0.0f;
             if (JOIN && wg == 1 && items > 0) wait(B::mlempty, (items - 1) & 1);   // its sums of the last item are read
-            for (int u = u0; u < U; u += C::WG) {
+            for (int u = u0; u < U; u += C::STEP) {
                 const int i = u / NT;
                 const uint32_t gu = units + (uint32_t)u;
                 wait(B::sfull + (gu & 1), (gu >> 1) & 1);
-                if (!ok) break;
+                if (!C::COLS && !ok) break;              // (with shared columns the warps go on to meet at the barriers)
                 tc_fence_after();
                 const uint32_t at = lanes + (gu & 1) * C::S_COL;
                 const int j0 = g.kv.at(g.i0 + i) * BN;
-                if (TMA && j0 + BN > g.s.L && (NT == 1 || t == 0)) {
+                if (TMA && j0 + BN > g.s.L && (NT == 2 ? t == 0 : !C::COLS || wg == 0)) {
                     // the boxes brought what the cache holds past the sequence's end: zeros in V's place, before
                     // any P is announced for it
                     const uint32_t p = base_tile + (uint32_t)(C::NB == 1 ? 2 * i + 1 : i == g.n - 1 ? 2 * i + 1 : 2 * i + 2), st = p % C::STAGES;
                     wait(B::full + (int)st, (p / C::STAGES) & 1);
-                    if (!ok) break;
+                    if (!C::COLS && !ok) break;
                     const int from = max(g.s.L - j0, 0);
                     uint8_t* tile = smem + C::CTRL + C::QB + st * C::TILE;
-                    for (int e = (int)(threadIdx.x & 127) + from * 8; e < BN * 8; e += 128)
+                    for (int e = (int)(threadIdx.x & 127) + from * 8; ok && e < BN * 8; e += 128)
 #pragma unroll
                         for (int cb = 0; cb < D / 64; ++cb) *reinterpret_cast<uint4*>(tile + cb * (BN * 128) + e * 16) = make_uint4(0, 0, 0, 0);
                     fence_proxy_async();
                 }
                 const bool all = __all_sync(0xffffffffu, (j0 >= lo && j0 + BN <= hi) || j0 + BN <= pre);
-                uint32_t x[BN];
+                uint32_t x[CW];
                 auto xf = [&](int k) -> float { return __uint_as_float(x[k]); };
 #pragma unroll
-                for (int k = 0; k < BN; k += 32) tmem_ld32_to(x + k, at + k);
+                for (int k = 0; k < CW; k += 32) tmem_ld32_to(x + k, at + c0 + k);
                 tmem_ld_wait();
 #pragma unroll
-                for (int k = 0; k < BN; k += 32) pin32(x + k);
+                for (int k = 0; k < CW; k += 32) pin32(x + k);
                 if constexpr (CAP) {
                     bool near = true;                    // all scores where the series holds: no branch per score
 #pragma unroll
-                    for (int k = 0; k < BN; ++k) {
+                    for (int k = 0; k < CW; ++k) {
                         const float y = xf(k) * (P.scale * inv_cap);
                         near = near && fabsf(y) < 0.5f;
                         x[k] = __float_as_uint(y);
                     }
                     if (__all_sync(0xffffffffu, near)) {
 #pragma unroll
-                        for (int k = 0; k < BN; ++k) x[k] = __float_as_uint(P.cap * kLog2e * tanh_series(xf(k)));
+                        for (int k = 0; k < CW; ++k) x[k] = __float_as_uint(P.cap * kLog2e * tanh_series(xf(k)));
                     } else {
 #pragma unroll
-                        for (int k = 0; k < BN; ++k)
+                        for (int k = 0; k < CW; ++k)
                             x[k] = __float_as_uint(P.cap * kLog2e * (fabsf(xf(k)) < 0.5f ? tanh_series(xf(k)) : tanh_far(xf(k))));
                     }
                 }
                 if (!all) {
 #pragma unroll
-                    for (int k0 = 0; k0 < BN; k0 += 32) {
-                        const uint32_t seen = range_bits(lo, hi, j0 + k0) | range_bits(0, pre, j0 + k0);
+                    for (int k0 = 0; k0 < CW; k0 += 32) {
+                        const uint32_t seen = range_bits(lo, hi, j0 + c0 + k0) | range_bits(0, pre, j0 + c0 + k0);
 #pragma unroll
                         for (int k = 0; k < 32; ++k)
                             if (!(seen >> k & 1u)) x[k0 + k] = 0xff800000u;
                     }
                 }
                 if (NT == 1 && P.scores && real && j0 < P.scores_stride) {   // for the weight sums, in log2 units
-                    float4* to = reinterpret_cast<float4*>(my_scores + j0);
+                    float4* to = reinterpret_cast<float4*>(my_scores + j0 + c0);
 #pragma unroll
-                    for (int k = 0; k < BN; k += 4) __stcg(to + k / 4, make_float4(xf(k) * c, xf(k + 1) * c, xf(k + 2) * c, xf(k + 3) * c));
+                    for (int k = 0; k < CW; k += 4) __stcg(to + k / 4, make_float4(xf(k) * c, xf(k + 1) * c, xf(k + 2) * c, xf(k + 3) * c));
                 }
                 float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                for (int k = 0; k < BN; k += 2) top[k >> 1 & 3] = max3(top[k >> 1 & 3], xf(k), xf(k + 1));
-                const float next = fmaxf(m, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * c);
-                // a row that grew by more than 2^8 (or had seen nothing) takes its new maximum, and its warp with it
-                if (__any_sync(0xffffffffu, next > m + 8.0f || (m == -INFINITY && next > m))) {
+                for (int k = 0; k < CW; k += 2) top[k >> 1 & 3] = max3(top[k >> 1 & 3], xf(k), xf(k + 1));
+                const float mine = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * c;
+                float next = fmaxf(m, mine);
+                // a row that grew by more than 2^8 (or had seen nothing) takes its new maximum, and its warp with it;
+                // with shared columns both warpgroups hold the same maximum and decide together
+                bool grown = __any_sync(0xffffffffu, next > m + 8.0f || (m == -INFINITY && next > m));
+                if constexpr (C::COLS) {
+                    grown = group_any(4, 256, grown && ok);
+                    if (grown) {
+                        shared_max[wg * 128] = mine;
+                        group_sync(4, 256);
+                        next = fmaxf(next, shared_max[(wg ^ 1) * 128]);
+                    }
+                }
+                if (grown) {
                     const float w = next == -INFINITY ? 1.0f : exp2_hw(m - next);
                     m = next;
                     l *= w;
-                    if (u >= C::WG) {                    // S(u) complete: so is the MMA that last added to O
+                    if (u >= C::OS) {                    // S(u) complete: so is the MMA that last added to O
 #pragma unroll 1
-                        for (int k = 0; k < D; k += 16) {
+                        for (int k = C::COLS ? wg * (D / 2) : 0; k < (C::COLS ? (wg + 1) * (D / 2) : D); k += 16) {
                             uint32_t o[16];
-                            tmem_ld16(lanes + C::O_COL + wg * D + k, o);
+                            tmem_ld16(lanes + o_col + k, o);
                             tmem_ld_wait();
 #pragma unroll
                             for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * w);
-                            tmem_st16(lanes + C::O_COL + wg * D + k, o);
+                            tmem_st16(lanes + o_col + k, o);
                         }
                     }
                 }
@@ -517,29 +534,30 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
                     sum[k >> 1 & 1] = add2(sum[k >> 1 & 1], y);
                     return y;
                 };
+                constexpr int STORE = CW < 64 ? CW : 64;   // columns of S whose P goes out with one store
                 if (two) {
 #pragma unroll
-                    for (int k0 = 0; k0 < BN; k0 += 64) {
-                        uint32_t low[32];
+                    for (int k0 = 0; k0 < CW; k0 += STORE) {
+                        uint32_t low[STORE / 2];
 #pragma unroll
-                        for (int k = 0; k < 64; k += 2) {
+                        for (int k = 0; k < STORE; k += 2) {
                             const float2 y = weights(k0 + k);
                             const uint32_t w = pack_bf16(y.x, y.y);
                             x[(k0 + k) >> 1] = w;
                             low[k >> 1] = pack_bf16(y.x - bf_lo(w), y.y - bf_hi(w));
                         }
-                        tmem_st32(at + k0 / 2, x + k0 / 2);
-                        tmem_st32(at + BN / 2 + k0 / 2, low);
+                        store_p<STORE / 2>(at + (c0 + k0) / 2, x + k0 / 2);
+                        store_p<STORE / 2>(at + (BN + c0 + k0) / 2, low);
                     }
                 } else {
 #pragma unroll
-                    for (int k0 = 0; k0 < BN; k0 += 64) {
+                    for (int k0 = 0; k0 < CW; k0 += STORE) {
 #pragma unroll
-                        for (int k = 0; k < 64; k += 2) {
+                        for (int k = 0; k < STORE; k += 2) {
                             const float2 y = weights(k0 + k);
                             x[(k0 + k) >> 1] = pack_bf16(y.x, y.y);
                         }
-                        tmem_st32(at + k0 / 2, x + k0 / 2);
+                        store_p<STORE / 2>(at + (c0 + k0) / 2, x + k0 / 2);
                     }
                 }
                 const float2 s2 = add2(sum[0], sum[1]);
@@ -549,10 +567,10 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(B::pfull + (gu & 1)));
             }
-            const int u1 = C::WG == 1 ? 1 : u0 ^ 1;          // the other warpgroup's first unit
+            const int u1 = u0 ^ 1;                           // the other warpgroup's first unit (a slot tile each)
             units += (uint32_t)U;
             base_tile += 2 * (uint32_t)g.n;
-            if (ok && u0 < U) wait(B::ofull + wg, filled[0] & 1);
+            if (ok && u0 < U) wait(B::ofull + (C::COLS ? 0 : wg), filled[0] & 1);
             filled[0] += u0 < U;
             bool other = false;                              // join: the other warpgroup has sums, too
             float w0 = 1.0f, w1 = 0.0f;
@@ -575,6 +593,11 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
                 l = l * w0 + x.y * w1;
                 m = top;
             }
+            if constexpr (C::COLS) {                         // the sums of both halves, added alike
+                shared_sum[wg * 128] = l;
+                group_sync(4, 256);
+                l = shared_sum[0] + shared_sum[128];
+            }
             ++items;
             tc_fence_after();
             const bool whole = g.whole();
@@ -585,10 +608,10 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
             bool fine = true;
             if (ok) {
 #pragma unroll 1                                             // short code: a cold instruction cache costs small calls most
-                for (int k = 0; k < D; k += 32) {
+                for (int k = C::COLS ? wg * (D / 2) : 0; k < (C::COLS ? (wg + 1) * (D / 2) : D); k += 32) {
                     uint32_t o[32];
                     if (!JOIN || u0 < U) {
-                        tmem_ld32(lanes + C::O_COL + wg * D + k, o);
+                        tmem_ld32(lanes + o_col + k, o);
                         tmem_ld_wait();
                     }
                     if constexpr (JOIN) {
@@ -629,17 +652,18 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
                 if (lane == 0) mbar_arrive(bar(B::mlempty));
             }
             if (whole) {
-                if (real && P.lse) P.lse[(long long)(g.s.t0 + id.t) * P.Hq + id.head] = lse2 * kLn2;
+                if (real && P.lse && !(C::COLS && wg)) P.lse[(long long)(g.s.t0 + id.t) * P.Hq + id.head] = lse2 * kLn2;
                 for (uint32_t bad = __ballot_sync(0xffffffffu, real && !fine); bad; bad &= bad - 1) {
                     const int who = __ffs(bad) - 1;
                     float o[D / 32];
                     resum_row<__nv_bfloat16, D>(P, g.s, g.b, g.h, row - lane + who, __shfl_sync(0xffffffffu, lse2, who), o);
                     const RowId bid = row_id(P, g.s, g.h, row - lane + who);
-                    store_f32<__nv_bfloat16, D / 32>((__nv_bfloat16*)P.out + (long long)(g.s.t0 + bid.t) * P.o_t + (long long)bid.head * P.o_h +
-                                                         lane * (D / 32), o);
+                    if (!C::COLS || lane >> 4 == wg)         // a half of the channels is this warpgroup's
+                        store_f32<__nv_bfloat16, D / 32>((__nv_bfloat16*)P.out + (long long)(g.s.t0 + bid.t) * P.o_t + (long long)bid.head * P.o_h +
+                                                             lane * (D / 32), o);
                 }
             } else {
-                if (real) __stcg(P.part_ml + part, make_float2(m, l));
+                if (real && !(C::COLS && wg)) __stcg(P.part_ml + part, make_float2(m, l));
             }
         }
         if (threadIdx.x == 128) leave_split(P, plan, g, have);

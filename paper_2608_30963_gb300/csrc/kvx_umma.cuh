@@ -112,6 +112,23 @@ __device__ __forceinline__ void tma_box3(uint32_t dst, const CUtensorMap* map, i
                  "l"(map), "r"(mbar), "r"(x), "r"(y), "r"(z)
                  : "memory");
 }
+// N (16 or 32) columns of the warp's lanes written
+template <int N> __device__ __forceinline__ void store_p(uint32_t taddr, const uint32_t* r)
+{
+    if constexpr (N == 32) tmem_st32(taddr, r);
+    else tmem_st16(taddr, *reinterpret_cast<const uint32_t(*)[16]>(r));
+}
+// Threads of a group (whole warps) wait for one another, and learn whether any of them says so.
+__device__ __forceinline__ bool group_any(int id, int threads, bool mine)
+{
+    uint32_t any;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, %2, %3, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+        : "=r"(any)
+        : "r"((uint32_t)mine), "r"(id), "r"(threads)
+        : "memory");
+    return any != 0;
+}
 // Threads of a group (whole warps) wait for one another.
 __device__ __forceinline__ void group_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 
