@@ -603,7 +603,11 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
             const bool whole = g.whole();
             const float inv = whole ? (l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : l)) : 1.0f;
             const float lse2 = l == 0.0f ? -INFINITY : m + log2f(l);
-            __nv_bfloat16* out = (__nv_bfloat16*)P.out + (long long)(g.s.t0 + id.t) * P.o_t + (long long)id.head * P.o_h;
+            const int quad_rows = rows - (my_r & ~3);        // real rows from the first of this lane's four on
+            const long long out_row = (long long)(g.s.t0 + id.t) * P.o_t + (long long)id.head * P.o_h;
+            long long out_of[4];                             // where the four rows' outputs begin
+#pragma unroll
+            for (int r = 0; r < 4; ++r) out_of[r] = __shfl_sync(0xffffffffu, out_row, (lane & ~3) + r);
             const size_t part = (size_t)(2 * blockIdx.x + (g.first ? 0 : 1)) * BM + my_r;
             bool fine = true;
             if (ok) {
@@ -624,24 +628,34 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
                         for (int e = 0; e < 32; ++e)
                             o[e] = __float_as_uint((u0 < U ? __uint_as_float(o[e]) * w0 : 0.0f) + (other ? __uint_as_float(o1[e]) * w1 : 0.0f));
                     }
-                    if (whole && real) {
+                    // Four lanes exchange chunks, so that a store writes 64 bytes of each of 8 rows (a row a lane: 16 of 32)
+                    if (whole) {
+                        uint32_t v[16];
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) {
-                            const float v = l == 0.0f ? 0.0f : __uint_as_float(o[e]) * inv;
-                            fine = fine && fabsf(v) <= 3.0e38f;
-                            o[e] = __float_as_uint(v);
+                        for (int e = 0; e < 32; e += 2) {
+                            const float y0 = l == 0.0f ? 0.0f : __uint_as_float(o[e]) * inv, y1 = l == 0.0f ? 0.0f : __uint_as_float(o[e + 1]) * inv;
+                            fine = fine && fabsf(y0) <= 3.0e38f && fabsf(y1) <= 3.0e38f;
+                            v[e >> 1] = pack_bf16(y0, y1);
                         }
+                        transpose_quad(v);
 #pragma unroll
-                        for (int e = 0; e < 32; e += 8)
-                            *reinterpret_cast<uint4*>(out + k + e) =
-                                make_uint4(pack_bf16(__uint_as_float(o[e]), __uint_as_float(o[e + 1])),
-                                           pack_bf16(__uint_as_float(o[e + 2]), __uint_as_float(o[e + 3])),
-                                           pack_bf16(__uint_as_float(o[e + 4]), __uint_as_float(o[e + 5])),
-                                           pack_bf16(__uint_as_float(o[e + 6]), __uint_as_float(o[e + 7])));
-                    } else if (real) {
+                        for (int r = 0; r < 4; ++r)
+                            if (quad_rows > r)
+                                *reinterpret_cast<uint4*>((__nv_bfloat16*)P.out + out_of[r] + k + (lane & 3) * 8) =
+                                    make_uint4(v[r * 4], v[r * 4 + 1], v[r * 4 + 2], v[r * 4 + 3]);
+                    } else {
 #pragma unroll
-                        for (int e = 0; e < 32; e += 4)
-                            __stcg(reinterpret_cast<uint4*>(P.part_o + part * D + k + e), make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]));
+                        for (int e = 0; e < 32; e += 16) {
+                            uint32_t v[16];
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) v[i] = o[e + i];
+                            transpose_quad(v);
+#pragma unroll
+                            for (int r = 0; r < 4; ++r)
+                                if (quad_rows > r)
+                                    __stcg(reinterpret_cast<uint4*>(P.part_o + (part - (lane & 3) + r) * D + k + e + (lane & 3) * 4),
+                                           make_uint4(v[r * 4], v[r * 4 + 1], v[r * 4 + 2], v[r * 4 + 3]));
+                        }
                     }
                     __syncwarp();
                 }

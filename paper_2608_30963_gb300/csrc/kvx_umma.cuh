@@ -112,6 +112,27 @@ __device__ __forceinline__ void tma_box3(uint32_t dst, const CUtensorMap* map, i
                  "l"(map), "r"(mbar), "r"(x), "r"(y), "r"(z)
                  : "memory");
 }
+// Lane j of four holds row j's chunks 0 .. 3 of four words; afterwards chunk j of rows 0 .. 3.
+__device__ __forceinline__ void transpose_quad(uint32_t (&v)[16])
+{
+    const uint32_t lane = threadIdx.x;
+#pragma unroll
+    for (int s = 1; s <= 2; s <<= 1) {
+        const bool up = lane & s;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            if (c & s) continue;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                uint32_t& a = v[c * 4 + e];
+                uint32_t& b = v[(c + s) * 4 + e];
+                const uint32_t t = __shfl_xor_sync(0xffffffffu, up ? a : b, s);
+                if (up) a = t;
+                else b = t;
+            }
+        }
+    }
+}
 // N (16 or 32) columns of the warp's lanes written
 template <int N> __device__ __forceinline__ void store_p(uint32_t taddr, const uint32_t* r)
 {
