@@ -1,4 +1,4 @@
-// kvx_attend.cu -- attention of new tokens over a cache on the CUDA cores, and the launch of the
+// kvx_attend.cu -- attention of new tokens over an fp32 cache on the CUDA cores, and the choice of the
 // attention kernels.
 //
 //   o_i = sum_j p_ij v_j / sum_j p_ij,  p_ij = exp(x_ij - m_i),  x_ij = cap(scale q_i . k_j)
@@ -23,27 +23,18 @@ __device__ __forceinline__ float2 ffma2(float2 a, float2 b, float2 c)
     return reinterpret_cast<float2&>(r);
 }
 
-// A tile of R rows (BM queries or kBN slots) of D channels as fp32 in shared memory, rows D + 4 floats
-// apart (float4 reads of neighbouring rows fall into different banks).  off(r) gives a row's element
-// offset, or -1 for a row of zeros.  fp32 rows are copied asynchronously, bf16 rows widened here.
-template <typename T, int D, int R, int THREADS, typename Off>
-__device__ __forceinline__ void load_tile(float* dst, const T* src, Off off)
+// A tile of R rows (BM queries or kBN slots) of D channels in shared memory, rows D + 4 floats apart (float4 reads of
+// neighbouring rows fall into different banks), copied asynchronously.  off(r) gives a row's element offset, or -1
+// for a row of zeros.
+template <int D, int R, int THREADS, typename Off> __device__ __forceinline__ void load_tile(float* dst, const float* src, Off off)
 {
-    constexpr int V = 16 / (int)sizeof(T), PER = D / V;
+    constexpr int PER = D / 4;
     for (int i = threadIdx.x; i < R * PER; i += THREADS) {
-        const int r = i / PER, c = (i - r * PER) * V;
+        const int r = i / PER, c = (i - r * PER) * 4;
         const long long at = off(r);
         float* d = dst + r * (D + 4) + c;
-        if (at < 0) {
-#pragma unroll
-            for (int e = 0; e < V; e += 4) *reinterpret_cast<float4*>(d + e) = make_float4(0.f, 0.f, 0.f, 0.f);
-        } else if constexpr (sizeof(T) == 4) {
-            cp_async16(smem_u32(d), src + at + c);
-        } else {
-            const uint4 w = *reinterpret_cast<const uint4*>(src + at + c);
-            *reinterpret_cast<float4*>(d) = make_float4(bf_lo(w.x), bf_hi(w.x), bf_lo(w.y), bf_hi(w.y));
-            *reinterpret_cast<float4*>(d + 4) = make_float4(bf_lo(w.z), bf_hi(w.z), bf_lo(w.w), bf_hi(w.w));
-        }
+        if (at < 0) *reinterpret_cast<float4*>(d) = make_float4(0.f, 0.f, 0.f, 0.f);
+        else cp_async16(smem_u32(d), src + at + c);
     }
 }
 __device__ __forceinline__ void async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
@@ -83,11 +74,12 @@ __device__ __forceinline__ void scores(const float* sQ, const float* sK, int tr,
         for (int j = 0; j < kKN; ++j) x[i][j] = acc[i][j].x + acc[i][j].y;
 }
 
-// A raw score in log2 units, capped.
-__device__ __forceinline__ float score2(const AttendParams& P, float dot, float inv_cap)
+// A raw score in log2 units, capped (the capped scores' code in kernels of its own: inlined for each score, it
+// would be most of a kernel's).
+template <bool CAP> __device__ __forceinline__ float score2(const AttendParams& P, float dot, float inv_cap)
 {
     float v = dot * P.scale;
-    if (P.cap > 0.0f) v = capped(v, P.cap, inv_cap);
+    if constexpr (CAP) v = capped(v, P.cap, inv_cap);
     return v * kLog2e;
 }
 
@@ -98,7 +90,7 @@ template <int D, int BM> constexpr int simt_smem()
 
 // 128 threads on a tile of BM rows and 32 slots; K of the next tile is copied while V is multiplied, V
 // while the scores are.
-template <typename T, int D, int BM>
+template <int D, int BM, bool CAP>
 __global__ void __launch_bounds__(kThreads) attend_simt_kernel(const __grid_constant__ AttendParams P)
 {
     constexpr int RM = BM / kTR, CN = D / 32;   // rows of a thread; its float4 column groups 4 tc + 32 n
@@ -129,10 +121,10 @@ __global__ void __launch_bounds__(kThreads) attend_simt_kernel(const __grid_cons
             return at;
         };
         auto load_slots = [&](float* dst, const void* src, int tile) {
-            load_tile<T, D, kBN, kThreads>(dst, (const T*)src, [&](int r) { return slot_row(tile, r); });
+            load_tile<D, kBN, kThreads>(dst, (const float*)src, [&](int r) { return slot_row(tile, r); });
             async_commit();
         };
-        load_tile<T, D, BM, kThreads>(sQ, (const T*)P.q, [&](int r) {
+        load_tile<D, BM, kThreads>(sQ, (const float*)P.q, [&](int r) {
             if (r >= rows) return -1ll;
             const RowId id = row_id(P, g.s, g.h, g.rt * BM + r);
             return (long long)(g.s.t0 + id.t) * P.q_t + (long long)id.head * P.q_h;
@@ -162,11 +154,16 @@ __global__ void __launch_bounds__(kThreads) attend_simt_kernel(const __grid_cons
 #pragma unroll
             for (int i = 0; i < RM; ++i) {
                 float top = -INFINITY;
+                const int j0 = tile * kBN, lo = window_lo(P, slot_i[i]);
+                const bool all = (j0 >= lo && j0 + kBN - 1 <= slot_i[i] && j0 + kBN <= g.s.L) || j0 + kBN <= g.s.pre;
 #pragma unroll
-                for (int j = 0; j < kKN; ++j) {
-                    x[i][j] = sees(P, g.s, slot_i[i], tile * kBN + tc + kTC * j) ? score2(P, x[i][j], inv_cap) : -INFINITY;
-                    top = fmaxf(top, x[i][j]);
-                }
+                for (int j = 0; j < kKN; ++j) x[i][j] = score2<CAP>(P, x[i][j], inv_cap);
+                if (!all)
+#pragma unroll
+                    for (int j = 0; j < kKN; ++j)
+                        if (!sees(P, g.s, slot_i[i], j0 + tc + kTC * j)) x[i][j] = -INFINITY;
+#pragma unroll
+                for (int j = 0; j < kKN; ++j) top = fmaxf(top, x[i][j]);
 #pragma unroll
                 for (int k = 4; k; k >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
                 const float next = fmaxf(m[i], top), base = next == -INFINITY ? 0.0f : next;
@@ -230,7 +227,7 @@ __global__ void __launch_bounds__(kThreads) attend_simt_kernel(const __grid_cons
                 float y[D / 32];
 #pragma unroll
                 for (int c = 0; c < D / 32; ++c) y[c] = sQ[r * (D + 4) + lane * (D / 32) + c];
-                finish_row<T, D>(P, g.s, g.b, g.h, g.rt * BM + r, sP[r * (kBN + 4)], sP[r * (kBN + 4) + 1], y);
+                finish_row<float, D>(P, g.s, g.b, g.h, g.rt * BM + r, sP[r * (kBN + 4)], sP[r * (kBN + 4) + 1], y);
             }
         } else {
             const size_t at = (size_t)(2 * blockIdx.x + (g.first ? 0 : 1)) * BM;
@@ -252,11 +249,11 @@ __global__ void __launch_bounds__(kThreads) attend_simt_kernel(const __grid_cons
 
 // key_weight[b, h, j] += sum over the rows i of (b, h) of exp(x_ij - lse_i): the scores are formed again, now
 // that every row's sum is known, one CTA to a tile of 32 slots, which no other CTA adds to.
-template <typename T, int D> constexpr int weight_smem()
+template <int D> constexpr int weight_smem()
 {
     return ((64 + kBN) * (D + 4) + 64 + kTR * kBN) * 4 + (kMaxAttendBatch + 2) * 8;
 }
-template <typename T, int D>
+template <int D, bool CAP>
 __global__ void __launch_bounds__(kThreads) key_weight_simt_kernel(const __grid_constant__ AttendParams P)
 {
     constexpr int BM = 64, RM = BM / kTR;
@@ -286,7 +283,7 @@ __global__ void __launch_bounds__(kThreads) key_weight_simt_kernel(const __grid_
         const int b = lo, j0 = (int)(ut - first[b]) * kBN;
         const Seq s = load_seq(P, b);
         __syncthreads();
-        load_tile<T, D, kBN, kThreads>(sK, (const T*)P.ck, [&](int r) {
+        load_tile<D, kBN, kThreads>(sK, (const float*)P.ck, [&](int r) {
             const long long at = j0 + r < s.L ? cache_row(P.cache, b, j0 + r) : -1;
             return at < 0 ? -1ll : at + cache_head(P.cache) * h;
         });
@@ -298,7 +295,7 @@ __global__ void __launch_bounds__(kThreads) key_weight_simt_kernel(const __grid_
         const int t_end = (j0 < s.pre || P.window == 0) ? s.n : (int)min((long long)s.n, (long long)j0 + kBN - 1 + P.window - (s.L - s.n));
         for (int r0 = t_first * P.G; r0 < t_end * P.G; r0 += BM) {
             const int rows = min(BM, t_end * P.G - r0);
-            load_tile<T, D, BM, kThreads>(sQ, (const T*)P.q, [&](int r) {
+            load_tile<D, BM, kThreads>(sQ, (const float*)P.q, [&](int r) {
                 if (r >= rows) return -1ll;
                 const RowId id = row_id(P, s, h, r0 + r);
                 return (long long)(s.t0 + id.t) * P.q_t + (long long)id.head * P.q_h;
@@ -322,7 +319,7 @@ __global__ void __launch_bounds__(kThreads) key_weight_simt_kernel(const __grid_
                 const int own = s.slot((r0 + r) / P.G);
 #pragma unroll
                 for (int j = 0; j < kKN; ++j)
-                    if (r < rows && sees(P, s, own, j0 + tc + kTC * j)) w[j] += exp2_hw(score2(P, x[i][j], inv_cap) - sL[r]);
+                    if (r < rows && sees(P, s, own, j0 + tc + kTC * j)) w[j] += exp2_hw(score2<CAP>(P, x[i][j], inv_cap) - sL[r]);
             }
             __syncthreads();
         }
@@ -351,31 +348,40 @@ template <auto Kernel> int ctas_per_sm(int smem, int threads)
     return n;
 }
 
-template <typename T, int D, int BM>
-cudaError_t run_simt(const AttendParams& call, int num_sms, cudaStream_t stream)
+template <int D, int BM, bool CAP> cudaError_t run_simt(const AttendParams& call, int num_sms, cudaStream_t stream)
 {
     AttendParams P = call;
     P.tile_rows = BM;
     constexpr int smem = simt_smem<D, BM>();
-    if (cudaError_t e = smem_opt_in<attend_simt_kernel<T, D, BM>>(smem); e != cudaSuccess) return e;
-    const int grid = min(num_sms * ctas_per_sm<attend_simt_kernel<T, D, BM>>(smem, kThreads), kAttendMaxRows / BM / 2);
-    attend_simt_kernel<T, D, BM><<<grid, kThreads, smem, stream>>>(P);
+    if (cudaError_t e = smem_opt_in<attend_simt_kernel<D, BM, CAP>>(smem); e != cudaSuccess) return e;
+    const int grid = min(num_sms * ctas_per_sm<attend_simt_kernel<D, BM, CAP>>(smem, kThreads), kAttendMaxRows / BM / 2);
+    attend_simt_kernel<D, BM, CAP><<<grid, kThreads, smem, stream>>>(P);
     if (cudaError_t e = cudaGetLastError(); e != cudaSuccess) return e;
-    return run_join<T, D, BM>(P, grid, stream);
+    return run_join<float, D, BM>(P, grid, stream);
 }
-template <typename T, int D> cudaError_t run_weight_simt(const AttendParams& P, int num_sms, cudaStream_t stream)
+template <int D, bool CAP> cudaError_t run_weight_simt(const AttendParams& P, int num_sms, cudaStream_t stream)
 {
-    constexpr int smem = weight_smem<T, D>();
-    if (cudaError_t e = smem_opt_in<key_weight_simt_kernel<T, D>>(smem); e != cudaSuccess) return e;
-    key_weight_simt_kernel<T, D><<<num_sms * ctas_per_sm<key_weight_simt_kernel<T, D>>(smem, kThreads), kThreads, smem, stream>>>(P);
+    constexpr int smem = weight_smem<D>();
+    if (cudaError_t e = smem_opt_in<key_weight_simt_kernel<D, CAP>>(smem); e != cudaSuccess) return e;
+    const int grid = num_sms * ctas_per_sm<key_weight_simt_kernel<D, CAP>>(smem, kThreads);
+    key_weight_simt_kernel<D, CAP><<<grid, kThreads, smem, stream>>>(P);
     return cudaGetLastError();
 }
 
-template <int D> cudaError_t run_fp32(const AttendParams& P, int num_sms, cudaStream_t stream)
+template <int D, bool CAP> cudaError_t run_fp32(const AttendParams& P, int num_sms, cudaStream_t stream)
 {
     // few rows for each sequence and head: 16-row tiles waste less of the arithmetic
     const bool few = (long long)P.T * P.G <= 16ll * P.batch;
-    return few ? run_simt<float, D, 16>(P, num_sms, stream) : run_simt<float, D, D == 256 ? 32 : 64>(P, num_sms, stream);
+    return few ? run_simt<D, 16, CAP>(P, num_sms, stream) : run_simt<D, D == 256 ? 32 : 64, CAP>(P, num_sms, stream);
+}
+template <bool CAP> cudaError_t attend_fp32(const AttendParams& P, int num_sms, cudaStream_t stream)
+{
+    return P.d == 64 ? run_fp32<64, CAP>(P, num_sms, stream) : P.d == 128 ? run_fp32<128, CAP>(P, num_sms, stream) : run_fp32<256, CAP>(P, num_sms, stream);
+}
+template <bool CAP> cudaError_t weigh_fp32(const AttendParams& P, int num_sms, cudaStream_t stream)
+{
+    return P.d == 64 ? run_weight_simt<64, CAP>(P, num_sms, stream) : P.d == 128 ? run_weight_simt<128, CAP>(P, num_sms, stream)
+                                                                             : run_weight_simt<256, CAP>(P, num_sms, stream);
 }
 
 }  // namespace
@@ -391,15 +397,14 @@ cudaError_t launch_attend(const AttendParams& call, int dtype, int num_sms, cuda
     P.scores_stride = (P.weight_stride + 63) / 64 * 64;
     const bool keep = bf16 && P.key_weight && (long long)P.T * P.G <= 16ll * P.batch && (long long)P.T * P.Hq * P.scores_stride <= kAttendScores;
     if (!keep) P.scores = nullptr;
-    cudaError_t e = bf16 ? launch_attend_tc(P, num_sms, stream)
-                         : P.d == 64 ? run_fp32<64>(P, num_sms, stream) : P.d == 128 ? run_fp32<128>(P, num_sms, stream) : run_fp32<256>(P, num_sms, stream);
+    const bool cap = P.cap > 0.0f;
+    cudaError_t e = bf16 ? launch_attend_tc(P, num_sms, stream) : cap ? attend_fp32<true>(P, num_sms, stream) : attend_fp32<false>(P, num_sms, stream);
     *launches = 2;
     if (e != cudaSuccess || !P.key_weight) return e;
     *launches = 3;
     if (keep) return launch_sum_scores(P, stream);
     if (bf16) return launch_key_weight(P, num_sms, stream);
-    return P.d == 64 ? run_weight_simt<float, 64>(P, num_sms, stream) : P.d == 128 ? run_weight_simt<float, 128>(P, num_sms, stream)
-                                                                              : run_weight_simt<float, 256>(P, num_sms, stream);
+    return cap ? weigh_fp32<true>(P, num_sms, stream) : weigh_fp32<false>(P, num_sms, stream);
 }
 
 }  // namespace kvx

@@ -7,8 +7,8 @@
 // many, by reading K where they are few.
 //   producer warps      two copy K of a slot tile with 16-byte cp.async, one brings Q by tensor copies: a row tile is
 //                       the G query heads of 128 / G tokens, one box for each 64 channels
-//   MMA thread          S^T into one of two score buffers
-//   softmax warps       two warpgroups, row tiles in turn; the second's sums go through shared memory
+//   MMA thread          S^T into one of four score buffers
+//   weight warps        four warpgroups, row tiles in turn, their sums added through shared memory
 #include <limits.h>
 
 #include "kvx_attend_rows.cuh"
@@ -17,18 +17,20 @@
 namespace kvx {
 namespace {
 
+constexpr int kKwGroups = 4;
+
 template <int D> struct KwShape {
     static constexpr int TILE = 128 * D * 2;
-    static constexpr int CTRL = 15 * 1024;                 // barriers; rows' lse and slots; sums; the units' plan
+    static constexpr int CTRL = 22 * 1024;                 // barriers; rows' lse and slots; sums; the units' plan
     static constexpr int SLOTS = (kSmemMax - CTRL) / TILE < 12 ? (kSmemMax - CTRL) / TILE : 12;   // K and Q tiles together
     static constexpr int SMEM = CTRL + SLOTS * TILE;
-    static constexpr int THREADS = 384;
-    static_assert(SLOTS >= 3 && 6144 + (kMaxAttendBatch + 1) * 8 <= CTRL);
+    static constexpr int THREADS = 128 + 128 * kKwGroups;
+    static_assert(SLOTS >= 3 && 13312 + (kMaxAttendBatch + 1) * 8 <= CTRL);
 };
 
-// Barriers: full and empty of every tile, scores full and free of both buffers.
+// Barriers: full and empty of every tile, scores full and free of every buffer.
 struct KwBars {
-    static constexpr int full = 0, empty = 12, sfull = 24, sfree = 26, done = 28;
+    static constexpr int full = 0, empty = 12, sfull = 24, sfree = sfull + kKwGroups, done = sfree + kKwGroups;
 };
 
 // A slot tile and KV head, and the tokens [t0, t1) that may see any of it, in tiles of `per` tokens.
@@ -67,22 +69,22 @@ __global__ void __launch_bounds__(KwShape<D>::THREADS, 1) key_weight_kernel(cons
     auto bar = [&](int i) { return s0 + (uint32_t)i * 8; };
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + 512);
     int* abort = reinterpret_cast<int*>(smem + 516);
-    float* row_lse = reinterpret_cast<float*>(smem + 1024);        // [2][2][128]: minus the rows' lse, log2 units
-    int* row_slot = reinterpret_cast<int*>(smem + 3072);           // [2][2][128]: the rows' own slots
-    float* sums = reinterpret_cast<float*>(smem + 5120);           // [2][128]
-    long long* first = reinterpret_cast<long long*>(smem + 6144);  // [batch + 1]: slot tiles before each sequence's
+    float* row_lse = reinterpret_cast<float*>(smem + 1024);        // [4][2][128]: minus the rows' lse, log2 units
+    int* row_slot = reinterpret_cast<int*>(smem + 5120);           // [4][2][128]: the rows' own slots
+    float* sums = reinterpret_cast<float*>(smem + 9216);           // [2][4][128]
+    long long* first = reinterpret_cast<long long*>(smem + 13312);  // [batch + 1]: slot tiles before each sequence's
     const uint32_t sT = s0 + C::CTRL;
     const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const int q_slots = C::SLOTS - k_slots;
     const int per = 128 / P.G;                             // tokens a row tile
 
-    if (warp == 3) tmem_alloc(smem_u32(tmem_slot), 256);
+    if (warp == 3) tmem_alloc(smem_u32(tmem_slot), 512);
     if (threadIdx.x == 0) {
         for (int i = 0; i < C::SLOTS; ++i) {
             mbar_init(bar(B::full + i), i < k_slots ? 64 : 1);
             mbar_init(bar(B::empty + i), 1);
         }
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < kKwGroups; ++i) {
             mbar_init(bar(B::sfull + i), 1);
             mbar_init(bar(B::sfree + i), 4);
         }
@@ -180,11 +182,11 @@ __global__ void __launch_bounds__(KwShape<D>::THREADS, 1) key_weight_kernel(cons
             const uint32_t ks = kn % (uint32_t)k_slots;
             wait(B::full + (int)ks, (kn / (uint32_t)k_slots) & 1);
             for (int i = 0; i < tiles && ok; ++i, ++qn) {
-                const uint32_t qs = (uint32_t)k_slots + qn % (uint32_t)q_slots, buf = qn & 1;
+                const uint32_t qs = (uint32_t)k_slots + qn % (uint32_t)q_slots, buf = qn % kKwGroups;
                 wait(B::full + (int)qs, (qn / (uint32_t)q_slots) & 1);
-                wait(B::sfree + (int)buf, ((qn >> 1) & 1) ^ 1);
+                wait(B::sfree + (int)buf, ((qn / kKwGroups) & 1) ^ 1);
                 if (!ok) break;
-                fence_proxy_async();
+                if (i == 0) fence_proxy_async();             // K came by thread copies
                 tc_fence_after();
                 const uint64_t kd = sw128_desc(sT + ks * C::TILE), qd = sw128_desc(sT + qs * C::TILE);
                 if (elect_one()) {
@@ -229,9 +231,9 @@ __global__ void __launch_bounds__(KwShape<D>::THREADS, 1) key_weight_kernel(cons
                 return my_row && i < tiles && t < x.t1
                            ? -__ldcg(&P.lse[(long long)(x.s.t0 + t) * P.Hq + x.h * P.G + my_head]) * kLog2e : -INFINITY;
             };
-            const int i0 = (int)((qn ^ (uint32_t)wg) & 1);
+            const int i0 = (int)(((uint32_t)wg - qn) % kKwGroups);
             float next = row_value(i0);
-            for (int i = i0; i < tiles; i += 2, ++turn) {
+            for (int i = i0; i < tiles; i += kKwGroups, ++turn) {
                 const uint32_t n = qn + (uint32_t)i;
                 const int t = x.t0 + i * per;
                 float* lse = row_lse + (wg * 2 + (turn & 1)) * 128;
@@ -239,8 +241,8 @@ __global__ void __launch_bounds__(KwShape<D>::THREADS, 1) key_weight_kernel(cons
                 lse[own] = next;
                 slot[own] = my_row && t + my_tok < x.t1 ? x.s.slot(t + my_tok) : INT_MIN;
                 group_sync(1 + wg, 128);
-                next = row_value(i + 2);
-                wait(B::sfull + (int)(n & 1), (n >> 1) & 1);
+                next = row_value(i + kKwGroups);
+                wait(B::sfull + wg, (n / kKwGroups) & 1);
                 tc_fence_after();
                 // do all rows of a whole tile see all its slots?
                 const int lo_slot = x.s.slot(t), hi_slot = x.s.slot(t + per - 1);
@@ -249,8 +251,8 @@ __global__ void __launch_bounds__(KwShape<D>::THREADS, 1) key_weight_kernel(cons
                 float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
                 if (ok) {
 #pragma unroll 1                                             // a body twice as long would miss the instruction cache
-                    for (int k0 = 0; k0 < 128; k0 += 64) {
-                        uint32_t s[64];
+                    for (int k0 = 0; k0 < 128; k0 += 32) {
+                        uint32_t s[32];
                         auto sf = [&](int k) -> float { return __uint_as_float(s[k]); };
                         // the weights of rows k .. k + 3
                         auto four = [&](int k0_, int k, float2& a, float2& b) {
@@ -261,36 +263,34 @@ __global__ void __launch_bounds__(KwShape<D>::THREADS, 1) key_weight_kernel(cons
                             b = make_float2(exp2_hw(b.x), exp2_hw(b.y));
                         };
                         tmem_ld32_to(s, lanes + k0);
-                        tmem_ld32_to(s + 32, lanes + k0 + 32);
                         tmem_ld_wait();
                         pin32(s);
-                        pin32(s + 32);
-                        if (k0 == 64) {                      // the buffer may be written again
+                        if (k0 == 96) {                      // the buffer may be written again
                             tc_fence_before();
                             __syncwarp();
-                            if (lane == 0) mbar_arrive(bar(B::sfree + (int)(n & 1)));
+                            if (lane == 0) mbar_arrive(bar(B::sfree + wg));
                         }
                         if constexpr (CAP) {
                             bool near = true;
 #pragma unroll
-                            for (int k = 0; k < 64; ++k) {
+                            for (int k = 0; k < 32; ++k) {
                                 const float y = sf(k) * (P.scale * inv_cap);
                                 near = near && fabsf(y) < 0.5f;
                                 s[k] = __float_as_uint(y);
                             }
                             if (__all_sync(0xffffffffu, near)) {
 #pragma unroll
-                                for (int k = 0; k < 64; ++k) s[k] = __float_as_uint(P.cap * kLog2e * tanh_series(sf(k)));
+                                for (int k = 0; k < 32; ++k) s[k] = __float_as_uint(P.cap * kLog2e * tanh_series(sf(k)));
                             } else {
 #pragma unroll
-                                for (int k = 0; k < 64; ++k)
+                                for (int k = 0; k < 32; ++k)
                                     s[k] = __float_as_uint(P.cap * kLog2e * (fabsf(sf(k)) < 0.5f ? tanh_series(sf(k)) : tanh_far(sf(k))));
                             }
                         }
                         // two bodies without a branch in them: the loads, exponentials and sums of many rows overlap
                         if (all) {
 #pragma unroll
-                            for (int k = 0; k < 64; k += 4) {
+                            for (int k = 0; k < 32; k += 4) {
                                 float2 a, b;
                                 four(k0, k, a, b);
                                 sum[0] = add2(sum[0], a);
@@ -298,7 +298,7 @@ __global__ void __launch_bounds__(KwShape<D>::THREADS, 1) key_weight_kernel(cons
                             }
                         } else {
 #pragma unroll
-                            for (int k = 0; k < 64; k += 4) {
+                            for (int k = 0; k < 32; k += 4) {
                                 float2 a, b;
                                 four(k0, k, a, b);
                                 const int4 at = *reinterpret_cast<const int4*>(slot + k0 + k);
@@ -314,12 +314,13 @@ __global__ void __launch_bounds__(KwShape<D>::THREADS, 1) key_weight_kernel(cons
                 }
                 w += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
             }
-            // one tile: its warpgroup has the whole sum; more: the second hands its part to the first
-            const bool mine = tiles == 1 ? ((qn ^ (uint32_t)wg) & 1) == 0 : wg == 0;
+            // one tile: its warpgroup has the whole sum; more: the first adds all warpgroups' in order
+            const bool mine = tiles == 1 ? i0 == 0 : wg == 0;
             if (tiles > 1) {
-                if (wg == 1) sums[(shared & 1) * 128 + own] = w;
-                group_sync(3, 256);
-                if (wg == 0) w += sums[(shared & 1) * 128 + own];
+                float* part = sums + (shared & 1) * (kKwGroups * 128) + own;
+                part[wg * 128] = w;
+                group_sync(1 + kKwGroups, 128 * kKwGroups);
+                if (wg == 0) w = (part[0] + part[128]) + (part[256] + part[384]);
                 ++shared;
             }
             if (mine && ok && j < x.s.L && j < P.weight_stride) {
@@ -333,7 +334,7 @@ __global__ void __launch_bounds__(KwShape<D>::THREADS, 1) key_weight_kernel(cons
     __syncthreads();
     if (warp == 3) {
         tmem_relinquish();
-        tmem_dealloc(tmem, 256);
+        tmem_dealloc(tmem, 512);
     }
 }
 
