@@ -28,13 +28,21 @@ __device__ __forceinline__ float2 ffma2(float2 a, float2 b, float2 c)
 // for a row of zeros.
 template <int D, int R, int THREADS, typename Off> __device__ __forceinline__ void load_tile(float* dst, const float* src, Off off)
 {
-    constexpr int PER = D / 4;
-    for (int i = threadIdx.x; i < R * PER; i += THREADS) {
-        const int r = i / PER, c = (i - r * PER) * 4;
-        const long long at = off(r);
-        float* d = dst + r * (D + 4) + c;
-        if (at < 0) *reinterpret_cast<float4*>(d) = make_float4(0.f, 0.f, 0.f, 0.f);
-        else cp_async16(smem_u32(d), src + at + c);
+    // a warp has R / 4 consecutive rows; lane l finds row l's place, so that lookups run side by side
+    static_assert(THREADS == 128);
+    constexpr int PER = D / 4, ROWS = R / 4, RPI = PER < 32 ? 32 / PER : 1;   // 16-byte chunks of a row; rows of one instruction
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const long long mine = lane < ROWS ? off(warp * ROWS + lane) : -1;
+#pragma unroll 4
+    for (int k = 0; k < ROWS; k += RPI) {
+        const int r = k + lane / PER % RPI;
+        const long long at = __shfl_sync(0xffffffffu, mine, r);
+        float* d = dst + (warp * ROWS + r) * (D + 4);
+#pragma unroll
+        for (int c = lane % PER * 4; c < D; c += 128) {
+            if (at < 0) *reinterpret_cast<float4*>(d + c) = make_float4(0.f, 0.f, 0.f, 0.f);
+            else cp_async16(smem_u32(d + c), src + at + c);
+        }
     }
 }
 __device__ __forceinline__ void async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
@@ -162,6 +170,12 @@ __global__ void __launch_bounds__(kThreads) attend_simt_kernel(const __grid_cons
 #pragma unroll
                     for (int j = 0; j < kKN; ++j)
                         if (!sees(P, g.s, slot_i[i], j0 + tc + kTC * j)) x[i][j] = -INFINITY;
+                if (P.scores && tr + kTR * i < rows && j0 < P.scores_stride) {   // for the weight sums
+                    const RowId id = row_id(P, g.s, g.h, g.rt * BM + tr + kTR * i);
+                    float* to = P.scores + ((long long)(g.s.t0 + id.t) * P.Hq + id.head) * P.scores_stride + j0 + tc;
+#pragma unroll
+                    for (int j = 0; j < kKN; ++j) __stcg(to + kTC * j, x[i][j]);
+                }
 #pragma unroll
                 for (int j = 0; j < kKN; ++j) top = fmaxf(top, x[i][j]);
 #pragma unroll
@@ -392,10 +406,11 @@ cudaError_t launch_attend(const AttendParams& call, int dtype, int num_sms, cuda
     if (call.T == 0) return cudaSuccess;
     AttendParams P = call;
     const bool bf16 = dtype == KVX_BF16;
-    // Weight sums of few rows (16 a sequence and KV head) add up the scores that the attention leaves, where they fit
-    // the workspace: 8 bytes a score are less than a slot's K.  Else the scores are formed again.
+    // Weight sums add up the scores that the attention leaves, where they fit the workspace and cost less than to be formed
+    // again: always in fp32 (8 bytes of traffic against 2 d operations on the CUDA cores: 512 tokens of 12 heads over
+    // 512 slots 209 us, 48 so), for few rows in bf16 (16 a sequence and KV head: less than a slot's K).
     P.scores_stride = (P.weight_stride + 63) / 64 * 64;
-    const bool keep = bf16 && P.key_weight && (long long)P.T * P.G <= 16ll * P.batch && (long long)P.T * P.Hq * P.scores_stride <= kAttendScores;
+    const bool keep = P.key_weight && (!bf16 || (long long)P.T * P.G <= 16ll * P.batch) && (long long)P.T * P.Hq * P.scores_stride <= kAttendScores;
     if (!keep) P.scores = nullptr;
     const bool cap = P.cap > 0.0f;
     cudaError_t e = bf16 ? launch_attend_tc(P, num_sms, stream) : cap ? attend_fp32<true>(P, num_sms, stream) : attend_fp32<false>(P, num_sms, stream);

@@ -156,7 +156,7 @@ extern "C" KVX_API kvx_status kvx_decoder_create(const kvx_decoder_desc* desc, k
         cudaMalloc(&d->part_o, rows * g.head_dim * sizeof(float)) != cudaSuccess ||
         cudaMalloc(&d->part_ml, rows * sizeof(float2)) != cudaSuccess ||
         cudaMalloc(&d->split, kAttendMaxCtas * sizeof(SplitItem)) != cudaSuccess ||
-        (desc->dtype == KVX_BF16 && cudaMalloc(&d->scores, kAttendScores * sizeof(float)) != cudaSuccess)) {
+        cudaMalloc(&d->scores, kAttendScores * sizeof(float)) != cudaSuccess) {
         cudaGetLastError();
         free_decoder(d);
         return fail(KVX_ERR_OOM, "decoder_create: device allocation");

@@ -338,32 +338,39 @@ __global__ void __launch_bounds__(KwShape<D>::THREADS, 1) key_weight_kernel(cons
     }
 }
 
-// The same sums from scores that the attention has left (few rows): a thread a slot.
-__global__ void __launch_bounds__(128) sum_scores_kernel(const __grid_constant__ AttendParams P)
+// The same sums from scores that the attention has left: 32 slots a CTA, a lane each, the rows dealt to its warps,
+// whose sums are added in order.
+template <int WARPS> __global__ void __launch_bounds__(WARPS * 32) sum_scores_kernel(const __grid_constant__ AttendParams P)
 {
-    __shared__ float lse[64];
-    const int b = blockIdx.z, h = blockIdx.y, j = blockIdx.x * 128 + threadIdx.x;
+    __shared__ float part[WARPS][33];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int b = blockIdx.z, h = blockIdx.y, j = blockIdx.x * 32 + lane;
     grid_dependency_wait();
     const Seq s = load_seq(P, b);
-    const int rows = s.n * P.G;
-    if (blockIdx.x * 128 >= s.L) return;
+    if (blockIdx.x * 32 >= s.L) return;
+    const bool in = j < s.L && j < P.weight_stride;
     float w = 0.0f;
-    for (int r0 = 0; r0 < rows; r0 += 64) {
-        __syncthreads();
-        if (threadIdx.x < 64 && r0 + (int)threadIdx.x < rows) {
-            const RowId id = row_id(P, s, h, r0 + threadIdx.x);
-            lse[threadIdx.x] = P.lse[(long long)(s.t0 + id.t) * P.Hq + id.head] * kLog2e;
-        }
-        __syncthreads();
-        const int n = min(64, rows - r0);
-#pragma unroll 8
-        for (int r = 0; r < n; ++r) {
-            const RowId id = row_id(P, s, h, r0 + r);
-            if (j < s.L && j < P.weight_stride && sees(P, s, s.slot(id.t), j))
-                w += exp2_hw(__ldcg(&P.scores[((long long)(s.t0 + id.t) * P.Hq + id.head) * P.scores_stride + j]) - lse[r]);
+    // few rows: a warp a row; many: a warp all query heads of a token
+    const int step = WARPS == 4 ? 1 : P.G;
+    for (int r = warp * step; r < s.n * P.G; r += WARPS * step) {
+        const int t = r / P.G;
+        const bool seen = in && sees(P, s, s.slot(t), j);
+        const long long at = (long long)(s.t0 + t) * P.Hq + h * P.G + (r - t * P.G);
+#pragma unroll 4
+        for (int k = 0; k < step; ++k) {
+            const float x = seen ? __ldcg(&P.scores[(at + k) * P.scores_stride + j]) : -INFINITY;
+            const float z = __ldcg(&P.lse[at + k]) * kLog2e;
+            w += seen ? exp2_hw(x - z) : 0.0f;
         }
     }
-    if (j < s.L && j < P.weight_stride) P.key_weight[((long long)b * P.H + h) * P.weight_stride + j] += w;
+    part[warp][lane] = w;
+    __syncthreads();
+    if (warp == 0 && in) {
+        w = 0.0f;
+#pragma unroll
+        for (int k = 0; k < WARPS; ++k) w += part[k][lane];
+        P.key_weight[((long long)b * P.H + h) * P.weight_stride + j] += w;
+    }
 }
 
 template <int D, bool CAP> cudaError_t run_key_weight(const AttendParams& P, int num_sms, cudaStream_t stream)
@@ -400,16 +407,17 @@ cudaError_t launch_key_weight(const AttendParams& P, int num_sms, cudaStream_t s
 
 cudaError_t launch_sum_scores(const AttendParams& P, cudaStream_t stream)
 {
+    const bool few = (long long)P.T * P.G <= 32ll * P.batch;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)((P.weight_stride + 127) / 128), P.H, P.batch);
-    cfg.blockDim = dim3(128);
+    cfg.gridDim = dim3((unsigned)((P.weight_stride + 31) / 32), P.H, P.batch);
+    cfg.blockDim = dim3(few ? 128 : 512);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, sum_scores_kernel, P);
+    return few ? cudaLaunchKernelEx(&cfg, sum_scores_kernel<4>, P) : cudaLaunchKernelEx(&cfg, sum_scores_kernel<16>, P);
 }
 
 }  // namespace kvx
