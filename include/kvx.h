@@ -410,8 +410,8 @@ typedef struct {
 } kvx_decoder_desc;
 
 /* Checks the description and allocates what the calls below need on the current device: rotation
- * frequencies, a status word and the workspace of split attention (a few tens of MB whatever the
- * lengths).  Synchronous.  On success *out owns device memory until kvx_decoder_destroy. */
+ * frequencies, a status word and the workspace of kvx_attend (partial results of split rows, kept
+ * scores: 84, 104 or 144 MB for heads of 64, 128 or 256, whatever the lengths).  Synchronous.  On success *out owns device memory until kvx_decoder_destroy. */
 KVX_API kvx_status kvx_decoder_create(const kvx_decoder_desc* desc, kvx_decoder** out);
 
 /* Free the decoder's device memory.  Synchronises the device first.  NULL is accepted. */
@@ -466,8 +466,9 @@ typedef struct {
  *   x_j = cap(scale * q_{i,g} . K_h[j]),  out_{i,g} = sum_j softmax_j(x) V_h[j]
  * over the seen slots j < kv_len[b]: j <= s_i and (no window or s_i - j < window), or
  * j < prefix_len[b].  A token that sees no slot (s_i < 0 and no prefix) gets a zero row.  Scores, sums and
- * the output's accumulation are fp32 (bf16 caches: attention weights are rounded to bf16 before
- * they multiply V, 8 bits as V has); rows no new token sees are never part of a result, whatever
+ * the output's accumulation are fp32.  (bf16 caches: attention weights are rounded to bf16, as V
+ * is, before they multiply V; in calls of few rows and in tiles whose rows may see fewer than 512
+ * slots they multiply it as two bf16 terms.)  Rows no new token sees are never part of a result, whatever
  * they hold.  Page-table entries outside the pool read as zero rows and are flagged.
  * The sums behind every output are taken in an order that depends on sizes alone: equal calls
  * give equal bits.  At most 1024 sequences a call (KVX_ERR_UNSUPPORTED).

@@ -1,7 +1,8 @@
 // kvx_append.cu -- new tokens' queries and keys rotated, their keys and values written into the cache.
 //
 //   q'_i = R(p_i) q_i,  K[s_i] = R(p_i) k_i,  V[s_i] = v_i
-// Every element is read once and written once: the bound is memory.  A thread takes one 16-byte chunk
+// Every element is read once and written once: the bound is memory (171 MB in 32.8 us: 5.2 TB/s, 77% of a copy's
+// rate).  A thread takes one 16-byte chunk
 // of a token's head and the chunk it is paired with, for several heads: the angles of the pairs are
 // the same in every head, so their sines are taken once.
 #include "kvx_decode.cuh"
@@ -105,10 +106,11 @@ cudaError_t launch_append(const AppendParams& P, int dtype, cudaStream_t stream)
     if (P.T == 0) return cudaSuccess;
     const int chunks = P.d / 2 / (dtype == KVX_BF16 ? 8 : 4), all = P.Hq + 2 * P.H;
     const long long items = (long long)P.T * chunks;
-    // a block's heads: all rotations' sines are shared, so as many as keep the device full of blocks
+    // a block's heads: they share the sines, so several, while that keeps the device full of blocks (10797 tokens of 36
+    // heads of 128: 34.8, 32.8 and 34.9 us with up to 2, 4 and 12 heads a block)
     const long long blocks = (items + kAppendThreads - 1) / kAppendThreads;
     int per = (int)(blocks * all / 2048);
-    per = per < 1 ? 1 : per > 8 ? 8 : per;
+    per = per < 1 ? 1 : per > 4 ? 4 : per;
     const dim3 grid((unsigned)blocks, (unsigned)((all + per - 1) / per));
     if (dtype == KVX_BF16) append_kernel<__nv_bfloat16><<<grid, kAppendThreads, 0, stream>>>(P, per);
     else append_kernel<float><<<grid, kAppendThreads, 0, stream>>>(P, per);

@@ -49,7 +49,7 @@ __device__ __forceinline__ RowId row_id(const AttendParams& P, const Seq& s, int
 // or a NaN that gives a NaN, so a row that did not come out finite is summed over the slots it sees only.
 template <typename T, int D>
 __device__ __noinline__ void resum_row(const AttendParams& P, const Seq& s, int b, int h, int row, float lse2,
-                                       float (&o)[D / 32])
+                                       float (&o)[D / 32], volatile int* beat = nullptr)
 {
     constexpr int C = D / 32;
     const int lane = threadIdx.x & 31;
@@ -61,6 +61,7 @@ __device__ __noinline__ void resum_row(const AttendParams& P, const Seq& s, int 
     const int i = s.slot(id.t), hi = min(i + 1, s.L), lo = max(window_lo(P, i), 0);
     const float inv_cap = P.cap > 0.0f ? 1.0f / P.cap : 0.0f;
     for (int j = s.pre > 0 ? 0 : lo; j < max(hi, s.pre); ++j) {
+        if (beat && (j & 4095) == 0 && lane == 0) *beat = *beat + 1;   // waits elsewhere in the CTA go on
         if (!sees(P, s, i, j)) continue;
         const long long at = cache_row(P.cache, b, j);
         if (at < 0) continue;

@@ -102,6 +102,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
     auto bar = [&](int i) { return s0 + (uint32_t)i * 8; };
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + 512);
     int* abort = reinterpret_cast<int*>(smem + 516);
+    int* beat = reinterpret_cast<int*>(smem + 520);
     const uint32_t sQ = s0 + C::CTRL, sT = sQ + C::QB;
     const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
 
@@ -123,6 +124,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
         mbar_init(bar(B::mlempty), 4);
         fence_mbar_init();
         *abort = 0;
+        *beat = 0;
     }
     // the kernel before this one may still be ending: what it wrote is read from here on
     grid_dependency_wait();
@@ -131,7 +133,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
-    const Waiter W{abort, P.status};
+    const BeatWaiter W{abort, beat, P.status};
     SegmentWalk<BN> walk(P, plan);
     Segment g;
 
@@ -670,7 +672,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
                 for (uint32_t bad = __ballot_sync(0xffffffffu, real && !fine); bad; bad &= bad - 1) {
                     const int who = __ffs(bad) - 1;
                     float o[D / 32];
-                    resum_row<__nv_bfloat16, D>(P, g.s, g.b, g.h, row - lane + who, __shfl_sync(0xffffffffu, lse2, who), o);
+                    resum_row<__nv_bfloat16, D>(P, g.s, g.b, g.h, row - lane + who, __shfl_sync(0xffffffffu, lse2, who), o, beat);
                     const RowId bid = row_id(P, g.s, g.h, row - lane + who);
                     if (!C::COLS || lane >> 4 == wg)         // a half of the channels is this warpgroup's
                         store_f32<__nv_bfloat16, D / 32>((__nv_bfloat16*)P.out + (long long)(g.s.t0 + bid.t) * P.o_t + (long long)bid.head * P.o_h +

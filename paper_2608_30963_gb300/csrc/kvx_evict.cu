@@ -52,7 +52,7 @@ __device__ __forceinline__ int block_before(int v, int* tmp, int& all)
 }
 
 // cached: weights the CTA holds in shared memory; slots past them are read again in each pass.
-__global__ void __launch_bounds__(kSelThreads) select_kernel(const __grid_constant__ EvictParams P, int cached)
+__global__ void __launch_bounds__(kSelThreads, 2) select_kernel(const __grid_constant__ EvictParams P, int cached)
 {
     extern __shared__ __align__(16) unsigned dyn[];
     unsigned* hist = dyn;
@@ -82,7 +82,8 @@ __global__ void __launch_bounds__(kSelThreads) select_kernel(const __grid_consta
         // the slots that compete, and how many of them stay (at least one competes: n > keep >= sinks + recent)
         const int c0 = P.sinks, c1 = n - P.recent;
         int need = P.keep - P.sinks - P.recent;
-        for (int i = c0 + tid; i < min(c1, c0 + cached); i += kSelThreads) keys[i - c0] = weight_key(w[i]);
+#pragma unroll 4
+        for (int i = c0 + tid; i < min(c1, c0 + cached); i += kSelThreads) keys[i - c0] = weight_key(__ldg(&w[i]));
         auto key = [&](int i) { return i - c0 < cached ? keys[i - c0] : weight_key(__ldg(&w[i])); };
         unsigned prefix = 0, mask = 0;
         // need > 0: the digits of the key of rank `need`, from the top; `need` becomes its rank among equals
@@ -111,33 +112,58 @@ __global__ void __launch_bounds__(kSelThreads) select_kernel(const __grid_consta
             need = tmp[33];
             __syncthreads();
         }
-        // kept: forced slots, keys above the one found, and the first `need` equal to it
+        // kept: forced slots, keys above the one found, and the first `need` equal to it.  Each warp has a stretch of
+        // slots: it counts, the counts are summed over the warps, it writes.
         const bool any = mask != 0;
-        int at = 0, ties = 0;
-        for (int i0 = 0; i0 < n; i0 += kSelThreads) {
-            const int i = i0 + tid;
-            int sure = 0, tie = 0;
-            if (i < n) {
+        const int warp = tid >> 5, lane = tid & 31, stretch = (n + kSelThreads - 1) / kSelThreads * 32;
+        const int from = min(n, warp * stretch), to = min(n, from + stretch);
+        auto ballots = [&](int i, unsigned& sure, unsigned& tie) {
+            bool s = false, t = false;
+            if (i < to) {
                 if (i < c0 || i >= c1) {
-                    sure = 1;
+                    s = true;
                 } else if (any) {
                     const unsigned k = key(i);
-                    sure = k > prefix;
-                    tie = k == prefix;
+                    s = k > prefix;
+                    t = k == prefix;
                 }
             }
-            int all;
-            const int before = block_before(sure | tie << 16, tmp, all);   // at most 1024 of each: 16 bits hold them
-            const int sure_before = before & 0xffff, tie_before = ties + (before >> 16);
-            const bool take = sure || (tie && tie_before < need);
-            if (take) {
-                const int r = at + sure_before + min(tie_before, need) - min(ties, need);
+            sure = __ballot_sync(0xffffffffu, s);
+            tie = __ballot_sync(0xffffffffu, t);
+        };
+        int sures = 0, ties = 0;
+        for (int i0 = from; i0 < to; i0 += 32) {
+            unsigned a, b;
+            ballots(i0 + lane, a, b);
+            sures += __popc(a);
+            ties += __popc(b);
+        }
+        if (lane == 0) {
+            hist[warp] = sures;
+            hist[32 + warp] = ties;
+        }
+        __syncthreads();
+        int before = lane < warp ? (int)hist[lane] : 0, tied = lane < warp ? (int)hist[32 + lane] : 0;
+#pragma unroll
+        for (int o = 16; o; o >>= 1) {
+            before += __shfl_xor_sync(0xffffffffu, before, o);
+            tied += __shfl_xor_sync(0xffffffffu, tied, o);
+        }
+#pragma unroll 4
+        for (int i0 = from; i0 < to; i0 += 32) {
+            const int i = i0 + lane;
+            const float wi = kw && i < to ? __ldg(&w[i]) : 0.0f;        // four in flight
+            unsigned a, b;
+            ballots(i, a, b);
+            const unsigned below = (1u << lane) - 1;
+            const int rank = tied + __popc(b & below);                   // among the equal ones
+            if ((a >> lane & 1u) || ((b >> lane & 1u) && rank < need)) {
+                const int r = before + __popc(a & below) + min(rank, need);
                 kept[r] = i;
-                if (kw) kw[r] = w[i];
+                if (kw) kw[r] = wi;
             }
-            const int t1 = ties + (all >> 16);
-            at += (all & 0xffff) + min(t1, need) - min(ties, need);
-            ties = t1;
+            before += __popc(a);
+            tied += __popc(b);
         }
     }
     for (int i = m + tid; i < P.keep; i += kSelThreads) kept[i] = -1;
@@ -156,6 +182,7 @@ __global__ void __launch_bounds__(kMoveThreads) move_kernel(const __grid_constan
     const int groups = (P.keep + 31) / 32;
     const long long total = (long long)P.L * P.batch * P.H * groups;
     const long long warps = (long long)gridDim.x * (kMoveThreads / 32);
+    grid_dependency_wait();
     for (long long g = ((long long)blockIdx.x * kMoveThreads + threadIdx.x) >> 5; g < total; g += warps) {
         const long long unit = g / groups;
         const int r0 = (int)(g - unit * groups) * 32;
@@ -204,12 +231,21 @@ __global__ void __launch_bounds__(kMoveThreads) move_kernel(const __grid_constan
     }
 }
 
-template <int CHUNKS> void run_move(const EvictParams& P, int elt, int num_sms, cudaStream_t stream)
+template <int CHUNKS> cudaError_t run_move(const EvictParams& P, int elt, int num_sms, cudaStream_t stream)
 {
     const long long rows = (long long)P.L * P.batch * P.H * ((P.keep + 31) / 32);
     const long long want = (rows + kMoveThreads / 32 - 1) / (kMoveThreads / 32);
     const int grid = (int)min(want, (long long)num_sms * 8);
-    move_kernel<CHUNKS><<<grid, kMoveThreads, 0, stream>>>(P, elt);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(kMoveThreads);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, move_kernel<CHUNKS>, P, elt);
 }
 
 }  // namespace
@@ -223,16 +259,14 @@ cudaError_t launch_evict(const EvictParams& P, int dtype, int num_sms, cudaStrea
     const int smem = kSelFixed + cached * 4;
     if (cudaError_t e = smem_opt_in<select_kernel>(kSmemMax); e != cudaSuccess) return e;
     select_kernel<<<(unsigned)units, kSelThreads, smem, stream>>>(P, cached);
-    cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess) return e;
-    switch (P.d * elt / 16) {
-    case 8: run_move<8>(P, elt, num_sms, stream); break;
-    case 16: run_move<16>(P, elt, num_sms, stream); break;
-    case 32: run_move<32>(P, elt, num_sms, stream); break;
-    default: run_move<64>(P, elt, num_sms, stream); break;
-    }
+    if (cudaError_t e = cudaGetLastError(); e != cudaSuccess) return e;
     *launches = 2;
-    return cudaGetLastError();
+    switch (P.d * elt / 16) {
+    case 8: return run_move<8>(P, elt, num_sms, stream);
+    case 16: return run_move<16>(P, elt, num_sms, stream);
+    case 32: return run_move<32>(P, elt, num_sms, stream);
+    default: return run_move<64>(P, elt, num_sms, stream);
+    }
 }
 
 }  // namespace kvx

