@@ -411,7 +411,7 @@ typedef struct {
 
 /* Checks the description and allocates what the calls below need on the current device: rotation
  * frequencies, a status word and the workspace of kvx_attend (partial results of split rows, kept
- * scores: 84, 104 or 144 MB for heads of 64, 128 or 256, whatever the lengths).  Synchronous.  On success *out owns device memory until kvx_decoder_destroy. */
+ * scores: 88, 108 or 147 MB for heads of 64, 128 or 256, whatever the lengths).  Synchronous.  On success *out owns device memory until kvx_decoder_destroy. */
 KVX_API kvx_status kvx_decoder_create(const kvx_decoder_desc* desc, kvx_decoder** out);
 
 /* Free the decoder's device memory.  Synchronises the device first.  NULL is accepted. */

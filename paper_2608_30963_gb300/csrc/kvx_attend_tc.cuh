@@ -145,7 +145,8 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
         constexpr int RPI = CPR < 32 ? 32 / CPR : 1;     // rows a warp copies with one instruction
         const int sub = lane / CPR;
         const uint32_t place = (uint32_t)((lane % CPR >> 3)), c0 = (uint32_t)(((lane % CPR & 7) ^ sub) << 4);
-        uint32_t pos = 0, items = 0;                     // tiles issued; items begun
+        uint32_t pos = 0, items = 0;                     // tiles and items begun
+        uint32_t issued = 0, q_issued = 0;               // tensor copies of tiles and of Q that were issued
         bool ok = true;
         auto wait = [&](int b, uint32_t parity) { ok = __all_sync(0xffffffffu, ok && W.wait(bar(b), parity)); };
         // The copies of a batch announce themselves: each thread's arrival follows its own copies.  The MMA warp
@@ -155,6 +156,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
                 // Q: the G query heads of tile_rows / G tokens, a box for each 64 channels; what it brings past the
                 // sequence's tokens is in rows that nothing is read from
                 if (items > 0) wait(B::qempty, (items - 1) & 1);
+                q_issued += ok;
                 if (ok && elect_one()) {
                     mbar_arrive_expect_tx(bar(B::qfull), (uint32_t)P.tile_rows * D * 2);
 #pragma unroll
@@ -197,6 +199,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
                         ok = __all_sync(0xffffffffu, ok && W.wait(bar(B::empty + st), ph ^ 1));
                         ++pos;
                         if (!ok) continue;
+                        issued = pos;
                         const uint32_t dst = sT + st * C::TILE, full = bar(B::full + st);
                         const CUtensorMap* map = kv ? &maps.v : &maps.k;
                         if (elect_one()) mbar_arrive_expect_tx(full, C::TILE);
@@ -317,6 +320,12 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
                 }
                 pos += (uint32_t)total;
             }
+        }
+        cp_async_wait_all();
+        if (!ok && warp == 0) {
+            if (q_issued > 0) drain(bar(B::qfull), (q_issued - 1) & 1);
+            if (TMA)
+                for (uint32_t q = issued > C::STAGES ? issued - C::STAGES : 0; q < issued; ++q) drain(bar(B::full + (int)(q % C::STAGES)), (q / C::STAGES) & 1);
         }
     } else {
         // ---------------------------------------------------------------- MMA
@@ -456,12 +465,12 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
                 }
                 const bool all = __all_sync(0xffffffffu, (j0 >= lo && j0 + BN <= hi) || j0 + BN <= pre);
                 uint32_t x[CW];
-                auto xf = [&](int k) -> float { return __uint_as_float(x[k]); };
 #pragma unroll
                 for (int k = 0; k < CW; k += 32) tmem_ld32_to(x + k, at + c0 + k);
                 tmem_ld_wait();
 #pragma unroll
                 for (int k = 0; k < CW; k += 32) pin32(x + k);
+                auto xf = [&](int k) -> float { return __uint_as_float(x[k]); };
                 if constexpr (CAP) {
                     bool near = true;                    // all scores where the series holds: no branch per score
 #pragma unroll

@@ -156,13 +156,14 @@ __global__ void __launch_bounds__(KwShape<D>::THREADS, 1) key_weight_kernel(cons
         cp_async_wait_all();
     } else if (warp == 2) {
         // ---------------------------------------------------------------- Q
-        uint32_t qn = 0;
+        uint32_t qn = 0, issued = 0;
         for (long long u = blockIdx.x; u < units; u += gridDim.x) {
             const KwUnit x = kw_unit(P, first, u, per);
             for (int i = 0; i < x.tiles; ++i, ++qn) {
                 const uint32_t qs = (uint32_t)k_slots + qn % (uint32_t)q_slots, full = bar(B::full + (int)qs);
                 wait(B::empty + (int)qs, ((qn / (uint32_t)q_slots) & 1) ^ 1);
                 if (!ok) continue;
+                issued = qn + 1;
                 if (elect_one()) {
                     mbar_arrive_expect_tx(full, (uint32_t)(per * P.G) * D * 2);
 #pragma unroll
@@ -172,6 +173,9 @@ __global__ void __launch_bounds__(KwShape<D>::THREADS, 1) key_weight_kernel(cons
                 __syncwarp();
             }
         }
+        if (!ok)
+            for (uint32_t q = issued > (uint32_t)q_slots ? issued - (uint32_t)q_slots : 0; q < issued; ++q)
+                drain(bar(B::full + k_slots + (int)(q % (uint32_t)q_slots)), (q / (uint32_t)q_slots) & 1);
     } else if (warp == 3) {
         // ---------------------------------------------------------------- MMA
         constexpr uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(128 >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
@@ -253,6 +257,9 @@ __global__ void __launch_bounds__(KwShape<D>::THREADS, 1) key_weight_kernel(cons
 #pragma unroll 1                                             // a body twice as long would miss the instruction cache
                     for (int k0 = 0; k0 < 128; k0 += 32) {
                         uint32_t s[32];
+                        tmem_ld32_to(s, lanes + k0);
+                        tmem_ld_wait();
+                        pin32(s);
                         auto sf = [&](int k) -> float { return __uint_as_float(s[k]); };
                         // the weights of rows k .. k + 3
                         auto four = [&](int k0_, int k, float2& a, float2& b) {
@@ -262,9 +269,6 @@ __global__ void __launch_bounds__(KwShape<D>::THREADS, 1) key_weight_kernel(cons
                             a = make_float2(exp2_hw(a.x), exp2_hw(a.y));
                             b = make_float2(exp2_hw(b.x), exp2_hw(b.y));
                         };
-                        tmem_ld32_to(s, lanes + k0);
-                        tmem_ld_wait();
-                        pin32(s);
                         if (k0 == 96) {                      // the buffer may be written again
                             tc_fence_before();
                             __syncwarp();

@@ -89,6 +89,12 @@ struct BeatWaiter {
         }
     }
 };
+// After a wait has run out: a copy still on its way must not land in shared memory that is no longer this CTA's.
+__device__ __forceinline__ void drain(uint32_t bar, uint32_t parity)
+{
+    const unsigned long long t0 = globaltimer();
+    while (!mbar_try_wait(bar, parity) && globaltimer() - t0 < kWaitNs) {}
+}
 __device__ __forceinline__ bool elect_one()
 {
     uint32_t one;

@@ -496,6 +496,51 @@ def test_refusals():
     assert p.dec.device_status() == 0
 
 
+@pytest.mark.parametrize("ps", [8, 16, 24, 32, 48, 128, 200])
+@pytest.mark.parametrize("H,G,d,ctx,new", [(2, 7, 128, [333, 90], [37, 1]), (1, 4, 64, [513], [130]), (2, 2, 256, [200, 40], [1, 66]),
+                                           (3, 5, 128, [400, 0, 31], [1, 1, 1])])
+def test_page_sizes(ps, H, G, d, ctx, new):
+    """Every way rows are brought: boxes, groups of eight rows and single rows; the same values whichever."""
+    p = Problem(H, G, d, ctx, new, "bf16", ps, seed=41)
+    w = torch.zeros((p.B, H, p.S), device="cuda")
+    out, lse = p.attend(weight=w)
+    eo, el, ew, to, tl, tw = p.exact()
+    check(p, out, eo, to, "out")
+    check_lse(lse, el, tl)
+    check(p, w.cpu(), ew, tw + 1e-30, "key_weight")
+    flat = Problem(H, G, d, ctx, new, "bf16", 0, seed=41)
+    base, _ = flat.attend(q=p.q, k=p.K, v=p.V)
+    assert torch.equal(base, out)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_many_sequences(dtype):
+    """Sequences of all lengths, most without new tokens: ranges begin and end anywhere."""
+    rng = np.random.default_rng(9)
+    new = [int(x) for x in rng.choice([0, 0, 1, 1, 2, 9], 200)]
+    ctx = [int(x) for x in rng.integers(0, 90, 200)]
+    p = Problem(2, 3, 64, ctx, new, dtype, 16, seed=43)
+    w = torch.zeros((p.B, 2, p.S), device="cuda")
+    out, lse = p.attend(weight=w)
+    eo, el, ew, to, tl, tw = p.exact()
+    check(p, out, eo, to, "out")
+    check_lse(lse, el, tl)
+    check(p, w.cpu(), ew, tw + 1e-30, "key_weight")
+
+
+def test_weights_where_scores_do_not_fit_the_workspace():
+    """The same sums from kept scores (few rows, or fp32) and from scores formed again."""
+    for dtype, new in (("bf16", 1), ("fp32", 20)):
+        p = Problem(1, 8, 64, [700], [new], dtype, 16, seed=44)
+        narrow, wide = torch.zeros((1, 1, p.S), device="cuda"), torch.zeros((1, 1, 16 << 20), device="cuda")
+        p.attend(weight=narrow)
+        p.attend(weight=wide)
+        _, _, ew, _, _, tw = p.exact()
+        for w in (narrow, wide[:, :, :p.S].contiguous()):
+            check(p, w.cpu(), ew, tw + 1e-30, "key_weight")
+        assert not wide[:, :, p.S:].any()
+
+
 # ------------------------------------------------------------------ the steps together
 def test_example_goes_on_from_a_handoff():
     """The example's steps: slots kept hold the sinks and the question, weights add up to one a row."""
