@@ -495,6 +495,7 @@ def build_alignment(src_seq_off, src_end, tgt_seq_off, tgt_end, span_lo, span_hi
 _PACK_ROWS = struct.Struct("@Pqq").pack              # kvx_rows
 _PACK_TOKENS = struct.Struct("@iiPPP").pack          # kvx_new_tokens
 _PACK_OPTS = struct.Struct("@iPPPq").pack            # kvx_attend_opts
+_PACK_PLAN = struct.Struct("@iiPPqiiiPPPq").pack     # kvx_evict_plan
 _PACK_CACHE = struct.Struct("@PPiiqqqPiii4x").pack   # kvx_dst_kv
 
 
@@ -618,11 +619,11 @@ class Decoder:
             raise ValueError(f"kept_weight must be contiguous float32 [{L}, {B}, {H}, slots]")
         if not len(src_v) == len(dst_k) == len(dst_v) == L:
             raise ValueError("src_k, src_v, dst_k and dst_v must have as many layers as one another")
-        plan = kvx_evict_plan(B, L, kv_len.data_ptr(), key_weight.data_ptr(), key_weight.shape[3], keep, sinks, recent, kept.data_ptr(),
-                              new_len.data_ptr(), _ptr(kept_weight), 0 if kept_weight is None else kept_weight.shape[3])
+        plan = _PACK_PLAN(B, L, kv_len.data_ptr(), key_weight.data_ptr(), key_weight.shape[3], keep, sinks, recent, kept.data_ptr(),
+                          new_len.data_ptr(), _ptr(kept_weight), 0 if kept_weight is None else kept_weight.shape[3])
         src, _keep_src = _cache(src_k, src_v, page_table, page_size, num_pages)
         dst, _keep_dst = _cache(dst_k, dst_v, dst_page_table, page_size, dst_num_pages)
-        _check(lib().kvx_evict(self.handle, ctypes.byref(plan), src, dst, _raw_stream(stream)))
+        _check(lib().kvx_evict(self.handle, plan, src, dst, _raw_stream(stream)))
 
     def device_status(self, stream=None, clear: bool = True) -> int:
         bits = ctypes.c_uint32(0)

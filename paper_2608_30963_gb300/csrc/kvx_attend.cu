@@ -111,7 +111,8 @@ __global__ void __launch_bounds__(kThreads) attend_simt_kernel(const __grid_cons
     const int tid = threadIdx.x, tc = tid & 7, tr = tid >> 3, lane = tid & 31, warp = tid >> 5;
     const float inv_cap = P.cap > 0.0f ? 1.0f / P.cap : 0.0f;
     const Plan plan = make_plan<kBN, kThreads>(P, sums);
-    SegmentWalk<kBN> walk(P, plan);
+    WalkState state;
+    SegmentWalk<kBN> walk(P, &plan, &state);
     Segment g;
     bool have = false;
     while (walk.next(g)) {
@@ -241,7 +242,8 @@ __global__ void __launch_bounds__(kThreads) attend_simt_kernel(const __grid_cons
                 float y[D / 32];
 #pragma unroll
                 for (int c = 0; c < D / 32; ++c) y[c] = sQ[r * (D + 4) + lane * (D / 32) + c];
-                finish_row<float, D>(P, g.s, g.b, g.h, g.rt * BM + r, sP[r * (kBN + 4)], sP[r * (kBN + 4) + 1], y);
+                const RowId id = row_id(P, g.s, g.h, g.rt * BM + r);
+                finish_row<float, D>(P, g.b, g.h, g.rt * BM + r, g.s.t0 + id.t, id.head, sP[r * (kBN + 4)], sP[r * (kBN + 4) + 1], y);
             }
         } else {
             const size_t at = (size_t)(2 * blockIdx.x + (g.first ? 0 : 1)) * BM;

@@ -83,15 +83,15 @@ __device__ __noinline__ void resum_row(const AttendParams& P, const Seq& s, int 
     for (int c = 0; c < C; ++c) o[c] = acc[c];
 }
 
-// Write one row from its unnormalised sums (lane holds C channels), its running maximum m (log2 units) and sum l.
-// Whole warps call it.
+// Write one row from its unnormalised sums (lane holds C channels), its running maximum m (log2 units) and sum l; the
+// row is row `row` of (sequence b, KV head h), its output that of packed token `token` and query head `head`.  Whole
+// warps call it.
 template <typename T, int D>
-__device__ __forceinline__ void finish_row(const AttendParams& P, const Seq& s, int b, int h, int row, float m, float l,
+__device__ __forceinline__ void finish_row(const AttendParams& P, int b, int h, int row, int token, int head, float m, float l,
                                            float (&o)[D / 32])
 {
     constexpr int C = D / 32;
     const int lane = threadIdx.x & 31;
-    const RowId id = row_id(P, s, h, row);
     const float inv = l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : l);   // nothing seen: zeros; NaN stays
     bool fine = true;
 #pragma unroll
@@ -105,12 +105,11 @@ __device__ __forceinline__ void finish_row(const AttendParams& P, const Seq& s, 
 #pragma unroll
             for (int c = 0; c < C; ++c) o[c] = 0.0f;
         } else {
-            resum_row<T, D>(P, s, b, h, row, lse2, o);
+            resum_row<T, D>(P, load_seq(P, b), b, h, row, lse2, o);
         }
     }
-    T* out = (T*)P.out + (long long)(s.t0 + id.t) * P.o_t + (long long)id.head * P.o_h + lane * C;
-    store_f32<T, C>(out, o);
-    if (P.lse && lane == 0) P.lse[(long long)(s.t0 + id.t) * P.Hq + id.head] = lse2 * kLn2;
+    store_f32<T, C>((T*)P.out + (long long)token * P.o_t + (long long)head * P.o_h + lane * C, o);
+    if (P.lse && lane == 0) P.lse[(long long)token * P.Hq + head] = lse2 * kLn2;
 }
 
 // C floats of a partial result.
@@ -139,78 +138,112 @@ __device__ __forceinline__ void leave_split(const AttendParams& P, const Plan& p
     SplitItem it = {};
     if (have && g.i0 == 0 && !g.whole()) {
         const Parts parts = item_parts(plan, g);
-        it = {g.b, g.rt, g.h, parts.parts, parts.slot0, parts.lines};
+        it = {g.b, g.rt, g.h, min(P.tile_rows, g.s.n * P.G - g.rt * P.tile_rows), g.s.t0 + g.rt * P.tile_rows / P.G,
+              parts.parts, parts.slot0, parts.lines};
     }
     P.split[blockIdx.x] = it;
 }
 
 // Joins the partial results of split items: CTA (c, y) takes rows [y * RPC, ...) of the item that CTA c of the
-// attention kernel left, WPR warps a row, each with every WPR-th part, their sums added in order.  The
-// reads come from L2, eight parts in flight a warp.
+// attention kernel left.  Bound by the latency of two reads from L2, the item's and the parts', so many of the
+// latter are in flight at once: a warp takes RW rows and two parts of each at a time; where rows are few (and
+// parts may be many), WPR warps a row, each with every WPR-th part, eight at a time, their sums added in order.
 template <typename T, int D, int BM, int WPR>
 __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ AttendParams P)
 {
-    constexpr int C = D / 32, RPC = 8 / WPR, U = C == 8 ? 4 : 8;
+    constexpr int C = D / 32, RW = WPR > 1 ? 1 : C == 8 ? 2 : 4, RPC = 8 / WPR * RW, U = WPR > 1 ? (C == 8 ? 4 : 8) : 2;
     __shared__ float sh[8][D + 2];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     grid_launch_dependents();
     grid_dependency_wait();
     const SplitItem it = P.split[blockIdx.x];
-    if (it.parts == 0) return;
-    const Seq s = load_seq(P, it.b);
-    const int r = blockIdx.y * RPC + warp / WPR, w0 = warp % WPR;
-    const bool real = r < min(P.tile_rows, s.n * P.G - it.rt * P.tile_rows);
+    const int r0 = blockIdx.y * RPC + warp / WPR * RW, w0 = warp % WPR;
+    if (r0 - warp / WPR * RW >= it.rows || it.parts == 0) return;      // the whole CTA
     const Parts parts = {(int)blockIdx.x, it.lines, it.parts, it.slot0};
-    float m = -INFINITY, l = 0.0f, o[C];
+    // running maximum, sum and channels of the rows over the parts so far
+    float m[RW], l[RW], o[RW][C];
 #pragma unroll
-    for (int c = 0; c < C; ++c) o[c] = 0.0f;
-    if (real) {
-        for (int i = lane; i < parts.parts; i += 32) m = fmaxf(m, __ldcg(&P.part_ml[(size_t)parts.slot(i) * BM + r]).x);
+    for (int k = 0; k < RW; ++k) {
+        m[k] = -INFINITY;
+        l[k] = 0.0f;
 #pragma unroll
-        for (int e = 16; e; e >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, e));
-        const float base = m == -INFINITY ? 0.0f : m;
-        for (int i0 = w0; i0 < parts.parts; i0 += U * WPR) {
-            float2 ml[U];
-            float v[U][C];
+        for (int c = 0; c < C; ++c) o[k][c] = 0.0f;
+    }
+    for (int i0 = w0; i0 < it.parts; i0 += U * WPR) {
+        float2 ml[U][RW];
+        float v[U][RW][C];
 #pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (i0 + u * WPR < parts.parts) {
-                    const size_t at = (size_t)parts.slot(i0 + u * WPR) * BM + r;
-                    ml[u] = __ldcg(&P.part_ml[at]);
-                    load_part<C>(P.part_o + at * D + lane * C, v[u]);
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int k = 0; k < RW; ++k) {
+                ml[u][k] = make_float2(-INFINITY, 0.0f);
+                if (i0 + u * WPR < it.parts && r0 + k < it.rows) {
+                    const size_t at = (size_t)parts.slot(i0 + u * WPR) * BM + r0 + k;
+                    ml[u][k] = __ldcg(&P.part_ml[at]);
+                    load_part<C>(P.part_o + at * D + lane * C, v[u][k]);
                 }
+            }
+#pragma unroll
+        for (int k = 0; k < RW; ++k) {
+            float top = m[k];
+#pragma unroll
+            for (int u = 0; u < U; ++u) top = fmaxf(top, ml[u][k].x);
+            const float base = top == -INFINITY ? 0.0f : top, w = exp2_hw(m[k] - base);
+            m[k] = top;
+            l[k] *= w;
+#pragma unroll
+            for (int c = 0; c < C; ++c) o[k][c] *= w;
 #pragma unroll
             for (int u = 0; u < U; ++u)
-                if (i0 + u * WPR < parts.parts) {
-                    const float w = exp2_hw(ml[u].x - base);
-                    l = fmaf(ml[u].y, w, l);
+                if (i0 + u * WPR < it.parts && r0 + k < it.rows) {
+                    const float e = exp2_hw(ml[u][k].x - base);
+                    l[k] = fmaf(ml[u][k].y, e, l[k]);
 #pragma unroll
-                    for (int c = 0; c < C; ++c) o[c] = fmaf(v[u][c], w, o[c]);
+                    for (int c = 0; c < C; ++c) o[k][c] = fmaf(v[u][k][c], e, o[k][c]);
                 }
         }
     }
     if constexpr (WPR > 1) {
 #pragma unroll
-        for (int c = 0; c < C; ++c) sh[warp][lane * C + c] = o[c];
-        if (lane == 0) sh[warp][D] = l;
+        for (int c = 0; c < C; ++c) sh[warp][lane * C + c] = o[0][c];
+        if (lane == 0) {
+            sh[warp][D] = m[0];
+            sh[warp][D + 1] = l[0];
+        }
         __syncthreads();
         if (w0 != 0) return;
+        float top = m[0];
+#pragma unroll
+        for (int k = 1; k < WPR; ++k) top = fmaxf(top, sh[warp + k][D]);
+        const float base = top == -INFINITY ? 0.0f : top, w = exp2_hw(m[0] - base);
+        m[0] = top;
+        l[0] *= w;
+#pragma unroll
+        for (int c = 0; c < C; ++c) o[0][c] *= w;
 #pragma unroll
         for (int k = 1; k < WPR; ++k) {
+            const float e = exp2_hw(sh[warp + k][D] - base);
+            l[0] = fmaf(sh[warp + k][D + 1], e, l[0]);
 #pragma unroll
-            for (int c = 0; c < C; ++c) o[c] += sh[warp + k][lane * C + c];
-            l += sh[warp + k][D];
+            for (int c = 0; c < C; ++c) o[0][c] = fmaf(sh[warp + k][lane * C + c], e, o[0][c]);
         }
     }
-    if (real) finish_row<T, D>(P, s, it.b, it.h, it.rt * P.tile_rows + r, m, l, o);
+#pragma unroll
+    for (int k = 0; k < RW; ++k)
+        if (r0 + k < it.rows) {
+            // (a tile that begins inside a token has its first row's head in it)
+            const int row = it.rt * P.tile_rows + r0 + k, t = row / P.G, t_first = it.rt * P.tile_rows / P.G;
+            finish_row<T, D>(P, it.b, it.h, row, it.token + t - t_first, it.h * P.G + (row - t * P.G), m[k], l[k], o[k]);
+        }
 }
 template <typename T, int D, int BM> cudaError_t run_join(const AttendParams& P, int grid, cudaStream_t stream)
 {
-    // an item has at most min(tile_rows, T G) rows; few of them: four warps a row, as there may be many parts
+    // an item has at most min(tile_rows, T G) rows; few in the whole call: four warps a row, as it may have many parts
     const long long rows = min((long long)P.tile_rows, (long long)P.T * P.G);
-    const bool few = rows <= 64;
+    const bool few = (long long)P.T * P.G <= 64;
+    const int rpc = few ? 2 : 8 * (D == 256 ? 2 : 4);
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(grid, (unsigned)(few ? (rows + 1) / 2 : (rows + 7) / 8));
+    cfg.gridDim = dim3(grid, (unsigned)((rows + rpc - 1) / rpc));
     cfg.blockDim = dim3(256);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];

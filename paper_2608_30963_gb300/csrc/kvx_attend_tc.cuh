@@ -129,12 +129,16 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
     // the kernel before this one may still be ending: what it wrote is read from here on
     grid_dependency_wait();
     grid_launch_dependents();
-    const Plan plan = make_plan<BN, C::THREADS>(P, reinterpret_cast<long long*>(smem + C::CTRL + C::QB));
+    const Plan mine_plan = make_plan<BN, C::THREADS>(P, reinterpret_cast<long long*>(smem + C::CTRL + C::QB));
+    Plan* plan = reinterpret_cast<Plan*>(smem + 544);               // the CTA's range, and where each warp stands on it
+    if (threadIdx.x == 0) *plan = mine_plan;
+    WalkState* state = reinterpret_cast<WalkState*>(smem + 640) + warp;
+    static_assert(sizeof(Plan) <= 96 && sizeof(WalkState) * (C::THREADS / 32) <= 1024 - 640);
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
     const BeatWaiter W{abort, beat, P.status};
-    SegmentWalk<BN> walk(P, plan);
+    SegmentWalk<BN> walk(P, plan, state);
     Segment g;
 
     if (warp < 4) {
@@ -691,7 +695,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
                 if (real && !(C::COLS && wg)) __stcg(P.part_ml + part, make_float2(m, l));
             }
         }
-        if (threadIdx.x == 128) leave_split(P, plan, g, have);
+        if (threadIdx.x == 128) leave_split(P, *plan, g, have);
     }
     tc_fence_before();
     __syncthreads();

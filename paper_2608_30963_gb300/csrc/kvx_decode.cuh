@@ -47,7 +47,9 @@ cudaError_t launch_append(const AppendParams& P, int dtype, cudaStream_t stream)
 
 // A row tile and KV head whose tiles several CTAs have, as the CTA where it begins leaves it; parts = 0: none.
 struct SplitItem {
-    int b, rt, h, parts, slot0, lines;
+    int b, rt, h, rows;       // rows of the tile that exist
+    int token;                // packed index of its first token
+    int parts, slot0, lines;
 };
 
 struct AttendParams {
@@ -280,36 +282,52 @@ struct Segment {
     bool first;               // the CTA's first segment (its partial result goes to the CTA's slot 0, else 1)
     __device__ __forceinline__ bool whole() const { return n == kv.count; }
 };
+// Where a warp stands on its CTA's range.
+struct WalkState {
+    long long x, at;          // next tile; first tile of (b, rt) on the line
+    int b, rt;
+};
+// plan and state may lie in shared memory (whole warps call next): in registers they would be live through a kernel's
+// inner loop.
 template <int BN> struct SegmentWalk {
     const AttendParams& P;
-    Plan p;
-    long long x;
-    __device__ __forceinline__ SegmentWalk(const AttendParams& P_, const Plan& p_) : P(P_), p(p_), x(p_.lo) {}
+    const Plan* p;
+    WalkState* w;
+    __device__ __forceinline__ SegmentWalk(const AttendParams& P_, const Plan* p_, WalkState* w_) : P(P_), p(p_), w(w_)
+    {
+        __syncwarp();
+        *w = {p->lo, p->at, p->b, p->rt};
+        __syncwarp();
+    }
     __device__ __forceinline__ bool next(Segment& g)
     {
-        if (x >= p.hi) return false;
+        WalkState s = *w;
+        if (s.x >= p->hi) return false;
         while (true) {
-            g.s = load_seq(P, p.b);
-            if (p.rt < row_tiles(P, g.s)) break;
-            ++p.b;                               // a sequence without new tokens, or past its last row tile
-            p.rt = 0;
+            g.s = load_seq(P, s.b);
+            if (s.rt < row_tiles(P, g.s)) break;
+            ++s.b;                               // a sequence without new tokens, or past its last row tile
+            s.rt = 0;
         }
         int ta, tb;
-        row_tile_tokens(P, g.s, p.rt, ta, tb);
+        row_tile_tokens(P, g.s, s.rt, ta, tb);
         g.kv = kv_tiles<BN>(P, g.s, ta, tb);
-        g.b = p.b;
-        g.rt = p.rt;
-        const int k = (int)((x - p.at) / g.kv.count);
-        g.h = p.lines == 1 ? k : p.line;
-        g.start = p.at + (long long)k * g.kv.count;
-        g.i0 = (int)(x - g.start);
-        g.n = (int)min((long long)(g.kv.count - g.i0), p.hi - x);
-        g.first = x == p.lo;
-        x += g.n;
-        if (x == p.at + (long long)g.kv.count * p.heads(P.H)) {
-            p.at = x;
-            ++p.rt;
+        g.b = s.b;
+        g.rt = s.rt;
+        const int k = (int)((s.x - s.at) / g.kv.count);
+        g.h = p->lines == 1 ? k : p->line;
+        g.start = s.at + (long long)k * g.kv.count;
+        g.i0 = (int)(s.x - g.start);
+        g.n = (int)min((long long)(g.kv.count - g.i0), p->hi - s.x);
+        g.first = s.x == p->lo;
+        s.x += g.n;
+        if (s.x == s.at + (long long)g.kv.count * p->heads(P.H)) {
+            s.at = s.x;
+            ++s.rt;
         }
+        __syncwarp();
+        *w = s;
+        __syncwarp();
         return true;
     }
 };

@@ -342,11 +342,40 @@ __global__ void __launch_bounds__(KwShape<D>::THREADS, 1) key_weight_kernel(cons
     }
 }
 
-// The same sums from scores that the attention has left: 32 slots a CTA, a lane each, the rows dealt to its warps,
-// whose sums are added in order.
-template <int WARPS> __global__ void __launch_bounds__(WARPS * 32) sum_scores_kernel(const __grid_constant__ AttendParams P)
+// The same sums from scores that the attention has left.  Few rows: a thread a slot, eight rows' scores in flight;
+// bound by latency (1.5 M scores in N us).
+__global__ void __launch_bounds__(128) sum_few_scores_kernel(const __grid_constant__ AttendParams P)
 {
-    __shared__ float part[WARPS][33];
+    const int b = blockIdx.z, h = blockIdx.y, j = blockIdx.x * 128 + threadIdx.x;
+    grid_dependency_wait();
+    const Seq s = load_seq(P, b);
+    if (j >= s.L || j >= P.weight_stride || s.n == 0) return;
+    float* to = P.key_weight + ((long long)b * P.H + h) * P.weight_stride + j;
+    float w = *to;
+    for (int t = 0; t < s.n; ++t) {
+        if (!sees(P, s, s.slot(t), j)) continue;
+        const long long at = (long long)(s.t0 + t) * P.Hq + h * P.G;
+        for (int g0 = 0; g0 < P.G; g0 += 8) {
+            float x[8], z[8];
+#pragma unroll
+            for (int g = 0; g < 8; ++g) {
+                const bool in = g0 + g < P.G;
+                x[g] = in ? __ldcg(&P.scores[(at + g0 + g) * P.scores_stride + j]) : -INFINITY;
+                z[g] = in ? __ldcg(&P.lse[at + g0 + g]) * kLog2e : 0.0f;
+            }
+            float sum = 0.0f;
+#pragma unroll
+            for (int g = 0; g < 8; ++g) sum += exp2_hw(x[g] - z[g]);
+            w += sum;
+        }
+    }
+    *to = w;
+}
+// Many: 32 slots a CTA, a lane each; a warp has all query heads of every 16th token, and the warps' sums are added
+// in order.
+__global__ void __launch_bounds__(512) sum_scores_kernel(const __grid_constant__ AttendParams P)
+{
+    __shared__ float part[16][33];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int b = blockIdx.z, h = blockIdx.y, j = blockIdx.x * 32 + lane;
     grid_dependency_wait();
@@ -354,16 +383,13 @@ template <int WARPS> __global__ void __launch_bounds__(WARPS * 32) sum_scores_ke
     if (blockIdx.x * 32 >= s.L) return;
     const bool in = j < s.L && j < P.weight_stride;
     float w = 0.0f;
-    // few rows: a warp a row; many: a warp all query heads of a token
-    const int step = WARPS == 4 ? 1 : P.G;
-    for (int r = warp * step; r < s.n * P.G; r += WARPS * step) {
-        const int t = r / P.G;
+    for (int t = warp; t < s.n; t += 16) {
         const bool seen = in && sees(P, s, s.slot(t), j);
-        const long long at = (long long)(s.t0 + t) * P.Hq + h * P.G + (r - t * P.G);
+        const long long at = (long long)(s.t0 + t) * P.Hq + h * P.G;
 #pragma unroll 4
-        for (int k = 0; k < step; ++k) {
-            const float x = seen ? __ldcg(&P.scores[(at + k) * P.scores_stride + j]) : -INFINITY;
-            const float z = __ldcg(&P.lse[at + k]) * kLog2e;
+        for (int g = 0; g < P.G; ++g) {
+            const float x = seen ? __ldcg(&P.scores[(at + g) * P.scores_stride + j]) : -INFINITY;
+            const float z = __ldcg(&P.lse[at + g]) * kLog2e;
             w += seen ? exp2_hw(x - z) : 0.0f;
         }
     }
@@ -372,7 +398,7 @@ template <int WARPS> __global__ void __launch_bounds__(WARPS * 32) sum_scores_ke
     if (warp == 0 && in) {
         w = 0.0f;
 #pragma unroll
-        for (int k = 0; k < WARPS; ++k) w += part[k][lane];
+        for (int k = 0; k < 16; ++k) w += part[k][lane];
         P.key_weight[((long long)b * P.H + h) * P.weight_stride + j] += w;
     }
 }
@@ -412,8 +438,9 @@ cudaError_t launch_key_weight(const AttendParams& P, int num_sms, cudaStream_t s
 cudaError_t launch_sum_scores(const AttendParams& P, cudaStream_t stream)
 {
     const bool few = (long long)P.T * P.G <= 32ll * P.batch;
+    const int slots = few ? 128 : 32;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)((P.weight_stride + 31) / 32), P.H, P.batch);
+    cfg.gridDim = dim3((unsigned)((P.weight_stride + slots - 1) / slots), P.H, P.batch);
     cfg.blockDim = dim3(few ? 128 : 512);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
@@ -421,7 +448,7 @@ cudaError_t launch_sum_scores(const AttendParams& P, cudaStream_t stream)
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return few ? cudaLaunchKernelEx(&cfg, sum_scores_kernel<4>, P) : cudaLaunchKernelEx(&cfg, sum_scores_kernel<16>, P);
+    return few ? cudaLaunchKernelEx(&cfg, sum_few_scores_kernel, P) : cudaLaunchKernelEx(&cfg, sum_scores_kernel, P);
 }
 
 }  // namespace kvx
