@@ -126,6 +126,7 @@ EXPORTS = ["kvx_translator_create", "kvx_translator_create_low_rank", "kvx_trans
            "kvx_decoder_destroy", "kvx_append", "kvx_attend", "kvx_evict", "kvx_decoder_status", "kvx_decoder_launches"]
 KVX_PEER_STORES, KVX_PEER_STAGED = 0, 1
 KVX_STATIC_SCRATCH_BYTES = 8 << 20
+KVX_MAX_ATTEND_BATCH = 1024   # sequences of one kvx_attend call
 
 _lib = None
 
@@ -565,6 +566,24 @@ class Decoder:
         if t.shape != (tokens, heads, self._dim) or t.element_size() != self._size:
             raise ValueError(f"rows must be [{tokens}, {heads}, {self._dim}] of {self._size}-byte elements, got {tuple(t.shape)}")
 
+    def _layer(self, k, v, batch: int, page_table, page_size: int, num_pages: int):
+        """One layer of a cache as kvx_dst_kv (and what has to live as long), checked: this decoder's heads, width and
+        element size, room for `batch` sequences, K and V alike."""
+        ks, st, H, d = k.shape, k.stride(), self._heads, self._dim
+        ptrs = array.array("Q", (k.data_ptr(), v.data_ptr()))
+        at = ptrs.buffer_info()[0]
+        alike = v.shape == ks and v.stride() == st and k.element_size() == v.element_size() == self._size
+        if page_table is None:
+            if alike and len(ks) == 4 and ks[0] >= batch and ks[1] == H and ks[3] == d and st[3] == 1:
+                return _PACK_CACHE(at, at + 8, 0, ks[2], st[0], st[1], st[2], 0, 0, 0, 0), ptrs
+        else:
+            ts = page_table.shape
+            if page_size < 1 or (alike and ks[1:] == (page_size, H, d) and k.is_contiguous() and ts[0] >= batch
+                                 and page_table.element_size() == 4 and page_table.is_contiguous()):   # (the library refuses page sizes below 1)
+                return _PACK_CACHE(at, at + 8, 1, 0, 0, 0, 0, page_table.data_ptr(), ts[1], page_size, num_pages or ks[0]), ptrs
+        raise ValueError(f"caches must be alike, [B, {H}, S, {d}] or pools [pages, {page_size}, {H}, {d}] with an int32 page table, of "
+                         f"{self._size}-byte elements, got {tuple(ks)} and {tuple(v.shape)}")
+
     def append(self, q, k, v, seq_off, kv_len, cache_k, cache_v, q_out, *, pos=None, page_table=None, page_size: int = 16,
                num_pages: int = 0, stream=None):
         """Rotate the new tokens' q [T, Hq, d] into q_out (q itself: in place) and k [T, H, d] into the cache, and
@@ -575,8 +594,12 @@ class Decoder:
         self._fits(k, T, H)
         self._fits(v, T, H)
         self._fits(q_out, T, Hq)
-        tok = _PACK_TOKENS(seq_off.shape[0] - 1, T, seq_off.data_ptr(), kv_len.data_ptr(), 0 if pos is None else pos.data_ptr())
-        cache, _keep = _cache((cache_k,), (cache_v,), page_table, page_size, num_pages)
+        B = seq_off.shape[0] - 1
+        if kv_len.shape[0] < B or seq_off.element_size() != 4 or kv_len.element_size() != 4 or \
+                (pos is not None and (pos.shape[0] != T or pos.element_size() != 4)):
+            raise ValueError("seq_off [B + 1], kv_len [B] and pos [tokens] must be int32")
+        tok = _PACK_TOKENS(B, T, seq_off.data_ptr(), kv_len.data_ptr(), 0 if pos is None else pos.data_ptr())
+        cache, _keep = self._layer(cache_k, cache_v, B, page_table, page_size, num_pages)
         st = lib().kvx_append(self.handle, tok, _rows(q), _rows(k), _rows(v), _rows(q_out), cache, 0, _raw_stream(stream))
         if st:
             _check(st)
@@ -595,10 +618,13 @@ class Decoder:
         if key_weight is not None and not (key_weight.shape[:2] == (B, self._heads) and key_weight.is_contiguous()
                                            and key_weight.element_size() == 4):
             raise ValueError("key_weight must be contiguous float32 [sequences, KV heads, slots]")
+        if kv_len.shape[0] < B or seq_off.element_size() != 4 or kv_len.element_size() != 4 or \
+                (prefix_len is not None and (prefix_len.shape[0] < B or prefix_len.element_size() != 4)):
+            raise ValueError("seq_off [B + 1], kv_len [B] and prefix_len [B] must be int32")
         tok = _PACK_TOKENS(B, T, seq_off.data_ptr(), kv_len.data_ptr(), 0)
         opts = _PACK_OPTS(window, 0 if prefix_len is None else prefix_len.data_ptr(), 0 if lse is None else lse.data_ptr(),
                           0 if key_weight is None else key_weight.data_ptr(), 0 if key_weight is None else key_weight.shape[2])
-        cache, _keep = _cache((cache_k,), (cache_v,), page_table, page_size, num_pages)
+        cache, _keep = self._layer(cache_k, cache_v, B if B <= KVX_MAX_ATTEND_BATCH else 0, page_table, page_size, num_pages)
         st = lib().kvx_attend(self.handle, tok, _rows(q), cache, 0, opts, _rows(out), _raw_stream(stream))
         if st:
             _check(st)
@@ -619,6 +645,10 @@ class Decoder:
             raise ValueError(f"kept_weight must be contiguous float32 [{L}, {B}, {H}, slots]")
         if not len(src_v) == len(dst_k) == len(dst_v) == L:
             raise ValueError("src_k, src_v, dst_k and dst_v must have as many layers as one another")
+        if kv_len.element_size() != 4 or new_len.element_size() != 4 or new_len.shape[0] != B:
+            raise ValueError("kv_len and new_len must be int32 [B]")
+        self._layer(src_k[0], src_v[0], B, page_table, page_size, num_pages)
+        self._layer(dst_k[0], dst_v[0], B, dst_page_table, page_size, dst_num_pages)
         plan = _PACK_PLAN(B, L, kv_len.data_ptr(), key_weight.data_ptr(), key_weight.shape[3], keep, sinks, recent, kept.data_ptr(),
                           new_len.data_ptr(), _ptr(kept_weight), 0 if kept_weight is None else kept_weight.shape[3])
         src, _keep_src = _cache(src_k, src_v, page_table, page_size, num_pages)

@@ -483,6 +483,12 @@ def test_refusals():
         p.dec.attend(q[:, :4], off, L, k, v, out, **ok)
     with pytest.raises(ValueError):
         p.dec.attend(q.float(), off, L, k, v, out, **ok)
+    with pytest.raises(ValueError):                      # lengths and offsets of another width, caches of another shape
+        p.dec.attend(q, off.long(), L, k, v, out, **ok)
+    with pytest.raises(ValueError):
+        p.dec.attend(q, off, L, k[:, :8], v[:, :8], out, **ok)
+    with pytest.raises(ValueError):
+        p.dec.append(q, q[:, :2], q[:, :2], off, L, k.float(), v.float(), q, **ok)
     kept, n = torch.zeros((1, 1, 2, 8), dtype=torch.int32, device="cuda"), i32([0])
     w = torch.zeros((1, 1, 2, 64), device="cuda")
     args = ([k], [v], [k], [v], kept, n)
