@@ -4,10 +4,9 @@
 //   S = Q K^T (fp32, TMEM),  P = exp2(c S - m),  O += P V (P bf16 from TMEM, O fp32 in TMEM)
 // in one pass over the slots, with the running maximum m and sum l of a row in the registers of the thread
 // that owns the row.  A CTA holds NT tiles of 128 rows and walks slot tiles of BN.
-//   producer warps (3)  copy Q, K and V rows into 128-byte-swizzled tiles.  Q: tensor copies.  K and V: tensor
-//                       copies (TMA) where a box holds 32 rows or more (contiguous caches, large pages), else
-//                       16-byte thread copies through the page table.  A K tile is read as a K-major
-//                       operand, a V tile, laid out alike, as an MN-major one.
+//   producer warps (3)  copy Q, K and V rows into 128-byte-swizzled tiles: Q by tensor copies (TMA), K and V by
+//                       16-byte thread copies through the page table, a tile a warp.  A K tile is read as a
+//                       K-major operand, a V tile, laid out alike, as an MN-major one.
 //   MMA warp            unit u = (slot tile, row tile): S(u) into score buffer u mod 2, then, when P(u)
 //                       is there, O += P(u) V; S(u + 2) is issued right behind it, so that the scores of
 //                       one unit are formed while the other's softmax runs.
@@ -21,11 +20,11 @@
 // anyway (one row tile), P goes in as two bf16 terms, high and low, at the price of a second product.
 //
 // What bounds it.  Many rows: the chain S -> softmax -> P V of each row tile, which the other tile's MMAs only partly
-// fill: 4096 tokens of 28 query heads (7 a KV head, 128 wide) over 32768 slots take 1.32 ms, 1.37 PFLOP/s or 72% of a large
-// library product's rate, with pages of 16 tokens, whose rows thread copies bring; 1.18 ms, 81%, with pages of 64, in
-// tensor copies.  Few rows: the reading of K and V: one token of each of eight sequences over up to 32768 slots, 411 MB,
-// 83 us, 4.9 TB/s.  Short calls: latency, about 11 us from launch to end (three dependent reads from DRAM: lengths, page table,
-// rows; code that is not in the instruction cache yet, which is why its loops are short where they can be).
+// fill: 4096 tokens of 28 query heads (7 a KV head, 128 wide) over 32768 slots take 1.13 ms, 1.6 PFLOP/s or 85% of a large
+// library product's rate, with pages of 16 tokens, of 64 or none.  Few rows: the reading of K and V: one token of each of
+// eight sequences over up to 32768 slots, 411 MB, 83 us, 4.9 TB/s.  Short calls: latency, about 11 us from launch to end
+// (three dependent reads from DRAM: lengths, page table, rows; code that is not in the instruction cache yet, which is
+// why its loops are short where they can be).
 #pragma once
 
 #include <atomic>
@@ -85,23 +84,17 @@ template <int D, int NT> __device__ __forceinline__ bool two_terms(const AttendP
     return own < kFewSlots || (P.window > 0 && P.window < kFewSlots);
 }
 
-// Tensor maps of K and V, and the rows of a box: a paged cache as (channel, head, slot in page, page), a
-// contiguous one as (channel, slot, head, sequence); boxes of 64 channels of one head.
-struct TileMaps {
-    CUtensorMap k, v, q;      // q: (channel, head, token), boxes of 64 channels of a row tile
-    int box_rows;
-};
-// How K and V tiles are brought: row by row (any page size), in groups of 8 rows a fixed stride apart (page sizes that
-// are multiples of 8), or by tensor copies.
-enum Source { kRows, kGroups, kBoxes };
+// How K and V tiles are brought: row by row (any page size), or in groups of 8 rows a fixed stride apart (contiguous caches
+// and page sizes that are multiples of 8).  (Tensor copies, a box a page, were slower: 4096 tokens over 32768 slots with
+// pages of 16, 32 and 64 slots 2.06, 1.29 and 1.18 ms against 1.13.)
+enum Source { kRows, kGroups };
 
 template <int D, int NT, Source SRC, bool CAP>
 __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
-    attend_tc_kernel(const __grid_constant__ AttendParams P, const __grid_constant__ TileMaps maps)
+    attend_tc_kernel(const __grid_constant__ AttendParams P, const __grid_constant__ CUtensorMap q_map)
 {
     using C = TcShape<D, NT>;
     using B = Bars<C::STAGES>;
-    constexpr bool TMA = SRC == kBoxes;
     constexpr int BM = C::BM, BN = C::BN;
     extern __shared__ __align__(1024) uint8_t smem[];
     const uint32_t s0 = smem_u32(smem);
@@ -115,7 +108,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
     if (warp == kMmaWarp) tmem_alloc(smem_u32(tmem_slot), C::TMEM);
     if (threadIdx.x == 0) {
         for (int i = 0; i < C::STAGES; ++i) {
-            mbar_init(bar(B::full + i), TMA ? 1 : NT == 2 ? kProdWarps * 32 : 32);
+            mbar_init(bar(B::full + i), 32);
             mbar_init(bar(B::empty + i), 1);
         }
         for (int i = 0; i < 2; ++i) {
@@ -156,7 +149,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
         const int sub = lane / CPR;
         const uint32_t place = (uint32_t)((lane % CPR >> 3)), c0 = (uint32_t)(((lane % CPR & 7) ^ sub) << 4);
         uint32_t pos = 0, items = 0;                     // tiles and items begun
-        uint32_t issued = 0, q_issued = 0;               // tensor copies of tiles and of Q that were issued
+        uint32_t q_issued = 0;                           // tensor copies of Q
         bool ok = true;
         auto wait = [&](int b, uint32_t parity) { ok = __all_sync(0xffffffffu, ok && W.wait(bar(b), parity)); };
         // The copies of a batch announce themselves: each thread's arrival follows its own copies.  The MMA warp
@@ -171,181 +164,115 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
                     mbar_arrive_expect_tx(bar(B::qfull), (uint32_t)P.tile_rows * D * 2);
 #pragma unroll
                     for (int cb = 0; cb < D / 64; ++cb)
-                        tma_box3(sQ + cb * (BM * 128), &maps.q, cb * 64, g.h * P.G, g.s.t0 + g.rt * (P.tile_rows / P.G), bar(B::qfull));
+                        tma_box3(sQ + cb * (BM * 128), &q_map, cb * 64, g.h * P.G, g.s.t0 + g.rt * (P.tile_rows / P.G), bar(B::qfull));
                 }
                 __syncwarp();
             }
             ++items;
             const long long head = cache_head(P.cache) * g.h;
             // tile i as K, tile i - NB + 1 as V, and at the end the V tiles left
-            if constexpr (TMA) {
-                if (warp > 0) continue;
-                // Lane r looks up the page of box r of the next tile while this one is issued; the issue itself is
-                // uniform (a lane of its own would take each copy's operands through uniform registers).
-                const int n = __shfl_sync(0xffffffffu, g.n, 0), b = __shfl_sync(0xffffffffu, g.b, 0), h = __shfl_sync(0xffffffffu, g.h, 0);
-                auto tile_slot = [&](int t) { return __shfl_sync(0xffffffffu, g.kv.at(g.i0 + t) * BN, 0); };
-                auto pages = [&](int t) {
-                    int page = -1;                       // outside the pool: the box is filled with zeros
-                    const int j = tile_slot(t) + lane * maps.box_rows;
-                    if (P.cache.paged && lane * maps.box_rows < BN && j < g.s.L) {
-                        const int pi = j >> P.cache.page_shift;
-                        if (pi < P.cache.max_pages) page = __ldg(&P.cache.page_table[(size_t)b * P.cache.max_pages + pi]);
-                        if (page < 0 || page >= P.cache.num_pages) {
-                            page = -1;
-                            set_status(P.status, KVX_DEV_PAGE_INVALID);
-                        }
-                    }
-                    return page;
-                };
-                int page_k = pages(0), page_v = page_k;  // of the tiles to be issued next as K and as V
-                for (int i = 0; i < n + C::NB - 1; ++i) {
-                    const int ahead = i + 1 < n ? pages(i + 1) : -1;
-#pragma unroll
-                    for (int kv = 0; kv < 2; ++kv) {
-                        const int t = kv ? i - (C::NB - 1) : i;
-                        if (t < 0 || t >= n) continue;
-                        const int j0 = tile_slot(t), page = kv ? (C::NB == 1 ? page_k : page_v) : page_k;
-                        const uint32_t st = pos % C::STAGES, ph = (pos / C::STAGES) & 1;
-                        ok = __all_sync(0xffffffffu, ok && W.wait(bar(B::empty + st), ph ^ 1));
-                        ++pos;
-                        if (!ok) continue;
-                        issued = pos;
-                        const uint32_t dst = sT + st * C::TILE, full = bar(B::full + st);
-                        const CUtensorMap* map = kv ? &maps.v : &maps.k;
-                        if (elect_one()) mbar_arrive_expect_tx(full, C::TILE);
-                        for (int r = 0; r < BN; r += maps.box_rows) {
-                            const int pg = __shfl_sync(0xffffffffu, page, r / maps.box_rows);
-                            const int in = (j0 + r) & (P.cache.page_size - 1);
-                            if (elect_one()) {
-#pragma unroll
-                                for (int cb = 0; cb < D / 64; ++cb) {
-                                    const uint32_t to = dst + (uint32_t)(cb * (BN * 128) + r * 128);
-                                    if (P.cache.paged) tma_box4(to, map, cb * 64, h, in, pg, full);
-                                    else tma_box4(to, map, cb * 64, j0 + r, h, b, full);
-                                }
-                            }
-                        }
-                        __syncwarp();
-                    }
-                    page_v = page_k;
-                    page_k = ahead;
+            // Each warp takes every third tile: a part of every tile each would spend most of its time on what a
+            // tile costs anyway (4096 tokens over 32768 slots 1.32 ms against 1.12, a token each of 8 sequences over
+            // 32768 slots 166 us against 117).  The next tile's pages are read while this one's copies are
+            // issued, and looked at only then.
+            constexpr int PER = SRC == kGroups ? 8 : 1;      // rows a stride apart: a lane finds the first of them
+            constexpr int FIND = BN / PER;                   // of these a tile has
+            constexpr int LOOK = (FIND + 31) / 32;
+            const long long stride = P.cache.paged ? (long long)P.cache.H * D : P.cache.st;
+            const long long mine = head + (PER > 1 ? sub * stride : 0) + lane % CPR * 8;
+            const int total = 2 * g.n;
+            // tile r of the item in the order of the ring: K or V, and the slot tile
+            auto tile_of = [&](int r, int& kv) {
+                if (C::NB == 1) {
+                    kv = r & 1;
+                    return r >> 1;
                 }
-            } else {
-                // One row tile: each warp takes every third tile (a part of every tile each would spend most of its time on
-                // what a tile costs anyway: 32768 slots x 8, heads of 128: 160 us, 132 so).  Two row tiles, whose
-                // larger tiles leave few in the ring: the warps share each, so that it is there sooner (4096
-                // tokens over 32768 slots: 1.75 ms, 1.48 so).  The next tile's pages are read while this one's copies
-                // are issued, and looked at only then.
-                constexpr bool SHARED = NT == 2;
-                constexpr int PER = SRC == kGroups ? 8 : 1;      // rows a stride apart: a lane finds the first of them
-                constexpr int PART = SHARED ? BN * 3 / 8 : BN;   // rows of a tile a warp copies at most
-                constexpr int FIND = PART / PER;
-                constexpr int LOOK = (FIND + 31) / 32;
-                // a warp's part of a shared tile: 3/8, 3/8 and 2/8 of its groups of 8 rows
-                const int q0 = SHARED ? warp * (PART / 8) : 0;
-                const long long stride = P.cache.paged ? (long long)P.cache.H * D : P.cache.st;
-                const long long mine = head + (PER > 1 ? sub * stride : 0) + lane % CPR * 8;
-                const int total = 2 * g.n;
-                // tile r of the item in the order of the ring: K or V, and the slot tile
-                auto tile_of = [&](int r, int& kv) {
-                    if (C::NB == 1) {
-                        kv = r & 1;
-                        return r >> 1;
-                    }
-                    kv = r == total - 1 || (r > 0 && !(r & 1));
-                    return r == total - 1 ? g.n - 1 : kv ? (r >> 1) - 1 : (r + 1) >> 1;
-                };
-                auto pages_of = [&](int r, int (&x)[LOOK]) {
-                    int kv;
-                    const int j0 = r < total ? g.kv.at(g.i0 + tile_of(r, kv)) * BN + q0 * 8 : g.s.L;
+                kv = r == total - 1 || (r > 0 && !(r & 1));
+                return r == total - 1 ? g.n - 1 : kv ? (r >> 1) - 1 : (r + 1) >> 1;
+            };
+            auto pages_of = [&](int r, int (&x)[LOOK]) {
+                int kv;
+                const int j0 = r < total ? g.kv.at(g.i0 + tile_of(r, kv)) * BN : g.s.L;
 #pragma unroll
-                    for (int k = 0; k < LOOK; ++k) {
-                        const int j = j0 + (k * 32 + lane) * PER;
-                        x[k] = -2;                               // past the end
-                        if (k * 32 + lane < FIND && j < g.s.L) {
-                            x[k] = 0;
-                            if (P.cache.paged) {
-                                const int pi = P.cache.page_shift >= 0 ? j >> P.cache.page_shift : j / P.cache.page_size;
-                                x[k] = pi < P.cache.max_pages ? __ldg(&P.cache.page_table[(size_t)g.b * P.cache.max_pages + pi]) : -1;
-                            }
+                for (int k = 0; k < LOOK; ++k) {
+                    const int j = j0 + (k * 32 + lane) * PER;
+                    x[k] = -2;                               // past the end
+                    if (k * 32 + lane < FIND && j < g.s.L) {
+                        x[k] = 0;
+                        if (P.cache.paged) {
+                            const int pi = P.cache.page_shift >= 0 ? j >> P.cache.page_shift : j / P.cache.page_size;
+                            x[k] = pi < P.cache.max_pages ? __ldg(&P.cache.page_table[(size_t)g.b * P.cache.max_pages + pi]) : -1;
                         }
                     }
-                };
-                auto row_at = [&](int j, int page) -> long long {
-                    if (page == -2) return -1;
-                    if (!P.cache.paged) return (long long)g.b * P.cache.sb + (long long)j * P.cache.st;
-                    if (page < 0 || page >= P.cache.num_pages) {
-                        set_status(P.status, KVX_DEV_PAGE_INVALID);
-                        return -1;
-                    }
-                    const int in = P.cache.page_shift >= 0 ? j & (P.cache.page_size - 1) : j % P.cache.page_size;
-                    return ((long long)page * P.cache.page_size + in) * stride;
-                };
-                int next[LOOK];
-                constexpr int STEP = SHARED ? 1 : kProdWarps;
-                int r = SHARED ? 0 : (int)((kProdWarps + (uint32_t)warp - pos % kProdWarps) % kProdWarps);
-                pages_of(r, next);
-                for (; r < total; r += STEP) {
-                    int kv;
-                    const int j0 = g.kv.at(g.i0 + tile_of(r, kv)) * BN;
-                    const __nv_bfloat16* src = (const __nv_bfloat16*)(kv ? P.cv : P.ck);
-                    const uint32_t p = pos + (uint32_t)r, st = p % C::STAGES, ph = (p / C::STAGES) & 1;
-                    long long at[LOOK];
+                }
+            };
+            auto row_at = [&](int j, int page) -> long long {
+                if (page == -2) return -1;
+                if (!P.cache.paged) return (long long)g.b * P.cache.sb + (long long)j * P.cache.st;
+                if (page < 0 || page >= P.cache.num_pages) {
+                    set_status(P.status, KVX_DEV_PAGE_INVALID);
+                    return -1;
+                }
+                const int in = P.cache.page_shift >= 0 ? j & (P.cache.page_size - 1) : j % P.cache.page_size;
+                return ((long long)page * P.cache.page_size + in) * stride;
+            };
+            int next[LOOK];
+            int r = (int)((kProdWarps + (uint32_t)warp - pos % kProdWarps) % kProdWarps);
+            pages_of(r, next);
+            for (; r < total; r += kProdWarps) {
+                int kv;
+                const int j0 = g.kv.at(g.i0 + tile_of(r, kv)) * BN;
+                const __nv_bfloat16* src = (const __nv_bfloat16*)(kv ? P.cv : P.ck);
+                const uint32_t p = pos + (uint32_t)r, st = p % C::STAGES, ph = (p / C::STAGES) & 1;
+                long long at[LOOK];
 #pragma unroll
-                    for (int k = 0; k < LOOK; ++k) at[k] = row_at(j0 + q0 * 8 + (k * 32 + lane) * PER, next[k]);
-                    pages_of(r + STEP, next);
-                    wait(B::empty + (int)st, ph ^ 1);
-                    if (ok) {
-                        const uint32_t d0 = sT + st * C::TILE + place * (BN * 128) + (uint32_t)(q0 * 1024 + sub * 128);
-                        if constexpr (SRC == kGroups) {
+                for (int k = 0; k < LOOK; ++k) at[k] = row_at(j0 + (k * 32 + lane) * PER, next[k]);
+                pages_of(r + kProdWarps, next);
+                wait(B::empty + (int)st, ph ^ 1);
+                if (ok) {
+                    const uint32_t d0 = sT + st * C::TILE + place * (BN * 128) + (uint32_t)sub * 128;
+                    if constexpr (SRC == kGroups) {
 #pragma unroll 1
-                            for (int q = 0; q < PART / 8; ++q) {
-                                if (SHARED && warp == 2 && q >= BN / 32) break;
-                                const long long first = __shfl_sync(0xffffffffu, at[0], q);
-                                const int left = g.s.L - (j0 + (q0 + q) * 8);   // rows of the sequence from here on
-                                const __nv_bfloat16* s1 = src + first + mine;
-                                if (first >= 0 && left >= 8) {
+                        for (int q = 0; q < BN / 8; ++q) {
+                            const long long first = __shfl_sync(0xffffffffu, at[0], q);
+                            const int left = g.s.L - (j0 + q * 8);   // rows of the sequence from here on
+                            const __nv_bfloat16* s1 = src + first + mine;
+                            if (first >= 0 && left >= 8) {
 #pragma unroll
-                                    for (int k = 0; k < 8; k += RPI)
-                                        cp_async16(d0 + (uint32_t)(q * 1024 + k * 128) + (c0 ^ (uint32_t)(k << 4)), s1 + k * stride);
-                                } else {
+                                for (int k = 0; k < 8; k += RPI)
+                                    cp_async16(d0 + (uint32_t)(q * 1024 + k * 128) + (c0 ^ (uint32_t)(k << 4)), s1 + k * stride);
+                            } else {
 #pragma unroll
-                                    for (int k = 0; k < 8; k += RPI) {
-                                        const bool real = first >= 0 && k + sub < left;
-                                        cp_async16_or_zero(d0 + (uint32_t)(q * 1024 + k * 128) + (c0 ^ (uint32_t)(k << 4)), real ? s1 + k * stride : src,
-                                                           real);
-                                    }
+                                for (int k = 0; k < 8; k += RPI) {
+                                    const bool real = first >= 0 && k + sub < left;
+                                    cp_async16_or_zero(d0 + (uint32_t)(q * 1024 + k * 128) + (c0 ^ (uint32_t)(k << 4)), real ? s1 + k * stride : src,
+                                                       real);
                                 }
                             }
-                        } else {
+                        }
+                    } else {
 #pragma unroll
-                            for (int k = 0; k < PART; k += RPI) {
-                                if (SHARED && warp == 2 && k >= BN / 4) break;
-                                const long long row = __shfl_sync(0xffffffffu, at[k / 32], (k & 31) + sub);
-                                cp_async16_or_zero(d0 + (uint32_t)k * 128 + (c0 ^ (uint32_t)((k & 7) << 4)), row < 0 ? src : src + row + mine, row >= 0);
-                            }
+                        for (int k = 0; k < BN; k += RPI) {
+                            const long long row = __shfl_sync(0xffffffffu, at[k / 32], (k & 31) + sub);
+                            cp_async16_or_zero(d0 + (uint32_t)k * 128 + (c0 ^ (uint32_t)((k & 7) << 4)), row < 0 ? src : src + row + mine, row >= 0);
                         }
                     }
-                    cp_async_arrive(bar(B::full + (int)st));
                 }
-                pos += (uint32_t)total;
+                cp_async_arrive(bar(B::full + (int)st));
             }
+            pos += (uint32_t)total;
         }
         cp_async_wait_all();
-        if (!ok && warp == 0) {
-            if (q_issued > 0) drain(bar(B::qfull), (q_issued - 1) & 1);
-            if (TMA)
-                for (uint32_t q = issued > C::STAGES ? issued - C::STAGES : 0; q < issued; ++q) drain(bar(B::full + (int)(q % C::STAGES)), (q / C::STAGES) & 1);
-        }
+        if (!ok && warp == 0 && q_issued > 0) drain(bar(B::qfull), (q_issued - 1) & 1);
     } else {
         // ---------------------------------------------------------------- MMA
         // The whole warp walks and waits, so that stages and descriptors stay in uniform registers (a lane of its own
         // moves every operand there first: 120 clocks an MMA instead of 64); one lane issues.
         constexpr uint32_t idesc_s = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
         constexpr uint32_t idesc_o = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
-        // Two row tiles and asynchronous thread copies: a slot tile's V and the next one's K are waited for, and fenced,
-        // while the first unit's softmax runs (behind it the fences stood in the MMAs' way: 150 clocks each).
-        constexpr bool EARLY = !TMA && NT == 2;
+        // Two row tiles: a slot tile's V and the next one's K are waited for, and fenced, while the first unit's softmax
+        // runs (behind it the fences stood in the MMAs' way: 150 clocks each).
+        constexpr bool EARLY = NT == 2;
         const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
         uint32_t base = 0, units = 0, items = 0;         // tiles and units of the items before; items begun
         bool ok = true;
@@ -359,7 +286,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
                 if (u == 0) wait(B::qfull, items & 1);
                 if (t == 0 && !(EARLY && u > 0)) wait(B::full + (int)st, (p / C::STAGES) & 1);
                 if (!ok) return;
-                if (!TMA && t == 0 && !(EARLY && u > 0)) fence_proxy_async();
+                if (t == 0 && !(EARLY && u > 0)) fence_proxy_async();
                 tc_fence_after();
                 const uint32_t d = tm + ((units + u) & 1) * C::S_COL;
                 // descriptors count 16-byte units in their low bits: steps along an operand are added
@@ -388,7 +315,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
                 wait(B::pfull + (int)(gu & 1), (gu >> 1) & 1);
                 if (!EARLY && t == 0) wait(B::full + (int)st, (p / C::STAGES) & 1);
                 if (!ok) break;
-                if (!TMA && !EARLY && t == 0) fence_proxy_async();
+                if (!EARLY && t == 0) fence_proxy_async();
                 tc_fence_after();
                 const uint64_t vd = mn_desc(sT + st * C::TILE, BN * 128);
                 const uint32_t wg = C::COLS ? 0 : gu & 1;
@@ -429,7 +356,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
         float* shared_max = reinterpret_cast<float*>(smem + 1024) + quad * 32 + lane;   // [2][128]
         float* shared_sum = reinterpret_cast<float*>(smem + 2048) + quad * 32 + lane;   // [2][128]
         const int my_r = t * 128 + quad * 32 + lane, my_tok = my_r / P.G, my_head = my_r - my_tok * P.G;   // this thread's row of a tile
-        uint32_t units = 0, items = 0, base_tile = 0, filled[2] = {0, 0};   // filled: times each O has been completed
+        uint32_t units = 0, items = 0, filled[2] = {0, 0};   // filled: times each O has been completed
         bool ok = true;                                  // the same in the lanes of a warp
         auto wait = [&](int b, uint32_t parity) { ok = __all_sync(0xffffffffu, ok && W.wait(bar(b), parity)); };
         bool have = false;
@@ -460,19 +387,6 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
                 tc_fence_after();
                 const uint32_t at = lanes + (gu & 1) * C::S_COL;
                 const int j0 = g.kv.at(g.i0 + i) * BN;
-                if (TMA && j0 + BN > g.s.L && (NT == 2 ? t == 0 : !C::COLS || wg == 0)) {
-                    // the boxes brought what the cache holds past the sequence's end: zeros in V's place, before
-                    // any P is announced for it
-                    const uint32_t p = base_tile + (uint32_t)(C::NB == 1 ? 2 * i + 1 : i == g.n - 1 ? 2 * i + 1 : 2 * i + 2), st = p % C::STAGES;
-                    wait(B::full + (int)st, (p / C::STAGES) & 1);
-                    if (!C::COLS && !ok) break;
-                    const int from = max(g.s.L - j0, 0);
-                    uint8_t* tile = smem + C::CTRL + C::QB + st * C::TILE;
-                    for (int e = (int)(threadIdx.x & 127) + from * 8; ok && e < BN * 8; e += 128)
-#pragma unroll
-                        for (int cb = 0; cb < D / 64; ++cb) *reinterpret_cast<uint4*>(tile + cb * (BN * 128) + e * 16) = make_uint4(0, 0, 0, 0);
-                    fence_proxy_async();
-                }
                 const bool all = __all_sync(0xffffffffu, (j0 >= lo && j0 + BN <= hi) || j0 + BN <= pre);
                 uint32_t x[CW];
 #pragma unroll
@@ -590,7 +504,6 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
             }
             const int u1 = u0 ^ 1;                           // the other warpgroup's first unit (a slot tile each)
             units += (uint32_t)U;
-            base_tile += 2 * (uint32_t)g.n;
             if (ok && u0 < U) wait(B::ofull + (C::COLS ? 0 : wg), filled[0] & 1);
             filled[0] += u0 < U;
             bool other = false;                              // join: the other warpgroup has sums, too
@@ -711,31 +624,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
     }
 }
 
-// The maps of a call's cache, tiles of bn slots; false where boxes cannot describe it.
-bool make_maps(const AttendParams& P, int bn, TileMaps& m)
-{
-    const CacheView& c = P.cache;
-    const EncodeTiled enc = tiled_encoder();
-    m.box_rows = c.paged && c.page_size < bn ? c.page_size : bn;
-    // boxes of 16 rows come one by one slower than thread copies (4096 tokens over 32768 slots 2.2 ms, 1.5 so); of 32
-    // rows faster (1.34 ms, 1.45)
-    if (!enc || c.capacity < 1 || (c.paged && c.page_shift < 0) || m.box_rows < 32) return false;
-    const cuuint64_t H = (cuuint64_t)c.H, d = (cuuint64_t)c.d;
-    const cuuint64_t dims_p[4] = {d, H, (cuuint64_t)c.page_size, (cuuint64_t)c.num_pages};
-    const cuuint64_t str_p[3] = {d * 2, H * d * 2, (cuuint64_t)c.page_size * H * d * 2};
-    const cuuint64_t dims_c[4] = {d, (cuuint64_t)c.capacity, H, (cuuint64_t)P.batch};
-    const cuuint64_t str_c[3] = {(cuuint64_t)c.st * 2, (cuuint64_t)c.sh * 2, (cuuint64_t)c.sb * 2};
-    const cuuint32_t box_p[4] = {64, 1, (cuuint32_t)m.box_rows, 1}, box_c[4] = {64, (cuuint32_t)m.box_rows, 1, 1};
-    const cuuint32_t one[4] = {1, 1, 1, 1};
-    for (int i = 0; i < 2; ++i)
-        if (enc(i ? &m.v : &m.k, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(i ? P.cv : P.ck), c.paged ? dims_p : dims_c,
-                c.paged ? str_p : str_c, c.paged ? box_p : box_c, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
-            return false;
-    return true;
-}
-
-template <int D, int NT, Source SRC, bool CAP> cudaError_t start_tc(const AttendParams& P, const TileMaps& maps, int num_sms, cudaStream_t stream)
+template <int D, int NT, Source SRC, bool CAP> cudaError_t start_tc(const AttendParams& P, const CUtensorMap& q_map, int num_sms, cudaStream_t stream)
 {
     using C = TcShape<D, NT>;
     const int grid = min(num_sms, kAttendMaxRows / C::BM / 2);
@@ -750,7 +639,7 @@ template <int D, int NT, Source SRC, bool CAP> cudaError_t start_tc(const Attend
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    if (cudaError_t e = cudaLaunchKernelEx(&cfg, attend_tc_kernel<D, NT, SRC, CAP>, P, maps); e != cudaSuccess) return e;
+    if (cudaError_t e = cudaLaunchKernelEx(&cfg, attend_tc_kernel<D, NT, SRC, CAP>, P, q_map); e != cudaSuccess) return e;
     return run_join<__nv_bfloat16, D, C::BM>(P, grid, stream);
 }
 template <int D, int NT, bool CAP> cudaError_t run_tc(const AttendParams& call, int num_sms, cudaStream_t stream)
@@ -758,17 +647,16 @@ template <int D, int NT, bool CAP> cudaError_t run_tc(const AttendParams& call, 
     using C = TcShape<D, NT>;
     AttendParams P = call;
     P.tile_rows = C::BM / P.G * P.G;               // whole tokens: with 7 query heads a KV head 126 or 252 rows
-    TileMaps maps;
+    CUtensorMap q_map;                             // (channel, head, token), boxes of 64 channels of a row tile
     const EncodeTiled enc = tiled_encoder();
     const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)P.Hq, (cuuint64_t)P.T};
     const cuuint64_t strides[2] = {(cuuint64_t)P.q_h * 2, (cuuint64_t)P.q_t * 2};
     const cuuint32_t box[3] = {64, (cuuint32_t)P.G, (cuuint32_t)(C::BM / P.G)}, one[3] = {1, 1, 1};
-    if (!enc || enc(&maps.q, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(P.q), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+    if (!enc || enc(&q_map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(P.q), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
                     CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
         return cudaErrorInvalidValue;
-    if (make_maps(P, C::BN, maps)) return start_tc<D, NT, kBoxes, CAP>(P, maps, num_sms, stream);
-    if (!P.cache.paged || P.cache.page_size % 8 == 0) return start_tc<D, NT, kGroups, CAP>(P, maps, num_sms, stream);
-    return start_tc<D, NT, kRows, CAP>(P, maps, num_sms, stream);
+    if (!P.cache.paged || P.cache.page_size % 8 == 0) return start_tc<D, NT, kGroups, CAP>(P, q_map, num_sms, stream);
+    return start_tc<D, NT, kRows, CAP>(P, q_map, num_sms, stream);
 }
 template <bool CAP> cudaError_t run_attend_tc(const AttendParams& P, int num_sms, cudaStream_t stream)
 {

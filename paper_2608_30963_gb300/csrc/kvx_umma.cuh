@@ -123,20 +123,12 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b)
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(reinterpret_cast<unsigned long long&>(a)), "l"(reinterpret_cast<unsigned long long&>(b)));
     return reinterpret_cast<float2&>(r);
 }
-// Tensor copies of a box, completing on an mbarrier.
-__device__ __forceinline__ void tma_box4(uint32_t dst, const CUtensorMap* map, int x, int y, int z, int w, uint32_t mbar)
-{
-    asm volatile(
-        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(dst),
-        "l"(map), "r"(mbar), "r"(x), "r"(y), "r"(z), "r"(w)
-        : "memory");
-}
-
 // Barriers (8 bytes each) in the control block.
 template <int STAGES> struct Bars {
     static constexpr int full = 0, empty = STAGES, sfull = 2 * STAGES, pfull = sfull + 2, ofull = pfull + 2, qfull = ofull + 2,
                          qempty = qfull + 1, done = qempty + 1, mlfull = done + 1, mlempty = mlfull + 1;
 };
+// Tensor copy of a box, completing on an mbarrier.
 __device__ __forceinline__ void tma_box3(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t mbar)
 {
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst),

@@ -506,7 +506,7 @@ def test_refusals():
 @pytest.mark.parametrize("H,G,d,ctx,new", [(2, 7, 128, [333, 90], [37, 1]), (1, 4, 64, [513], [130]), (2, 2, 256, [200, 40], [1, 66]),
                                            (3, 5, 128, [400, 0, 31], [1, 1, 1])])
 def test_page_sizes(ps, H, G, d, ctx, new):
-    """Every way rows are brought: boxes, groups of eight rows and single rows; the same values whichever."""
+    """Every way rows are brought: groups of eight rows and single rows; the same values whichever."""
     p = Problem(H, G, d, ctx, new, "bf16", ps, seed=41)
     w = torch.zeros((p.B, H, p.S), device="cuda")
     out, lse = p.attend(weight=w)
