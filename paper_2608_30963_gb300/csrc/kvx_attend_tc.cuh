@@ -201,7 +201,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
                         x[k] = 0;
                         if (P.cache.paged) {
                             const int pi = P.cache.page_shift >= 0 ? j >> P.cache.page_shift : j / P.cache.page_size;
-                            x[k] = pi < P.cache.max_pages ? __ldg(&P.cache.page_table[(size_t)g.b * P.cache.max_pages + pi]) : -1;
+                            x[k] = pi < P.cache.max_pages ? P.cache.page_table[(size_t)g.b * P.cache.max_pages + pi] : -1;
                         }
                     }
                 }

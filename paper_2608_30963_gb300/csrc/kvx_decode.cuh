@@ -18,13 +18,15 @@ struct CacheView {
     int H, d;
 };
 
+// Lengths and tables are read by plain loads: one through the read-only path might be moved up past the wait for the
+// kernel before, which may have written them.
 // Element offset of slot s of sequence b, head 0 (add head_stride * h), or -1 if its page is not in the pool.
 __device__ __forceinline__ long long cache_row(const CacheView& C, int b, int s)
 {
     if (!C.paged) return (long long)b * C.sb + (long long)s * C.st;
     const int pi = C.page_shift >= 0 ? s >> C.page_shift : s / C.page_size;
     const int in = s - pi * C.page_size;
-    const int page = pi < C.max_pages ? __ldg(&C.page_table[(size_t)b * C.max_pages + pi]) : -1;
+    const int page = pi < C.max_pages ? C.page_table[(size_t)b * C.max_pages + pi] : -1;
     if (page < 0 || page >= C.num_pages) return -1;
     return ((long long)page * C.page_size + in) * ((long long)C.H * C.d);
 }
@@ -110,7 +112,7 @@ cudaError_t launch_attend(const AttendParams& P, int dtype, int num_sms, cudaStr
 // Cached tokens of sequence b, clamped to the cache.
 __device__ __forceinline__ int seq_slots(const int* kv_len, int capacity, int b, unsigned* status)
 {
-    int n = __ldg(&kv_len[b]);
+    int n = kv_len[b];
     if (n < 0 || n > capacity) {
         set_status(status, KVX_DEV_SEQ_CLAMPED);
         n = n < 0 ? 0 : capacity;
@@ -127,10 +129,10 @@ struct Seq {
 __device__ __forceinline__ Seq load_seq(const AttendParams& P, int b)
 {
     Seq s;
-    s.t0 = min(max(__ldg(&P.seq_off[b]), 0), P.T);
-    s.n = min(max(__ldg(&P.seq_off[b + 1]), s.t0), P.T) - s.t0;
+    s.t0 = min(max(P.seq_off[b], 0), P.T);
+    s.n = min(max(P.seq_off[b + 1], s.t0), P.T) - s.t0;
     s.L = seq_slots(P.kv_len, P.cache.capacity, b, P.status);
-    s.pre = P.prefix_len ? min(max(__ldg(&P.prefix_len[b]), 0), s.L) : 0;
+    s.pre = P.prefix_len ? min(max(P.prefix_len[b], 0), s.L) : 0;
     return s;
 }
 // First slot that the window leaves the token in slot i, and whether it sees slot j < L.

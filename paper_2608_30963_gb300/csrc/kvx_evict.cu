@@ -193,7 +193,7 @@ __global__ void __launch_bounds__(kMoveThreads) move_kernel(const __grid_constan
         const int r = r0 + lane;
         long long from = -1, to = -1;
         if (r < P.keep) {
-            const int s = __ldg(&P.kept[unit * P.keep + r]);
+            const int s = P.kept[unit * P.keep + r];
             if (s >= 0) {
                 from = cache_row(P.src, b, s);
                 if (r < P.dst.capacity) to = cache_row(P.dst, b, r);
