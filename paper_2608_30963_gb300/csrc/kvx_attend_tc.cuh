@@ -121,6 +121,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
         mbar_init(bar(B::done), 1);
         mbar_init(bar(B::mlfull), 4);
         mbar_init(bar(B::mlempty), 4);
+        mbar_init(bar(B::added), 1);
         fence_mbar_init();
         *abort = 0;
         *beat = 0;
@@ -327,6 +328,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
 #pragma unroll
                         for (int k = 0; k < BN / 16; ++k) umma_bf16_ts(od, pd + BN / 2 + k * 8, vd + k * (2048 / 16), idesc_o, 1);
                     if (t == NT - 1) umma_commit(bar(B::empty + st));
+                    if (C::OS == 1) umma_commit(bar(B::added));   // phase: the unit
                     if (u >= U - C::OS) umma_commit(bar(B::ofull + wg));
                 }
                 __syncwarp();
@@ -446,7 +448,14 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
                     const float w = next == -INFINITY ? 1.0f : exp2_hw(m - next);
                     m = next;
                     l *= w;
-                    if (u >= C::OS) {                    // S(u) complete: so is the MMA that last added to O
+                    if (u >= C::OS) {
+                        // The product that last added to this O must be complete.  With two O it is the one of unit u - 2,
+                        // issued before S(u); with one it is that of unit u - 1, issued after S(u) (and the next waits for
+                        // this unit's P, so that the barrier is at most one phase ahead).
+                        if constexpr (C::OS == 1) {
+                            wait(B::added, (gu - 1) & 1);
+                            tc_fence_after();
+                        }
 #pragma unroll 1
                         for (int k = C::COLS ? wg * (D / 2) : 0; k < (C::COLS ? (wg + 1) * (D / 2) : D); k += 16) {
                             uint32_t o[16];

@@ -126,7 +126,7 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b)
 // Barriers (8 bytes each) in the control block.
 template <int STAGES> struct Bars {
     static constexpr int full = 0, empty = STAGES, sfull = 2 * STAGES, pfull = sfull + 2, ofull = pfull + 2, qfull = ofull + 2,
-                         qempty = qfull + 1, done = qempty + 1, mlfull = done + 1, mlempty = mlfull + 1;
+                         qempty = qfull + 1, done = qempty + 1, mlfull = done + 1, mlempty = mlfull + 1, added = mlempty + 1;
 };
 // Tensor copy of a box, completing on an mbarrier.
 __device__ __forceinline__ void tma_box3(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t mbar)
