@@ -433,9 +433,11 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
                 for (int k = 0; k < CW; k += 2) top[k >> 1 & 3] = max3(top[k >> 1 & 3], xf(k), xf(k + 1));
                 const float mine = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * c;
                 float next = fmaxf(m, mine);
-                // a row that grew by more than 2^8 (or had seen nothing) takes its new maximum, and its warp with it;
-                // with shared columns both warpgroups hold the same maximum and decide together
-                bool grown = __any_sync(0xffffffffu, next > m + 8.0f || (m == -INFINITY && next > m));
+                // A row that grew by more than 2^8 (or had seen nothing) takes its new maximum, and its warp with it;
+                // with shared columns both warpgroups hold the same maximum and decide together.  Only rows of the
+                // sequence have a say: the others hold the next one's queries, or what an earlier kernel left in
+                // shared memory, and the result's bits may depend on neither.
+                bool grown = __any_sync(0xffffffffu, real && (next > m + 8.0f || (m == -INFINITY && next > m)));
                 if constexpr (C::COLS) {
                     grown = group_any(4, 256, grown && ok);
                     if (grown) {

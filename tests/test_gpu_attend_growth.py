@@ -146,3 +146,32 @@ def test_single_tokens_whose_maxima_grow(name, window, d):
         out, lse = c.run()
         c.check(out, lse, two_terms)
         c.repeats(out, lse)
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("G,new,ctx", [(7, [301], [5003]), (6, [200, 90], [3000, 2100]), (7, [1], [20001]), (6, [1, 9], [9000, 4097])])
+def test_bits_do_not_depend_on_what_ran_before(G, new, ctx, d):
+    """Query heads that do not fill a row tile: its last rows hold what an earlier kernel left in shared memory."""
+    c = Call(2, G, d, ctx, new, 3.0, seed=d + 3)
+    full = Call(2, 8, d, ctx, [max(n, 200) if max(new) > 9 else n for n in new], 3.0, seed=d + 4)   # heads that fill it
+    base = None
+    for gain in (0.0, 1.0, 300.0, 1.0):
+        full.q.copy_((gain * torch.randn(full.q.shape, device="cuda")).bfloat16())
+        full.run()
+        out, lse = c.run()
+        base = base or (out, lse)
+        assert torch.equal(out, base[0]) and torch.equal(lse, base[1])
+    c.check(out, lse, one_term)
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("G,new,ctx", [(2, [70, 300], [3000, 3000]), (7, [30, 40, 50], [4000, 100, 2000]), (7, [1, 1, 1], [9000, 300, 4000])])
+def test_bits_do_not_depend_on_the_next_sequence(G, new, ctx, d):
+    """Row tiles that end inside a sequence's last tokens hold the next sequence's queries, too."""
+    c = Call(2, G, d, ctx, new, 3.0, seed=d + 5)
+    out, lse = c.run()
+    n = new[0]
+    for gain in (0.0, 300.0, float("inf"), float("nan")):
+        c.q[n:] = gain * torch.randn_like(c.q[n:])
+        o, z = c.run()
+        assert torch.equal(o[:n], out[:n]) and torch.equal(z[:n], lse[:n])
