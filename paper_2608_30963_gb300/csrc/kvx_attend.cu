@@ -302,6 +302,10 @@ __global__ void __launch_bounds__(kThreads) key_weight_simt_kernel(const __grid_
         }
         const int b = lo, j0 = (int)(ut - first[b]) * kBN;
         const Seq s = load_seq(P, b);
+        // rows of tokens before the first that sees the tile need not be formed
+        const int t_first = j0 < s.pre ? 0 : max(0, j0 - (s.L - s.n));
+        const int t_end = (j0 < s.pre || P.window == 0) ? s.n : (int)min((long long)s.n, (long long)j0 + kBN - 1 + P.window - (s.L - s.n));
+        if (t_end <= t_first) continue;         // no token sees the tile (the whole CTA): no copy is begun that nothing waits for
         __syncthreads();
         load_tile<D, kBN, kThreads>(sK, (const float*)P.ck, [&](int r) {
             const long long at = j0 + r < s.L ? cache_row(P.cache, b, j0 + r) : -1;
@@ -310,9 +314,6 @@ __global__ void __launch_bounds__(kThreads) key_weight_simt_kernel(const __grid_
         float w[kKN];
 #pragma unroll
         for (int j = 0; j < kKN; ++j) w[j] = 0.0f;
-        // rows of tokens before the first that sees the tile need not be formed
-        const int t_first = j0 < s.pre ? 0 : max(0, j0 - (s.L - s.n));
-        const int t_end = (j0 < s.pre || P.window == 0) ? s.n : (int)min((long long)s.n, (long long)j0 + kBN - 1 + P.window - (s.L - s.n));
         for (int r0 = t_first * P.G; r0 < t_end * P.G; r0 += BM) {
             const int rows = min(BM, t_end * P.G - r0);
             load_tile<D, BM, kThreads>(sQ, (const float*)P.q, [&](int r) {
@@ -343,7 +344,6 @@ __global__ void __launch_bounds__(kThreads) key_weight_simt_kernel(const __grid_
             }
             __syncthreads();
         }
-        async_wait<0>();
 #pragma unroll
         for (int j = 0; j < kKN; ++j) sW[tr * kBN + tc + kTC * j] = w[j];
         __syncthreads();
