@@ -488,7 +488,7 @@ typedef struct {
     int32_t keep;               /* slots a sequence may keep, >= 1; shorter sequences keep every slot */
     int32_t sinks, recent;      /* of them the first `sinks` and the last `recent` in any case; sinks + recent <= keep */
     int32_t* kept;              /* device int32[L][batch][H][keep]: the slots kept, ascending, then -1 */
-    int32_t* new_len;           /* device int32[batch]: min(kv_len, keep) */
+    int32_t* new_len;           /* device int32[batch]: min(kv_len, keep).  May be kv_len: in place */
     float* kept_weight;         /* device float[L][batch][H][kept_weight_stride] or NULL: the kept slots'
                                    weights, then zeros up to the stride */
     int64_t kept_weight_stride; /* >= keep */

@@ -634,7 +634,7 @@ class Decoder:
               num_pages: int = 0, dst_num_pages: int = 0, stream=None):
         """Cut the cache (lists of layers) down to `keep` slots per sequence, KV head and layer, by key_weight float32[L, B, H, S]:
         rows into dst_k / dst_v, their slots into kept int32[L, B, H, keep] (-1 past the end), the lengths
-        into new_len int32[B], the weights into kept_weight float32[L, B, H, >= keep]."""
+        into new_len int32[B] (kv_len itself: in place), the weights into kept_weight float32[L, B, H, >= keep]."""
         L, B, H = len(src_k), kv_len.shape[0], self._heads
         if not (tuple(key_weight.shape[:3]) == (L, B, H) and key_weight.is_contiguous() and key_weight.element_size() == 4):
             raise ValueError(f"key_weight must be contiguous float32 [{L}, {B}, {H}, slots]")

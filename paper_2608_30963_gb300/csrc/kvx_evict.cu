@@ -54,6 +54,14 @@ __device__ __forceinline__ int block_before(int v, int* tmp, int& all)
     return before;
 }
 
+// Cached tokens of sequence b, clamped to the cache and the weights.
+__device__ __forceinline__ int cached_slots(const EvictParams& P, int b, bool& clamped)
+{
+    const int n = P.kv_len[b], most = (int)min((long long)min(P.src.capacity, 1 << 30), P.weight_stride);
+    clamped = n < 0 || n > most;
+    return n < 0 ? 0 : min(n, most);
+}
+
 // cached: weights the CTA holds in shared memory; slots past them are read again in each pass.
 __global__ void __launch_bounds__(kSelThreads, 2) select_kernel(const __grid_constant__ EvictParams P, int cached)
 {
@@ -64,13 +72,9 @@ __global__ void __launch_bounds__(kSelThreads, 2) select_kernel(const __grid_con
     const int tid = threadIdx.x;
     const long long unit = blockIdx.x;
     const int b = (int)((unit / P.H) % P.batch);
-    int n = __ldg(&P.kv_len[b]);
-    const int most = (int)min((long long)min(P.src.capacity, 1 << 30), P.weight_stride);
-    if (n < 0 || n > most) {
-        if (tid == 0) set_status(P.status, KVX_DEV_SEQ_CLAMPED);
-        n = n < 0 ? 0 : most;
-    }
-    if (P.new_len && unit < (long long)P.batch * P.H && unit % P.H == 0 && tid == 0) P.new_len[b] = min(n, P.keep);
+    bool clamped;
+    const int n = cached_slots(P, b, clamped);
+    if (clamped && tid == 0) set_status(P.status, KVX_DEV_SEQ_CLAMPED);
     int* kept = P.kept + unit * P.keep;
     float* kw = P.kept_weight ? P.kept_weight + unit * P.kept_stride : nullptr;
     const float* w = P.weight + unit * P.weight_stride;
@@ -186,6 +190,12 @@ __global__ void __launch_bounds__(kMoveThreads) move_kernel(const __grid_constan
     const long long total = (long long)P.L * P.batch * P.H * groups;
     const long long warps = (long long)gridDim.x * (kMoveThreads / 32);
     grid_dependency_wait();
+    // the new lengths, now that every selection has read the old ones, whose place they may take
+    if (blockIdx.x == 0)
+        for (int b = threadIdx.x; b < P.batch; b += kMoveThreads) {
+            bool clamped;
+            P.new_len[b] = min(cached_slots(P, b, clamped), P.keep);
+        }
     for (long long g = ((long long)blockIdx.x * kMoveThreads + threadIdx.x) >> 5; g < total; g += warps) {
         const long long unit = g / groups;
         const int r0 = (int)(g - unit * groups) * 32;
