@@ -490,7 +490,7 @@ typedef struct {
     int32_t* kept;              /* device int32[L][batch][H][keep]: the slots kept, ascending, then -1 */
     int32_t* new_len;           /* device int32[batch]: min(kv_len, keep).  May be kv_len: in place */
     float* kept_weight;         /* device float[L][batch][H][kept_weight_stride] or NULL: the kept slots'
-                                   weights, then zeros up to the stride */
+                                   weights, then zeros up to the stride.  Must not overlap key_weight */
     int64_t kept_weight_stride; /* >= keep */
 } kvx_evict_plan;
 

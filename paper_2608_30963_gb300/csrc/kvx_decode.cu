@@ -106,6 +106,13 @@ kvx_status make_view(const kvx_decoder* d, const char* who, const char* what, co
     return KVX_OK;
 }
 
+// Do `units` rows of sa floats from a and of sb floats from b share an address?  (Without products, which could wrap.)
+bool rows_overlap(long long units, const float* a, long long sa, const float* b, long long sb)
+{
+    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+    return x <= y ? (y - x) / 4 / (uintptr_t)units < (uintptr_t)sa : (x - y) / 4 / (uintptr_t)units < (uintptr_t)sb;
+}
+
 kvx_status check_layer(const kvx_decoder* d, const char* who, int layer)
 {
     if (layer < 0 || layer >= d->desc.model.num_layers)
@@ -266,6 +273,8 @@ extern "C" KVX_API kvx_status kvx_evict(kvx_decoder* dec, const kvx_evict_plan* 
         return fail(KVX_ERR_INVALID_ARG, "evict: weight_stride must be >= 1 and kept_weight_stride >= keep");
     const long long units = (long long)L * plan->batch * dec->desc.model.num_kv_heads;
     if (units > 0x7fffffffll) return fail(KVX_ERR_UNSUPPORTED, "evict: too many (layer, sequence, head) units in one call");
+    if (plan->kept_weight && rows_overlap(units, plan->key_weight, plan->weight_stride, plan->kept_weight, plan->kept_weight_stride))
+        return fail(KVX_ERR_INVALID_ARG, "evict: kept_weight must not overlap key_weight");
     EvictParams P;
     memset(&P, 0, sizeof P);
     kvx_status st;

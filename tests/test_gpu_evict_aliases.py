@@ -49,3 +49,25 @@ def test_lengths_in_place(dtype):
     n = i32(c.lens)
     c.evict(n, n)
     c.check(n)
+
+
+def test_kept_weights_over_the_weights_are_refused():
+    """Units would overwrite weights that others have yet to read."""
+    c = Cut(L=2, B=2, H=2, S=400, keep=200)
+    n, new_len = i32(c.lens), i32([0] * 2)
+    own, w = c.kept_weight, c.w
+    flat = torch.zeros(2 * w.numel(), device="cuda")
+    inner = flat[w.numel() // 2:w.numel() // 2 + own.numel()].view(own.shape)
+    for key_weight, kept_weight in ((w, w), (flat[:w.numel()].view(w.shape), inner), (flat[w.numel() // 2:][:w.numel()].view(w.shape), flat[
+            w.numel() // 2 - 1:][:own.numel()].view(own.shape)), (flat[:w.numel()].view(w.shape), flat[w.numel() - 1:][:own.numel()].view(own.shape))):
+        c.w, c.kept_weight = key_weight, kept_weight
+        with pytest.raises(kvx.KvxError) as e:
+            c.evict(n, new_len)
+        assert e.value.status == kvx.KVX_ERR_INVALID_ARG and "overlap" in kvx.kvx_last_error()
+    # one behind the other, either way round
+    both = torch.zeros(w.numel() + own.numel(), device="cuda")
+    for first in (0, own.numel()):
+        c.w = both[first:first + w.numel()].view(w.shape).copy_(w)
+        c.kept_weight = (both[w.numel():] if first == 0 else both[:own.numel()]).view(own.shape)
+        c.evict(n, new_len)
+        c.check(new_len)
