@@ -247,7 +247,8 @@ extern "C" KVX_API kvx_status kvx_attend(kvx_decoder* dec, const kvx_new_tokens*
     P.out = out->ptr; P.o_t = out->stride_t; P.o_h = out->stride_h;
     P.ck = cache->k[layer]; P.cv = cache->v[layer];
     P.scale = (float)dec->desc.scale; P.cap = (float)dec->desc.score_cap;
-    P.window = opts->window; P.prefix_len = opts->prefix_len;
+    // Slots lie in [-2^30, 2^30), those seen from zero on: a window of 2^30 hides none, and slot - window does not wrap.
+    P.window = opts->window < 1 << 30 ? opts->window : 1 << 30; P.prefix_len = opts->prefix_len;
     P.lse = opts->lse; P.key_weight = opts->key_weight; P.weight_stride = opts->weight_stride;
     P.status = dec->status;
     P.part_o = dec->part_o; P.part_ml = dec->part_ml; P.split = dec->split;
