@@ -485,7 +485,7 @@ typedef struct {
     const int32_t* kv_len;      /* device int32[batch]: cached tokens of each sequence */
     const float* key_weight;    /* device float[L][batch][H][weight_stride]: weight of each slot */
     int64_t weight_stride;      /* at least every kv_len (longer lengths are clamped and flagged) */
-    int32_t keep;               /* slots a sequence may keep, >= 1; shorter sequences keep every slot */
+    int32_t keep;               /* slots a sequence may keep, 1 .. 2^30; shorter sequences keep every slot */
     int32_t sinks, recent;      /* of them the first `sinks` and the last `recent` in any case; sinks + recent <= keep */
     int32_t* kept;              /* device int32[L][batch][H][keep]: the slots kept, ascending, then -1 */
     int32_t* new_len;           /* device int32[batch]: min(kv_len, keep).  May be kv_len: in place */

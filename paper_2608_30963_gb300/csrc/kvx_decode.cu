@@ -266,8 +266,9 @@ extern "C" KVX_API kvx_status kvx_evict(kvx_decoder* dec, const kvx_evict_plan* 
     const int L = plan->num_layers;
     if (plan->batch < 1 || L < 1 || L > KVX_MAX_TARGET_LAYERS || L > dec->desc.model.num_layers)
         return fail(KVX_ERR_INVALID_ARG, "evict: batch must be >= 1 and num_layers in [1, %d], at most the model's", KVX_MAX_TARGET_LAYERS);
-    if (plan->keep < 1 || plan->sinks < 0 || plan->recent < 0 || (long long)plan->sinks + plan->recent > plan->keep)
-        return fail(KVX_ERR_INVALID_ARG, "evict: need keep >= 1, sinks and recent >= 0 and sinks + recent <= keep");
+    // (a cache holds at most 2^30 slots; the kernels step past keep by a block's threads)
+    if (plan->keep < 1 || plan->keep > 1 << 30 || plan->sinks < 0 || plan->recent < 0 || (long long)plan->sinks + plan->recent > plan->keep)
+        return fail(KVX_ERR_INVALID_ARG, "evict: need keep in [1, 2^30], sinks and recent >= 0 and sinks + recent <= keep");
     if (!plan->kv_len || !plan->key_weight || !plan->kept || !plan->new_len)
         return fail(KVX_ERR_INVALID_ARG, "evict: kv_len, key_weight, kept and new_len must be set");
     if (plan->weight_stride < 1 || (plan->kept_weight && plan->kept_weight_stride < plan->keep))

@@ -25,3 +25,19 @@ def test_windows_wider_than_any_cache(d, new, kv_len, prefix, window, dtype):
     check(p, w.cpu(), ew, tw + 1e-30, "key_weight")
     base, _ = p.attend(0, prefix)
     assert torch.equal(out, base)
+
+
+@pytest.mark.parametrize("keep", [2 ** 31 - 1, 2 ** 31 - 500, 2 ** 30 + 1, 0, -1])
+def test_keeps_out_of_range_are_refused(keep):
+    """On the host, before anything is launched: no array of such a size is needed."""
+    p = Problem(1, 1, 64, [40], [0], "bf16", 0, seed=62)
+    k, v = p.cache(p.K), p.cache(p.V)
+    n, w, kept = i32([40]), torch.zeros((1, 1, 1, 40), device="cuda"), torch.zeros(64, dtype=torch.int32, device="cuda")
+    new_len = i32([-7])
+    plan = kvx.kvx_evict_plan(1, 1, n.data_ptr(), w.data_ptr(), 40, keep, 0, 0, kept.data_ptr(), new_len.data_ptr(), None, 0)
+    ks, vs = (ctypes.c_void_p * 1)(k.data_ptr()), (ctypes.c_void_p * 1)(v.data_ptr())
+    cache = kvx.kvx_dst_kv(ctypes.cast(ks, ctypes.POINTER(ctypes.c_void_p)), ctypes.cast(vs, ctypes.POINTER(ctypes.c_void_p)), 0, 40, *k.stride()[:3], None, 0, 0, 0)
+    at = ctypes.byref
+    assert kvx.lib().kvx_evict(p.dec.handle, at(plan), at(cache), at(cache), None) == kvx.KVX_ERR_INVALID_ARG
+    assert "keep" in kvx.kvx_last_error()
+    assert p.dec.device_status() == 0 and new_len.tolist() == [-7]
