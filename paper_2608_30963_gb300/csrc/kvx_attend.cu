@@ -415,8 +415,10 @@ cudaError_t launch_attend(const AttendParams& call, int dtype, int num_sms, cuda
     // Weight sums add up the scores that the attention leaves, where they fit the workspace and cost less than to be formed
     // again: always in fp32 (8 bytes of traffic against 2 d operations on the CUDA cores: 512 tokens of 12 heads over
     // 512 slots 209 us, 48 so), for few rows in bf16 (16 a sequence and KV head: less than a slot's K).
-    P.scores_stride = (P.weight_stride + 63) / 64 * 64;
-    const bool keep = P.key_weight && (!bf16 || (long long)P.T * P.G <= 16ll * P.batch) && (long long)P.T * P.Hq * P.scores_stride <= kAttendScores;
+    // (weight_stride is the caller's, up to 2^63: divided by, not multiplied)
+    const long long most = kAttendScores / ((long long)P.T * P.Hq) / 64 * 64;   // slots a row of the workspace may have
+    const bool keep = P.key_weight && (!bf16 || (long long)P.T * P.G <= 16ll * P.batch) && P.weight_stride <= most;
+    P.scores_stride = keep ? (P.weight_stride + 63) / 64 * 64 : 0;
     if (!keep) P.scores = nullptr;
     const bool cap = P.cap > 0.0f;
     cudaError_t e = bf16 ? launch_attend_tc(P, num_sms, stream) : cap ? attend_fp32<true>(P, num_sms, stream) : attend_fp32<false>(P, num_sms, stream);

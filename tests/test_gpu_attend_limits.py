@@ -41,3 +41,27 @@ def test_keeps_out_of_range_are_refused(keep):
     assert kvx.lib().kvx_evict(p.dec.handle, at(plan), at(cache), at(cache), None) == kvx.KVX_ERR_INVALID_ARG
     assert "keep" in kvx.kvx_last_error()
     assert p.dec.device_status() == 0 and new_len.tolist() == [-7]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("stride", [2 ** 62, 2 ** 63 - 1, 2 ** 40])
+def test_weight_strides_of_any_size(dtype, stride):
+    """One sequence of one KV head has one row of sums, whose stride nothing is addressed by: products of it must not wrap."""
+    p = Problem(1, 4, 64, [300], [1], dtype, 0, seed=63)
+    q, k, v = p.q.cuda(), p.cache(p.K), p.cache(p.V)
+    out, lse, w = torch.zeros_like(q), torch.zeros((1, 4), device="cuda"), torch.zeros(p.S + 64, device="cuda")
+    off, n = i32(p.off), i32(p.L)
+    ks, vs = (ctypes.c_void_p * 1)(k.data_ptr()), (ctypes.c_void_p * 1)(v.data_ptr())
+    cache = kvx.kvx_dst_kv(ctypes.cast(ks, ctypes.POINTER(ctypes.c_void_p)), ctypes.cast(vs, ctypes.POINTER(ctypes.c_void_p)), 0, p.S,
+                           *k.stride()[:3], None, 0, 0, 0)
+    tok = kvx.kvx_new_tokens(1, 1, off.data_ptr(), n.data_ptr(), None)
+    opts = kvx.kvx_attend_opts(0, None, lse.data_ptr(), w.data_ptr(), stride)
+    rows = [kvx.kvx_rows(t.data_ptr(), *t.stride()[:2]) for t in (q, out)]
+    at = ctypes.byref
+    assert kvx.lib().kvx_attend(p.dec.handle, at(tok), at(rows[0]), at(cache), 0, at(opts), at(rows[1]), None) == kvx.KVX_OK
+    assert p.dec.device_status() == 0
+    eo, el, ew, to, tl, tw = p.exact()
+    check(p, out.cpu(), eo, to, "out")
+    check_lse(lse.cpu(), el, tl)
+    check(p, w[:p.S].cpu(), ew[0, 0], tw[0, 0] + 1e-30, "key_weight")
+    assert not w[p.S:].any()
