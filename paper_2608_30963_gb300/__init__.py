@@ -554,7 +554,9 @@ class Decoder:
         self.desc = kvx_decoder_desc(model_geom(geom), int(num_q_heads), dtype, max_position, float(scale), float(score_cap))
         self.geom = geom
         self._heads, self._dim, self._q_heads = self.desc.model.num_kv_heads, self.desc.model.head_dim, int(num_q_heads)
-        self._size = 2 if dtype == KVX_BF16 else 4
+        import torch
+        self._type = torch.bfloat16 if dtype == KVX_BF16 else torch.float32
+        self._f32, self._i32 = torch.float32, torch.int32
         global _current_raw_stream
         _current_raw_stream = _current_raw_stream or _find_raw_stream()
         h = VP()
@@ -562,27 +564,27 @@ class Decoder:
         self.handle = h.value
 
     def _fits(self, t, tokens: int, heads: int):
-        """Rows of one token count, of this decoder's heads, width and element size."""
-        if t.shape != (tokens, heads, self._dim) or t.element_size() != self._size:
-            raise ValueError(f"rows must be [{tokens}, {heads}, {self._dim}] of {self._size}-byte elements, got {tuple(t.shape)}")
+        """Rows of one token count, of this decoder's heads, width and type."""
+        if t.shape != (tokens, heads, self._dim) or t.dtype != self._type:
+            raise ValueError(f"rows must be [{tokens}, {heads}, {self._dim}] of {self._type}, got {tuple(t.shape)} of {t.dtype}")
 
     def _layer(self, k, v, batch: int, page_table, page_size: int, num_pages: int):
         """One layer of a cache as kvx_dst_kv (and what has to live as long), checked: this decoder's heads, width and
-        element size, room for `batch` sequences, K and V alike."""
+        type, room for `batch` sequences, K and V alike."""
         ks, st, H, d = k.shape, k.stride(), self._heads, self._dim
         ptrs = array.array("Q", (k.data_ptr(), v.data_ptr()))
         at = ptrs.buffer_info()[0]
-        alike = v.shape == ks and v.stride() == st and k.element_size() == v.element_size() == self._size
+        alike = v.shape == ks and v.stride() == st and k.dtype == v.dtype == self._type
         if page_table is None:
             if alike and len(ks) == 4 and ks[0] >= batch and ks[1] == H and ks[3] == d and st[3] == 1:
                 return _PACK_CACHE(at, at + 8, 0, ks[2], st[0], st[1], st[2], 0, 0, 0, 0), ptrs
         else:
             ts = page_table.shape
             if page_size < 1 or (alike and ks[1:] == (page_size, H, d) and k.is_contiguous() and ts[0] >= batch
-                                 and page_table.element_size() == 4 and page_table.is_contiguous()):   # (the library refuses page sizes below 1)
+                                 and page_table.dtype == self._i32 and page_table.is_contiguous()):   # (the library refuses page sizes below 1)
                 return _PACK_CACHE(at, at + 8, 1, 0, 0, 0, 0, page_table.data_ptr(), ts[1], page_size, num_pages or ks[0]), ptrs
         raise ValueError(f"caches must be alike, [B, {H}, S, {d}] or pools [pages, {page_size}, {H}, {d}] with an int32 page table, of "
-                         f"{self._size}-byte elements, got {tuple(ks)} and {tuple(v.shape)}")
+                         f"{self._type}, got {tuple(ks)} and {tuple(v.shape)} of {k.dtype} and {v.dtype}")
 
     def append(self, q, k, v, seq_off, kv_len, cache_k, cache_v, q_out, *, pos=None, page_table=None, page_size: int = 16,
                num_pages: int = 0, stream=None):
@@ -595,8 +597,8 @@ class Decoder:
         self._fits(v, T, H)
         self._fits(q_out, T, Hq)
         B = seq_off.shape[0] - 1
-        if kv_len.shape[0] < B or seq_off.element_size() != 4 or kv_len.element_size() != 4 or \
-                (pos is not None and (pos.shape[0] != T or pos.element_size() != 4)):
+        if kv_len.shape[0] < B or seq_off.dtype != self._i32 or kv_len.dtype != self._i32 or \
+                (pos is not None and (pos.shape[0] != T or pos.dtype != self._i32)):
             raise ValueError("seq_off [B + 1], kv_len [B] and pos [tokens] must be int32")
         tok = _PACK_TOKENS(B, T, seq_off.data_ptr(), kv_len.data_ptr(), 0 if pos is None else pos.data_ptr())
         cache, _keep = self._layer(cache_k, cache_v, B, page_table, page_size, num_pages)
@@ -613,13 +615,13 @@ class Decoder:
         T, Hq, B = q.shape[0], self._q_heads, seq_off.shape[0] - 1
         self._fits(q, T, Hq)
         self._fits(out, T, Hq)
-        if lse is not None and not (lse.shape == (T, Hq) and lse.is_contiguous() and lse.element_size() == 4):
+        if lse is not None and not (lse.shape == (T, Hq) and lse.is_contiguous() and lse.dtype == self._f32):
             raise ValueError("lse must be contiguous float32 [tokens, query heads]")
         if key_weight is not None and not (key_weight.shape[:2] == (B, self._heads) and key_weight.is_contiguous()
-                                           and key_weight.element_size() == 4):
+                                           and key_weight.dtype == self._f32):
             raise ValueError("key_weight must be contiguous float32 [sequences, KV heads, slots]")
-        if kv_len.shape[0] < B or seq_off.element_size() != 4 or kv_len.element_size() != 4 or \
-                (prefix_len is not None and (prefix_len.shape[0] < B or prefix_len.element_size() != 4)):
+        if kv_len.shape[0] < B or seq_off.dtype != self._i32 or kv_len.dtype != self._i32 or \
+                (prefix_len is not None and (prefix_len.shape[0] < B or prefix_len.dtype != self._i32)):
             raise ValueError("seq_off [B + 1], kv_len [B] and prefix_len [B] must be int32")
         tok = _PACK_TOKENS(B, T, seq_off.data_ptr(), kv_len.data_ptr(), 0)
         opts = _PACK_OPTS(window, 0 if prefix_len is None else prefix_len.data_ptr(), 0 if lse is None else lse.data_ptr(),
@@ -636,16 +638,16 @@ class Decoder:
         rows into dst_k / dst_v, their slots into kept int32[L, B, H, keep] (-1 past the end), the lengths
         into new_len int32[B] (kv_len itself: in place), the weights into kept_weight float32[L, B, H, >= keep]."""
         L, B, H = len(src_k), kv_len.shape[0], self._heads
-        if not (tuple(key_weight.shape[:3]) == (L, B, H) and key_weight.is_contiguous() and key_weight.element_size() == 4):
+        if not (tuple(key_weight.shape[:3]) == (L, B, H) and key_weight.is_contiguous() and key_weight.dtype == self._f32):
             raise ValueError(f"key_weight must be contiguous float32 [{L}, {B}, {H}, slots]")
-        if not (tuple(kept.shape) == (L, B, H, keep) and kept.is_contiguous() and kept.element_size() == 4):
+        if not (tuple(kept.shape) == (L, B, H, keep) and kept.is_contiguous() and kept.dtype == self._i32):
             raise ValueError(f"kept must be contiguous int32 [{L}, {B}, {H}, {keep}]")
         if kept_weight is not None and not (tuple(kept_weight.shape[:3]) == (L, B, H) and kept_weight.is_contiguous()
-                                            and kept_weight.element_size() == 4):
+                                            and kept_weight.dtype == self._f32):
             raise ValueError(f"kept_weight must be contiguous float32 [{L}, {B}, {H}, slots]")
         if not len(src_v) == len(dst_k) == len(dst_v) == L:
             raise ValueError("src_k, src_v, dst_k and dst_v must have as many layers as one another")
-        if kv_len.element_size() != 4 or new_len.element_size() != 4 or new_len.shape[0] != B:
+        if kv_len.dtype != self._i32 or new_len.dtype != self._i32 or new_len.shape[0] != B:
             raise ValueError("kv_len and new_len must be int32 [B]")
         self._layer(src_k[0], src_v[0], B, page_table, page_size, num_pages)
         self._layer(dst_k[0], dst_v[0], B, dst_page_table, page_size, dst_num_pages)
