@@ -568,6 +568,10 @@ class Decoder:
         if t.shape != (tokens, heads, self._dim) or t.dtype != self._type:
             raise ValueError(f"rows must be [{tokens}, {heads}, {self._dim}] of {self._type}, got {tuple(t.shape)} of {t.dtype}")
 
+    def _index(self, t, least: int) -> bool:
+        """Is t an int32 array of so many elements or more, one behind the other?"""
+        return t.dtype == self._i32 and t.shape[0] >= least and t.is_contiguous()
+
     def _layer(self, k, v, batch: int, page_table, page_size: int, num_pages: int):
         """One layer of a cache as kvx_dst_kv (and what has to live as long), checked: this decoder's heads, width and
         type, room for `batch` sequences, K and V alike."""
@@ -597,9 +601,8 @@ class Decoder:
         self._fits(v, T, H)
         self._fits(q_out, T, Hq)
         B = seq_off.shape[0] - 1
-        if kv_len.shape[0] < B or seq_off.dtype != self._i32 or kv_len.dtype != self._i32 or \
-                (pos is not None and (pos.shape[0] != T or pos.dtype != self._i32)):
-            raise ValueError("seq_off [B + 1], kv_len [B] and pos [tokens] must be int32")
+        if not (self._index(seq_off, 1) and self._index(kv_len, B) and (pos is None or (self._index(pos, T) and pos.shape[0] == T))):
+            raise ValueError("seq_off [B + 1], kv_len [B] and pos [tokens] must be contiguous int32")
         tok = _PACK_TOKENS(B, T, seq_off.data_ptr(), kv_len.data_ptr(), 0 if pos is None else pos.data_ptr())
         cache, _keep = self._layer(cache_k, cache_v, B, page_table, page_size, num_pages)
         st = lib().kvx_append(self.handle, tok, _rows(q), _rows(k), _rows(v), _rows(q_out), cache, 0, _raw_stream(stream))
@@ -620,9 +623,8 @@ class Decoder:
         if key_weight is not None and not (key_weight.shape[:2] == (B, self._heads) and key_weight.is_contiguous()
                                            and key_weight.dtype == self._f32):
             raise ValueError("key_weight must be contiguous float32 [sequences, KV heads, slots]")
-        if kv_len.shape[0] < B or seq_off.dtype != self._i32 or kv_len.dtype != self._i32 or \
-                (prefix_len is not None and (prefix_len.shape[0] < B or prefix_len.dtype != self._i32)):
-            raise ValueError("seq_off [B + 1], kv_len [B] and prefix_len [B] must be int32")
+        if not (self._index(seq_off, 1) and self._index(kv_len, B) and (prefix_len is None or self._index(prefix_len, B))):
+            raise ValueError("seq_off [B + 1], kv_len [B] and prefix_len [B] must be contiguous int32")
         tok = _PACK_TOKENS(B, T, seq_off.data_ptr(), kv_len.data_ptr(), 0)
         opts = _PACK_OPTS(window, 0 if prefix_len is None else prefix_len.data_ptr(), 0 if lse is None else lse.data_ptr(),
                           0 if key_weight is None else key_weight.data_ptr(), 0 if key_weight is None else key_weight.shape[2])
@@ -647,8 +649,8 @@ class Decoder:
             raise ValueError(f"kept_weight must be contiguous float32 [{L}, {B}, {H}, slots]")
         if not len(src_v) == len(dst_k) == len(dst_v) == L:
             raise ValueError("src_k, src_v, dst_k and dst_v must have as many layers as one another")
-        if kv_len.dtype != self._i32 or new_len.dtype != self._i32 or new_len.shape[0] != B:
-            raise ValueError("kv_len and new_len must be int32 [B]")
+        if not (self._index(kv_len, B) and self._index(new_len, B) and new_len.shape[0] == B):
+            raise ValueError("kv_len and new_len must be contiguous int32 [B]")
         self._layer(src_k[0], src_v[0], B, page_table, page_size, num_pages)
         self._layer(dst_k[0], dst_v[0], B, dst_page_table, page_size, dst_num_pages)
         plan = _PACK_PLAN(B, L, kv_len.data_ptr(), key_weight.data_ptr(), key_weight.shape[3], keep, sinks, recent, kept.data_ptr(),

@@ -60,3 +60,22 @@ def test_types(dtype, ps):
             elif isinstance(t, list):
                 x.refused(call, name, [y.view(other) for y in t])
     x.right()
+
+
+@pytest.mark.parametrize("ps", [0, 16])
+def test_strides(ps):
+    """Lengths, offsets, positions, tables and sums are read as arrays without gaps: a view with gaps is another array."""
+    x = Args("bf16", ps)
+    x.right()
+    for call, (_, args) in enumerate(x.calls()):
+        for name, t in args.items():
+            if isinstance(t, torch.Tensor) and t.dtype != torch.bfloat16:
+                gaps = torch.zeros((*t.shape[:-1], 2 * t.shape[-1]), dtype=t.dtype, device="cuda")[..., ::2]
+                gaps.copy_(t)
+                x.refused(call, name, gaps)
+    # one sequence, one element: nothing can have a gap
+    one = Problem(2, 4, 128, [60], [1], "bf16", ps, seed=72)
+    out = torch.zeros_like(one.q, device="cuda")
+    length = torch.tensor([one.L[0], -5], dtype=torch.int32, device="cuda")[::2]
+    one.dec.attend(one.q.cuda(), i32(one.off), length, one.cache(one.K), one.cache(one.V), out, **one.paged())
+    assert torch.equal(out.cpu(), one.attend()[0])
