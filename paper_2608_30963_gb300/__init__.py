@@ -653,6 +653,13 @@ class Decoder:
             raise ValueError("kv_len and new_len must be contiguous int32 [B]")
         self._layer(src_k[0], src_v[0], B, page_table, page_size, num_pages)
         self._layer(dst_k[0], dst_v[0], B, dst_page_table, page_size, dst_num_pages)
+        for first, rest in ((src_k[0], (src_k, src_v)), (dst_k[0], (dst_k, dst_v))):   # one shape and strides serve all layers
+            shape, stride, plain = first.shape, first.stride(), first.is_contiguous()
+            for tensors in rest:
+                for t in tensors:
+                    if t.shape != shape or t.dtype != self._type or not (t.is_contiguous() if plain else t.stride() == stride):
+                        raise ValueError(f"the layers of a cache must be alike, of {self._type}: {tuple(shape)} with strides {stride}, got "
+                                         f"{tuple(t.shape)} with strides {t.stride()} of {t.dtype}")
         plan = _PACK_PLAN(B, L, kv_len.data_ptr(), key_weight.data_ptr(), key_weight.shape[3], keep, sinks, recent, kept.data_ptr(),
                           new_len.data_ptr(), _ptr(kept_weight), 0 if kept_weight is None else kept_weight.shape[3])
         src, _keep_src = _cache(src_k, src_v, page_table, page_size, num_pages)

@@ -79,3 +79,22 @@ def test_strides(ps):
     length = torch.tensor([one.L[0], -5], dtype=torch.int32, device="cuda")[::2]
     one.dec.attend(one.q.cuda(), i32(one.off), length, one.cache(one.K), one.cache(one.V), out, **one.paged())
     assert torch.equal(out.cpu(), one.attend()[0])
+
+
+@pytest.mark.parametrize("ps", [0, 16])
+@pytest.mark.parametrize("name", ["src_k", "src_v", "dst_k", "dst_v"])
+def test_every_layer_of_an_eviction(name, ps):
+    """A later layer that is smaller, wider apart or of another type than the first."""
+    x = Args("bf16", ps)
+    x.right()
+    t = x.c[name][1]
+    wide = torch.empty((*t.shape[:-1], 2 * t.shape[-1]), dtype=t.dtype, device="cuda")[..., :t.shape[-1]]
+    for bad in (t[:-1], t[:, :, :-1], wide, t.view(torch.float16), t.float(), t.transpose(1, 2), t[:, :, :, :64]):
+        x.refused(EVICT, name, [x.c[name][0], bad])
+        x.refused(EVICT, name, [bad, x.c[name][1]])
+    x.refused(EVICT, name, x.c[name][:1])
+    x.right()
+    if not ps:      # layers that are all alike views of something wider are taken
+        x.c["src_k"] = [torch.cat([t, t], -1)[..., :128] for t in x.c["src_k"]]
+        x.c["src_v"] = [torch.cat([t, t], -1)[..., :128] for t in x.c["src_v"]]
+        x.right()
