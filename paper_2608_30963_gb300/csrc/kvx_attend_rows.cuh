@@ -46,7 +46,8 @@ __device__ __forceinline__ RowId row_id(const AttendParams& P, const Seq& s, int
 
 // The output of one row taken again slot by slot, by one warp, lane holding channels [lane * C, lane * C + C).
 // The tiled sums multiply hidden slots' rows by a weight of zero; where such a row holds an infinity
-// or a NaN that gives a NaN, so a row that did not come out finite is summed over the slots it sees only.
+// or a NaN that gives a NaN, so a row that did not come out finite is summed over the slots it sees only.  (Not where
+// its sum of weights is NaN: hidden scores never enter that, so a score that is seen is not finite, and every output is NaN.)
 template <typename T, int D>
 __device__ __noinline__ void resum_row(const AttendParams& P, const Seq& s, int b, int h, int row, float lse2,
                                        float (&o)[D / 32], volatile int* beat = nullptr)
@@ -104,7 +105,7 @@ __device__ __forceinline__ void finish_row(const AttendParams& P, int b, int h, 
         if (l == 0.0f) {
 #pragma unroll
             for (int c = 0; c < C; ++c) o[c] = 0.0f;
-        } else {
+        } else if (l == l) {
             resum_row<T, D>(P, load_seq(P, b), b, h, row, lse2, o);
         }
     }

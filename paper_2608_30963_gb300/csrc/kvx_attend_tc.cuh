@@ -612,7 +612,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
             }
             if (whole) {
                 if (real && P.lse && !(C::COLS && wg)) P.lse[(long long)(g.s.t0 + id.t) * P.Hq + id.head] = lse2 * kLn2;
-                for (uint32_t bad = __ballot_sync(0xffffffffu, real && !fine); bad; bad &= bad - 1) {
+                for (uint32_t bad = __ballot_sync(0xffffffffu, real && !fine && l == l); bad; bad &= bad - 1) {
                     const int who = __ffs(bad) - 1;
                     float o[D / 32];
                     resum_row<__nv_bfloat16, D>(P, g.s, g.b, g.h, row - lane + who, __shfl_sync(0xffffffffu, lse2, who), o, beat);
