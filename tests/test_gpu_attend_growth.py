@@ -62,8 +62,9 @@ class Call:
         return out, lse
 
     def check(self, out, lse, weight_eps):
-        """out and lse within the bounds; weight_eps(slots seen by each token): the weights' rounding."""
-        t0 = 0
+        """out and lse within the bounds; weight_eps(slots seen by each token): the weights' rounding.  Returns by how much the definition
+        with its weights rounded to one bf16 term would be beyond the bound (a mistake planted here, in 64 bits)."""
+        t0, planted = 0, 0.0
         for b, (n, L) in enumerate(zip(self.new, self.L)):
             i = torch.arange(L - n, L, device="cuda")[:, None]
             j = torch.arange(L, device="cuda")
@@ -83,9 +84,12 @@ class Call:
                 tol = 1.05 * rel * mass + 1.01 * 2.0 ** -8 * want.abs() + 1e-30
                 err = (out[t0:t0 + n, head].double() - want).abs()
                 assert bool((err <= tol).all()), f"out, sequence {b}, head {head}: {float((err / tol).max()):.3g} times the bound"
+                rounded = torch.exp(x - x.amax(1, keepdim=True)).bfloat16().double() * torch.exp(x.amax(1, keepdim=True) - z)
+                planted = max(planted, float(((rounded @ v - want).abs() / tol).max()))
                 lerr, ltol = (lse[t0:t0 + n, head].double() - z[:, 0]).abs(), e[:, 0] + 2.0 ** -20 + 2.0 ** -22 * z[:, 0].abs()
                 assert bool((lerr <= ltol).all()), f"lse, sequence {b}, head {head}"
             t0 += n
+        return planted
 
     def repeats(self, out, lse, times=4):
         for _ in range(times):
