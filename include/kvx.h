@@ -405,8 +405,9 @@ typedef struct {
                                    head g reads KV head g / (num_q_heads / num_kv_heads) */
     int32_t dtype;              /* kvx_dtype of queries, keys, values, caches and outputs */
     int32_t max_position;       /* as in kvx_translator_desc */
-    double  scale;              /* factor of q.k; 0 = 1 / sqrt(head_dim); else finite and > 0 */
-    double  score_cap;          /* c > 0: a scaled score s becomes c * tanh(s / c); 0 = no cap */
+    double  scale;              /* factor of q.k; 0 = 1 / sqrt(head_dim); else > 0 */
+    double  score_cap;          /* c > 0: a scaled score s becomes c * tanh(s / c); 0 = no cap.  (scale, c, 1 / c and
+                                   scale / c: normal numbers in 32 bits, which the kernels hold them in) */
 } kvx_decoder_desc;
 
 /* Checks the description and allocates what the calls below need on the current device: rotation

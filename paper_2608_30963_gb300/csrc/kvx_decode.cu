@@ -1,5 +1,6 @@
 // kvx_decode.cu -- host side of the calls that go on from a cache: kvx_decoder_*, kvx_append,
 // kvx_attend and kvx_evict (argument checks, workspace, launches).
+#include <float.h>
 #include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
@@ -143,10 +144,15 @@ extern "C" KVX_API kvx_status kvx_decoder_create(const kvx_decoder_desc* desc, k
     if (max_pos < 1 || max_pos > 1 << 30) return fail(KVX_ERR_INVALID_ARG, "decoder_create: max_position must be in [1, 1<<30]");
     if (!(desc->scale >= 0.0) || !isfinite(desc->scale) || !(desc->score_cap >= 0.0) || !isfinite(desc->score_cap))
         return fail(KVX_ERR_INVALID_ARG, "decoder_create: scale and score_cap must be finite and not negative");
+    // the kernels hold them, and what a scaled score is divided by, in 32 bits
+    const double scale = desc->scale > 0.0 ? desc->scale : 1.0 / sqrt((double)g.head_dim);
+    auto normal = [](double x) { return x >= FLT_MIN && x <= FLT_MAX; };
+    if (!normal(scale) || (desc->score_cap > 0.0 && (!normal(desc->score_cap) || !normal(1.0 / desc->score_cap) || !normal(scale / desc->score_cap))))
+        return fail(KVX_ERR_INVALID_ARG, "decoder_create: scale, score_cap, 1 / score_cap and scale / score_cap must be normal numbers in 32 bits");
     kvx_decoder* d = new (std::nothrow) kvx_decoder();
     if (!d) return fail(KVX_ERR_OOM, "decoder_create: host allocation");
     d->desc = *desc;
-    if (d->desc.scale == 0.0) d->desc.scale = 1.0 / sqrt((double)g.head_dim);
+    d->desc.scale = scale;
     d->max_position = max_pos;
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess ||
