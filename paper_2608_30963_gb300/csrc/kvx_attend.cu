@@ -5,8 +5,10 @@
 // in one pass over the slots j with the running maximum m_i and sum (kept in units of log2).
 //
 // Bound by the fp32 FMA pipe where rows are many: a thread takes 4 rows by 4 slots (packed products, 8 16-byte reads of
-// shared memory for 32 of them), 64 rows a CTA of 128 threads; 512 tokens of 12 heads of 128 over 512 slots run at 31
-// TFLOP/s, half of what the masked tiles leave.  Few rows (16 a tile): by reading K and V, and by the fixed cost of a call.
+// shared memory for 32 of them), 64 rows a CTA of 128 threads; 512 tokens of 12 heads of 128 over 1024 slots take 92 us, 26
+// TFLOP/s of what the masks leave.  Few rows (16 a tile): by the copies of K and V, whose next tile is only begun when this
+// one's is used up: a token of each of eight sequences over up to 16384 slots, 209 MB, 123 us, 1.7 TB/s; short ones by the
+// fixed cost of a call.
 #include <atomic>
 
 #include "kvx_attend_rows.cuh"
@@ -390,7 +392,8 @@ template <int D, bool CAP> cudaError_t run_weight_simt(const AttendParams& P, in
 
 template <int D, bool CAP> cudaError_t run_fp32(const AttendParams& P, int num_sms, cudaStream_t stream)
 {
-    // few rows for each sequence and head: 16-row tiles waste less of the arithmetic
+    // Few rows for each sequence and head: 16-row tiles waste less of the arithmetic (eight sequences of 4096 slots, heads of
+    // 128: 12 rows 79.5 us in tiles of 16 and 89.8 of 64, 18 rows 96.9 and 90.8; heads of 256: 93.9 and 99.0, 162 and 102)
     const bool few = (long long)P.T * P.G <= 16ll * P.batch;
     return few ? run_simt<D, 16, CAP>(P, num_sms, stream) : run_simt<D, D == 256 ? 32 : 64, CAP>(P, num_sms, stream);
 }
@@ -414,7 +417,8 @@ cudaError_t launch_attend(const AttendParams& call, int dtype, int num_sms, cuda
     const bool bf16 = dtype == KVX_BF16;
     // Weight sums add up the scores that the attention leaves, where they fit the workspace and cost less than to be formed
     // again: always in fp32 (8 bytes of traffic against 2 d operations on the CUDA cores: 512 tokens of 12 heads over
-    // 512 slots 209 us, 48 so), for few rows in bf16 (16 a sequence and KV head: less than a slot's K).
+    // 512 slots 209 us, 48 so), for few rows in bf16 (16 a sequence and KV head: less than a slot's K; four sequences of 16000
+    // slots, 14 rows 83.6 us kept and 91.8 formed again, 28 rows 97.9 and 98.9; one sequence, 28 rows 50.8 and 46.8).
     // (weight_stride is the caller's, up to 2^63: divided by, not multiplied)
     const long long most = kAttendScores / ((long long)P.T * P.Hq) / 64 * 64;   // slots a row of the workspace may have
     const bool keep = P.key_weight && (!bf16 || (long long)P.T * P.G <= 16ll * P.batch) && P.weight_stride <= most;

@@ -239,7 +239,9 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Atten
 }
 template <typename T, int D, int BM> cudaError_t run_join(const AttendParams& P, int grid, cudaStream_t stream)
 {
-    // an item has at most min(tile_rows, T G) rows; few in the whole call: four warps a row, as it may have many parts
+    // An item has at most min(tile_rows, T G) rows; few in the whole call: four warps a row, as it may have many parts (16384
+    // slots, 7 rows a KV head 29 us so and 54 with one warp, 63 rows 35 and 54; 16 sequences of 8192 slots, 112 rows in all
+    // 82.6 and 76.5)
     const long long rows = min((long long)P.tile_rows, (long long)P.T * P.G);
     const bool few = (long long)P.T * P.G <= 64;
     const int rpc = few ? 2 : 8 * (D == 256 ? 2 : 4);

@@ -15,16 +15,20 @@
 //                       which the first joins at the end.  Heads of 256, whose two O would not fit TMEM: both
 //                       on every unit, half the columns each.  P takes the place of S.  O is rescaled only
 //                       when a row's maximum has grown by more than 2^8 since the last time.
-// P is rounded to bf16 for the MMA, as V is.  Where a row sees few slots the roundings of its few weights do
-// not average out, and the error comes near 2^-8 |v|; there, and where the copies bound the kernel
-// anyway (one row tile), P goes in as two bf16 terms, high and low, at the price of a second product.
+// P is rounded to bf16 for the MMA, as V is, in calls of many rows: out is then off by 2.2e-3 (relative, 4096 slots) where
+// its own rounding to bf16 is 1.66e-3, and a second term everywhere would cost 4096 tokens over 32768 slots 43% (1.64 ms
+// against 1.15).  Where the copies bound the kernel (one row tile: 99 us against 97 for a token of each of eight sequences),
+// and where rows see few slots, so that the rounding of one weight shows (worst element over 16 slots 1.26 times as far off;
+// 1 to 3 us of 30), P goes in as two bf16 terms, high and low: 1.66e-3.
 //
 // What bounds it.  Many rows: the chain S -> softmax -> P V of each row tile, which the other tile's MMAs only partly
-// fill: 4096 tokens of 28 query heads (7 a KV head, 128 wide) over 32768 slots take 1.13 ms, 1.6 PFLOP/s or 85% of a large
-// library product's rate, with pages of 16 tokens, of 64 or none.  Few rows: the reading of K and V: one token of each of
-// eight sequences over up to 32768 slots, 411 MB, 83 us, 4.9 TB/s.  Short calls: latency, about 11 us from launch to end
-// (three dependent reads from DRAM: lengths, page table, rows; code that is not in the instruction cache yet, which is
-// why its loops are short where they can be).
+// fill: 4096 tokens of 28 query heads (7 a KV head, 128 wide) over 32768 slots take 1.22 ms a call among others, 1.48 PFLOP/s
+// or 78% of a large library product's burst rate (1.11 ms alone behind a flush of L2), with pages of 16 tokens, of 64 or
+// none.  Few rows: the reading of K and V: one token of each of eight sequences over up to 32768 slots, 411 MB, 83 us, 4.9
+// TB/s.  Heads of 256: the softmax, whose two warpgroups agree on a maximum for every 64 slots: 512 tokens of 8 query
+// heads over 8192 slots 40 us, the tensor pipe 39% busy.  Short calls: latency, about 11 us from launch to end (three
+// dependent reads from DRAM: lengths, page table, rows; code that is not in the instruction cache yet, which is why its
+// loops are short where they can be).
 #pragma once
 
 #include <atomic>
@@ -70,7 +74,10 @@ template <int N> __device__ __forceinline__ void regs_take() { asm volatile("set
 
 constexpr int kFewSlots = 512;   // rows that see fewer slots get their weights in two terms
 
-// Sequences of up to 128 rows a KV head: one row tile, bound by the copies.
+// Sequences of up to 128 rows a KV head: one row tile, bound by the copies.  Eight sequences of 16384 slots, 7 query heads on
+// each of 4 KV heads of 128: 126 rows 87.7 us with one row tile and 91.8 with two, 133 rows 127.6 and 92.8; heads of 64,
+// 128 rows 41.6 and 43.7, 144 rows 48.8 and 43.7.  (The lengths are on the device, so the rule goes by the call's mean: one
+// sequence of 256 tokens among 63 without any takes 111 us where two row tiles would take 83.)
 __host__ __device__ __forceinline__ bool one_tile(const AttendParams& P) { return (long long)P.T * P.G <= 128ll * P.batch; }
 
 // Whether an item's weights are multiplied in two terms: its first token sees fewest slots.
@@ -85,8 +92,8 @@ template <int D, int NT> __device__ __forceinline__ bool two_terms(const AttendP
 }
 
 // How K and V tiles are brought: row by row (any page size), or in groups of 8 rows a fixed stride apart (contiguous caches
-// and page sizes that are multiples of 8).  (Tensor copies, a box a page, were slower: 4096 tokens over 32768 slots with
-// pages of 16, 32 and 64 slots 2.06, 1.29 and 1.18 ms against 1.13.)
+// and page sizes that are multiples of 8: 4096 tokens over 32768 slots 1.13 ms against 1.35).  (Tensor copies, a box a page,
+// were slower: with pages of 16, 32 and 64 slots 2.06, 1.29 and 1.18 ms.)
 enum Source { kRows, kGroups };
 
 template <int D, int NT, Source SRC, bool CAP>

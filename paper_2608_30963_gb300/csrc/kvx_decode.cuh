@@ -351,7 +351,8 @@ __device__ __forceinline__ Parts item_parts(const Plan& p, const Segment& g)
     return r;
 }
 
-// Base-2 exponential of the hardware (2 ulp); the argument is at most 0.
+// Base-2 exponential of the hardware (2 ulp).  The argument is at most 0, but for the weights of the tensor-core attention:
+// there a row's maximum may stay behind by up to 8.
 __device__ __forceinline__ float exp2_hw(float x)
 {
     float y;
