@@ -471,6 +471,7 @@ typedef struct {
  * is, before they multiply V; in calls of few rows and in tiles whose rows may see fewer than 512
  * slots they multiply it as two bf16 terms.)  Rows no new token sees are never part of a result, whatever
  * they hold.  Page-table entries outside the pool read as zero rows and are flagged.
+ * out must not overlap q, which the weight sums and rows summed again read after the first outputs are written.
  * The sums behind every output are taken in an order that depends on sizes alone: equal calls
  * give equal bits.  At most 1024 sequences a call (KVX_ERR_UNSUPPORTED).
  * Asynchronous on stream; allocates nothing.  Calls on one decoder share its workspace: issue them on

@@ -611,7 +611,8 @@ class Decoder:
 
     def attend(self, q, seq_off, kv_len, cache_k, cache_v, out, *, window: int = 0, prefix_len=None, lse=None, key_weight=None,
                page_table=None, page_size: int = 16, num_pages: int = 0, stream=None):
-        """Attention of the rotated queries q [T, Hq, d] over the cache (their own rows appended before), into out.
+        """Attention of the rotated queries q [T, Hq, d] over the cache (their own rows appended before), into out
+        (not q itself).
         window: slots a token sees up to its own (0: all); prefix_len int32[B]: slots every token sees;
         lse float32[T, Hq]: log-sum-exp of each row; key_weight float32[B, H, S]: has the attention weights
         each slot receives added to it (needs lse)."""
