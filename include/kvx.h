@@ -507,10 +507,46 @@ typedef struct {
 KVX_API kvx_status kvx_evict(kvx_decoder* dec, const kvx_evict_plan* plan, const kvx_dst_kv* src,
                              const kvx_dst_kv* dst, void* stream);
 
+/* A cache held in 8 bits.  The row of a (slot, KV head) of K or V is head_dim codes in e4m3, a byte each, and one scale byte s,
+ * a power of two:  value = code * 2^(s - 127)  (s = 0 stands for a scale of 0, 255 for infinity, so that memory filled with
+ * zeros reads as zeros).  A row x is quantised as
+ *   s = the smallest scale in [10, 247] with max |x| <= 448 * 2^(s - 127),  code = x / 2^(s - 127) to nearest even
+ * which leaves each value within 2^-4 of itself (2^-16 of the row's largest near zero).  Every value such a row stands for is
+ * exact in bf16 and fp32.  Values that are not finite have no say in the scale and become NaN; magnitudes above
+ * 1.875 * 2^127 are taken as that. */
+typedef struct {
+    kvx_dst_kv codes;           /* K and V codes, as a cache of bytes: contiguous strides (bytes) are multiples of 16,
+                                   pointers 16-byte aligned, pools [num_pages][page_size][num_kv_heads][head_dim] */
+    uint8_t* const* k_scale;    /* host arrays [num_layers] of device pointers.  Contiguous: the scale of (b, h, t) lies at */
+    uint8_t* const* v_scale;    /* b * scale_stride_b + h * scale_stride_h + t.  Paged: [num_pages][num_kv_heads][page_size] */
+    int64_t scale_stride_b, scale_stride_h;    /* contiguous: bytes, >= 1 */
+} kvx_quantised_kv;
+
+/* As kvx_append, into a cache held in 8 bits: K rows rotated, then quantised from 32 bits, V rows quantised as they are. */
+KVX_API kvx_status kvx_append_quantised(kvx_decoder* dec, const kvx_new_tokens* tok, const kvx_rows* q, const kvx_rows* k,
+                                        const kvx_rows* v, const kvx_rows* q_out, const kvx_quantised_kv* cache, int32_t layer,
+                                        void* stream);
+
+/* As kvx_attend, over a cache held in 8 bits: K_h[j] and V_h[j] are the values that its rows stand for.  No weight sums: opts'
+ * key_weight must be NULL (KVX_ERR_UNSUPPORTED). */
+KVX_API kvx_status kvx_attend_quantised(kvx_decoder* dec, const kvx_new_tokens* tok, const kvx_rows* q, const kvx_quantised_kv* cache,
+                                        int32_t layer, const kvx_attend_opts* opts, const kvx_rows* out, void* stream);
+
+/* Slots [0, kv_len[b]) of layers [0, num_layers) of a cache of the decoder's dtype, as a translation leaves it, into one held in
+ * 8 bits (kvx_quantise), or back (kvx_dequantise; the values are exact).  Each cache has its own layout and page
+ * table; dst must not overlap src.
+ *   kv_len: device int32[batch]; lengths above either cache's capacity per sequence are clamped and flagged.
+ * Rows of pages outside a pool, on either side, are skipped and flagged; slots past kv_len are not touched.  At most 1024
+ * sequences a call (KVX_ERR_UNSUPPORTED).  Asynchronous on stream; allocates nothing. */
+KVX_API kvx_status kvx_quantise(kvx_decoder* dec, int32_t batch, int32_t num_layers, const int32_t* kv_len, const kvx_dst_kv* src,
+                                const kvx_quantised_kv* dst, void* stream);
+KVX_API kvx_status kvx_dequantise(kvx_decoder* dec, int32_t batch, int32_t num_layers, const int32_t* kv_len,
+                                  const kvx_quantised_kv* src, const kvx_dst_kv* dst, void* stream);
+
 /* As kvx_get_device_status, for a decoder (KVX_DEV_* bits of its calls). */
 KVX_API kvx_status kvx_decoder_status(kvx_decoder* dec, void* stream, uint32_t* bits, int32_t clear);
 
-/* Kernel launches the most recent kvx_append, kvx_attend or kvx_evict on this decoder made. */
+/* Kernel launches the most recent call that goes on from a cache (kvx_append to kvx_dequantise) on this decoder made. */
 KVX_API int32_t kvx_decoder_launches(const kvx_decoder* dec);
 
 /* Size of the device scratch array kvx_translate_static works in (8 MiB). */

@@ -112,6 +112,11 @@ class kvx_evict_plan(ctypes.Structure):
                 ("kept_weight_stride", ctypes.c_int64)]
 
 
+class kvx_quantised_kv(ctypes.Structure):
+    _fields_ = [("codes", kvx_dst_kv), ("k_scale", VP), ("v_scale", VP), ("scale_stride_b", ctypes.c_int64),
+                ("scale_stride_h", ctypes.c_int64)]
+
+
 class kvx_translator_info(ctypes.Structure):
     _fields_ = [("path", ctypes.c_int32), ("group_in", ctypes.c_int32), ("n_tile", ctypes.c_int32),
                 ("smem_bytes", ctypes.c_int32), ("threads", ctypes.c_int32), ("num_sms", ctypes.c_int32),
@@ -123,7 +128,8 @@ EXPORTS = ["kvx_translator_create", "kvx_translator_create_low_rank", "kvx_trans
            "kvx_get_device_status", "kvx_get_info", "kvx_launches_per_translate", "kvx_last_error",
            "kvx_destroy", "kvx_translate_static", "kvx_static_last_error", "kvx_span_plan_stats",
            "kvx_enable_peer", "kvx_translate_to_device", "kvx_debug_stall_next_translate", "kvx_decoder_create",
-           "kvx_decoder_destroy", "kvx_append", "kvx_attend", "kvx_evict", "kvx_decoder_status", "kvx_decoder_launches"]
+           "kvx_decoder_destroy", "kvx_append", "kvx_attend", "kvx_evict", "kvx_decoder_status", "kvx_decoder_launches",
+           "kvx_append_quantised", "kvx_attend_quantised", "kvx_quantise", "kvx_dequantise"]
 KVX_PEER_STORES, KVX_PEER_STAGED = 0, 1
 KVX_STATIC_SCRATCH_BYTES = 8 << 20
 KVX_MAX_ATTEND_BATCH = 1024   # sequences of one kvx_attend call
@@ -193,6 +199,9 @@ def lib():
         L.kvx_append.argtypes = [VP, VP, VP, VP, VP, VP, VP, ctypes.c_int32, VP]
         L.kvx_attend.argtypes = [VP, VP, VP, VP, ctypes.c_int32, VP, VP, VP]
         L.kvx_evict.argtypes = [VP, VP, VP, VP, VP]
+        L.kvx_append_quantised.argtypes = L.kvx_append.argtypes
+        L.kvx_attend_quantised.argtypes = L.kvx_attend.argtypes
+        L.kvx_quantise.argtypes = L.kvx_dequantise.argtypes = [VP, ctypes.c_int32, ctypes.c_int32, VP, VP, VP, VP]
         L.kvx_decoder_status.argtypes = [VP, VP, ctypes.POINTER(ctypes.c_uint32), ctypes.c_int32]
         L.kvx_decoder_launches.argtypes = [VP]
         L.kvx_decoder_launches.restype = ctypes.c_int32
@@ -498,6 +507,7 @@ _PACK_TOKENS = struct.Struct("@iiPPP").pack          # kvx_new_tokens
 _PACK_OPTS = struct.Struct("@iPPPq").pack            # kvx_attend_opts
 _PACK_PLAN = struct.Struct("@iiPPqiiiPPPq").pack     # kvx_evict_plan
 _PACK_CACHE = struct.Struct("@PPiiqqqPiii4x").pack   # kvx_dst_kv
+_PACK_SCALES = struct.Struct("@PPqq").pack           # the end of kvx_quantised_kv, behind its kvx_dst_kv
 
 
 def _rows(t) -> bytes:
@@ -557,6 +567,7 @@ class Decoder:
         import torch
         self._type = torch.bfloat16 if dtype == KVX_BF16 else torch.float32
         self._f32, self._i32 = torch.float32, torch.int32
+        self._code_types, self._scale_types = (torch.float8_e4m3fn, torch.uint8), (torch.float8_e8m0fnu, torch.uint8)
         global _current_raw_stream
         _current_raw_stream = _current_raw_stream or _find_raw_stream()
         h = VP()
@@ -589,6 +600,43 @@ class Decoder:
                 return _PACK_CACHE(at, at + 8, 1, 0, 0, 0, 0, page_table.data_ptr(), ts[1], page_size, num_pages or ks[0]), ptrs
         raise ValueError(f"caches must be alike, [B, {H}, S, {d}] or pools [pages, {page_size}, {H}, {d}] with an int32 page table, of "
                          f"{self._type}, got {tuple(ks)} and {tuple(v.shape)} of {k.dtype} and {v.dtype}")
+
+    def _code_layers(self, k: Sequence, v: Sequence, k_scale: Sequence, v_scale: Sequence, batch: int, page_table, page_size: int,
+                     num_pages: int):
+        """Layers of an 8-bit cache as kvx_quantised_kv (and what has to live as long), checked: as _layer, codes and scales alike in
+        every layer."""
+        H, d, k0, s0 = self._heads, self._dim, k[0], k_scale[0]
+        ks, st, ss, sst = k0.shape, k0.stride(), s0.shape, s0.stride()
+        n = len(k)
+        ok = len(v) == len(k_scale) == len(v_scale) == n
+        for some, shape, stride, types in ((k, ks, st, self._code_types), (v, ks, st, self._code_types), (k_scale, ss, sst, self._scale_types),
+                                           (v_scale, ss, sst, self._scale_types)):
+            for t in some:
+                ok = ok and t.shape == shape and t.dtype in types and (t.stride() == stride)
+        ptrs = array.array("Q", [t.data_ptr() for some in (k, v, k_scale, v_scale) for t in some])
+        at = ptrs.buffer_info()[0]
+        if page_table is None:
+            if (ok and len(ks) == 4 and ks[0] >= batch and ks[1] == H and ks[3] == d and st[3] == 1
+                    and ss == ks[:3] and (ss[2] <= 1 or sst[2] == 1)):
+                return (_PACK_CACHE(at, at + 8 * n, 0, ks[2], st[0], st[1], st[2], 0, 0, 0, 0)
+                        + _PACK_SCALES(at + 16 * n, at + 24 * n, sst[0], sst[1])), ptrs
+        else:
+            ts = page_table.shape
+            if page_size < 1 or (ok and ks[1:] == (page_size, H, d) and k0.is_contiguous() and ss == (ks[0], H, page_size)
+                                 and s0.is_contiguous() and ts[0] >= batch and page_table.dtype == self._i32 and page_table.is_contiguous()):
+                return (_PACK_CACHE(at, at + 8 * n, 1, 0, 0, 0, 0, page_table.data_ptr(), ts[1], page_size, num_pages or ks[0])
+                        + _PACK_SCALES(at + 16 * n, at + 24 * n, 1, 1)), ptrs
+        raise ValueError(f"8-bit caches must be alike: codes [B, {H}, S, {d}] of float8_e4m3fn or uint8 with scales [B, {H}, S] of float8_e8m0fnu or "
+                         f"uint8, or pools [pages, {page_size}, {H}, {d}] with scales [pages, {H}, {page_size}] and an int32 page table, got "
+                         f"{tuple(ks)} of {k0.dtype} with {tuple(ss)} of {s0.dtype}")
+
+    def _full_layers(self, k: Sequence, v: Sequence, batch: int, page_table, page_size: int, num_pages: int):
+        """Layers of a cache of the decoder's type as kvx_dst_kv, checked alike."""
+        self._layer(k[0], v[0], batch, page_table, page_size, num_pages)
+        shape, stride = k[0].shape, k[0].stride()
+        if len(v) != len(k) or any(t.shape != shape or t.dtype != self._type or t.stride() != stride for some in (k, v) for t in some):
+            raise ValueError(f"the layers of a cache must be alike, of {self._type}: {tuple(shape)} with strides {stride}")
+        return _cache(k, v, page_table, page_size, num_pages)
 
     def append(self, q, k, v, seq_off, kv_len, cache_k, cache_v, q_out, *, pos=None, page_table=None, page_size: int = 16,
                num_pages: int = 0, stream=None):
@@ -666,6 +714,69 @@ class Decoder:
         src, _keep_src = _cache(src_k, src_v, page_table, page_size, num_pages)
         dst, _keep_dst = _cache(dst_k, dst_v, dst_page_table, page_size, dst_num_pages)
         _check(lib().kvx_evict(self.handle, plan, src, dst, _raw_stream(stream)))
+
+    def append_quantised(self, q, k, v, seq_off, kv_len, cache_k, cache_v, k_scale, v_scale, q_out, *, pos=None, page_table=None,
+                         page_size: int = 16, num_pages: int = 0, stream=None):
+        """As append, into one layer of a cache held in 8 bits: codes cache_k, cache_v (float8_e4m3fn or uint8) [B, H, S, d] with scales
+        k_scale, v_scale (float8_e8m0fnu or uint8) [B, H, S], or pools [pages, page_size, H, d] with scales [pages, H, page_size].
+        A value is its code times its row's scale."""
+        T, H, Hq = q.shape[0], self._heads, self._q_heads
+        self._fits(q, T, Hq)
+        self._fits(k, T, H)
+        self._fits(v, T, H)
+        self._fits(q_out, T, Hq)
+        B = seq_off.shape[0] - 1
+        if not (self._index(seq_off, 1) and self._index(kv_len, B) and (pos is None or (self._index(pos, T) and pos.shape[0] == T))):
+            raise ValueError("seq_off [B + 1], kv_len [B] and pos [tokens] must be contiguous int32")
+        tok = _PACK_TOKENS(B, T, seq_off.data_ptr(), kv_len.data_ptr(), 0 if pos is None else pos.data_ptr())
+        cache, _keep = self._code_layers((cache_k,), (cache_v,), (k_scale,), (v_scale,), B, page_table, page_size, num_pages)
+        st = lib().kvx_append_quantised(self.handle, tok, _rows(q), _rows(k), _rows(v), _rows(q_out), cache, 0, _raw_stream(stream))
+        if st:
+            _check(st)
+
+    def attend_quantised(self, q, seq_off, kv_len, cache_k, cache_v, k_scale, v_scale, out, *, window: int = 0, prefix_len=None, lse=None,
+                         page_table=None, page_size: int = 16, num_pages: int = 0, stream=None):
+        """As attend (without weight sums), over one layer of a cache held in 8 bits (as for append_quantised)."""
+        T, Hq, B = q.shape[0], self._q_heads, seq_off.shape[0] - 1
+        self._fits(q, T, Hq)
+        self._fits(out, T, Hq)
+        if lse is not None and not (lse.shape == (T, Hq) and lse.is_contiguous() and lse.dtype == self._f32):
+            raise ValueError("lse must be contiguous float32 [tokens, query heads]")
+        if not (self._index(seq_off, 1) and self._index(kv_len, B) and (prefix_len is None or self._index(prefix_len, B))):
+            raise ValueError("seq_off [B + 1], kv_len [B] and prefix_len [B] must be contiguous int32")
+        tok = _PACK_TOKENS(B, T, seq_off.data_ptr(), kv_len.data_ptr(), 0)
+        opts = _PACK_OPTS(window, 0 if prefix_len is None else prefix_len.data_ptr(), 0 if lse is None else lse.data_ptr(), 0, 0)
+        cache, _keep = self._code_layers((cache_k,), (cache_v,), (k_scale,), (v_scale,), B if B <= KVX_MAX_ATTEND_BATCH else 0, page_table,
+                                         page_size, num_pages)
+        st = lib().kvx_attend_quantised(self.handle, tok, _rows(q), cache, 0, opts, _rows(out), _raw_stream(stream))
+        if st:
+            _check(st)
+
+    def quantise(self, kv_len, src_k: Sequence, src_v: Sequence, dst_k: Sequence, dst_v: Sequence, dst_k_scale: Sequence,
+                 dst_v_scale: Sequence, *, page_table=None, dst_page_table=None, page_size: int = 16, num_pages: int = 0,
+                 dst_num_pages: int = 0, stream=None):
+        """Slots [0, kv_len[b]) of a cache (lists of layers, as a translation leaves it) into one held in 8 bits (lists of layers, as
+        for append_quantised).  kv_len int32[B]."""
+        self._convert("kvx_quantise", kv_len, (src_k, src_v), page_table, num_pages, (dst_k, dst_v, dst_k_scale, dst_v_scale), dst_page_table,
+                      dst_num_pages, page_size, stream)
+
+    def dequantise(self, kv_len, src_k: Sequence, src_v: Sequence, src_k_scale: Sequence, src_v_scale: Sequence, dst_k: Sequence,
+                   dst_v: Sequence, *, page_table=None, dst_page_table=None, page_size: int = 16, num_pages: int = 0, dst_num_pages: int = 0,
+                   stream=None):
+        """The reverse of quantise: the values of a cache held in 8 bits, in the decoder's type (exact)."""
+        self._convert("kvx_dequantise", kv_len, (src_k, src_v, src_k_scale, src_v_scale), page_table, num_pages, (dst_k, dst_v), dst_page_table,
+                      dst_num_pages, page_size, stream)
+
+    def _convert(self, call: str, kv_len, src, table, pages: int, dst, dst_table, dst_pages: int, page_size: int, stream):
+        B, L = kv_len.shape[0], len(src[0])
+        if not self._index(kv_len, B):
+            raise ValueError("kv_len must be contiguous int32 [B]")
+        if L < 1 or len(dst[0]) != L:
+            raise ValueError("the caches must have as many layers as one another, one or more")
+        least = B if B <= KVX_MAX_ATTEND_BATCH else 0
+        of = {2: self._full_layers, 4: self._code_layers}
+        (a, _keep_a), (b, _keep_b) = (of[len(x)](*x, least, t, page_size, n) for x, t, n in ((src, table, pages), (dst, dst_table, dst_pages)))
+        _check(getattr(lib(), call)(self.handle, B, L, kv_len.data_ptr(), a, b, _raw_stream(stream)))
 
     def device_status(self, stream=None, clear: bool = True) -> int:
         bits = ctypes.c_uint32(0)

@@ -3,6 +3,7 @@
 // that is not finite.
 #pragma once
 
+#include "kvx_codes.cuh"
 #include "kvx_decode.cuh"
 #include "kvx_tc_common.cuh"
 
@@ -29,6 +30,17 @@ template <typename T, int C> __device__ __forceinline__ void store_f32(T* p, con
         if constexpr (B == 16) *reinterpret_cast<uint4*>(p + i) = *reinterpret_cast<const uint4*>(v);
         else if constexpr (B == 8) *reinterpret_cast<uint2*>(p + i) = *reinterpret_cast<const uint2*>(v);
         else *reinterpret_cast<uint32_t*>(p + i) = *reinterpret_cast<const uint32_t*>(v);
+    }
+}
+
+// C consecutive codes of an 8-bit row (C a multiple of 2) as floats.
+template <int C> __device__ __forceinline__ void load_codes(const uint8_t* p, float scale, float (&x)[C])
+{
+#pragma unroll
+    for (int i = 0; i < C; i += 2) {
+        const float2 f = codes_f32(*reinterpret_cast<const unsigned short*>(p + i));
+        x[i] = f.x * scale;
+        x[i + 1] = f.y * scale;
     }
 }
 
@@ -64,10 +76,12 @@ __device__ __noinline__ void resum_row(const AttendParams& P, const Seq& s, int 
     for (int j = s.pre > 0 ? 0 : lo; j < max(hi, s.pre); ++j) {
         if (beat && (j & 4095) == 0 && lane == 0) *beat = *beat + 1;   // waits elsewhere in the CTA go on
         if (!sees(P, s, i, j)) continue;
-        const long long at = cache_row(P.cache, b, j);
-        if (at < 0) continue;
-        const long long off = at + cache_head(P.cache) * h + lane * C;
-        load_f32<T, C>((const T*)P.ck + off, x);
+        const CodePlace at = P.k_scale ? code_place(P.cache, P.scales, b, j) : CodePlace{cache_row(P.cache, b, j), 0};
+        if (at.row < 0) continue;
+        const long long off = at.row + cache_head(P.cache) * h + lane * C;
+        const long long scale = at.scale + scale_head(P.cache, P.scales) * h;
+        if (P.k_scale) load_codes<C>((const uint8_t*)P.ck + off, scale_of(P.k_scale[scale]), x);
+        else load_f32<T, C>((const T*)P.ck + off, x);
         float dot = 0.0f;
 #pragma unroll
         for (int c = 0; c < C; ++c) dot = fmaf(q[c], x[c], dot);
@@ -76,7 +90,8 @@ __device__ __noinline__ void resum_row(const AttendParams& P, const Seq& s, int 
         float v = dot * P.scale;
         if (P.cap > 0.0f) v = capped(v, P.cap, inv_cap);
         const float p = exp2_hw(v * kLog2e - lse2);
-        load_f32<T, C>((const T*)P.cv + off, x);
+        if (P.k_scale) load_codes<C>((const uint8_t*)P.cv + off, scale_of(P.v_scale[scale]), x);
+        else load_f32<T, C>((const T*)P.cv + off, x);
 #pragma unroll
         for (int c = 0; c < C; ++c) acc[c] = fmaf(p, x[c], acc[c]);
     }

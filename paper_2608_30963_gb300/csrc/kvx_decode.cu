@@ -1,5 +1,5 @@
-// kvx_decode.cu -- host side of the calls that go on from a cache: kvx_decoder_*, kvx_append,
-// kvx_attend and kvx_evict (argument checks, workspace, launches).
+// kvx_decode.cu -- host side of the calls that go on from a cache: kvx_decoder_*, kvx_append, kvx_attend, kvx_evict and
+// those of 8-bit caches (argument checks, workspace, launches).
 #include <float.h>
 #include <math.h>
 #include <stdarg.h>
@@ -72,10 +72,11 @@ kvx_status check_tokens(const kvx_decoder* d, const char* who, const kvx_new_tok
     return KVX_OK;
 }
 
-// The view of a cache, layers [l0, l0 + n) of it checked.
-kvx_status make_view(const kvx_decoder* d, const char* who, const char* what, const kvx_dst_kv* c, int l0, int n, CacheView& v)
+// The view of a cache, layers [l0, l0 + n) of it checked; vec: elements of 16 bytes (0: of the decoder's type).
+kvx_status make_view(const kvx_decoder* d, const char* who, const char* what, const kvx_dst_kv* c, int l0, int n, CacheView& v, int vec = 0)
 {
-    const int vec = vec_of(d), dim = d->desc.model.head_dim;
+    const int dim = d->desc.model.head_dim;
+    if (!vec) vec = vec_of(d);
     if (!c || !c->k || !c->v) return fail(KVX_ERR_INVALID_ARG, "%s: %s is NULL", who, what);
     memset(&v, 0, sizeof v);
     v.H = d->desc.model.num_kv_heads;
@@ -118,6 +119,135 @@ kvx_status check_layer(const kvx_decoder* d, const char* who, int layer)
 {
     if (layer < 0 || layer >= d->desc.model.num_layers)
         return fail(KVX_ERR_INVALID_ARG, "%s: layer %d outside [0, %d)", who, layer, d->desc.model.num_layers);
+    return KVX_OK;
+}
+
+// The view of an 8-bit cache's codes and of their scales.
+kvx_status make_code_view(const kvx_decoder* d, const char* who, const char* what, const kvx_quantised_kv* c, int l0, int n, CacheView& v, ScaleView& z)
+{
+    if (!c) return fail(KVX_ERR_INVALID_ARG, "%s: %s is NULL", who, what);
+    if (kvx_status st = make_view(d, who, what, &c->codes, l0, n, v, 16)) return st;
+    if (!c->k_scale || !c->v_scale) return fail(KVX_ERR_INVALID_ARG, "%s: the scales of %s are NULL", who, what);
+    if (!c->codes.paged && (c->scale_stride_b < 1 || c->scale_stride_h < 1))
+        return fail(KVX_ERR_INVALID_ARG, "%s: scale strides of %s must be positive", who, what);
+    for (int l = l0; l < l0 + n; ++l)
+        if (!c->k_scale[l] || !c->v_scale[l]) return fail(KVX_ERR_INVALID_ARG, "%s: NULL scale pointer in %s, layer %d", who, what, l);
+    z.sb = c->scale_stride_b;
+    z.sh = c->scale_stride_h;
+    return KVX_OK;
+}
+
+// kvx_append and kvx_append_quantised: one of cache and codes is NULL.
+kvx_status append(kvx_decoder* dec, const char* who, const kvx_new_tokens* tok, const kvx_rows* q, const kvx_rows* k, const kvx_rows* v,
+                  const kvx_rows* q_out, const kvx_dst_kv* cache, const kvx_quantised_kv* codes, bool quantised, int layer, void* stream)
+{
+    if (!dec) return fail(KVX_ERR_INVALID_ARG, "%s: NULL decoder", who);
+    dec->last_launches = 0;
+    kvx_status st;
+    AppendParams P;
+    memset(&P, 0, sizeof P);
+    if ((st = check_tokens(dec, who, tok)) || (st = check_layer(dec, who, layer))) return st;
+    if (tok->total_tokens == 0) return KVX_OK;
+    if ((st = check_rows(dec, who, "q", q)) || (st = check_rows(dec, who, "k", k)) || (st = check_rows(dec, who, "v", v)) ||
+        (st = check_rows(dec, who, "q_out", q_out)) ||
+        (st = quantised ? make_code_view(dec, who, "the cache", codes, layer, 1, P.cache, P.scales)
+                        : make_view(dec, who, "the cache", cache, layer, 1, P.cache)))
+        return st;
+    if (quantised) {
+        cache = &codes->codes;
+        P.k_scale = codes->k_scale[layer];
+        P.v_scale = codes->v_scale[layer];
+    }
+    const kvx_model_geom& g = dec->desc.model;
+    P.T = tok->total_tokens; P.batch = tok->batch;
+    P.Hq = dec->desc.num_q_heads; P.H = g.num_kv_heads; P.d = g.head_dim;
+    P.rhalf = rope_rot_dim(g) / 2; P.rope = g.rope_base > 0.0; P.max_position = dec->max_position;
+    P.seq_off = tok->seq_off; P.kv_len = tok->kv_len; P.pos = tok->pos;
+    P.turns = dec->turns;
+    P.q = q->ptr; P.q_t = q->stride_t; P.q_h = q->stride_h;
+    P.k = k->ptr; P.k_t = k->stride_t; P.k_h = k->stride_h;
+    P.v = v->ptr; P.v_t = v->stride_t; P.v_h = v->stride_h;
+    P.q_out = q_out->ptr; P.o_t = q_out->stride_t; P.o_h = q_out->stride_h;
+    P.ck = cache->k[layer]; P.cv = cache->v[layer];
+    P.status = dec->status;
+    const cudaError_t e = quantised ? launch_append_codes(P, dec->desc.dtype, (cudaStream_t)stream) : launch_append(P, dec->desc.dtype, (cudaStream_t)stream);
+    if (e != cudaSuccess) return fail(KVX_ERR_CUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
+    dec->last_launches = 1;
+    return KVX_OK;
+}
+
+// kvx_attend and kvx_attend_quantised, likewise.
+kvx_status attend(kvx_decoder* dec, const char* who, const kvx_new_tokens* tok, const kvx_rows* q, const kvx_dst_kv* cache,
+                  const kvx_quantised_kv* codes, bool quantised, int layer, const kvx_attend_opts* opts, const kvx_rows* out, void* stream)
+{
+    if (!dec) return fail(KVX_ERR_INVALID_ARG, "%s: NULL decoder", who);
+    dec->last_launches = 0;
+    static const kvx_attend_opts none = {};
+    if (!opts) opts = &none;
+    kvx_status st;
+    AttendParams P;
+    memset(&P, 0, sizeof P);
+    if ((st = check_tokens(dec, who, tok)) || (st = check_layer(dec, who, layer))) return st;
+    if (tok->total_tokens == 0) return KVX_OK;
+    if ((st = check_rows(dec, who, "q", q)) || (st = check_rows(dec, who, "out", out)) ||
+        (st = quantised ? make_code_view(dec, who, "the cache", codes, layer, 1, P.cache, P.scales)
+                        : make_view(dec, who, "the cache", cache, layer, 1, P.cache)))
+        return st;
+    if (quantised) {
+        if (opts->key_weight) return fail(KVX_ERR_UNSUPPORTED, "%s: no weight sums over a cache held in 8 bits", who);
+        cache = &codes->codes;
+        P.k_scale = codes->k_scale[layer];
+        P.v_scale = codes->v_scale[layer];
+    }
+    if (tok->batch > kMaxAttendBatch) return fail(KVX_ERR_UNSUPPORTED, "%s: at most %d sequences a call", who, kMaxAttendBatch);
+    if (opts->window < 0) return fail(KVX_ERR_INVALID_ARG, "%s: window must not be negative", who);
+    if (opts->key_weight && (!opts->lse || opts->weight_stride < 1))
+        return fail(KVX_ERR_INVALID_ARG, "%s: key_weight needs lse and weight_stride >= 1", who);
+    const kvx_model_geom& g = dec->desc.model;
+    P.T = tok->total_tokens; P.batch = tok->batch;
+    P.Hq = dec->desc.num_q_heads; P.H = g.num_kv_heads; P.G = P.Hq / P.H; P.d = g.head_dim;
+    P.seq_off = tok->seq_off; P.kv_len = tok->kv_len;
+    P.q = q->ptr; P.q_t = q->stride_t; P.q_h = q->stride_h;
+    P.out = out->ptr; P.o_t = out->stride_t; P.o_h = out->stride_h;
+    P.ck = cache->k[layer]; P.cv = cache->v[layer];
+    P.scale = (float)dec->desc.scale; P.cap = (float)dec->desc.score_cap;
+    // Slots lie in [-2^30, 2^30), those seen from zero on: a window of 2^30 hides none, and slot - window does not wrap.
+    P.window = opts->window < 1 << 30 ? opts->window : 1 << 30; P.prefix_len = opts->prefix_len;
+    P.lse = opts->lse; P.key_weight = opts->key_weight; P.weight_stride = opts->weight_stride;
+    P.status = dec->status;
+    P.part_o = dec->part_o; P.part_ml = dec->part_ml; P.split = dec->split;
+    P.scores = dec->scores;
+    const cudaError_t e = (quantised ? launch_attend_codes : launch_attend)(P, dec->desc.dtype, dec->num_sms, (cudaStream_t)stream, &dec->last_launches);
+    if (e != cudaSuccess) return fail(KVX_ERR_CUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
+    return KVX_OK;
+}
+
+// kvx_quantise and kvx_dequantise.
+kvx_status convert(kvx_decoder* dec, const char* who, int batch, int L, const int32_t* kv_len, const kvx_dst_kv* full, const char* full_name,
+                   const kvx_quantised_kv* codes, const char* codes_name, bool to_codes, void* stream)
+{
+    if (!dec) return fail(KVX_ERR_INVALID_ARG, "%s: NULL decoder", who);
+    dec->last_launches = 0;
+    if (batch < 1 || L < 1 || L > KVX_MAX_TARGET_LAYERS || L > dec->desc.model.num_layers)
+        return fail(KVX_ERR_INVALID_ARG, "%s: batch must be >= 1 and num_layers in [1, %d], at most the model's", who, KVX_MAX_TARGET_LAYERS);
+    if (batch > kMaxAttendBatch) return fail(KVX_ERR_UNSUPPORTED, "%s: at most %d sequences a call", who, kMaxAttendBatch);
+    if (!kv_len) return fail(KVX_ERR_INVALID_ARG, "%s: kv_len must be set", who);
+    ConvertParams P;
+    memset(&P, 0, sizeof P);
+    kvx_status st;
+    if ((st = make_view(dec, who, full_name, full, 0, L, P.full)) || (st = make_code_view(dec, who, codes_name, codes, 0, L, P.codes, P.scales)))
+        return st;
+    P.L = L; P.batch = batch; P.H = dec->desc.model.num_kv_heads; P.d = dec->desc.model.head_dim;
+    P.kv_len = kv_len;
+    P.status = dec->status;
+    for (int l = 0; l < L; ++l) {
+        P.full_k[l] = full->k[l]; P.full_v[l] = full->v[l];
+        P.code_k[l] = codes->codes.k[l]; P.code_v[l] = codes->codes.v[l];
+        P.k_scale[l] = codes->k_scale[l]; P.v_scale[l] = codes->v_scale[l];
+    }
+    const cudaError_t e = launch_convert(P, to_codes, dec->desc.dtype, dec->num_sms, (cudaStream_t)stream);
+    if (e != cudaSuccess) return fail(KVX_ERR_CUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
+    dec->last_launches = 1;
     return KVX_OK;
 }
 
@@ -197,71 +327,38 @@ extern "C" KVX_API kvx_status kvx_append(kvx_decoder* dec, const kvx_new_tokens*
                                          const kvx_rows* v, const kvx_rows* q_out, const kvx_dst_kv* cache, int32_t layer,
                                          void* stream)
 {
-    if (!dec) return fail(KVX_ERR_INVALID_ARG, "append: NULL decoder");
-    dec->last_launches = 0;
-    kvx_status st;
-    AppendParams P;
-    memset(&P, 0, sizeof P);
-    if ((st = check_tokens(dec, "append", tok)) || (st = check_layer(dec, "append", layer))) return st;
-    if (tok->total_tokens == 0) return KVX_OK;
-    if ((st = check_rows(dec, "append", "q", q)) || (st = check_rows(dec, "append", "k", k)) ||
-        (st = check_rows(dec, "append", "v", v)) || (st = check_rows(dec, "append", "q_out", q_out)) ||
-        (st = make_view(dec, "append", "the cache", cache, layer, 1, P.cache)))
-        return st;
-    const kvx_model_geom& g = dec->desc.model;
-    P.T = tok->total_tokens; P.batch = tok->batch;
-    P.Hq = dec->desc.num_q_heads; P.H = g.num_kv_heads; P.d = g.head_dim;
-    P.rhalf = rope_rot_dim(g) / 2; P.rope = g.rope_base > 0.0; P.max_position = dec->max_position;
-    P.seq_off = tok->seq_off; P.kv_len = tok->kv_len; P.pos = tok->pos;
-    P.turns = dec->turns;
-    P.q = q->ptr; P.q_t = q->stride_t; P.q_h = q->stride_h;
-    P.k = k->ptr; P.k_t = k->stride_t; P.k_h = k->stride_h;
-    P.v = v->ptr; P.v_t = v->stride_t; P.v_h = v->stride_h;
-    P.q_out = q_out->ptr; P.o_t = q_out->stride_t; P.o_h = q_out->stride_h;
-    P.ck = cache->k[layer]; P.cv = cache->v[layer];
-    P.status = dec->status;
-    const cudaError_t e = launch_append(P, dec->desc.dtype, (cudaStream_t)stream);
-    if (e != cudaSuccess) return fail(KVX_ERR_CUDA, "append: launch failed: %s", cudaGetErrorString(e));
-    dec->last_launches = 1;
-    return KVX_OK;
+    return append(dec, "append", tok, q, k, v, q_out, cache, nullptr, false, layer, stream);
+}
+
+extern "C" KVX_API kvx_status kvx_append_quantised(kvx_decoder* dec, const kvx_new_tokens* tok, const kvx_rows* q, const kvx_rows* k,
+                                                   const kvx_rows* v, const kvx_rows* q_out, const kvx_quantised_kv* cache,
+                                                   int32_t layer, void* stream)
+{
+    return append(dec, "append_quantised", tok, q, k, v, q_out, nullptr, cache, true, layer, stream);
 }
 
 extern "C" KVX_API kvx_status kvx_attend(kvx_decoder* dec, const kvx_new_tokens* tok, const kvx_rows* q, const kvx_dst_kv* cache,
                                          int32_t layer, const kvx_attend_opts* opts, const kvx_rows* out, void* stream)
 {
-    if (!dec) return fail(KVX_ERR_INVALID_ARG, "attend: NULL decoder");
-    dec->last_launches = 0;
-    static const kvx_attend_opts none = {};
-    if (!opts) opts = &none;
-    kvx_status st;
-    AttendParams P;
-    memset(&P, 0, sizeof P);
-    if ((st = check_tokens(dec, "attend", tok)) || (st = check_layer(dec, "attend", layer))) return st;
-    if (tok->total_tokens == 0) return KVX_OK;
-    if ((st = check_rows(dec, "attend", "q", q)) || (st = check_rows(dec, "attend", "out", out)) ||
-        (st = make_view(dec, "attend", "the cache", cache, layer, 1, P.cache)))
-        return st;
-    if (tok->batch > kMaxAttendBatch) return fail(KVX_ERR_UNSUPPORTED, "attend: at most %d sequences a call", kMaxAttendBatch);
-    if (opts->window < 0) return fail(KVX_ERR_INVALID_ARG, "attend: window must not be negative");
-    if (opts->key_weight && (!opts->lse || opts->weight_stride < 1))
-        return fail(KVX_ERR_INVALID_ARG, "attend: key_weight needs lse and weight_stride >= 1");
-    const kvx_model_geom& g = dec->desc.model;
-    P.T = tok->total_tokens; P.batch = tok->batch;
-    P.Hq = dec->desc.num_q_heads; P.H = g.num_kv_heads; P.G = P.Hq / P.H; P.d = g.head_dim;
-    P.seq_off = tok->seq_off; P.kv_len = tok->kv_len;
-    P.q = q->ptr; P.q_t = q->stride_t; P.q_h = q->stride_h;
-    P.out = out->ptr; P.o_t = out->stride_t; P.o_h = out->stride_h;
-    P.ck = cache->k[layer]; P.cv = cache->v[layer];
-    P.scale = (float)dec->desc.scale; P.cap = (float)dec->desc.score_cap;
-    // Slots lie in [-2^30, 2^30), those seen from zero on: a window of 2^30 hides none, and slot - window does not wrap.
-    P.window = opts->window < 1 << 30 ? opts->window : 1 << 30; P.prefix_len = opts->prefix_len;
-    P.lse = opts->lse; P.key_weight = opts->key_weight; P.weight_stride = opts->weight_stride;
-    P.status = dec->status;
-    P.part_o = dec->part_o; P.part_ml = dec->part_ml; P.split = dec->split;
-    P.scores = dec->scores;
-    const cudaError_t e = launch_attend(P, dec->desc.dtype, dec->num_sms, (cudaStream_t)stream, &dec->last_launches);
-    if (e != cudaSuccess) return fail(KVX_ERR_CUDA, "attend: launch failed: %s", cudaGetErrorString(e));
-    return KVX_OK;
+    return attend(dec, "attend", tok, q, cache, nullptr, false, layer, opts, out, stream);
+}
+
+extern "C" KVX_API kvx_status kvx_attend_quantised(kvx_decoder* dec, const kvx_new_tokens* tok, const kvx_rows* q, const kvx_quantised_kv* cache,
+                                                   int32_t layer, const kvx_attend_opts* opts, const kvx_rows* out, void* stream)
+{
+    return attend(dec, "attend_quantised", tok, q, nullptr, cache, true, layer, opts, out, stream);
+}
+
+extern "C" KVX_API kvx_status kvx_quantise(kvx_decoder* dec, int32_t batch, int32_t num_layers, const int32_t* kv_len, const kvx_dst_kv* src,
+                                           const kvx_quantised_kv* dst, void* stream)
+{
+    return convert(dec, "quantise", batch, num_layers, kv_len, src, "the source cache", dst, "the destination cache", true, stream);
+}
+
+extern "C" KVX_API kvx_status kvx_dequantise(kvx_decoder* dec, int32_t batch, int32_t num_layers, const int32_t* kv_len,
+                                             const kvx_quantised_kv* src, const kvx_dst_kv* dst, void* stream)
+{
+    return convert(dec, "dequantise", batch, num_layers, kv_len, dst, "the destination cache", src, "the source cache", false, stream);
 }
 
 extern "C" KVX_API kvx_status kvx_evict(kvx_decoder* dec, const kvx_evict_plan* plan, const kvx_dst_kv* src, const kvx_dst_kv* dst,

@@ -32,6 +32,28 @@ __device__ __forceinline__ long long cache_row(const CacheView& C, int b, int s)
 }
 __host__ __device__ __forceinline__ long long cache_head(const CacheView& C) { return C.paged ? C.d : C.sh; }
 
+// The scales of an 8-bit cache's rows (kvx_quantised_kv): bytes, a contiguous cache's at b * sb + h * sh + slot, a paged one's
+// as pages [H][page_size].
+struct ScaleView {
+    long long sb, sh;                   // contiguous: strides
+};
+__host__ __device__ __forceinline__ long long scale_head(const CacheView& C, const ScaleView& S) { return C.paged ? C.page_size : S.sh; }
+
+// Where the row of slot s of sequence b and its scale lie, head 0 (add cache_head * h and scale_head * h); row = -1 if its
+// page is not in the pool.
+struct CodePlace {
+    long long row, scale;
+};
+__device__ __forceinline__ CodePlace code_place(const CacheView& C, const ScaleView& S, int b, int s)
+{
+    if (!C.paged) return {(long long)b * C.sb + (long long)s * C.st, (long long)b * S.sb + s};
+    const int pi = C.page_shift >= 0 ? s >> C.page_shift : s / C.page_size;
+    const int in = s - pi * C.page_size;
+    const int page = pi < C.max_pages ? C.page_table[(size_t)b * C.max_pages + pi] : -1;
+    if (page < 0 || page >= C.num_pages) return {-1, -1};
+    return {((long long)page * C.page_size + in) * ((long long)C.H * C.d), (long long)page * C.H * C.page_size + in};
+}
+
 struct AppendParams {
     int T, batch, Hq, H, d, rhalf, rope, max_position;
     const int* seq_off;
@@ -44,8 +66,28 @@ struct AppendParams {
     void *ck, *cv;
     CacheView cache;
     unsigned* status;
+    // an 8-bit cache's scales
+    unsigned char *k_scale, *v_scale;
+    ScaleView scales;
 };
 cudaError_t launch_append(const AppendParams& P, int dtype, cudaStream_t stream);
+cudaError_t launch_append_codes(const AppendParams& P, int dtype, cudaStream_t stream);
+
+// Rows of layers [0, L) between a cache of the decoder's type (full) and an 8-bit one (codes).
+struct ConvertParams {
+    int L, batch, H, d;
+    const int* kv_len;
+    CacheView full, codes;
+    ScaleView scales;
+    unsigned* status;
+    void* full_k[KVX_MAX_TARGET_LAYERS];
+    void* full_v[KVX_MAX_TARGET_LAYERS];
+    void* code_k[KVX_MAX_TARGET_LAYERS];
+    void* code_v[KVX_MAX_TARGET_LAYERS];
+    unsigned char* k_scale[KVX_MAX_TARGET_LAYERS];
+    unsigned char* v_scale[KVX_MAX_TARGET_LAYERS];
+};
+cudaError_t launch_convert(const ConvertParams& P, bool to_codes, int dtype, int num_sms, cudaStream_t stream);
 
 // A row tile and KV head whose tiles several CTAs have, as the CTA where it begins leaves it; parts = 0: none.
 struct SplitItem {
@@ -79,6 +121,9 @@ struct AttendParams {
     // scores of few rows, kept for the weight sums (log2 units): [T][Hq][scores_stride], or NULL
     float* scores;
     long long scores_stride;
+    // an 8-bit cache's scales; NULL: ck and cv are of the decoder's type
+    const unsigned char *k_scale, *v_scale;
+    ScaleView scales;
 };
 
 struct EvictParams {
@@ -107,6 +152,7 @@ cudaError_t launch_key_weight(const AttendParams& P, int num_sms, cudaStream_t s
 cudaError_t launch_attend_tc_capped(const AttendParams& P, int num_sms, cudaStream_t stream);
 cudaError_t launch_attend_tc(const AttendParams& P, int num_sms, cudaStream_t stream);
 cudaError_t launch_attend(const AttendParams& P, int dtype, int num_sms, cudaStream_t stream, int* launches);
+cudaError_t launch_attend_codes(const AttendParams& P, int dtype, int num_sms, cudaStream_t stream, int* launches);
 
 // ------------------------------------------------------------------ sequences and masks
 // Cached tokens of sequence b, clamped to the cache.
