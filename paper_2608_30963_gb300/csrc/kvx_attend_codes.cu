@@ -23,7 +23,7 @@ cudaError_t launch_attend_codes(const AttendParams& P, int dtype, int num_sms, c
     *launches = 0;
     if (P.T == 0) return cudaSuccess;
     *launches = 2;
-    if (dtype == KVX_BF16) return P.cap > 0.0f ? run_codes<__nv_bfloat16, true>(P, num_sms, stream) : run_codes<__nv_bfloat16, false>(P, num_sms, stream);
+    if (dtype == KVX_BF16) return P.cap > 0.0f ? launch_attend_tc_codes_capped(P, num_sms, stream) : launch_attend_tc_codes(P, num_sms, stream);
     return P.cap > 0.0f ? run_codes<float, true>(P, num_sms, stream) : run_codes<float, false>(P, num_sms, stream);
 }
 

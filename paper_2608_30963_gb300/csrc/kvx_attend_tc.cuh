@@ -41,18 +41,19 @@
 namespace kvx {
 namespace {
 
-template <int D, int NT> struct TcShape {
+template <int D, int NT, bool CODES = false> struct TcShape {
     static constexpr int BM = 128 * NT, BN = NT == 1 ? 64 : 128, NB = 2 / NT;
     static constexpr bool COLS = D == 256;                 // the softmax warpgroups share every unit's columns
     static constexpr int STEP = COLS ? 1 : 2;              // a warpgroup's units: every, or every second
     static constexpr int OS = COLS ? 1 : 2;                // O accumulators
     static constexpr int TILE = BN * D * 2, QB = BM * D * 2;
     static constexpr int CTRL = 3072;                      // barriers and flags; what the warpgroups tell each other of rows
-    static constexpr int STAGES = (kSmemMax - CTRL - QB) / TILE < 12 ? (kSmemMax - CTRL - QB) / TILE : 12;
-    static constexpr int THREADS = 384;
+    static constexpr int RAW_DEPTH = 8, RAW = CODES ? 2 * 3 * 512 * RAW_DEPTH : 0;   // 8-bit caches: codes on their way to the producer warps
+    static constexpr int STAGES = (kSmemMax - CTRL - QB - RAW) / TILE < 12 ? (kSmemMax - CTRL - QB - RAW) / TILE : 12;
+    static constexpr int THREADS = CODES ? 512 : 384;
     static constexpr int S_COL = BN, O_COL = 2 * BN;       // TMEM columns: scores u mod 2, then the O tiles
     static constexpr int TMEM = 512;
-    static constexpr int SMEM = CTRL + QB + STAGES * TILE;
+    static constexpr int SMEM = CTRL + QB + STAGES * TILE + RAW;
     static_assert(SMEM <= kSmemMax && O_COL + OS * D <= TMEM);
     static_assert((kMaxAttendBatch + 2) * 8 <= STAGES * TILE);   // the plan's sums lie where the tiles come later
 };
@@ -80,6 +81,23 @@ constexpr int kFewSlots = 512;   // rows that see fewer slots get their weights 
 // sequence of 256 tokens among 63 without any takes 111 us where two row tiles would take 83.)
 __host__ __device__ __forceinline__ bool one_tile(const AttendParams& P) { return (long long)P.T * P.G <= 128ll * P.batch; }
 
+// Sixteen codes of a row of scale f as bf16, exactly: first and second eight.  (By way of fp32: moving exponent and mantissa to
+// bf16's places and multiplying there takes more instructions, and NaN codes and far scales more of them; 27 clocks of an SM
+// for 512 codes against 20.)
+__device__ __forceinline__ void row_bf16(uint4 w, float f, uint4& lo, uint4& hi)
+{
+    uint32_t v[8];
+    const uint32_t in[4] = {w.x, w.y, w.z, w.w};
+    const float2 f2 = make_float2(f, f);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float2 y = mul2(codes_f32((unsigned short)(in[i >> 1] >> (i & 1) * 16)), f2);
+        v[i] = pack_bf16(y.x, y.y);
+    }
+    lo = make_uint4(v[0], v[1], v[2], v[3]);
+    hi = make_uint4(v[4], v[5], v[6], v[7]);
+}
+
 // Whether an item's weights are multiplied in two terms: its first token sees fewest slots.
 template <int D, int NT> __device__ __forceinline__ bool two_terms(const AttendParams& P, const Segment& g)
 {
@@ -94,13 +112,13 @@ template <int D, int NT> __device__ __forceinline__ bool two_terms(const AttendP
 // How K and V tiles are brought: row by row (any page size), or in groups of 8 rows a fixed stride apart (contiguous caches
 // and page sizes that are multiples of 8: 4096 tokens over 32768 slots 1.13 ms against 1.35).  (Tensor copies, a box a page,
 // were slower: with pages of 16, 32 and 64 slots 2.06, 1.29 and 1.18 ms.)
-enum Source { kRows, kGroups };
+enum Source { kRows, kGroups, kCodes };
 
 template <int D, int NT, Source SRC, bool CAP>
-__global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
+__global__ void __launch_bounds__(TcShape<D, NT, SRC == kCodes>::THREADS, 1)
     attend_tc_kernel(const __grid_constant__ AttendParams P, const __grid_constant__ CUtensorMap q_map)
 {
-    using C = TcShape<D, NT>;
+    using C = TcShape<D, NT, SRC == kCodes>;
     using B = Bars<C::STAGES>;
     constexpr int BM = C::BM, BN = C::BN;
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -115,7 +133,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
     if (warp == kMmaWarp) tmem_alloc(smem_u32(tmem_slot), C::TMEM);
     if (threadIdx.x == 0) {
         for (int i = 0; i < C::STAGES; ++i) {
-            mbar_init(bar(B::full + i), 32);
+            mbar_init(bar(B::full + i), SRC == kCodes ? 2 : 32);
             mbar_init(bar(B::empty + i), 1);
         }
         for (int i = 0; i < 2; ++i) {
@@ -148,9 +166,161 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
     SegmentWalk<BN> walk(P, plan, state);
     Segment g;
 
-    if (warp < 4) {
-    regs_give<88>();
-    if (warp < kProdWarps) {
+    if (warp < 4 || warp >= 12) {
+    if constexpr (SRC == kCodes) regs_give<56>();
+    else regs_give<88>();
+    if (SRC == kCodes && warp != kMmaWarp) {
+        // ---------------------------------------------------------------- producers, 8-bit caches
+        // Three pairs of warps, a half of every third tile's rows each.  A lane's 16 codes come by an asynchronous copy into a
+        // place of its own (RAW_DEPTH of them, so that the copies run ahead over the tiles), become bf16 and go to the
+        // tile.  The writer orders them before the MMA's reads.
+        if constexpr (SRC == kCodes) {
+            if (warp < 15) {
+            constexpr int CPR = D / 16, RPI = 32 / CPR, HR = BN / 2;   // 16-code chunks of a row; rows of an instruction, of a warp
+            constexpr int NCH = HR / RPI, DEP = NCH < C::RAW_DEPTH ? NCH : C::RAW_DEPTH, LOOK = HR / 32;
+            const int third = warp < 3 ? warp : warp - 12, half = warp < 3 ? 0 : 1, sub = lane / CPR, chunk = lane % CPR;
+            const uint32_t raw = s0 + C::CTRL + C::QB + C::STAGES * C::TILE + (uint32_t)(half * 3 + third) * (512 * C::RAW_DEPTH) + (uint32_t)lane * 16;
+            // where the row's first and second eight values go: with 8 lanes or more a row, half the lanes take them the other way
+            // round, so that eight lanes' stores fall into different banks
+            const bool swap = D >= 128 && (lane & 4);
+            const uint32_t q0 = (uint32_t)(2 * chunk + (swap ? 1 : 0)), block = (q0 >> 3) * (uint32_t)(BN * 128), in0 = q0 & 7;
+            uint32_t pos = 0, items = 0;                 // tiles and items begun
+            uint32_t q_issued = 0;
+            bool ok = true;
+            auto wait = [&](int b, uint32_t parity) { ok = __all_sync(0xffffffffu, ok && W.wait(bar(b), parity)); };
+            while (walk.next(g)) {
+                if (warp == 0) {
+                    if (items > 0) wait(B::qempty, (items - 1) & 1);
+                    q_issued += ok;
+                    if (ok && elect_one()) {
+                        mbar_arrive_expect_tx(bar(B::qfull), (uint32_t)P.tile_rows * D * 2);
+#pragma unroll
+                        for (int cb = 0; cb < D / 64; ++cb)
+                            tma_box3(sQ + cb * (BM * 128), &q_map, cb * 64, g.h * P.G, g.s.t0 + g.rt * (P.tile_rows / P.G), bar(B::qfull));
+                    }
+                    __syncwarp();
+                }
+                ++items;
+                const long long head = cache_head(P.cache) * g.h + chunk * 16, shead = scale_head(P.cache, P.scales) * g.h;
+                const int total = 2 * g.n;
+                auto tile_of = [&](int r, int& kv) {
+                    if (C::NB == 1) {
+                        kv = r & 1;
+                        return r >> 1;
+                    }
+                    kv = r == total - 1 || (r > 0 && !(r & 1));
+                    return r == total - 1 ? g.n - 1 : kv ? (r >> 1) - 1 : (r + 1) >> 1;
+                };
+                auto first_slot = [&](int r, int& kv) { return g.kv.at(g.i0 + tile_of(r, kv)) * BN + half * HR; };
+                // pages of this warp's rows of tile r, a tile ahead of their use
+                auto pages_of = [&](int r, int (&x)[LOOK]) {
+                    int kv;
+                    const int j0 = r < total ? first_slot(r, kv) : g.s.L;
+#pragma unroll
+                    for (int k = 0; k < LOOK; ++k) {
+                        const int j = j0 + k * 32 + lane;
+                        x[k] = -2;                       // past the end
+                        if (j < g.s.L) {
+                            x[k] = 0;
+                            if (P.cache.paged) {
+                                const int pi = P.cache.page_shift >= 0 ? j >> P.cache.page_shift : j / P.cache.page_size;
+                                x[k] = pi < P.cache.max_pages ? P.cache.page_table[(size_t)g.b * P.cache.max_pages + pi] : -1;
+                            }
+                        }
+                    }
+                };
+                // where they lie (-1: zeros) and their scales
+                auto rows_of = [&](int r, const int (&page)[LOOK], long long (&at)[LOOK], uint32_t (&scale)[LOOK]) {
+                    int kv = 0;
+                    const int j0 = r < total ? first_slot(r, kv) : 0;
+                    const unsigned char* scales = kv ? P.v_scale : P.k_scale;
+#pragma unroll
+                    for (int k = 0; k < LOOK; ++k) {
+                        const int j = j0 + k * 32 + lane;
+                        at[k] = -1;
+                        scale[k] = 0;
+                        if (page[k] == -2) continue;
+                        long long z;
+                        if (!P.cache.paged) {
+                            at[k] = (long long)g.b * P.cache.sb + (long long)j * P.cache.st;
+                            z = (long long)g.b * P.scales.sb + j;
+                        } else {
+                            if (page[k] < 0 || page[k] >= P.cache.num_pages) {
+                                set_status(P.status, KVX_DEV_PAGE_INVALID);
+                                continue;
+                            }
+                            const int in = P.cache.page_shift >= 0 ? j & (P.cache.page_size - 1) : j % P.cache.page_size;
+                            at[k] = ((long long)page[k] * P.cache.page_size + in) * ((long long)P.cache.H * D);
+                            z = (long long)page[k] * P.cache.H * P.cache.page_size + in;
+                        }
+                        scale[k] = scales[z + shead];
+                    }
+                };
+                auto fetch = [&](const long long (&at)[LOOK], int kv, int c) {
+                    const uint8_t* src = (const uint8_t*)(kv ? P.cv : P.ck);
+                    const long long row = __shfl_sync(0xffffffffu, at[c * RPI / 32], c * RPI % 32 + sub);
+                    cp_async16_or_zero(raw + (uint32_t)(c % DEP) * 512, row < 0 ? src : src + row + head, row >= 0);
+                };
+                int page[LOOK];
+                long long at[LOOK], at2[LOOK];
+                uint32_t scale[LOOK], scale2[LOOK];
+                int r = (int)((kProdWarps + (uint32_t)third - pos % kProdWarps) % kProdWarps), kv = 0, kv2 = 0;
+                pages_of(r, page);
+                rows_of(r, page, at, scale);
+                pages_of(r + kProdWarps, page);
+                if (r < total) tile_of(r, kv);
+#pragma unroll
+                for (int c = 0; c < DEP; ++c) {
+                    if (r < total) fetch(at, kv, c);
+                    cp_async_commit();
+                }
+                for (; r < total; r += kProdWarps) {
+                    const uint32_t p = pos + (uint32_t)r, st = p % C::STAGES, ph = (p / C::STAGES) & 1;
+                    rows_of(r + kProdWarps, page, at2, scale2);
+                    pages_of(r + 2 * kProdWarps, page);
+                    const bool more = r + kProdWarps < total;
+                    if (more) tile_of(r + kProdWarps, kv2);
+                    wait(B::empty + (int)st, ph ^ 1);
+                    if (!ok) break;
+                    const uint32_t d0 = sT + st * C::TILE + block + (uint32_t)(half * HR + sub) * 128;
+#pragma unroll
+                    for (int c0 = 0; c0 < NCH; c0 += 2) {
+                        cp_async_wait<DEP - 2>();
+                        uint4 w[2];
+#pragma unroll
+                        for (int c = c0; c < c0 + 2; ++c) w[c - c0] = lds128(raw + (uint32_t)(c % DEP) * 512);
+#pragma unroll
+                        for (int c = c0; c < c0 + 2; ++c) {
+                            uint4 lo, hi;
+                            row_bf16(w[c - c0], scale_of(__shfl_sync(0xffffffffu, scale[c * RPI / 32], c * RPI % 32 + sub)), lo, hi);
+                            const uint32_t d = d0 + (uint32_t)(c * RPI) * 128, x = (uint32_t)((c * RPI + sub) & 7);
+                            sts128(d + ((in0 ^ x) << 4), swap ? hi : lo);
+                            sts128(d + ((in0 ^ 1 ^ x) << 4), swap ? lo : hi);
+                        }
+#pragma unroll
+                        for (int c = c0; c < c0 + 2; ++c) {
+                            if (c + DEP < NCH) fetch(at, kv, c + DEP);
+                            else if (more) fetch(at2, kv2, c + DEP - NCH);
+                            cp_async_commit();
+                        }
+                    }
+                    fence_proxy_async();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar(B::full + (int)st));
+#pragma unroll
+                    for (int k = 0; k < LOOK; ++k) {
+                        at[k] = at2[k];
+                        scale[k] = scale2[k];
+                    }
+                    kv = kv2;
+                }
+                pos += (uint32_t)total;
+            }
+            cp_async_wait_all();
+            if (!ok && warp == 0 && q_issued > 0) drain(bar(B::qfull), (q_issued - 1) & 1);
+            }
+        }
+    } else if (warp < kProdWarps) {
         // ---------------------------------------------------------------- producers
         constexpr int CPR = D / 8;                       // 16-byte chunks of a row
         constexpr int RPI = CPR < 32 ? 32 / CPR : 1;     // rows a warp copies with one instruction
@@ -294,7 +464,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
                 if (u == 0) wait(B::qfull, items & 1);
                 if (t == 0 && !(EARLY && u > 0)) wait(B::full + (int)st, (p / C::STAGES) & 1);
                 if (!ok) return;
-                if (t == 0 && !(EARLY && u > 0)) fence_proxy_async();
+                if (SRC != kCodes && t == 0 && !(EARLY && u > 0)) fence_proxy_async();
                 tc_fence_after();
                 const uint32_t d = tm + ((units + u) & 1) * C::S_COL;
                 // descriptors count 16-byte units in their low bits: steps along an operand are added
@@ -318,12 +488,12 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
                 if (EARLY && t == 0) {
                     wait(B::full + (int)st, (p / C::STAGES) & 1);
                     if (i + 1 < n) wait(B::full + (int)((p + 1) % C::STAGES), ((p + 1) / C::STAGES) & 1);
-                    fence_proxy_async();
+                    if (SRC != kCodes) fence_proxy_async();
                 }
                 wait(B::pfull + (int)(gu & 1), (gu >> 1) & 1);
                 if (!EARLY && t == 0) wait(B::full + (int)st, (p / C::STAGES) & 1);
                 if (!ok) break;
-                if (!EARLY && t == 0) fence_proxy_async();
+                if (SRC != kCodes && !EARLY && t == 0) fence_proxy_async();
                 tc_fence_after();
                 const uint64_t vd = mn_desc(sT + st * C::TILE, BN * 128);
                 const uint32_t wg = C::COLS ? 0 : gu & 1;
@@ -353,7 +523,8 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
     }
     } else {
         // ---------------------------------------------------------------- softmax
-        regs_take<208>();
+        if constexpr (SRC == kCodes) regs_take<200>();
+        else regs_take<208>();
         const int wg = (warp - 4) >> 2, t = NT == 2 ? wg : 0, quad = warp & 3;
         const uint32_t lanes = tmem + ((uint32_t)(quad * 32) << 16);
         const float inv_cap = CAP ? 1.0f / P.cap : 0.0f;
@@ -644,7 +815,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, 1)
 
 template <int D, int NT, Source SRC, bool CAP> cudaError_t start_tc(const AttendParams& P, const CUtensorMap& q_map, int num_sms, cudaStream_t stream)
 {
-    using C = TcShape<D, NT>;
+    using C = TcShape<D, NT, SRC == kCodes>;
     const int grid = min(num_sms, kAttendMaxRows / C::BM / 2);
     if (cudaError_t e = smem_opt_in<attend_tc_kernel<D, NT, SRC, CAP>>(C::SMEM); e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
@@ -660,7 +831,7 @@ template <int D, int NT, Source SRC, bool CAP> cudaError_t start_tc(const Attend
     if (cudaError_t e = cudaLaunchKernelEx(&cfg, attend_tc_kernel<D, NT, SRC, CAP>, P, q_map); e != cudaSuccess) return e;
     return run_join<__nv_bfloat16, D, C::BM>(P, grid, stream);
 }
-template <int D, int NT, bool CAP> cudaError_t run_tc(const AttendParams& call, int num_sms, cudaStream_t stream)
+template <int D, int NT, bool CAP, bool CODES> cudaError_t run_tc(const AttendParams& call, int num_sms, cudaStream_t stream)
 {
     using C = TcShape<D, NT>;
     AttendParams P = call;
@@ -673,15 +844,16 @@ template <int D, int NT, bool CAP> cudaError_t run_tc(const AttendParams& call, 
     if (!enc || enc(&q_map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(P.q), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
                     CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
         return cudaErrorInvalidValue;
-    if (!P.cache.paged || P.cache.page_size % 8 == 0) return start_tc<D, NT, kGroups, CAP>(P, q_map, num_sms, stream);
-    return start_tc<D, NT, kRows, CAP>(P, q_map, num_sms, stream);
+    if constexpr (CODES) return start_tc<D, NT, kCodes, CAP>(P, q_map, num_sms, stream);
+    else if (!P.cache.paged || P.cache.page_size % 8 == 0) return start_tc<D, NT, kGroups, CAP>(P, q_map, num_sms, stream);
+    else return start_tc<D, NT, kRows, CAP>(P, q_map, num_sms, stream);
 }
-template <bool CAP> cudaError_t run_attend_tc(const AttendParams& P, int num_sms, cudaStream_t stream)
+template <bool CAP, bool CODES = false> cudaError_t run_attend_tc(const AttendParams& P, int num_sms, cudaStream_t stream)
 {
     const bool one = one_tile(P);
-    if (P.d == 64) return one ? run_tc<64, 1, CAP>(P, num_sms, stream) : run_tc<64, 2, CAP>(P, num_sms, stream);
-    if (P.d == 128) return one ? run_tc<128, 1, CAP>(P, num_sms, stream) : run_tc<128, 2, CAP>(P, num_sms, stream);
-    return run_tc<256, 1, CAP>(P, num_sms, stream);
+    if (P.d == 64) return one ? run_tc<64, 1, CAP, CODES>(P, num_sms, stream) : run_tc<64, 2, CAP, CODES>(P, num_sms, stream);
+    if (P.d == 128) return one ? run_tc<128, 1, CAP, CODES>(P, num_sms, stream) : run_tc<128, 2, CAP, CODES>(P, num_sms, stream);
+    return run_tc<256, 1, CAP, CODES>(P, num_sms, stream);
 }
 
 }  // namespace

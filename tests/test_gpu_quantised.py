@@ -642,3 +642,21 @@ def test_refusals():
     assert kvx.lib().kvx_attend_quantised(p.dec.handle, ctypes.byref(tok), ctypes.byref(rows), c, 0, ctypes.byref(opts), ctypes.byref(rows),
                                           None) == kvx.KVX_ERR_UNSUPPORTED
     assert p.dec.device_status() == 0
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("d,G,n", [(128, 1, 256), (128, 6, 100), (64, 4, 256), (256, 2, 256), (128, 4, 3), (64, 2, 2), (256, 4, 1)])
+def test_a_single_seen_row_comes_back_exactly(dtype, d, G, n):
+    """Every code under every scale byte that is written (values up to 2^120): tokens that see their own slot alone return its V row."""
+    p = Problem(2, G, d, [0], [n], dtype, 16, seed=8)
+    g = torch.Generator().manual_seed(n)
+    p.code[0].zero_()                                    # scores of zero: weights of one
+    p.code[1] = torch.stack([torch.stack([torch.randint(0, 256, (d,), generator=g, dtype=torch.uint8) for _ in range(n)]) for _ in range(2)])[None]
+    p.byte[1] = torch.randint(10, 239, (1, 2, n), generator=g, dtype=torch.int64).to(torch.uint8)
+    out, lse = p.attend(window=1)
+    assert not lse.any()
+    want = value(p.code[1], p.byte[1])[0].transpose(0, 1).repeat_interleave(G, 1).to(p.tdt)       # [n, Hq, d]
+    assert torch.equal(out.isnan(), want.isnan())
+    fine = ~want.isnan()
+    tol = 2.0 ** -20 if dtype == "fp32" else 0.0         # (rows summed again have a weight within 2^-20 of one)
+    assert bool(((out[fine].double() - want[fine].double()).abs() <= tol * want[fine].double().abs()).all())
