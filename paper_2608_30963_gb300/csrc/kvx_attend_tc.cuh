@@ -48,7 +48,9 @@ template <int D, int NT, bool CODES = false> struct TcShape {
     static constexpr int OS = COLS ? 1 : 2;                // O accumulators
     static constexpr int TILE = BN * D * 2, QB = BM * D * 2;
     static constexpr int CTRL = 3072;                      // barriers and flags; what the warpgroups tell each other of rows
-    static constexpr int RAW_DEPTH = 8, RAW = CODES ? 2 * 3 * 512 * RAW_DEPTH : 0;   // 8-bit caches: codes on their way to the producer warps
+    // 8-bit caches: units of rows as codes (and their scales), which become bf16 tiles
+    static constexpr int RU = D == 256 ? 32 : D == 128 || NT == 1 ? 64 : 128, RAW_STAGES = 4, RAW_UNIT = RU * D, UNITS = BN / RU;
+    static constexpr int RAW = CODES ? RAW_STAGES * RAW_UNIT : 0, SCALES = D == 256 ? 256 : 2048;   // (their scales lie in the control block)
     static constexpr int STAGES = (kSmemMax - CTRL - QB - RAW) / TILE < 12 ? (kSmemMax - CTRL - QB - RAW) / TILE : 12;
     static constexpr int THREADS = CODES ? 512 : 384;
     static constexpr int S_COL = BN, O_COL = 2 * BN;       // TMEM columns: scores u mod 2, then the O tiles
@@ -133,7 +135,7 @@ __global__ void __launch_bounds__(TcShape<D, NT, SRC == kCodes>::THREADS, 1)
     if (warp == kMmaWarp) tmem_alloc(smem_u32(tmem_slot), C::TMEM);
     if (threadIdx.x == 0) {
         for (int i = 0; i < C::STAGES; ++i) {
-            mbar_init(bar(B::full + i), SRC == kCodes ? 2 : 32);
+            mbar_init(bar(B::full + i), SRC == kCodes ? 4 : 32);
             mbar_init(bar(B::empty + i), 1);
         }
         for (int i = 0; i < 2; ++i) {
@@ -141,6 +143,11 @@ __global__ void __launch_bounds__(TcShape<D, NT, SRC == kCodes>::THREADS, 1)
             mbar_init(bar(B::pfull + i), C::COLS ? 8 : 4);
             mbar_init(bar(B::ofull + i), 1);
         }
+        if (SRC == kCodes)
+            for (int i = 0; i < C::RAW_STAGES; ++i) {
+                mbar_init(bar(B::raw_full + i), 33);
+                mbar_init(bar(B::raw_empty + i), 4);
+            }
         mbar_init(bar(B::qfull), 1);
         mbar_init(bar(B::qempty), 1);
         mbar_init(bar(B::done), 1);
@@ -171,153 +178,150 @@ __global__ void __launch_bounds__(TcShape<D, NT, SRC == kCodes>::THREADS, 1)
     else regs_give<88>();
     if (SRC == kCodes && warp != kMmaWarp) {
         // ---------------------------------------------------------------- producers, 8-bit caches
-        // Three pairs of warps, a half of every third tile's rows each.  A lane's 16 codes come by an asynchronous copy into a
-        // place of its own (RAW_DEPTH of them, so that the copies run ahead over the tiles), become bf16 and go to the
-        // tile.  The writer orders them before the MMA's reads.
+        // Three warps copy units of RU rows as they are, with their scales, every third unit each; four turn them into bf16
+        // tiles, a quarter of every unit each.  (Warps that both copied and converted halves of every third tile spent most of
+        // their time on one another's latency: 304 us for 1024 tokens over 16384 slots.)
         if constexpr (SRC == kCodes) {
-            if (warp < 15) {
-            constexpr int CPR = D / 16, RPI = 32 / CPR, HR = BN / 2;   // 16-code chunks of a row; rows of an instruction, of a warp
-            constexpr int NCH = HR / RPI, DEP = NCH < C::RAW_DEPTH ? NCH : C::RAW_DEPTH, LOOK = HR / 32;
-            const int third = warp < 3 ? warp : warp - 12, half = warp < 3 ? 0 : 1, sub = lane / CPR, chunk = lane % CPR;
-            const uint32_t raw = s0 + C::CTRL + C::QB + C::STAGES * C::TILE + (uint32_t)(half * 3 + third) * (512 * C::RAW_DEPTH) + (uint32_t)lane * 16;
-            // where the row's first and second eight values go: with 8 lanes or more a row, half the lanes take them the other way
-            // round, so that eight lanes' stores fall into different banks
-            const bool swap = D >= 128 && (lane & 4);
-            const uint32_t q0 = (uint32_t)(2 * chunk + (swap ? 1 : 0)), block = (q0 >> 3) * (uint32_t)(BN * 128), in0 = q0 & 7;
-            uint32_t pos = 0, items = 0;                 // tiles and items begun
-            uint32_t q_issued = 0;
+            constexpr int CPR = D / 16, RPI = 32 / CPR, UNITS = C::UNITS;      // 16-code chunks of a row; rows of an instruction
+            const int sub = lane / CPR, chunk = lane % CPR;
+            const uint32_t sRaw = sT + C::STAGES * C::TILE;
+            static_assert(C::COLS ? 8 * (2 * C::STAGES + 19) <= C::SCALES && C::SCALES + C::RAW_STAGES * C::RU <= 512
+                                  : C::SCALES + C::RAW_STAGES * C::RU <= C::CTRL);
+            uint32_t pos = 0, items = 0;                 // units and items begun
             bool ok = true;
             auto wait = [&](int b, uint32_t parity) { ok = __all_sync(0xffffffffu, ok && W.wait(bar(b), parity)); };
-            while (walk.next(g)) {
-                if (warp == 0) {
-                    if (items > 0) wait(B::qempty, (items - 1) & 1);
-                    q_issued += ok;
-                    if (ok && elect_one()) {
-                        mbar_arrive_expect_tx(bar(B::qfull), (uint32_t)P.tile_rows * D * 2);
+            if (warp < kProdWarps) {
+                uint32_t q_issued = 0;
+                while (walk.next(g)) {
+                    if (warp == 0) {
+                        if (items > 0) wait(B::qempty, (items - 1) & 1);
+                        q_issued += ok;
+                        if (ok && elect_one()) {
+                            mbar_arrive_expect_tx(bar(B::qfull), (uint32_t)P.tile_rows * D * 2);
 #pragma unroll
-                        for (int cb = 0; cb < D / 64; ++cb)
-                            tma_box3(sQ + cb * (BM * 128), &q_map, cb * 64, g.h * P.G, g.s.t0 + g.rt * (P.tile_rows / P.G), bar(B::qfull));
+                            for (int cb = 0; cb < D / 64; ++cb)
+                                tma_box3(sQ + cb * (BM * 128), &q_map, cb * 64, g.h * P.G, g.s.t0 + g.rt * (P.tile_rows / P.G), bar(B::qfull));
+                        }
+                        __syncwarp();
                     }
-                    __syncwarp();
-                }
-                ++items;
-                const long long head = cache_head(P.cache) * g.h + chunk * 16, shead = scale_head(P.cache, P.scales) * g.h;
-                const int total = 2 * g.n;
-                auto tile_of = [&](int r, int& kv) {
-                    if (C::NB == 1) {
-                        kv = r & 1;
-                        return r >> 1;
-                    }
-                    kv = r == total - 1 || (r > 0 && !(r & 1));
-                    return r == total - 1 ? g.n - 1 : kv ? (r >> 1) - 1 : (r + 1) >> 1;
-                };
-                auto first_slot = [&](int r, int& kv) { return g.kv.at(g.i0 + tile_of(r, kv)) * BN + half * HR; };
-                // pages of this warp's rows of tile r, a tile ahead of their use
-                auto pages_of = [&](int r, int (&x)[LOOK]) {
-                    int kv;
-                    const int j0 = r < total ? first_slot(r, kv) : g.s.L;
+                    ++items;
+                    constexpr int LOOK = C::RU / 32;
+                    const long long head = cache_head(P.cache) * g.h + chunk * 16, shead = scale_head(P.cache, P.scales) * g.h;
+                    const int total = 2 * g.n, all = total * UNITS;
+                    // unit r of the item: its first slot, and whether it is of K or V
+                    auto first_slot = [&](int r, int& kv) {
+                        const int x = r / UNITS;
+                        kv = C::NB == 1 ? x & 1 : x == total - 1 || (x > 0 && !(x & 1));
+                        const int i = C::NB == 1 ? x >> 1 : x == total - 1 ? g.n - 1 : kv ? (x >> 1) - 1 : (x + 1) >> 1;
+                        return g.kv.at(g.i0 + i) * BN + (r - x * UNITS) * C::RU;
+                    };
+                    auto pages_of = [&](int r, int (&x)[LOOK]) {
+                        int kv;
+                        const int j0 = r < all ? first_slot(r, kv) : g.s.L;
 #pragma unroll
-                    for (int k = 0; k < LOOK; ++k) {
-                        const int j = j0 + k * 32 + lane;
-                        x[k] = -2;                       // past the end
-                        if (j < g.s.L) {
-                            x[k] = 0;
-                            if (P.cache.paged) {
-                                const int pi = P.cache.page_shift >= 0 ? j >> P.cache.page_shift : j / P.cache.page_size;
-                                x[k] = pi < P.cache.max_pages ? P.cache.page_table[(size_t)g.b * P.cache.max_pages + pi] : -1;
+                        for (int k = 0; k < LOOK; ++k) {
+                            const int j = j0 + k * 32 + lane;
+                            x[k] = -2;                   // past the end
+                            if (j < g.s.L) {
+                                x[k] = 0;
+                                if (P.cache.paged) {
+                                    const int pi = P.cache.page_shift >= 0 ? j >> P.cache.page_shift : j / P.cache.page_size;
+                                    x[k] = pi < P.cache.max_pages ? P.cache.page_table[(size_t)g.b * P.cache.max_pages + pi] : -1;
+                                }
                             }
                         }
-                    }
-                };
-                // where they lie (-1: zeros) and their scales
-                auto rows_of = [&](int r, const int (&page)[LOOK], long long (&at)[LOOK], uint32_t (&scale)[LOOK]) {
-                    int kv = 0;
-                    const int j0 = r < total ? first_slot(r, kv) : 0;
-                    const unsigned char* scales = kv ? P.v_scale : P.k_scale;
+                    };
+                    int page[LOOK];
+                    int r = (int)((kProdWarps + (uint32_t)warp - pos % kProdWarps) % kProdWarps);
+                    pages_of(r, page);
+                    for (; r < all; r += kProdWarps) {
+                        const uint32_t p = pos + (uint32_t)r, st = p % C::RAW_STAGES, ph = (p / C::RAW_STAGES) & 1;
+                        int kv;
+                        const int j0 = first_slot(r, kv);
+                        const uint8_t* src = (const uint8_t*)(kv ? P.cv : P.ck);
+                        const unsigned char* scales = kv ? P.v_scale : P.k_scale;
+                        long long at[LOOK];
+                        uint32_t scale[LOOK];
 #pragma unroll
-                    for (int k = 0; k < LOOK; ++k) {
-                        const int j = j0 + k * 32 + lane;
-                        at[k] = -1;
-                        scale[k] = 0;
-                        if (page[k] == -2) continue;
-                        long long z;
-                        if (!P.cache.paged) {
-                            at[k] = (long long)g.b * P.cache.sb + (long long)j * P.cache.st;
-                            z = (long long)g.b * P.scales.sb + j;
-                        } else {
-                            if (page[k] < 0 || page[k] >= P.cache.num_pages) {
-                                set_status(P.status, KVX_DEV_PAGE_INVALID);
-                                continue;
+                        for (int k = 0; k < LOOK; ++k) {
+                            const int j = j0 + k * 32 + lane;
+                            at[k] = -1;
+                            scale[k] = 0;
+                            if (page[k] == -2) continue;
+                            long long z;
+                            if (!P.cache.paged) {
+                                at[k] = (long long)g.b * P.cache.sb + (long long)j * P.cache.st;
+                                z = (long long)g.b * P.scales.sb + j;
+                            } else {
+                                if (page[k] < 0 || page[k] >= P.cache.num_pages) {
+                                    set_status(P.status, KVX_DEV_PAGE_INVALID);
+                                    continue;
+                                }
+                                const int in = P.cache.page_shift >= 0 ? j & (P.cache.page_size - 1) : j % P.cache.page_size;
+                                at[k] = ((long long)page[k] * P.cache.page_size + in) * ((long long)P.cache.H * D);
+                                z = (long long)page[k] * P.cache.H * P.cache.page_size + in;
                             }
-                            const int in = P.cache.page_shift >= 0 ? j & (P.cache.page_size - 1) : j % P.cache.page_size;
-                            at[k] = ((long long)page[k] * P.cache.page_size + in) * ((long long)P.cache.H * D);
-                            z = (long long)page[k] * P.cache.H * P.cache.page_size + in;
+                            scale[k] = scales[z + shead];
                         }
-                        scale[k] = scales[z + shead];
+                        pages_of(r + kProdWarps, page);
+                        wait(B::raw_empty + (int)st, ph ^ 1);
+                        if (!ok) break;
+                        const uint32_t d = sRaw + st * C::RAW_UNIT + (uint32_t)lane * 16;
+#pragma unroll 8
+                        for (int c = 0; c < C::RU / RPI; ++c) {
+                            const long long row = __shfl_sync(0xffffffffu, at[LOOK == 1 ? 0 : c * RPI / 32], c * RPI % 32 + sub);
+                            cp_async16_or_zero(d + (uint32_t)c * 512, row < 0 ? src : src + row + head, row >= 0);
+                        }
+                        cp_async_arrive(bar(B::raw_full + (int)st));
+#pragma unroll
+                        for (int k = 0; k < LOOK; ++k) smem[C::SCALES + st * C::RU + k * 32 + lane] = (uint8_t)scale[k];
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(bar(B::raw_full + (int)st));
                     }
-                };
-                auto fetch = [&](const long long (&at)[LOOK], int kv, int c) {
-                    const uint8_t* src = (const uint8_t*)(kv ? P.cv : P.ck);
-                    const long long row = __shfl_sync(0xffffffffu, at[c * RPI / 32], c * RPI % 32 + sub);
-                    cp_async16_or_zero(raw + (uint32_t)(c % DEP) * 512, row < 0 ? src : src + row + head, row >= 0);
-                };
-                int page[LOOK];
-                long long at[LOOK], at2[LOOK];
-                uint32_t scale[LOOK], scale2[LOOK];
-                int r = (int)((kProdWarps + (uint32_t)third - pos % kProdWarps) % kProdWarps), kv = 0, kv2 = 0;
-                pages_of(r, page);
-                rows_of(r, page, at, scale);
-                pages_of(r + kProdWarps, page);
-                if (r < total) tile_of(r, kv);
-#pragma unroll
-                for (int c = 0; c < DEP; ++c) {
-                    if (r < total) fetch(at, kv, c);
-                    cp_async_commit();
+                    pos += (uint32_t)all;
                 }
-                for (; r < total; r += kProdWarps) {
-                    const uint32_t p = pos + (uint32_t)r, st = p % C::STAGES, ph = (p / C::STAGES) & 1;
-                    rows_of(r + kProdWarps, page, at2, scale2);
-                    pages_of(r + 2 * kProdWarps, page);
-                    const bool more = r + kProdWarps < total;
-                    if (more) tile_of(r + kProdWarps, kv2);
-                    wait(B::empty + (int)st, ph ^ 1);
-                    if (!ok) break;
-                    const uint32_t d0 = sT + st * C::TILE + block + (uint32_t)(half * HR + sub) * 128;
+                cp_async_wait_all();
+                if (!ok && warp == 0 && q_issued > 0) drain(bar(B::qfull), (q_issued - 1) & 1);
+            } else {
+                constexpr int QR = C::RU / 4, N = QR / RPI;                    // rows of a unit that this warp has; its instructions
+                const int quarter = warp - 12;
+                // where a row's first and second eight values go: with 8 lanes or more a row, half the lanes take them the other
+                // way round, so that eight lanes' stores fall into different banks
+                const bool swap = D >= 128 && (lane & 4);
+                const uint32_t q0 = (uint32_t)(2 * chunk + (swap ? 1 : 0)), block = (q0 >> 3) * (uint32_t)(BN * 128), in0 = q0 & 7;
+                while (ok && walk.next(g)) {
+                    const int all = 2 * g.n * UNITS;
+                    for (int r = 0; r < all && ok; ++r, ++pos) {
+                        const uint32_t rs = pos % C::RAW_STAGES, p = pos / UNITS, st = p % C::STAGES;
+                        wait(B::raw_full + (int)rs, (pos / C::RAW_STAGES) & 1);
+                        if (pos % UNITS == 0) wait(B::empty + (int)st, ((p / C::STAGES) & 1) ^ 1);
+                        if (!ok) break;
+                        uint4 w[N];
+                        float f[N];
+                        const int row0 = quarter * QR + sub;
 #pragma unroll
-                    for (int c0 = 0; c0 < NCH; c0 += 2) {
-                        cp_async_wait<DEP - 2>();
-                        uint4 w[2];
+                        for (int c = 0; c < N; ++c) {
+                            w[c] = lds128(sRaw + rs * C::RAW_UNIT + (uint32_t)((quarter * N + c) * 512 + lane * 16));
+                            f[c] = scale_of(smem[C::SCALES + rs * C::RU + row0 + c * RPI]);
+                        }
+                        const uint32_t d = sT + st * C::TILE + block + (uint32_t)((int)(pos % UNITS) * C::RU + row0) * 128;
 #pragma unroll
-                        for (int c = c0; c < c0 + 2; ++c) w[c - c0] = lds128(raw + (uint32_t)(c % DEP) * 512);
-#pragma unroll
-                        for (int c = c0; c < c0 + 2; ++c) {
+                        for (int c = 0; c < N; ++c) {
                             uint4 lo, hi;
-                            row_bf16(w[c - c0], scale_of(__shfl_sync(0xffffffffu, scale[c * RPI / 32], c * RPI % 32 + sub)), lo, hi);
-                            const uint32_t d = d0 + (uint32_t)(c * RPI) * 128, x = (uint32_t)((c * RPI + sub) & 7);
-                            sts128(d + ((in0 ^ x) << 4), swap ? hi : lo);
-                            sts128(d + ((in0 ^ 1 ^ x) << 4), swap ? lo : hi);
+                            row_bf16(w[c], f[c], lo, hi);
+                            const uint32_t x = (uint32_t)((row0 + c * RPI) & 7);
+                            sts128(d + c * RPI * 128 + ((in0 ^ x) << 4), swap ? hi : lo);
+                            sts128(d + c * RPI * 128 + ((in0 ^ 1 ^ x) << 4), swap ? lo : hi);
                         }
-#pragma unroll
-                        for (int c = c0; c < c0 + 2; ++c) {
-                            if (c + DEP < NCH) fetch(at, kv, c + DEP);
-                            else if (more) fetch(at2, kv2, c + DEP - NCH);
-                            cp_async_commit();
+                        const bool last = pos % UNITS == UNITS - 1;
+                        if (last) fence_proxy_async();
+                        __syncwarp();
+                        if (lane == 0) {
+                            mbar_arrive(bar(B::raw_empty + (int)rs));
+                            if (last) mbar_arrive(bar(B::full + (int)st));
                         }
                     }
-                    fence_proxy_async();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(bar(B::full + (int)st));
-#pragma unroll
-                    for (int k = 0; k < LOOK; ++k) {
-                        at[k] = at2[k];
-                        scale[k] = scale2[k];
-                    }
-                    kv = kv2;
                 }
-                pos += (uint32_t)total;
-            }
-            cp_async_wait_all();
-            if (!ok && warp == 0 && q_issued > 0) drain(bar(B::qfull), (q_issued - 1) & 1);
             }
         }
     } else if (warp < kProdWarps) {
