@@ -16,13 +16,48 @@ template <typename T, bool CAP> cudaError_t run_codes(const AttendParams& P, int
                                                                              : run_codes<T, 256, CAP>(P, num_sms, stream);
 }
 
+// Prompts: every row tile of a (sequence, KV head) reads its slots again, so from some row tiles on the slots become bf16
+// once, in the workspace (64 MiB, where the call's cache may fit it), and the kernels of bf16 caches take them from there.
+// (One sequence, us so and with the codes converted by each tile: 7 query heads on each of 4 KV heads of 128 over 16384 slots,
+// 896 rows 62 and 57, 1792 rows 82 and 84, 7168 rows 212 and 247; heads of 256, whose tiles have 128 rows, 512 rows 58 and 56, 1024
+// rows 70 and 79; 4096 tokens over 32768 slots 1171 and 1568.)
+bool expands(const AttendParams& P)
+{
+    const int tile = P.d == 256 ? 128 : 256;
+    // (batch <= 1024, capacity <= 2^30: no product wraps)
+    return (long long)P.T * P.G > 6ll * tile * P.batch && (long long)P.batch * P.cache.capacity <= kAttendScores / ((long long)P.H * P.d);
+}
+cudaError_t attend_expanded(const AttendParams& call, int num_sms, cudaStream_t stream)
+{
+    AttendParams P = call;
+    __nv_bfloat16* k = reinterpret_cast<__nv_bfloat16*>(call.scores);
+    __nv_bfloat16* v = k + (long long)P.batch * P.H * P.cache.capacity * P.d;
+    if (cudaError_t e = launch_expand(call, k, v, num_sms, stream); e != cudaSuccess) return e;
+    P.ck = k;
+    P.cv = v;
+    P.k_scale = P.v_scale = nullptr;
+    P.scores = nullptr;
+    P.cache.paged = 0;
+    P.cache.page_table = nullptr;
+    P.cache.st = P.d;
+    P.cache.sh = (long long)P.cache.capacity * P.d;
+    P.cache.sb = P.cache.sh * P.H;
+    return launch_attend_tc(P, num_sms, stream);
+}
+
 }  // namespace
 
-cudaError_t launch_attend_codes(const AttendParams& P, int dtype, int num_sms, cudaStream_t stream, int* launches)
+cudaError_t launch_attend_codes(const AttendParams& call, int dtype, int num_sms, cudaStream_t stream, int* launches)
 {
     *launches = 0;
-    if (P.T == 0) return cudaSuccess;
+    if (call.T == 0) return cudaSuccess;
+    AttendParams P = call;
     *launches = 2;
+    if (dtype == KVX_BF16 && expands(P)) {
+        *launches = 3;
+        return attend_expanded(P, num_sms, stream);
+    }
+    P.scores = nullptr;                          // no weight sums
     if (dtype == KVX_BF16) return P.cap > 0.0f ? launch_attend_tc_codes_capped(P, num_sms, stream) : launch_attend_tc_codes(P, num_sms, stream);
     return P.cap > 0.0f ? run_codes<float, true>(P, num_sms, stream) : run_codes<float, false>(P, num_sms, stream);
 }

@@ -7,6 +7,7 @@
 // half and the 8 that lie half a head further on (append: the channels paired with them), so that every 16-byte load of
 // neighbouring lanes is contiguous and the row's largest magnitude takes 2 to 4 exchanges.
 #include "kvx_codes.cuh"
+#include "kvx_tc_common.cuh"
 
 namespace kvx {
 namespace {
@@ -116,6 +117,94 @@ __global__ void __launch_bounds__(kConvertThreads) convert_kernel(const __grid_c
     }
 }
 
+// The slots of an 8-bit layer that a call's tokens see, as bf16 rows [batch][H][capacity][D] in the workspace: whole tiles of
+// 128 slots, so that no tile of the attention that reads them holds what an earlier call left there.  Rows of pages that are
+// not in the pool are zeros.
+template <int D>
+__global__ void __launch_bounds__(kConvertThreads) expand_kernel(const __grid_constant__ AttendParams P, __nv_bfloat16* to_k, __nv_bfloat16* to_v)
+{
+    constexpr int LANES = D / 16, ROWS = 32 / LANES, U = 4;
+    extern __shared__ long long first[];             // groups of 32 slots before each sequence's
+    const int tid = threadIdx.x, lane = tid & 31, sub = lane / LANES, c = lane % LANES * 8;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    // slots [0, a) and [z, L) of a sequence, in tiles
+    auto range = [&](int b, int& a, int& z, int& L) {
+        const Seq s = load_seq(P, b);
+        L = s.L;
+        a = min((s.pre + 127) / 128 * 128, L);
+        z = max(max(window_lo(P, s.slot(0)), 0) / 128 * 128, a);
+        if (s.n == 0) a = z = L = 0;
+    };
+    for (int b = tid; b < P.batch; b += kConvertThreads) {
+        int a, z, L;
+        range(b, a, z, L);
+        first[b + 1] = (a + 31) / 32 + (max(L - z, 0) + 31) / 32;
+    }
+    if (tid == 0) first[0] = 0;
+    __syncthreads();
+    if (tid == 0)
+        for (int b = 0; b < P.batch; ++b) first[b + 1] += first[b];
+    __syncthreads();
+    const long long groups = first[P.batch], total = groups * 2 * P.H, warps = (long long)gridDim.x * (kConvertThreads / 32);
+    for (long long i = (long long)blockIdx.x * (kConvertThreads / 32) + (tid >> 5); i < total; i += warps) {
+        // heads one after the other: a token's lie side by side in a pool
+        const long long g = i / (2 * P.H);
+        const int hk = (int)(i - g * (2 * P.H)), h = hk >> 1;
+        const bool key = !(hk & 1);
+        int lo = 0, hi = P.batch - 1;                // the sequence of group g
+        while (lo < hi) {
+            const int m = (lo + hi + 1) >> 1;
+            if (first[m] <= g) lo = m; else hi = m - 1;
+        }
+        const int b = lo;
+        int a, z, L;
+        range(b, a, z, L);
+        const int k = (int)(g - first[b]), s0 = k < (a + 31) / 32 ? k * 32 : z + (k - (a + 31) / 32) * 32, s = s0 + lane;
+        long long code = -1;
+        float scale = 0.0f;
+        if (s < L) {
+            const CodePlace at = code_place(P.cache, P.scales, b, s);
+            if (at.row < 0) {
+                set_status(P.status, KVX_DEV_PAGE_INVALID);
+            } else {
+                code = at.row + cache_head(P.cache) * h;
+                scale = scale_of((key ? P.k_scale : P.v_scale)[at.scale + scale_head(P.cache, P.scales) * h]);
+            }
+        }
+        const uint8_t* cp = (const uint8_t*)(key ? P.ck : P.cv);
+        __nv_bfloat16* out = (key ? to_k : to_v) + (((long long)b * P.H + h) * P.cache.capacity + s0) * D;
+#pragma unroll 1
+        for (int k0 = 0; k0 < 32; k0 += U * ROWS) {
+            uint2 x[U], y[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const long long w = __shfl_sync(0xffffffffu, code, k0 + u * ROWS + sub);
+                x[u] = y[u] = make_uint2(0u, 0u);
+                if (w >= 0) {
+                    x[u] = *reinterpret_cast<const uint2*>(cp + w + c);
+                    y[u] = *reinterpret_cast<const uint2*>(cp + w + D / 2 + c);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int r = k0 + u * ROWS + sub;
+                const float f = __shfl_sync(0xffffffffu, scale, r);
+                if (s0 + r < L) {
+                    float p[8], q[8];
+                    unpack_codes(x[u], f, p);
+                    unpack_codes(y[u], f, q);
+                    uint4 v;
+                    v = make_uint4(pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3]), pack_bf16(p[4], p[5]), pack_bf16(p[6], p[7]));
+                    *reinterpret_cast<uint4*>(out + (long long)r * D + c) = v;
+                    v = make_uint4(pack_bf16(q[0], q[1]), pack_bf16(q[2], q[3]), pack_bf16(q[4], q[5]), pack_bf16(q[6], q[7]));
+                    *reinterpret_cast<uint4*>(out + (long long)r * D + D / 2 + c) = v;
+                }
+            }
+        }
+    }
+}
+
 // heads: query heads, then K heads, then V heads; blockIdx.y takes `per` of them.  A thread has one chunk of 8 channels of a
 // token's heads and the chunk paired with it, whose sines are taken once.
 template <typename T, int D>
@@ -194,6 +283,21 @@ template <typename T, bool TO_CODES> cudaError_t run_convert(const ConvertParams
     return P.d == 64 ? run_convert<T, 64, TO_CODES>(P, num_sms, stream) : P.d == 128 ? run_convert<T, 128, TO_CODES>(P, num_sms, stream)
                                                                                      : run_convert<T, 256, TO_CODES>(P, num_sms, stream);
 }
+template <int D> cudaError_t run_expand(const AttendParams& P, void* to_k, void* to_v, int num_sms, cudaStream_t stream)
+{
+    const long long groups = ((long long)P.cache.capacity + 63) / 32 * P.batch * P.H * 2;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)min((groups + kConvertThreads / 32 - 1) / (kConvertThreads / 32), (long long)num_sms * 8));
+    cfg.blockDim = dim3(kConvertThreads);
+    cfg.dynamicSmemBytes = (P.batch + 1) * sizeof(long long);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, expand_kernel<D>, P, (__nv_bfloat16*)to_k, (__nv_bfloat16*)to_v);
+}
 template <typename T> cudaError_t run_append(const AppendParams& P, dim3 grid, int per, cudaStream_t stream)
 {
     if (P.d == 64) append_codes_kernel<T, 64><<<grid, kAppendThreads, 0, stream>>>(P, per);
@@ -208,6 +312,12 @@ cudaError_t launch_convert(const ConvertParams& P, bool to_codes, int dtype, int
 {
     if (dtype == KVX_BF16) return to_codes ? run_convert<__nv_bfloat16, true>(P, num_sms, stream) : run_convert<__nv_bfloat16, false>(P, num_sms, stream);
     return to_codes ? run_convert<float, true>(P, num_sms, stream) : run_convert<float, false>(P, num_sms, stream);
+}
+
+cudaError_t launch_expand(const AttendParams& P, void* to_k, void* to_v, int num_sms, cudaStream_t stream)
+{
+    return P.d == 64 ? run_expand<64>(P, to_k, to_v, num_sms, stream) : P.d == 128 ? run_expand<128>(P, to_k, to_v, num_sms, stream)
+                                                                               : run_expand<256>(P, to_k, to_v, num_sms, stream);
 }
 
 cudaError_t launch_append_codes(const AppendParams& P, int dtype, cudaStream_t stream)

@@ -151,6 +151,7 @@ cudaError_t launch_sum_scores(const AttendParams& P, cudaStream_t stream);
 cudaError_t launch_key_weight(const AttendParams& P, int num_sms, cudaStream_t stream);
 cudaError_t launch_attend_tc_capped(const AttendParams& P, int num_sms, cudaStream_t stream);
 cudaError_t launch_attend_tc(const AttendParams& P, int num_sms, cudaStream_t stream);
+cudaError_t launch_expand(const AttendParams& P, void* to_k, void* to_v, int num_sms, cudaStream_t stream);
 cudaError_t launch_attend_tc_codes_capped(const AttendParams& P, int num_sms, cudaStream_t stream);
 cudaError_t launch_attend_tc_codes(const AttendParams& P, int num_sms, cudaStream_t stream);
 cudaError_t launch_attend(const AttendParams& P, int dtype, int num_sms, cudaStream_t stream, int* launches);
