@@ -27,6 +27,14 @@ bool expands(const AttendParams& P)
     // (batch <= 1024, capacity <= 2^30: no product wraps)
     return (long long)P.T * P.G > 6ll * tile * P.batch && (long long)P.batch * P.cache.capacity <= kAttendScores / ((long long)P.H * P.d);
 }
+// Few rows: the tile's rows (8, 16 or 32) that take the call's mean a sequence and KV head in whole tokens, or 0.
+int few_rows(const AttendParams& P)
+{
+    if (P.d == 64) return 0;
+    for (int r = 8; r <= 32; r *= 2)
+        if (P.G <= r && (long long)P.T * P.G <= (long long)(r / P.G * P.G) * P.batch) return r;
+    return 0;
+}
 cudaError_t attend_expanded(const AttendParams& call, int num_sms, cudaStream_t stream)
 {
     AttendParams P = call;
@@ -58,6 +66,8 @@ cudaError_t launch_attend_codes(const AttendParams& call, int dtype, int num_sms
         return attend_expanded(P, num_sms, stream);
     }
     P.scores = nullptr;                          // no weight sums
+    if (const int rows = dtype == KVX_BF16 ? few_rows(P) : 0)
+        return P.cap > 0.0f ? launch_attend_few_capped(P, rows, num_sms, stream) : launch_attend_few(P, rows, num_sms, stream);
     if (dtype == KVX_BF16) return P.cap > 0.0f ? launch_attend_tc_codes_capped(P, num_sms, stream) : launch_attend_tc_codes(P, num_sms, stream);
     return P.cap > 0.0f ? run_codes<float, true>(P, num_sms, stream) : run_codes<float, false>(P, num_sms, stream);
 }

@@ -1,0 +1,619 @@
+// kvx_attend_few.cuh -- attention of few new tokens over an 8-bit cache on the tensor cores, its codes multiplied as they are
+// (library-internal; tcgen05 kind::f8f6f4).  Compiled twice, with and without the capped scores' code.
+//
+//   S^T = K (Qh + Ql / 16)^T,   P = exp2(f S^T - m),   O^T += V^T (P1 + P2 / 16 + P3 / 256)
+// With few rows (query heads of a token) the products have room to spare, and what costs is bringing K and V: so the
+// cache's codes are the operands, straight from memory, and the other side is split into e4m3 terms that make up for its
+// 4 bits.  A query row is scaled by a power of two and split in two (bf16's 8 bits exactly, down to 2^-14 of the row's largest
+// value, below that to 2^-22 of it), a weight in three (to 2^-12 of itself, 2^-25 of the row's largest).  Terms lie side by
+// side as columns of one product; sums are fp32.  Slots are the rows of S^T and channels those of O^T, so the rows of a tile
+// are its columns: 128 slots by 8, 16 or 32 rows.
+//   copying warps (7)   128-byte blocks of K and V rows into 128-byte-swizzled tiles, every seventh each
+//   MMA warp            tile i: S(i) into buffer i mod 2; O of warpgroup i mod 2 += V P(i) when P(i) is there
+//   softmax warps (8)   two warpgroups, every other tile each; a thread has a slot.  A score x takes its K row's scale; a weight
+//                       takes its V row's, in its exponent, z = x + log2 of it, and a reference n of its own beside the sums'
+//                       reference m, so that far scales do not leave e4m3's range.  A row takes new references when x or z
+//                       has grown by more than 1 (a factor of two) beyond them; each warpgroup has its own references, sums
+//                       and O, joined at the end.
+// The last rows of the split work are joined as those of the other attention kernels.
+#pragma once
+
+#include "kvx_attend_rows.cuh"
+#include "kvx_kernels.h"
+#include "kvx_umma.cuh"
+
+namespace kvx {
+namespace {
+
+template <int D, int R> struct FewShape {
+    static constexpr int BN = 128, DB = D / 128;               // slots a tile; 128-channel blocks of a head
+    static constexpr int NQ = 2 * R, NP = R == 8 ? 32 : 3 * R;  // columns of S^T and of O^T (a multiple of 16)
+    static constexpr int UNIT = BN * 128;                      // a block of a K or V tile
+    static constexpr int CTRL = 7168, QB = NQ * 128 * DB, PB = NP * 128;
+    static constexpr int FIT = (kSmemMax - CTRL - QB - 2 * PB) / UNIT, STAGES = FIT < 12 ? FIT : 12;
+    static constexpr int SMEM = CTRL + STAGES * UNIT + QB + 2 * PB;
+    static constexpr int THREADS = 512, COPY = 7;
+    static constexpr int O_COL = 2 * NQ;                       // TMEM columns: S^T of even and odd tiles, then O^T of each
+    static constexpr int USED = O_COL + 2 * NP * DB, TMEM = USED <= 128 ? 128 : USED <= 256 ? 256 : 512;
+    static_assert(SMEM <= kSmemMax && USED <= 512 && COPY <= STAGES);
+    static_assert((kMaxAttendBatch + 2) * 8 <= STAGES * UNIT);
+    // the control block: barriers up to 512, plan and states up to 1024, then rows' tables
+    static constexpr int SEES = 1024, REF = SEES + 32 * 16, LESS = REF + 2 * 32 * 16, RED = LESS + 2 * 32 * 8, SUM = RED + 2 * 4 * 32 * 8,
+                         BAD = SUM + 2 * 4 * 32 * 4;
+    static_assert(BAD + 8 * 4 <= CTRL);
+};
+
+// D[tmem] (+)= A[smem] . B[smem], e4m3 inputs, fp32 accumulate
+__device__ __forceinline__ void umma_e4m3(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+        "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+// N columns of the warp's lanes
+template <int N> __device__ __forceinline__ void tmem_load(uint32_t at, uint32_t (&v)[N])
+{
+    if constexpr (N == 32) tmem_ld32(at, v);
+    else if constexpr (N == 16) tmem_ld16(at, v);
+    else if constexpr (N == 8) tmem_ld8(at, v);
+    else asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(at));
+}
+template <int N> __device__ __forceinline__ void tmem_store(uint32_t at, const uint32_t (&v)[N])
+{
+    if constexpr (N == 32) tmem_st32(at, v);
+    else if constexpr (N == 16) tmem_st16(at, v);
+    else
+        asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(at), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]),
+                     "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+                     : "memory");
+}
+// Two values rounded to e4m3 and what they leave.
+__device__ __forceinline__ uint32_t take_term(float2& y)
+{
+    const uint32_t t = to_codes(y.x, y.y);
+    const float2 f = codes_f32((unsigned short)t);
+    y.x = (y.x - f.x) * 16.0f;
+    y.y = (y.y - f.y) * 16.0f;
+    return t;
+}
+
+// A row of a tile sees the slots [lo, hi) and [0, pre).
+struct __align__(16) FewSees {
+    int lo, hi, pre;
+};
+// The factor of its scores, and a warpgroup's references of x and z (log2 units; not infinite, so that differences are numbers).
+struct __align__(16) FewRef {
+    float f, m, n;
+};
+constexpr float kNoRef = -3.0e38f;
+
+template <int D, int R, bool GROUPS, bool CAP>
+__global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constant__ AttendParams P)
+{
+    using C = FewShape<D, R>;
+    constexpr int BN = C::BN, DB = C::DB;
+    extern __shared__ __align__(1024) uint8_t smem[];
+    const uint32_t s0 = smem_u32(smem);
+    constexpr int kFull = 0, kEmpty = C::STAGES, kS = 2 * C::STAGES, kP = kS + 2, kO = kP + 2, kQ = kO + 2, kDone = kQ + 1;
+    auto bar = [&](int i) { return s0 + (uint32_t)i * 8; };
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + 512);
+    int* abort = reinterpret_cast<int*>(smem + 516);
+    int* beat = reinterpret_cast<int*>(smem + 520);
+    const uint32_t sT = s0 + C::CTRL, sQ = sT + C::STAGES * C::UNIT, sP = sQ + C::QB;
+    const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+
+    if (warp == 3) tmem_alloc(smem_u32(tmem_slot), C::TMEM);
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < C::STAGES; ++i) {
+            mbar_init(bar(kFull + i), 32);
+            mbar_init(bar(kEmpty + i), 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(bar(kS + i), 1);
+            mbar_init(bar(kP + i), 4);
+            mbar_init(bar(kO + i), 1);
+        }
+        mbar_init(bar(kQ), 8);
+        mbar_init(bar(kDone), 1);
+        fence_mbar_init();
+        *abort = 0;
+        *beat = 0;
+    }
+    // the kernel before this one may still be ending: what it wrote is read from here on
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const Plan mine_plan = make_plan<BN, C::THREADS>(P, reinterpret_cast<long long*>(smem + C::CTRL));
+    Plan* plan = reinterpret_cast<Plan*>(smem + 544);
+    if (threadIdx.x == 0) *plan = mine_plan;
+    WalkState* state = reinterpret_cast<WalkState*>(smem + 640) + warp;
+    static_assert(sizeof(Plan) <= 96 && sizeof(WalkState) * (C::THREADS / 32) <= 1024 - 640);
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    const BeatWaiter W{abort, beat, P.status};
+    SegmentWalk<BN> walk(P, plan, state);
+    Segment g;
+    bool ok = true;
+    auto wait = [&](int b, uint32_t parity) { ok = __all_sync(0xffffffffu, ok && W.wait(bar(b), parity)); };
+
+    if (warp < 4 || warp >= 12) {
+        regs_give<56>();
+        if (warp != 3) {
+            // ---------------------------------------------------------------- copies
+            const int me = warp < 3 ? warp : warp - 9, sub = lane >> 3;        // a row of an instruction: 8 lanes
+            const uint32_t c0 = (uint32_t)(((lane & 7) ^ sub) << 4);
+            uint32_t pos = 0;                            // units of the items before
+            constexpr int PER = GROUPS ? 8 : 1, FIND = BN / PER, LOOK = (FIND + 31) / 32;
+            const long long stride = P.cache.paged ? (long long)P.cache.H * D : P.cache.st;
+            while (walk.next(g)) {
+                const int total = 2 * g.n, all = total * DB;
+                const long long mine = cache_head(P.cache) * g.h + (PER > 1 ? sub * stride : 0) + (lane & 7) * 16;
+                // unit r of the item in the order of the ring: a block of K or V and its slot tile
+                auto tile_of = [&](int r, int& kv) {
+                    const int x = r / DB;
+                    kv = x == total - 1 || (x > 0 && !(x & 1));
+                    return g.kv.at(g.i0 + (x == total - 1 ? g.n - 1 : kv ? (x >> 1) - 1 : (x + 1) >> 1)) * BN;
+                };
+                auto pages_of = [&](int r, int (&x)[LOOK]) {
+                    int kv;
+                    const int j0 = r < all ? tile_of(r, kv) : g.s.L;
+#pragma unroll
+                    for (int k = 0; k < LOOK; ++k) {
+                        const int j = j0 + (k * 32 + lane) * PER;
+                        x[k] = -2;                       // past the end
+                        if (k * 32 + lane < FIND && j < g.s.L) {
+                            x[k] = 0;
+                            if (P.cache.paged) {
+                                const int pi = P.cache.page_shift >= 0 ? j >> P.cache.page_shift : j / P.cache.page_size;
+                                x[k] = pi < P.cache.max_pages ? P.cache.page_table[(size_t)g.b * P.cache.max_pages + pi] : -1;
+                            }
+                        }
+                    }
+                };
+                auto row_at = [&](int j, int page) -> long long {
+                    if (page == -2) return -1;
+                    if (!P.cache.paged) return (long long)g.b * P.cache.sb + (long long)j * P.cache.st;
+                    if (page < 0 || page >= P.cache.num_pages) {
+                        set_status(P.status, KVX_DEV_PAGE_INVALID);
+                        return -1;
+                    }
+                    const int in = P.cache.page_shift >= 0 ? j & (P.cache.page_size - 1) : j % P.cache.page_size;
+                    return ((long long)page * P.cache.page_size + in) * stride;
+                };
+                int next[LOOK];
+                int r = (int)((C::COPY + (uint32_t)me - pos % C::COPY) % C::COPY);
+                pages_of(r, next);
+                for (; r < all; r += C::COPY) {
+                    int kv;
+                    const int j0 = tile_of(r, kv);
+                    const uint8_t* src = (const uint8_t*)(kv ? P.cv : P.ck) + (r % DB) * 128;
+                    const uint32_t p = pos + (uint32_t)r, st = p % C::STAGES, ph = (p / C::STAGES) & 1;
+                    long long at[LOOK];
+#pragma unroll
+                    for (int k = 0; k < LOOK; ++k) at[k] = row_at(j0 + (k * 32 + lane) * PER, next[k]);
+                    pages_of(r + C::COPY, next);
+                    wait(kEmpty + (int)st, ph ^ 1);
+                    if (!ok) break;
+                    const uint32_t d0 = sT + st * C::UNIT + (uint32_t)sub * 128;
+                    if constexpr (GROUPS) {
+#pragma unroll 4
+                        for (int q = 0; q < BN / 8; ++q) {
+                            const long long first = __shfl_sync(0xffffffffu, at[0], q);
+                            const int left = g.s.L - (j0 + q * 8);
+                            const uint8_t* s1 = src + first + mine;
+#pragma unroll
+                            for (int k = 0; k < 8; k += 4) {
+                                const bool real = first >= 0 && k + sub < left;
+                                cp_async16_or_zero(d0 + (uint32_t)(q * 1024 + k * 128) + (c0 ^ (uint32_t)(k << 4)), real ? s1 + k * stride : src, real);
+                            }
+                        }
+                    } else {
+#pragma unroll 4
+                        for (int k = 0; k < BN; k += 4) {
+                            const long long row = __shfl_sync(0xffffffffu, at[k / 32], (k & 31) + sub);
+                            cp_async16_or_zero(d0 + (uint32_t)k * 128 + (c0 ^ (uint32_t)((k & 7) << 4)), row < 0 ? src : src + row + mine, row >= 0);
+                        }
+                    }
+                    cp_async_arrive(bar(kFull + (int)st));
+                }
+                pos += (uint32_t)all;
+            }
+            cp_async_wait_all();
+        } else {
+            // ---------------------------------------------------------------- MMA
+            constexpr uint32_t idesc_s = (1u << 4) | ((uint32_t)(C::NQ >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+            constexpr uint32_t idesc_o = (1u << 4) | (1u << 15) | ((uint32_t)(C::NP >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+            const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+            uint32_t base = 0, tiles = 0, items = 0;     // units and tiles of the items before; items begun
+            while (ok && walk.next(g)) {
+                const int n = __shfl_sync(0xffffffffu, g.n, 0);
+                wait(kQ, items & 1);
+                auto scores = [&](int i) {
+                    const uint32_t p = base + (uint32_t)(i == 0 ? 0 : 2 * i - 1) * DB, d = tm + ((tiles + i) & 1) * C::NQ;
+#pragma unroll
+                    for (int b = 0; b < DB; ++b) wait(kFull + (int)((p + b) % C::STAGES), ((p + b) / C::STAGES) & 1);
+                    if (!ok) return;
+                    fence_proxy_async();
+                    tc_fence_after();
+                    if (elect_one()) {
+#pragma unroll
+                        for (int b = 0; b < DB; ++b) {
+                            const uint64_t kd = sw128_desc(sT + (p + b) % C::STAGES * C::UNIT), qd = sw128_desc(sQ + b * (C::NQ * 128));
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) umma_e4m3(d, kd + k * 2, qd + k * 2, idesc_s, b > 0 || k > 0);
+                            umma_commit(bar(kEmpty + (int)((p + b) % C::STAGES)));
+                        }
+                        umma_commit(bar(kS + (int)((tiles + i) & 1)));
+                    }
+                    __syncwarp();
+                };
+                scores(0);
+                if (n > 1) scores(1);
+                for (int i = 0; i < n && ok; ++i) {
+                    const uint32_t gu = tiles + (uint32_t)i, wg = gu & 1;
+                    const uint32_t p = base + (uint32_t)(i == n - 1 ? 2 * i + 1 : 2 * i + 2) * DB;
+#pragma unroll
+                    for (int b = 0; b < DB; ++b) wait(kFull + (int)((p + b) % C::STAGES), ((p + b) / C::STAGES) & 1);
+                    fence_proxy_async();
+                    wait(kP + (int)wg, (gu >> 1) & 1);
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (elect_one()) {
+                        const uint64_t pd = sw128_desc(sP + wg * C::PB);
+#pragma unroll
+                        for (int b = 0; b < DB; ++b) {
+                            const uint64_t vd = mn_desc(sT + (p + b) % C::STAGES * C::UNIT, C::UNIT);
+                            const uint32_t od = tm + C::O_COL + (wg * DB + b) * C::NP;
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) umma_e4m3(od, vd + k * (4096 / 16), pd + k * 2, idesc_o, i >= 2 || k > 0);
+                            umma_commit(bar(kEmpty + (int)((p + b) % C::STAGES)));
+                        }
+                        umma_commit(bar(kO + (int)wg));
+                    }
+                    __syncwarp();
+                    if (i + 2 < n) scores(i + 2);
+                }
+                base += 2 * (uint32_t)n * DB;
+                tiles += (uint32_t)n;
+                ++items;
+            }
+            // every MMA issued has completed before TMEM is freed
+            if (elect_one()) umma_commit(bar(kDone));
+            const unsigned long long t0 = globaltimer();
+            while (!mbar_try_wait(bar(kDone), 0) && globaltimer() - t0 < kWaitNs) {}
+            __syncwarp();
+        }
+    } else {
+        // ---------------------------------------------------------------- softmax
+        regs_take<200>();
+        const int sw = warp - 4, wg = sw >> 2, quad = warp & 3, slot = quad * 32 + lane;
+        const uint32_t lanes = tmem + ((uint32_t)(quad * 32) << 16);
+        const float inv_cap = CAP ? 1.0f / P.cap : 0.0f;
+        FewSees* sees_of = reinterpret_cast<FewSees*>(smem + C::SEES);           // [32]
+        FewRef* refs = reinterpret_cast<FewRef*>(smem + C::REF);                 // [warpgroup][32]
+        FewRef* ref = refs + wg * 32;
+        float2* less = reinterpret_cast<float2*>(smem + C::LESS) + wg * 32;      // what sums and O are multiplied by
+        float2* red = reinterpret_cast<float2*>(smem + C::RED) + wg * 4 * 32;    // [warp][32]
+        float* sums = reinterpret_cast<float*>(smem + C::SUM);                   // [warpgroup][warp][32]
+        uint32_t* bad = reinterpret_cast<uint32_t*>(smem + C::BAD);              // [warp]
+        // where this thread's bytes of P go: row n at n * 128, its 16-byte chunks exchanged by n & 7
+        uint8_t* p_row = smem + (sP - s0) + wg * C::PB;
+        const uint32_t p_chunk = (uint32_t)(slot >> 4), p_in = (uint32_t)(slot & 15);
+        uint32_t tiles = 0, done = 0;                    // tiles of the items before; products of this warpgroup waited for
+        bool have = false;
+        while (walk.next(g)) {
+            have = true;
+            const int ta = g.rt * (P.tile_rows / P.G), rows = min(P.tile_rows, (g.s.n - ta) * P.G);
+            const long long shead = scale_head(P.cache, P.scales) * g.h;
+            // the queries' terms, a row a warp, and what the rows see
+            for (int r = sw; r < R; r += 8) {
+                constexpr int CH = D / 32;               // channels of a lane
+                float q[CH];
+                const RowId id = row_id(P, g.s, g.h, g.rt * P.tile_rows + r);
+#pragma unroll
+                for (int c = 0; c < CH; ++c) q[c] = 0.0f;
+                if (r < rows) load_f32<__nv_bfloat16, CH>((const __nv_bfloat16*)P.q + (long long)(g.s.t0 + id.t) * P.q_t + (long long)id.head * P.q_h + lane * CH, q);
+                float top = 0.0f;
+#pragma unroll
+                for (int c = 0; c < CH; ++c) {
+                    if (!(fabsf(q[c]) <= 3.402823466e38f)) q[c] = __uint_as_float(0x7fffffffu);   // (an infinity makes its scores NaN)
+                    top = fmaxf(top, fabsf(q[c]));
+                }
+#pragma unroll
+                for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                const unsigned s = scale_for(top);
+                const float inv = inv_scale(s);
+                uint32_t hi[CH / 4], lo[CH / 4];
+#pragma unroll
+                for (int c = 0; c < CH; c += 2) {
+                    float2 y = make_float2(q[c] * inv, q[c + 1] * inv);
+                    const uint32_t h = take_term(y), l = to_codes(y.x, y.y);
+                    if (c % 4 == 0) {
+                        hi[c / 4] = h;
+                        lo[c / 4] = l;
+                    } else {
+                        hi[c / 4] |= h << 16;
+                        lo[c / 4] |= l << 16;
+                    }
+                }
+                const int ch = lane * CH, block = ch >> 7, chunk = (ch & 127) >> 4, in = ch & 15;
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    const int n = t * R + r;
+                    uint32_t* to = reinterpret_cast<uint32_t*>(smem + (sQ - s0) + block * (C::NQ * 128) + n * 128 + ((chunk ^ (n & 7)) << 4) + in);
+#pragma unroll
+                    for (int c = 0; c < CH / 4; ++c) to[c] = t ? lo[c] : hi[c];
+                }
+                if (lane == 0) {
+                    const int own = g.s.slot(id.t);
+                    const bool real = r < rows;
+                    sees_of[r] = {real ? max(window_lo(P, own), 0) : 0, real ? min(own + 1, g.s.L) : 0, real ? g.s.pre : 0};
+                    refs[r] = refs[32 + r] = {real ? scale_of(s) * P.scale * (CAP ? 1.0f : kLog2e) : 0.0f, kNoRef, kNoRef};
+                }
+            }
+            fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(kQ));
+            group_sync(3, 256);
+            const int tb = min(g.s.n, ta + P.tile_rows / P.G) - 1;             // slots that every row sees: [all_lo, all_hi), [0, pre)
+            const int all_lo = max(window_lo(P, g.s.slot(tb)), 0), all_hi = min(g.s.slot(ta) + 1, g.s.L);
+
+            float l[R];
+#pragma unroll
+            for (int r = 0; r < R; ++r) l[r] = 0.0f;
+            const int u0 = (int)((tiles + (uint32_t)wg) & 1);
+            // this thread's slot's page two tiles of the warpgroup ahead, its scales one
+            auto page_of = [&](int u) {
+                const int j = u < g.n ? g.kv.at(g.i0 + u) * BN + slot : g.s.L;
+                if (j >= g.s.L) return -1;
+                if (!P.cache.paged) return 0;
+                const int pi = P.cache.page_shift >= 0 ? j >> P.cache.page_shift : j / P.cache.page_size;
+                const int page = pi < P.cache.max_pages ? P.cache.page_table[(size_t)g.b * P.cache.max_pages + pi] : -1;
+                return page < P.cache.num_pages ? page : -1;
+            };
+            auto scales_of = [&](int u, int page, unsigned& k, unsigned& v) {
+                k = v = 0;
+                if (page < 0) return;
+                const int j = g.kv.at(g.i0 + u) * BN + slot;
+                long long z = shead;
+                if (!P.cache.paged) z += (long long)g.b * P.scales.sb + j;
+                else z += (long long)page * P.cache.H * P.cache.page_size + (P.cache.page_shift >= 0 ? j & (P.cache.page_size - 1) : j % P.cache.page_size);
+                k = P.k_scale[z];
+                v = P.v_scale[z];
+            };
+            unsigned ks, vs, ks2, vs2;
+            scales_of(u0, page_of(u0), ks, vs);
+            int page = page_of(u0 + 2);
+            for (int u = u0; u < g.n; u += 2) {
+                scales_of(u + 2, page, ks2, vs2);
+                page = page_of(u + 4);
+                const uint32_t gu = tiles + (uint32_t)u;
+                wait(kS + wg, (gu >> 1) & 1);
+                tc_fence_after();
+                float x[R];
+                {
+                    uint32_t hi[R], lo[R];
+                    tmem_load<R>(lanes + wg * C::NQ, hi);
+                    tmem_load<R>(lanes + wg * C::NQ + R, lo);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int r = 0; r < R; ++r) x[r] = fmaf(__uint_as_float(lo[r]), 0.0625f, __uint_as_float(hi[r]));
+                }
+                const int j0 = g.kv.at(g.i0 + u) * BN, j = j0 + slot;
+                const bool all = (j0 >= all_lo && j0 + BN <= all_hi) || j0 + BN <= g.s.pre;
+                const float kf = scale_of(ks), vz = vs == 0u ? -INFINITY : vs == 255u ? INFINITY : (float)((int)vs - 127);
+                float grown = -INFINITY;                 // by how much a score is beyond its reference
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    const FewRef f = ref[r];
+                    float y = x[r] * f.f * kf;
+                    if constexpr (CAP) y = capped(y, P.cap, inv_cap) * kLog2e;
+                    x[r] = y;
+                }
+                if (!all) {
+#pragma unroll
+                    for (int r = 0; r < R; ++r) {
+                        const FewSees v = sees_of[r];
+                        if (!((j >= v.lo && j < v.hi) || j < v.pre)) x[r] = -INFINITY;
+                    }
+                }
+#pragma unroll
+                for (int r = 0; r < R; ++r) grown = max3(grown, x[r] - ref[r].m, x[r] + vz - ref[r].n);
+                // the product that last added to this O, and read P, is complete
+                if (u > u0) {
+                    wait(kO + wg, done & 1);
+                    ++done;
+                    tc_fence_after();
+                }
+                if (group_any(1 + wg, 128, grown > 1.0f && ok)) {
+#pragma unroll
+                    for (int r = 0; r < R; ++r) {
+                        float a = x[r], b = x[r] + vz;
+#pragma unroll
+                        for (int o = 16; o; o >>= 1) {
+                            a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, o));
+                            b = fmaxf(b, __shfl_xor_sync(0xffffffffu, b, o));
+                        }
+                        if (lane == 0) red[quad * 32 + r] = make_float2(a, b);
+                    }
+                    group_sync(1 + wg, 128);
+                    if (slot < R) {
+                        const float2 a = red[slot], b = red[32 + slot], c = red[64 + slot], d = red[96 + slot];
+                        const FewRef old = ref[slot];
+                        const float m = fmaxf(old.m, fmaxf(fmaxf(a.x, b.x), fmaxf(c.x, d.x))), n = fmaxf(old.n, fmaxf(fmaxf(a.y, b.y), fmaxf(c.y, d.y)));
+                        ref[slot].m = m;
+                        ref[slot].n = n;
+                        less[slot] = make_float2(exp2_hw(old.m - m), exp2_hw(old.n - n));
+                    }
+                    group_sync(1 + wg, 128);
+#pragma unroll
+                    for (int r = 0; r < R; ++r) l[r] *= less[r].x;
+                    if (u > u0) {
+#pragma unroll 1
+                        for (int k = 0; k < 3 * DB; ++k) {
+                            const uint32_t at = lanes + C::O_COL + (wg * DB + k / 3) * C::NP + k % 3 * R;
+                            uint32_t o[R];
+                            tmem_load<R>(at, o);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int r = 0; r < R; ++r) o[r] = __float_as_uint(__uint_as_float(o[r]) * less[r].y);
+                            tmem_store<R>(at, o);
+                        }
+                        tmem_st_wait();
+                    }
+                }
+                // weights, 128 for the largest (at most 256: the reference may stay behind by a factor of two)
+                float2 y[R / 2];
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    const FewRef f = ref[r];
+                    l[r] += exp2_hw(x[r] - f.m);
+                    (r & 1 ? y[r / 2].y : y[r / 2].x) = exp2_hw(x[r] + vz - f.n + 7.0f);
+                }
+#pragma unroll
+                for (int t = 0; t < 3; ++t)
+#pragma unroll
+                    for (int r = 0; r < R; r += 2) {
+                        const uint32_t two = t < 2 ? take_term(y[r / 2]) : to_codes(y[r / 2].x, y[r / 2].y);
+                        const uint32_t n = (uint32_t)(t * R + r);
+                        p_row[n * 128 + ((p_chunk ^ (n & 7)) << 4) + p_in] = (uint8_t)two;
+                        p_row[(n + 1) * 128 + ((p_chunk ^ ((n + 1) & 7)) << 4) + p_in] = (uint8_t)(two >> 8);
+                    }
+                fence_proxy_async();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(kP + wg));
+                ks = ks2;
+                vs = vs2;
+            }
+            if (u0 < g.n) {
+                wait(kO + wg, done & 1);
+                ++done;
+            }
+            tiles += (uint32_t)g.n;
+            // the rows' sums over the warpgroup's threads
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                float s = l[r];
+#pragma unroll
+                for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+                if (lane == 0) sums[(wg * 4 + quad) * 32 + r] = s;
+            }
+            group_sync(3, 256);
+            tc_fence_after();
+            // heads of 128: half the rows a warpgroup, heads of 256: half the channels
+            const bool whole = g.whole(), one = g.n > (int)((tiles - g.n) & 1), two = g.n > (int)((tiles - g.n + 1) & 1);   // warpgroups that had tiles
+            constexpr int RW = DB == 1 ? R / 2 : R;
+            const int r0 = DB == 1 ? wg * RW : 0, k = DB == 1 ? 0 : wg;
+            // reference and sum of a row over both warpgroups
+            auto joined = [&](int row, float& sum) {
+                const float ma = one ? refs[row].m : kNoRef, mb = two ? refs[32 + row].m : kNoRef, top = fmaxf(ma, mb);
+                sum = 0.0f;
+                if (one) sum += (sums[row] + sums[32 + row] + sums[64 + row] + sums[96 + row]) * exp2_hw(ma - top);
+                if (two) sum += (sums[128 + row] + sums[160 + row] + sums[192 + row] + sums[224 + row]) * exp2_hw(mb - top);
+                return top;
+            };
+            uint32_t not_fine = 0;
+            if (ok) {
+                float o[RW];
+#pragma unroll
+                for (int r = 0; r < RW; ++r) o[r] = 0.0f;
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    if (!(x ? two : one)) continue;
+#pragma unroll
+                    for (int t = 0; t < 3; ++t) {
+                        uint32_t v[RW];
+                        tmem_load<RW>(lanes + C::O_COL + (x * DB + k) * C::NP + t * R + r0, v);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int r = 0; r < RW; ++r) {
+                            // (every O: 128 for a weight of one)
+                            const float top = fmaxf(one ? refs[r0 + r].m : kNoRef, two ? refs[32 + r0 + r].m : kNoRef);
+                            const float f = exp2_hw(refs[x * 32 + r0 + r].n - top - (t == 0 ? 7.0f : t == 1 ? 11.0f : 15.0f));
+                            o[r] = fmaf(__uint_as_float(v[r]), f, o[r]);
+                        }
+                    }
+                }
+                const size_t part = (size_t)(2 * blockIdx.x + (g.first ? 0 : 1)) * R;
+#pragma unroll
+                for (int r = 0; r < RW; ++r) {
+                    const int row = r0 + r;
+                    if (row >= rows) continue;
+                    float sum;
+                    const float top = joined(row, sum);
+                    const int channel = k * 128 + slot;
+                    if (whole) {
+                        const float inv = sum > 0.0f ? 1.0f / sum : (sum == 0.0f ? 0.0f : sum);
+                        const float y = sum == 0.0f ? 0.0f : o[r] * inv;
+                        const RowId id = row_id(P, g.s, g.h, g.rt * P.tile_rows + row);
+                        ((__nv_bfloat16*)P.out)[(long long)(g.s.t0 + id.t) * P.o_t + (long long)id.head * P.o_h + channel] = __float2bfloat16_rn(y);
+                        if (!(fabsf(y) <= 3.0e38f) && sum == sum) not_fine |= 1u << row;
+                        if (P.lse && slot == 0 && k == 0) P.lse[(long long)(g.s.t0 + id.t) * P.Hq + id.head] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * kLn2;
+                    } else {
+                        __stcg(P.part_o + (part + row) * D + channel, o[r]);
+                        if (slot == 0 && k == 0) __stcg(P.part_ml + part + row, make_float2(sum == 0.0f ? -INFINITY : top, sum));
+                    }
+                }
+            }
+            tc_fence_before();
+            if (whole) {
+                not_fine = __reduce_or_sync(0xffffffffu, not_fine);
+                if (lane == 0) bad[sw] = not_fine;
+                group_sync(3, 256);
+                uint32_t all_bad = 0;
+#pragma unroll
+                for (int x = 0; x < 8; ++x) all_bad |= bad[x];
+                for (int row = sw; row < rows; row += 8) {
+                    if (!(all_bad >> row & 1u)) continue;
+                    float sum;
+                    const float top = joined(row, sum);
+                    float o[D / 32];
+                    resum_row<__nv_bfloat16, D>(P, g.s, g.b, g.h, g.rt * P.tile_rows + row, top + log2f(sum), o, beat);
+                    const RowId id = row_id(P, g.s, g.h, g.rt * P.tile_rows + row);
+                    store_f32<__nv_bfloat16, D / 32>((__nv_bfloat16*)P.out + (long long)(g.s.t0 + id.t) * P.o_t + (long long)id.head * P.o_h + lane * (D / 32), o);
+                }
+            }
+            group_sync(3, 256);                          // the tables and the sums are the next item's
+        }
+        if (threadIdx.x == 128) leave_split(P, *plan, g, have);
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 3) {
+        tmem_relinquish();
+        tmem_dealloc(tmem, C::TMEM);
+    }
+}
+
+template <int D, int R, bool GROUPS, bool CAP> cudaError_t start_few(const AttendParams& P, int num_sms, cudaStream_t stream)
+{
+    using C = FewShape<D, R>;
+    const int grid = min(num_sms, kAttendMaxRows / R / 2);
+    if (cudaError_t e = smem_opt_in<attend_few_kernel<D, R, GROUPS, CAP>>(C::SMEM); e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(C::THREADS);
+    cfg.dynamicSmemBytes = C::SMEM;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaError_t e = cudaLaunchKernelEx(&cfg, attend_few_kernel<D, R, GROUPS, CAP>, P); e != cudaSuccess) return e;
+    return run_join<__nv_bfloat16, D, R>(P, grid, stream);
+}
+template <int D, int R, bool CAP> cudaError_t run_few(const AttendParams& call, int num_sms, cudaStream_t stream)
+{
+    AttendParams P = call;
+    P.tile_rows = R / P.G * P.G;
+    if (!P.cache.paged || P.cache.page_size % 8 == 0) return start_few<D, R, true, CAP>(P, num_sms, stream);
+    return start_few<D, R, false, CAP>(P, num_sms, stream);
+}
+
+}  // namespace
+}  // namespace kvx

@@ -70,10 +70,8 @@ __device__ __forceinline__ uint32_t range_bits(int a, int b, int base)
     return (hi == 32 ? 0xffffffffu : (1u << hi) - 1u) & ~((1u << lo) - 1u);
 }
 
-// Registers of a thread once the warps have taken their parts (two softmax warpgroups: 384 threads launched with 168):
-// 128 x 88 + 256 x 208 = 384 x 168.
-template <int N> __device__ __forceinline__ void regs_give() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
-template <int N> __device__ __forceinline__ void regs_take() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+// Registers of a thread once the warps have taken their parts (two softmax warpgroups: 384 threads launched with 168, or 512
+// with 128): 128 x 88 + 256 x 208 = 384 x 168, 256 x 56 + 256 x 200 = 512 x 128.
 
 constexpr int kFewSlots = 512;   // rows that see fewer slots get their weights in two terms
 

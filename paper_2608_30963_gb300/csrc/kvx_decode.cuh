@@ -152,6 +152,9 @@ cudaError_t launch_key_weight(const AttendParams& P, int num_sms, cudaStream_t s
 cudaError_t launch_attend_tc_capped(const AttendParams& P, int num_sms, cudaStream_t stream);
 cudaError_t launch_attend_tc(const AttendParams& P, int num_sms, cudaStream_t stream);
 cudaError_t launch_expand(const AttendParams& P, void* to_k, void* to_v, int num_sms, cudaStream_t stream);
+// rows: most rows of a tile (a KV head's, whole tokens), 8, 16 or 32
+cudaError_t launch_attend_few(const AttendParams& P, int rows, int num_sms, cudaStream_t stream);
+cudaError_t launch_attend_few_capped(const AttendParams& P, int rows, int num_sms, cudaStream_t stream);
 cudaError_t launch_attend_tc_codes_capped(const AttendParams& P, int num_sms, cudaStream_t stream);
 cudaError_t launch_attend_tc_codes(const AttendParams& P, int num_sms, cudaStream_t stream);
 cudaError_t launch_attend(const AttendParams& P, int dtype, int num_sms, cudaStream_t stream, int* launches);
