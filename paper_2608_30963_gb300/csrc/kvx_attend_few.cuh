@@ -9,7 +9,7 @@
 // side as columns of one product; sums are fp32.  Slots are the rows of S^T and channels those of O^T, so the rows of a tile
 // are its columns: 128 slots by 8, 16 or 32 rows.
 //   copying warps (7)   128-byte blocks of K and V rows into 128-byte-swizzled tiles, every seventh each
-//   MMA warp            tile i: S(i) into buffer i mod 2; O of warpgroup i mod 2 += V P(i) when P(i) is there
+//   MMA warp            tile i: S(i + 2) into S(i)'s place once that has been read; O of warpgroup i mod 2 += V P(i) when P(i) is there
 //   softmax warps (8)   two warpgroups, every other tile each; a thread has a slot.  A score x takes its K row's scale; a weight
 //                       takes its V row's, in its exponent, z = x + log2 of it, and a reference n of its own beside the sums'
 //                       reference m, so that far scales do not leave e4m3's range.  A row takes new references when x or z
@@ -89,6 +89,13 @@ struct __align__(16) FewRef {
     float f, m, n;
 };
 constexpr float kNoRef = -3.0e38f;
+constexpr float kAhead = 2.0f;   // references are taken so far above the largest, so that they last (a tile with new ones costs 1200 clocks)
+__device__ __forceinline__ float warp_max(float x)
+{
+    float y;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
+    return y;
+}
 
 template <int D, int R, bool GROUPS, bool CAP>
 __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constant__ AttendParams P)
@@ -97,7 +104,7 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
     constexpr int BN = C::BN, DB = C::DB;
     extern __shared__ __align__(1024) uint8_t smem[];
     const uint32_t s0 = smem_u32(smem);
-    constexpr int kFull = 0, kEmpty = C::STAGES, kS = 2 * C::STAGES, kP = kS + 2, kO = kP + 2, kQ = kO + 2, kDone = kQ + 1;
+    constexpr int kFull = 0, kEmpty = C::STAGES, kS = 2 * C::STAGES, kP = kS + 2, kO = kP + 2, kFree = kO + 2, kQ = kFree + 2, kDone = kQ + 1;
     auto bar = [&](int i) { return s0 + (uint32_t)i * 8; };
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + 512);
     int* abort = reinterpret_cast<int*>(smem + 516);
@@ -115,6 +122,7 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
             mbar_init(bar(kS + i), 1);
             mbar_init(bar(kP + i), 4);
             mbar_init(bar(kO + i), 1);
+            mbar_init(bar(kFree + i), 4);
         }
         mbar_init(bar(kQ), 8);
         mbar_init(bar(kDone), 1);
@@ -254,6 +262,9 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
                 if (n > 1) scores(1);
                 for (int i = 0; i < n && ok; ++i) {
                     const uint32_t gu = tiles + (uint32_t)i, wg = gu & 1;
+                    // S(i) has been read: its place is S(i + 2)'s
+                    wait(kFree + (int)wg, (gu >> 1) & 1);
+                    if (ok && i + 2 < n) scores(i + 2);
                     const uint32_t p = base + (uint32_t)(i == n - 1 ? 2 * i + 1 : 2 * i + 2) * DB;
 #pragma unroll
                     for (int b = 0; b < DB; ++b) wait(kFull + (int)((p + b) % C::STAGES), ((p + b) / C::STAGES) & 1);
@@ -274,7 +285,6 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
                         umma_commit(bar(kO + (int)wg));
                     }
                     __syncwarp();
-                    if (i + 2 < n) scores(i + 2);
                 }
                 base += 2 * (uint32_t)n * DB;
                 tiles += (uint32_t)n;
@@ -361,22 +371,24 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
             const int tb = min(g.s.n, ta + P.tile_rows / P.G) - 1;             // slots that every row sees: [all_lo, all_hi), [0, pre)
             const int all_lo = max(window_lo(P, g.s.slot(tb)), 0), all_hi = min(g.s.slot(ta) + 1, g.s.L);
 
-            float l[R];
+            // rows are taken 16 at a time, so that a thread's scores and sums stay in registers; with 32 the halves of the sums
+            // change places after each half
+            constexpr int RH = R < 16 ? R : 16, HALVES = R / RH;
+            float l[HALVES][RH];
 #pragma unroll
-            for (int r = 0; r < R; ++r) l[r] = 0.0f;
+            for (int r = 0; r < R; ++r) l[r / RH][r % RH] = 0.0f;
             const int u0 = (int)((tiles + (uint32_t)wg) & 1);
-            // this thread's slot's page two tiles of the warpgroup ahead, its scales one
+            // this thread's slot's page two tiles of the warpgroup ahead (looked at only then), its scales one
             auto page_of = [&](int u) {
                 const int j = u < g.n ? g.kv.at(g.i0 + u) * BN + slot : g.s.L;
                 if (j >= g.s.L) return -1;
                 if (!P.cache.paged) return 0;
                 const int pi = P.cache.page_shift >= 0 ? j >> P.cache.page_shift : j / P.cache.page_size;
-                const int page = pi < P.cache.max_pages ? P.cache.page_table[(size_t)g.b * P.cache.max_pages + pi] : -1;
-                return page < P.cache.num_pages ? page : -1;
+                return pi < P.cache.max_pages ? P.cache.page_table[(size_t)g.b * P.cache.max_pages + pi] : -1;
             };
             auto scales_of = [&](int u, int page, unsigned& k, unsigned& v) {
                 k = v = 0;
-                if (page < 0) return;
+                if (page < 0 || (P.cache.paged && page >= P.cache.num_pages)) return;
                 const int j = g.kv.at(g.i0 + u) * BN + slot;
                 long long z = shead;
                 if (!P.cache.paged) z += (long long)g.b * P.scales.sb + j;
@@ -384,110 +396,118 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
                 k = P.k_scale[z];
                 v = P.v_scale[z];
             };
-            unsigned ks, vs, ks2, vs2;
-            scales_of(u0, page_of(u0), ks, vs);
+            unsigned ks2, vs2;
+            scales_of(u0, page_of(u0), ks2, vs2);
             int page = page_of(u0 + 2);
             for (int u = u0; u < g.n; u += 2) {
-                scales_of(u + 2, page, ks2, vs2);
-                page = page_of(u + 4);
                 const uint32_t gu = tiles + (uint32_t)u;
                 wait(kS + wg, (gu >> 1) & 1);
                 tc_fence_after();
-                float x[R];
-                {
-                    uint32_t hi[R], lo[R];
-                    tmem_load<R>(lanes + wg * C::NQ, hi);
-                    tmem_load<R>(lanes + wg * C::NQ + R, lo);
-                    tmem_ld_wait();
-#pragma unroll
-                    for (int r = 0; r < R; ++r) x[r] = fmaf(__uint_as_float(lo[r]), 0.0625f, __uint_as_float(hi[r]));
-                }
+                const unsigned ks = ks2, vs = vs2;       // (read a tile ago: the next ones have until here, too)
+                scales_of(u + 2, page, ks2, vs2);
+                page = page_of(u + 4);
                 const int j0 = g.kv.at(g.i0 + u) * BN, j = j0 + slot;
                 const bool all = (j0 >= all_lo && j0 + BN <= all_hi) || j0 + BN <= g.s.pre;
                 const float kf = scale_of(ks), vz = vs == 0u ? -INFINITY : vs == 255u ? INFINITY : (float)((int)vs - 127);
-                float grown = -INFINITY;                 // by how much a score is beyond its reference
-#pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    const FewRef f = ref[r];
-                    float y = x[r] * f.f * kf;
-                    if constexpr (CAP) y = capped(y, P.cap, inv_cap) * kLog2e;
-                    x[r] = y;
-                }
-                if (!all) {
-#pragma unroll
-                    for (int r = 0; r < R; ++r) {
-                        const FewSees v = sees_of[r];
-                        if (!((j >= v.lo && j < v.hi) || j < v.pre)) x[r] = -INFINITY;
-                    }
-                }
-#pragma unroll
-                for (int r = 0; r < R; ++r) grown = max3(grown, x[r] - ref[r].m, x[r] + vz - ref[r].n);
                 // the product that last added to this O, and read P, is complete
                 if (u > u0) {
                     wait(kO + wg, done & 1);
                     ++done;
                     tc_fence_after();
                 }
-                if (group_any(1 + wg, 128, grown > 1.0f && ok)) {
-#pragma unroll
-                    for (int r = 0; r < R; ++r) {
-                        float a = x[r], b = x[r] + vz;
-#pragma unroll
-                        for (int o = 16; o; o >>= 1) {
-                            a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, o));
-                            b = fmaxf(b, __shfl_xor_sync(0xffffffffu, b, o));
-                        }
-                        if (lane == 0) red[quad * 32 + r] = make_float2(a, b);
-                    }
-                    group_sync(1 + wg, 128);
-                    if (slot < R) {
-                        const float2 a = red[slot], b = red[32 + slot], c = red[64 + slot], d = red[96 + slot];
-                        const FewRef old = ref[slot];
-                        const float m = fmaxf(old.m, fmaxf(fmaxf(a.x, b.x), fmaxf(c.x, d.x))), n = fmaxf(old.n, fmaxf(fmaxf(a.y, b.y), fmaxf(c.y, d.y)));
-                        ref[slot].m = m;
-                        ref[slot].n = n;
-                        less[slot] = make_float2(exp2_hw(old.m - m), exp2_hw(old.n - n));
-                    }
-                    group_sync(1 + wg, 128);
-#pragma unroll
-                    for (int r = 0; r < R; ++r) l[r] *= less[r].x;
-                    if (u > u0) {
 #pragma unroll 1
-                        for (int k = 0; k < 3 * DB; ++k) {
-                            const uint32_t at = lanes + C::O_COL + (wg * DB + k / 3) * C::NP + k % 3 * R;
-                            uint32_t o[R];
-                            tmem_load<R>(at, o);
-                            tmem_ld_wait();
-#pragma unroll
-                            for (int r = 0; r < R; ++r) o[r] = __float_as_uint(__uint_as_float(o[r]) * less[r].y);
-                            tmem_store<R>(at, o);
+                for (int r0 = 0; r0 < R; r0 += RH) {
+                    float x[RH];
+                    {
+                        uint32_t hi[RH], lo[RH];
+                        tmem_load<RH>(lanes + wg * C::NQ + r0, hi);
+                        tmem_load<RH>(lanes + wg * C::NQ + R + r0, lo);
+                        tmem_ld_wait();
+                        if (r0 + RH == R) {
+                            tc_fence_before();
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(bar(kFree + wg));
                         }
-                        tmem_st_wait();
+#pragma unroll
+                        for (int r = 0; r < RH; ++r) x[r] = fmaf(__uint_as_float(lo[r]), 0.0625f, __uint_as_float(hi[r]));
                     }
-                }
-                // weights, 128 for the largest (at most 256: the reference may stay behind by a factor of two)
-                float2 y[R / 2];
 #pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    const FewRef f = ref[r];
-                    l[r] += exp2_hw(x[r] - f.m);
-                    (r & 1 ? y[r / 2].y : y[r / 2].x) = exp2_hw(x[r] + vz - f.n + 7.0f);
-                }
-#pragma unroll
-                for (int t = 0; t < 3; ++t)
-#pragma unroll
-                    for (int r = 0; r < R; r += 2) {
-                        const uint32_t two = t < 2 ? take_term(y[r / 2]) : to_codes(y[r / 2].x, y[r / 2].y);
-                        const uint32_t n = (uint32_t)(t * R + r);
-                        p_row[n * 128 + ((p_chunk ^ (n & 7)) << 4) + p_in] = (uint8_t)two;
-                        p_row[(n + 1) * 128 + ((p_chunk ^ ((n + 1) & 7)) << 4) + p_in] = (uint8_t)(two >> 8);
+                    for (int r = 0; r < RH; ++r) {
+                        float y = x[r] * ref[r0 + r].f * kf;
+                        if constexpr (CAP) y = capped(y, P.cap, inv_cap) * kLog2e;
+                        x[r] = y;
                     }
+                    if (!all) {
+#pragma unroll
+                        for (int r = 0; r < RH; ++r) {
+                            const FewSees v = sees_of[r0 + r];
+                            if (!((j >= v.lo && j < v.hi) || j < v.pre)) x[r] = -INFINITY;
+                        }
+                    }
+                    float grown = -INFINITY;             // by how much a score is beyond its reference
+#pragma unroll
+                    for (int r = 0; r < RH; ++r) grown = max3(grown, x[r] - ref[r0 + r].m, x[r] + vz - ref[r0 + r].n);
+                    if (group_any(1 + wg, 128, grown > 1.0f && ok)) {
+#pragma unroll
+                        for (int r = 0; r < RH; ++r) {
+                            const float a = warp_max(x[r]), b = warp_max(x[r] + vz);
+                            if (lane == 0) red[quad * 32 + r] = make_float2(a, b);
+                        }
+                        group_sync(1 + wg, 128);
+                        if (slot < RH) {
+                            const float2 a = red[slot], b = red[32 + slot], c = red[64 + slot], d = red[96 + slot];
+                            const FewRef old = ref[r0 + slot];
+                            const float m = fmaxf(old.m, fmaxf(fmaxf(a.x, b.x), fmaxf(c.x, d.x)) + kAhead), n = fmaxf(old.n, fmaxf(fmaxf(a.y, b.y), fmaxf(c.y, d.y)) + kAhead);
+                            ref[r0 + slot].m = m;
+                            ref[r0 + slot].n = n;
+                            less[slot] = make_float2(exp2_hw(old.m - m), exp2_hw(old.n - n));
+                        }
+                        group_sync(1 + wg, 128);
+#pragma unroll
+                        for (int r = 0; r < RH; ++r) l[0][r] *= less[r].x;
+                        if (u > u0) {
+#pragma unroll 1
+                            for (int k = 0; k < 3 * DB; ++k) {
+                                const uint32_t at = lanes + C::O_COL + (wg * DB + k / 3) * C::NP + k % 3 * R + r0;
+                                uint32_t o[RH];
+                                tmem_load<RH>(at, o);
+                                tmem_ld_wait();
+#pragma unroll
+                                for (int r = 0; r < RH; ++r) o[r] = __float_as_uint(__uint_as_float(o[r]) * less[r].y);
+                                tmem_store<RH>(at, o);
+                            }
+                            tmem_st_wait();
+                        }
+                    }
+                    // weights, 128 for the largest (at most 256: the reference may stay behind by a factor of two)
+                    float2 y[RH / 2];
+#pragma unroll
+                    for (int r = 0; r < RH; ++r) {
+                        const FewRef f = ref[r0 + r];
+                        l[0][r] += exp2_hw(x[r] - f.m);
+                        (r & 1 ? y[r / 2].y : y[r / 2].x) = exp2_hw(x[r] + vz - f.n + 7.0f);
+                    }
+#pragma unroll
+                    for (int t = 0; t < 3; ++t)
+#pragma unroll
+                        for (int r = 0; r < RH; r += 2) {
+                            const uint32_t two = t < 2 ? take_term(y[r / 2]) : to_codes(y[r / 2].x, y[r / 2].y);
+                            uint8_t* to = p_row + (t * R + r0 + r) * 128 + p_in;      // (r0 and t R are multiples of 8)
+                            to[(p_chunk ^ (uint32_t)(r & 7)) << 4] = (uint8_t)two;
+                            to[128 + ((p_chunk ^ (uint32_t)((r + 1) & 7)) << 4)] = (uint8_t)(two >> 8);
+                        }
+                    if constexpr (HALVES == 2)
+#pragma unroll
+                        for (int r = 0; r < RH; ++r) {
+                            const float t = l[0][r];
+                            l[0][r] = l[1][r];
+                            l[1][r] = t;
+                        }
+                }
                 fence_proxy_async();
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(kP + wg));
-                ks = ks2;
-                vs = vs2;
             }
             if (u0 < g.n) {
                 wait(kO + wg, done & 1);
@@ -497,7 +517,7 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
             // the rows' sums over the warpgroup's threads
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-                float s = l[r];
+                float s = l[r / RH][r % RH];
 #pragma unroll
                 for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
                 if (lane == 0) sums[(wg * 4 + quad) * 32 + r] = s;
