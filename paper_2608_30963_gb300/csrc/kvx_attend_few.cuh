@@ -1,13 +1,13 @@
 // kvx_attend_few.cuh -- attention of few new tokens over an 8-bit cache on the tensor cores, its codes multiplied as they are
 // (library-internal; tcgen05 kind::f8f6f4).  Compiled twice, with and without the capped scores' code.
 //
-//   S^T = K (Qh + Ql / 16)^T,   P = exp2(f S^T - m),   O^T += V^T (P1 + P2 / 16 + P3 / 256)
+//   S^T = K (Qh + Ql / 16)^T,   P = exp2(f S^T - m),   O^T += V^T (P1 + P2 / 32 + P3 / 1024)
 // With few rows (query heads of a token) the products have room to spare, and what costs is bringing K and V: so the
 // cache's codes are the operands, straight from memory, and the other side is split into e4m3 terms that make up for its
 // 4 bits.  A query row is scaled by a power of two and split in two (bf16's 8 bits exactly, down to 2^-14 of the row's largest
-// value, below that to 2^-22 of it), a weight in three (to 2^-12 of itself, 2^-25 of the row's largest).  Terms lie side by
+// value, below that to 2^-22 of it), a weight in three (to 2^-12 of itself, 2^-23 of the row's largest).  Terms lie side by
 // side as columns of one product; sums are fp32.  Slots are the rows of S^T and channels those of O^T, so the rows of a tile
-// are its columns: 128 slots by 8, 16 or 32 rows.
+// are its columns: 256 slots by 8, 16 or 32 rows.
 //   copying warps (7)   128-byte blocks of K and V rows into 128-byte-swizzled tiles, every seventh each
 //   MMA warp            tile i: S(i + 2) into S(i)'s place once that has been read; O of warpgroup i mod 2 += V P(i) when P(i) is there
 //   softmax warps (8)   two warpgroups, every other tile each; a thread has a slot.  A score x takes its K row's scale; a weight
@@ -26,16 +26,21 @@ namespace kvx {
 namespace {
 
 template <int D, int R> struct FewShape {
-    static constexpr int BN = 128, DB = D / 128;               // slots a tile; 128-channel blocks of a head
-    static constexpr int NQ = 2 * R, NP = R == 8 ? 32 : 3 * R;  // columns of S^T and of O^T (a multiple of 16)
-    static constexpr int UNIT = BN * 128;                      // a block of a K or V tile
-    static constexpr int CTRL = 7168, QB = NQ * 128 * DB, PB = NP * 128;
-    static constexpr int FIT = (kSmemMax - CTRL - QB - 2 * PB) / UNIT, STAGES = FIT < 12 ? FIT : 12;
-    static constexpr int SMEM = CTRL + STAGES * UNIT + QB + 2 * PB;
+    // A tile has 256 slots, two a thread (what a tile costs anyway, and the latencies, shared by two: with 128 a token each of 8
+    // sequences over up to 32768 slots took 54 us, and 46 with no tile copied at all), or 128 where TMEM has no room for more.
+    static constexpr int HB = D == 256 && R == 32 ? 1 : 2, BN = 128 * HB, DB = D / 128;   // halves of a tile; 128-channel blocks of a head
+    static constexpr int NQ = 2 * R, NP = (3 * R + 31) / 32 * 32;  // columns of S^T and of O^T
+    static constexpr int UNIT = 128 * 128, UNITS = HB * DB;    // a block of half a K or V tile; units of a tile
+    static constexpr int CTRL = 7168, QB = NQ * 128 * DB, PB = BN * NP;
+    // Scales of a tile's K and V rows, 8 tiles: a unit of tile i + 8 is copied only when a later one than V's of tile i has been
+    // multiplied (11 tiles of K or V lie between them, more than the ring holds).
+    static constexpr int TURNS = 8, SCALES = TURNS * 2 * BN;
+    static constexpr int FIT = (kSmemMax - CTRL - QB - 2 * PB - SCALES) / UNIT, STAGES = FIT < 12 ? FIT : 12;
+    static constexpr int SMEM = CTRL + STAGES * UNIT + QB + 2 * PB + SCALES;
     static constexpr int THREADS = 512, COPY = 7;
-    static constexpr int O_COL = 2 * NQ;                       // TMEM columns: S^T of even and odd tiles, then O^T of each
+    static constexpr int O_COL = 2 * HB * NQ;                  // TMEM columns: S^T of even and odd tiles, then O^T of each
     static constexpr int USED = O_COL + 2 * NP * DB, TMEM = USED <= 128 ? 128 : USED <= 256 ? 256 : 512;
-    static_assert(SMEM <= kSmemMax && USED <= 512 && COPY <= STAGES);
+    static_assert(SMEM <= kSmemMax && USED <= 512 && COPY <= STAGES && 2 * UNITS <= STAGES && STAGES <= 11 * UNITS);
     static_assert((kMaxAttendBatch + 2) * 8 <= STAGES * UNIT);
     // the control block: barriers up to 512, plan and states up to 1024, then rows' tables
     static constexpr int SEES = 1024, REF = SEES + 32 * 16, LESS = REF + 2 * 32 * 16, RED = LESS + 2 * 32 * 8, SUM = RED + 2 * 4 * 32 * 8,
@@ -70,14 +75,19 @@ template <int N> __device__ __forceinline__ void tmem_store(uint32_t at, const u
                      "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
                      : "memory");
 }
-// Two values rounded to e4m3 and what they leave.
-__device__ __forceinline__ uint32_t take_term(float2& y)
+// Two values rounded to e4m3, and `by` times what that leaves of them.
+__device__ __forceinline__ uint32_t take_term(float2& y, float by)
 {
     const uint32_t t = to_codes(y.x, y.y);
     const float2 f = codes_f32((unsigned short)t);
-    y.x = (y.x - f.x) * 16.0f;
-    y.y = (y.y - f.y) * 16.0f;
+    y.x = (y.x - f.x) * by;
+    y.y = (y.y - f.y) * by;
     return t;
+}
+// MN-major operand in blocks of 32 bytes a row, 32-byte-swizzled: lbo between the blocks, 256 bytes between 8-row groups.
+__device__ __forceinline__ uint64_t mn32_desc(uint32_t saddr, uint32_t lbo)
+{
+    return (uint64_t)((saddr & 0x3FFFFu) >> 4) | (uint64_t)((lbo >> 4) & 0x3FFFu) << 16 | (uint64_t)(256u >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)6 << 61;
 }
 
 // A row of a tile sees the slots [lo, hi) and [0, pre).
@@ -89,7 +99,7 @@ struct __align__(16) FewRef {
     float f, m, n;
 };
 constexpr float kNoRef = -3.0e38f;
-constexpr float kAhead = 2.0f;   // references are taken so far above the largest, so that they last (a tile with new ones costs 1200 clocks)
+constexpr float kAhead = 4.0f;   // references are taken so far above the largest, so that they last (a tile with new ones costs 1200 clocks)
 __device__ __forceinline__ float warp_max(float x)
 {
     float y;
@@ -101,10 +111,10 @@ template <int D, int R, bool GROUPS, bool CAP>
 __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constant__ AttendParams P)
 {
     using C = FewShape<D, R>;
-    constexpr int BN = C::BN, DB = C::DB;
+    constexpr int BN = C::BN, DB = C::DB, HB = C::HB;
     extern __shared__ __align__(1024) uint8_t smem[];
     const uint32_t s0 = smem_u32(smem);
-    constexpr int kFull = 0, kEmpty = C::STAGES, kS = 2 * C::STAGES, kP = kS + 2, kO = kP + 2, kFree = kO + 2, kQ = kFree + 2, kDone = kQ + 1;
+    constexpr int kFull = 0, kEmpty = C::STAGES, kS = 2 * C::STAGES, kP = kS + 2, kO = kP + 2, kFree = kO + 2, kScale = kFree + 2, kQ = kScale + C::TURNS, kDone = kQ + 1;
     auto bar = [&](int i) { return s0 + (uint32_t)i * 8; };
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + 512);
     int* abort = reinterpret_cast<int*>(smem + 516);
@@ -124,6 +134,7 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
             mbar_init(bar(kO + i), 1);
             mbar_init(bar(kFree + i), 4);
         }
+        for (int i = 0; i < C::TURNS; ++i) mbar_init(bar(kScale + i), 2 * HB);
         mbar_init(bar(kQ), 8);
         mbar_init(bar(kDone), 1);
         fence_mbar_init();
@@ -153,21 +164,24 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
             // ---------------------------------------------------------------- copies
             const int me = warp < 3 ? warp : warp - 9, sub = lane >> 3;        // a row of an instruction: 8 lanes
             const uint32_t c0 = (uint32_t)(((lane & 7) ^ sub) << 4);
+            uint8_t* scale_to = smem + C::SMEM - C::SCALES;
             uint32_t pos = 0;                            // units of the items before
-            constexpr int PER = GROUPS ? 8 : 1, FIND = BN / PER, LOOK = (FIND + 31) / 32;
-            const long long stride = P.cache.paged ? (long long)P.cache.H * D : P.cache.st;
+            constexpr int PER = GROUPS ? 8 : 1, FIND = 128 / PER, LOOK = (FIND + 31) / 32;
+            const long long stride = P.cache.paged ? (long long)P.cache.H * D : P.cache.st, per_page = (long long)P.cache.H * P.cache.page_size;
             while (walk.next(g)) {
-                const int total = 2 * g.n, all = total * DB;
+                const int total = 2 * g.n, all = total * C::UNITS;
                 const long long mine = cache_head(P.cache) * g.h + (PER > 1 ? sub * stride : 0) + (lane & 7) * 16;
-                // unit r of the item in the order of the ring: a block of K or V and its slot tile
-                auto tile_of = [&](int r, int& kv) {
-                    const int x = r / DB;
-                    kv = x == total - 1 || (x > 0 && !(x & 1));
-                    return g.kv.at(g.i0 + (x == total - 1 ? g.n - 1 : kv ? (x >> 1) - 1 : (x + 1) >> 1)) * BN;
+                // First slot of unit r of the item in the order of the ring, in which the MMA warp takes them (so that a wait for an empty one by
+                // parity cannot pass a phase early): K0 K1 K2 V0 K3 V1 .. and the last three V.
+                auto tile_of = [&](int r, int& kv, int& i) {
+                    const int x = r / C::UNITS, end = max(total - 2, g.n);
+                    kv = x >= end || (x >= 3 && (x & 1));
+                    i = x >= end ? x - g.n : x < 3 ? x : kv ? (x - 3) >> 1 : (x >> 1) + 1;
+                    return g.kv.at(g.i0 + i) * BN + (r - x * C::UNITS) / DB * 128;
                 };
                 auto pages_of = [&](int r, int (&x)[LOOK]) {
-                    int kv;
-                    const int j0 = r < all ? tile_of(r, kv) : g.s.L;
+                    int kv, i;
+                    const int j0 = r < all ? tile_of(r, kv, i) : g.s.L;
 #pragma unroll
                     for (int k = 0; k < LOOK; ++k) {
                         const int j = j0 + (k * 32 + lane) * PER;
@@ -195,37 +209,64 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
                 int r = (int)((C::COPY + (uint32_t)me - pos % C::COPY) % C::COPY);
                 pages_of(r, next);
                 for (; r < all; r += C::COPY) {
-                    int kv;
-                    const int j0 = tile_of(r, kv);
+                    int kv, tile;
+                    const int j0 = tile_of(r, kv, tile);
                     const uint8_t* src = (const uint8_t*)(kv ? P.cv : P.ck) + (r % DB) * 128;
                     const uint32_t p = pos + (uint32_t)r, st = p % C::STAGES, ph = (p / C::STAGES) & 1;
                     long long at[LOOK];
 #pragma unroll
                     for (int k = 0; k < LOOK; ++k) at[k] = row_at(j0 + (k * 32 + lane) * PER, next[k]);
+                    // the scales of a half tile's rows, four a lane, with its first block
+                    const bool with_scales = r % DB == 0;
+                    uint32_t scale[4] = {};
+                    if (with_scales) {
+                        const unsigned char* from = (kv ? P.v_scale : P.k_scale) + scale_head(P.cache, P.scales) * g.h;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const int j = j0 + k * 32 + lane, page = GROUPS ? __shfl_sync(0xffffffffu, next[0], k * 4 + (lane >> 3)) : next[LOOK == 1 ? 0 : k];
+                            if (j >= g.s.L) continue;
+                            if (!P.cache.paged) scale[k] = from[(long long)g.b * P.scales.sb + j];
+                            else if (page >= 0 && page < P.cache.num_pages)
+                                scale[k] = from[per_page * (unsigned)page + (P.cache.page_shift >= 0 ? j & (P.cache.page_size - 1) : j % P.cache.page_size)];
+                        }
+                    }
                     pages_of(r + C::COPY, next);
                     wait(kEmpty + (int)st, ph ^ 1);
                     if (!ok) break;
                     const uint32_t d0 = sT + st * C::UNIT + (uint32_t)sub * 128;
                     if constexpr (GROUPS) {
 #pragma unroll 4
-                        for (int q = 0; q < BN / 8; ++q) {
+                        for (int q = 0; q < 16; ++q) {
                             const long long first = __shfl_sync(0xffffffffu, at[0], q);
                             const int left = g.s.L - (j0 + q * 8);
                             const uint8_t* s1 = src + first + mine;
+                            if (first >= 0 && left >= 8) {
 #pragma unroll
-                            for (int k = 0; k < 8; k += 4) {
-                                const bool real = first >= 0 && k + sub < left;
-                                cp_async16_or_zero(d0 + (uint32_t)(q * 1024 + k * 128) + (c0 ^ (uint32_t)(k << 4)), real ? s1 + k * stride : src, real);
+                                for (int k = 0; k < 8; k += 4) cp_async16(d0 + (uint32_t)(q * 1024 + k * 128) + (c0 ^ (uint32_t)(k << 4)), s1 + k * stride);
+                            } else {
+#pragma unroll
+                                for (int k = 0; k < 8; k += 4) {
+                                    const bool real = first >= 0 && k + sub < left;
+                                    cp_async16_or_zero(d0 + (uint32_t)(q * 1024 + k * 128) + (c0 ^ (uint32_t)(k << 4)), real ? s1 + k * stride : src, real);
+                                }
                             }
                         }
                     } else {
 #pragma unroll 4
-                        for (int k = 0; k < BN; k += 4) {
+                        for (int k = 0; k < 128; k += 4) {
                             const long long row = __shfl_sync(0xffffffffu, at[k / 32], (k & 31) + sub);
                             cp_async16_or_zero(d0 + (uint32_t)k * 128 + (c0 ^ (uint32_t)((k & 7) << 4)), row < 0 ? src : src + row + mine, row >= 0);
                         }
                     }
                     cp_async_arrive(bar(kFull + (int)st));
+                    if (with_scales) {
+                        const uint32_t turn = (pos / (2 * C::UNITS) + (uint32_t)tile) % C::TURNS;
+                        uint8_t* to = scale_to + (turn * 2 + (uint32_t)kv) * BN + (r % C::UNITS) / DB * 128 + lane;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) to[k * 32] = (uint8_t)scale[k];
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(bar(kScale + (int)turn));
+                    }
                 }
                 pos += (uint32_t)all;
             }
@@ -233,26 +274,26 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
         } else {
             // ---------------------------------------------------------------- MMA
             constexpr uint32_t idesc_s = (1u << 4) | ((uint32_t)(C::NQ >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
-            constexpr uint32_t idesc_o = (1u << 4) | (1u << 15) | ((uint32_t)(C::NP >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+            constexpr uint32_t idesc_o = (1u << 4) | (1u << 15) | (1u << 16) | ((uint32_t)(C::NP >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
             const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
             uint32_t base = 0, tiles = 0, items = 0;     // units and tiles of the items before; items begun
             while (ok && walk.next(g)) {
                 const int n = __shfl_sync(0xffffffffu, g.n, 0);
                 wait(kQ, items & 1);
                 auto scores = [&](int i) {
-                    const uint32_t p = base + (uint32_t)(i == 0 ? 0 : 2 * i - 1) * DB, d = tm + ((tiles + i) & 1) * C::NQ;
+                    const uint32_t p = base + (uint32_t)(i < 3 ? i : 2 * i - 2) * C::UNITS, d = tm + ((tiles + i) & 1) * (HB * C::NQ);
 #pragma unroll
-                    for (int b = 0; b < DB; ++b) wait(kFull + (int)((p + b) % C::STAGES), ((p + b) / C::STAGES) & 1);
+                    for (int x = 0; x < C::UNITS; ++x) wait(kFull + (int)((p + x) % C::STAGES), ((p + x) / C::STAGES) & 1);
                     if (!ok) return;
                     fence_proxy_async();
                     tc_fence_after();
                     if (elect_one()) {
 #pragma unroll
-                        for (int b = 0; b < DB; ++b) {
-                            const uint64_t kd = sw128_desc(sT + (p + b) % C::STAGES * C::UNIT), qd = sw128_desc(sQ + b * (C::NQ * 128));
+                        for (int x = 0; x < C::UNITS; ++x) {
+                            const uint64_t kd = sw128_desc(sT + (p + x) % C::STAGES * C::UNIT), qd = sw128_desc(sQ + x % DB * (C::NQ * 128));
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) umma_e4m3(d, kd + k * 2, qd + k * 2, idesc_s, b > 0 || k > 0);
-                            umma_commit(bar(kEmpty + (int)((p + b) % C::STAGES)));
+                            for (int k = 0; k < 4; ++k) umma_e4m3(d + x / DB * C::NQ, kd + k * 2, qd + k * 2, idesc_s, x % DB > 0 || k > 0);
+                            umma_commit(bar(kEmpty + (int)((p + x) % C::STAGES)));
                         }
                         umma_commit(bar(kS + (int)((tiles + i) & 1)));
                     }
@@ -265,28 +306,27 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
                     // S(i) has been read: its place is S(i + 2)'s
                     wait(kFree + (int)wg, (gu >> 1) & 1);
                     if (ok && i + 2 < n) scores(i + 2);
-                    const uint32_t p = base + (uint32_t)(i == n - 1 ? 2 * i + 1 : 2 * i + 2) * DB;
+                    const uint32_t p = base + (uint32_t)(i >= n - 2 ? n + i : 2 * i + 3) * C::UNITS;
 #pragma unroll
-                    for (int b = 0; b < DB; ++b) wait(kFull + (int)((p + b) % C::STAGES), ((p + b) / C::STAGES) & 1);
+                    for (int x = 0; x < C::UNITS; ++x) wait(kFull + (int)((p + x) % C::STAGES), ((p + x) / C::STAGES) & 1);
                     fence_proxy_async();
                     wait(kP + (int)wg, (gu >> 1) & 1);
                     if (!ok) break;
                     tc_fence_after();
                     if (elect_one()) {
-                        const uint64_t pd = sw128_desc(sP + wg * C::PB);
 #pragma unroll
-                        for (int b = 0; b < DB; ++b) {
-                            const uint64_t vd = mn_desc(sT + (p + b) % C::STAGES * C::UNIT, C::UNIT);
-                            const uint32_t od = tm + C::O_COL + (wg * DB + b) * C::NP;
+                        for (int x = 0; x < C::UNITS; ++x) {
+                            const uint64_t vd = mn_desc(sT + (p + x) % C::STAGES * C::UNIT, C::UNIT), pd = mn32_desc(sP + wg * C::PB + x / DB * 4096, BN * 32);
+                            const uint32_t od = tm + C::O_COL + (wg * DB + x % DB) * C::NP;
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) umma_e4m3(od, vd + k * (4096 / 16), pd + k * 2, idesc_o, i >= 2 || k > 0);
-                            umma_commit(bar(kEmpty + (int)((p + b) % C::STAGES)));
+                            for (int k = 0; k < 4; ++k) umma_e4m3(od, vd + k * (4096 / 16), pd + k * (1024 / 16), idesc_o, i >= 2 || x / DB > 0 || k > 0);
+                            umma_commit(bar(kEmpty + (int)((p + x) % C::STAGES)));
                         }
                         umma_commit(bar(kO + (int)wg));
                     }
                     __syncwarp();
                 }
-                base += 2 * (uint32_t)n * DB;
+                base += 2 * (uint32_t)n * C::UNITS;
                 tiles += (uint32_t)n;
                 ++items;
             }
@@ -309,15 +349,13 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
         float2* red = reinterpret_cast<float2*>(smem + C::RED) + wg * 4 * 32;    // [warp][32]
         float* sums = reinterpret_cast<float*>(smem + C::SUM);                   // [warpgroup][warp][32]
         uint32_t* bad = reinterpret_cast<uint32_t*>(smem + C::BAD);              // [warp]
-        // where this thread's bytes of P go: row n at n * 128, its 16-byte chunks exchanged by n & 7
-        uint8_t* p_row = smem + (sP - s0) + wg * C::PB;
-        const uint32_t p_chunk = (uint32_t)(slot >> 4), p_in = (uint32_t)(slot & 15);
+        // where this thread's slot of P lies: 32 bytes in each block of 32 columns, their 16-byte halves exchanged every fourth slot
+        const uint32_t p_row = sP + wg * C::PB + (uint32_t)slot * 32, p_swap = (uint32_t)(slot >> 2 & 1) << 4;
         uint32_t tiles = 0, done = 0;                    // tiles of the items before; products of this warpgroup waited for
         bool have = false;
         while (walk.next(g)) {
             have = true;
             const int ta = g.rt * (P.tile_rows / P.G), rows = min(P.tile_rows, (g.s.n - ta) * P.G);
-            const long long shead = scale_head(P.cache, P.scales) * g.h;
             // the queries' terms, a row a warp, and what the rows see
             for (int r = sw; r < R; r += 8) {
                 constexpr int CH = D / 32;               // channels of a lane
@@ -340,7 +378,7 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
 #pragma unroll
                 for (int c = 0; c < CH; c += 2) {
                     float2 y = make_float2(q[c] * inv, q[c + 1] * inv);
-                    const uint32_t h = take_term(y), l = to_codes(y.x, y.y);
+                    const uint32_t h = take_term(y, 16.0f), l = to_codes(y.x, y.y);
                     if (c % 4 == 0) {
                         hi[c / 4] = h;
                         lo[c / 4] = l;
@@ -377,38 +415,33 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
             float l[HALVES][RH];
 #pragma unroll
             for (int r = 0; r < R; ++r) l[r / RH][r % RH] = 0.0f;
+            float f[RH], m[RH], n[RH];                   // their factors and references
+            auto load_refs = [&](int r0) {
+#pragma unroll
+                for (int r = 0; r < RH; ++r) {
+                    const FewRef v = ref[r0 + r];
+                    f[r] = v.f;
+                    m[r] = v.m;
+                    n[r] = v.n;
+                }
+            };
+            load_refs(0);
             const int u0 = (int)((tiles + (uint32_t)wg) & 1);
-            // this thread's slot's page two tiles of the warpgroup ahead (looked at only then), its scales one
-            auto page_of = [&](int u) {
-                const int j = u < g.n ? g.kv.at(g.i0 + u) * BN + slot : g.s.L;
-                if (j >= g.s.L) return -1;
-                if (!P.cache.paged) return 0;
-                const int pi = P.cache.page_shift >= 0 ? j >> P.cache.page_shift : j / P.cache.page_size;
-                return pi < P.cache.max_pages ? P.cache.page_table[(size_t)g.b * P.cache.max_pages + pi] : -1;
-            };
-            auto scales_of = [&](int u, int page, unsigned& k, unsigned& v) {
-                k = v = 0;
-                if (page < 0 || (P.cache.paged && page >= P.cache.num_pages)) return;
-                const int j = g.kv.at(g.i0 + u) * BN + slot;
-                long long z = shead;
-                if (!P.cache.paged) z += (long long)g.b * P.scales.sb + j;
-                else z += (long long)page * P.cache.H * P.cache.page_size + (P.cache.page_shift >= 0 ? j & (P.cache.page_size - 1) : j % P.cache.page_size);
-                k = P.k_scale[z];
-                v = P.v_scale[z];
-            };
-            unsigned ks2, vs2;
-            scales_of(u0, page_of(u0), ks2, vs2);
-            int page = page_of(u0 + 2);
             for (int u = u0; u < g.n; u += 2) {
                 const uint32_t gu = tiles + (uint32_t)u;
                 wait(kS + wg, (gu >> 1) & 1);
                 tc_fence_after();
-                const unsigned ks = ks2, vs = vs2;       // (read a tile ago: the next ones have until here, too)
-                scales_of(u + 2, page, ks2, vs2);
-                page = page_of(u + 4);
+                wait(kScale + (int)(gu % C::TURNS), (gu / C::TURNS) & 1);
+                float kf[HB], vz[HB];                    // K's scale; log2 of V's
+#pragma unroll
+                for (int h = 0; h < HB; ++h) {
+                    const uint8_t* from = smem + C::SMEM - C::SCALES + (gu % C::TURNS) * 2 * BN + h * 128 + slot;
+                    const unsigned vs = from[BN];
+                    kf[h] = scale_of(from[0]);
+                    vz[h] = vs == 0u ? -INFINITY : vs == 255u ? INFINITY : (float)((int)vs - 127);
+                }
                 const int j0 = g.kv.at(g.i0 + u) * BN, j = j0 + slot;
                 const bool all = (j0 >= all_lo && j0 + BN <= all_hi) || j0 + BN <= g.s.pre;
-                const float kf = scale_of(ks), vz = vs == 0u ? -INFINITY : vs == 255u ? INFINITY : (float)((int)vs - 127);
                 // the product that last added to this O, and read P, is complete
                 if (u > u0) {
                     wait(kO + wg, done & 1);
@@ -417,52 +450,67 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
                 }
 #pragma unroll 1
                 for (int r0 = 0; r0 < R; r0 += RH) {
-                    float x[RH];
-                    {
+                    float x[HB][RH];
+#pragma unroll
+                    for (int h = 0; h < HB; ++h) {
                         uint32_t hi[RH], lo[RH];
-                        tmem_load<RH>(lanes + wg * C::NQ + r0, hi);
-                        tmem_load<RH>(lanes + wg * C::NQ + R + r0, lo);
+                        tmem_load<RH>(lanes + (wg * HB + h) * C::NQ + r0, hi);
+                        tmem_load<RH>(lanes + (wg * HB + h) * C::NQ + R + r0, lo);
                         tmem_ld_wait();
-                        if (r0 + RH == R) {
-                            tc_fence_before();
-                            __syncwarp();
-                            if (lane == 0) mbar_arrive(bar(kFree + wg));
+#pragma unroll
+                        for (int r = 0; r < RH; ++r) x[h][r] = fmaf(__uint_as_float(lo[r]), 0.0625f, __uint_as_float(hi[r]));
+                    }
+                    if (r0 + RH == R) {
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(bar(kFree + wg));
+                    }
+                    if (HALVES == 2) load_refs(r0);
+#pragma unroll
+                    for (int h = 0; h < HB; ++h)
+#pragma unroll
+                        for (int r = 0; r < RH; ++r) {
+                            float y = x[h][r] * f[r] * kf[h];
+                            if constexpr (CAP) y = capped(y, P.cap, inv_cap) * kLog2e;
+                            x[h][r] = y;
                         }
-#pragma unroll
-                        for (int r = 0; r < RH; ++r) x[r] = fmaf(__uint_as_float(lo[r]), 0.0625f, __uint_as_float(hi[r]));
-                    }
-#pragma unroll
-                    for (int r = 0; r < RH; ++r) {
-                        float y = x[r] * ref[r0 + r].f * kf;
-                        if constexpr (CAP) y = capped(y, P.cap, inv_cap) * kLog2e;
-                        x[r] = y;
-                    }
                     if (!all) {
 #pragma unroll
                         for (int r = 0; r < RH; ++r) {
                             const FewSees v = sees_of[r0 + r];
-                            if (!((j >= v.lo && j < v.hi) || j < v.pre)) x[r] = -INFINITY;
+#pragma unroll
+                            for (int h = 0; h < HB; ++h)
+                                if (!((j + h * 128 >= v.lo && j + h * 128 < v.hi) || j + h * 128 < v.pre)) x[h][r] = -INFINITY;
                         }
                     }
-                    float grown = -INFINITY;             // by how much a score is beyond its reference
+                    float ahead = -INFINITY;             // by how much a score is beyond its reference
 #pragma unroll
-                    for (int r = 0; r < RH; ++r) grown = max3(grown, x[r] - ref[r0 + r].m, x[r] + vz - ref[r0 + r].n);
-                    if (group_any(1 + wg, 128, grown > 1.0f && ok)) {
+                    for (int h = 0; h < HB; ++h)
+#pragma unroll
+                        for (int r = 0; r < RH; ++r) ahead = max3(ahead, x[h][r] - m[r], x[h][r] + vz[h] - n[r]);
+                    if (group_any(1 + wg, 128, ahead > 1.0f && ok)) {
 #pragma unroll
                         for (int r = 0; r < RH; ++r) {
-                            const float a = warp_max(x[r]), b = warp_max(x[r] + vz);
+                            float a = x[0][r], b = x[0][r] + vz[0];
+                            if constexpr (HB == 2) {
+                                a = fmaxf(a, x[HB - 1][r]);
+                                b = fmaxf(b, x[HB - 1][r] + vz[HB - 1]);
+                            }
+                            a = warp_max(a);
+                            b = warp_max(b);
                             if (lane == 0) red[quad * 32 + r] = make_float2(a, b);
                         }
                         group_sync(1 + wg, 128);
                         if (slot < RH) {
                             const float2 a = red[slot], b = red[32 + slot], c = red[64 + slot], d = red[96 + slot];
                             const FewRef old = ref[r0 + slot];
-                            const float m = fmaxf(old.m, fmaxf(fmaxf(a.x, b.x), fmaxf(c.x, d.x)) + kAhead), n = fmaxf(old.n, fmaxf(fmaxf(a.y, b.y), fmaxf(c.y, d.y)) + kAhead);
-                            ref[r0 + slot].m = m;
-                            ref[r0 + slot].n = n;
-                            less[slot] = make_float2(exp2_hw(old.m - m), exp2_hw(old.n - n));
+                            const float m1 = fmaxf(old.m, fmaxf(fmaxf(a.x, b.x), fmaxf(c.x, d.x)) + kAhead), n1 = fmaxf(old.n, fmaxf(fmaxf(a.y, b.y), fmaxf(c.y, d.y)) + kAhead);
+                            ref[r0 + slot].m = m1;
+                            ref[r0 + slot].n = n1;
+                            less[slot] = make_float2(exp2_hw(old.m - m1), exp2_hw(old.n - n1));
                         }
                         group_sync(1 + wg, 128);
+                        load_refs(r0);
 #pragma unroll
                         for (int r = 0; r < RH; ++r) l[0][r] *= less[r].x;
                         if (u > u0) {
@@ -480,22 +528,36 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
                         }
                     }
                     // weights, 128 for the largest (at most 256: the reference may stay behind by a factor of two)
-                    float2 y[RH / 2];
 #pragma unroll
-                    for (int r = 0; r < RH; ++r) {
-                        const FewRef f = ref[r0 + r];
-                        l[0][r] += exp2_hw(x[r] - f.m);
-                        (r & 1 ? y[r / 2].y : y[r / 2].x) = exp2_hw(x[r] + vz - f.n + 7.0f);
-                    }
+                    for (int h = 0; h < HB; ++h) {
+                        float2 y[RH / 2];
 #pragma unroll
-                    for (int t = 0; t < 3; ++t)
-#pragma unroll
-                        for (int r = 0; r < RH; r += 2) {
-                            const uint32_t two = t < 2 ? take_term(y[r / 2]) : to_codes(y[r / 2].x, y[r / 2].y);
-                            uint8_t* to = p_row + (t * R + r0 + r) * 128 + p_in;      // (r0 and t R are multiples of 8)
-                            to[(p_chunk ^ (uint32_t)(r & 7)) << 4] = (uint8_t)two;
-                            to[128 + ((p_chunk ^ (uint32_t)((r + 1) & 7)) << 4)] = (uint8_t)(two >> 8);
+                        for (int r = 0; r < RH; ++r) {
+                            l[0][r] += exp2_hw(x[h][r] - m[r]);
+                            (r & 1 ? y[r / 2].y : y[r / 2].x) = exp2_hw(x[h][r] + vz[h] - n[r] + 7.0f);
                         }
+                        uint32_t w[3][RH / 4];
+#pragma unroll
+                        for (int t = 0; t < 3; ++t)
+#pragma unroll
+                            for (int r = 0; r < RH; r += 4) {
+                                const uint32_t a = t < 2 ? take_term(y[r / 2], 32.0f) : to_codes(y[r / 2].x, y[r / 2].y);
+                                const uint32_t b = t < 2 ? take_term(y[r / 2 + 1], 32.0f) : to_codes(y[r / 2 + 1].x, y[r / 2 + 1].y);
+                                w[t][r / 4] = a | b << 16;
+                            }
+                        // column t R + r: 16 columns a store
+                        const uint32_t to = p_row + h * 4096;
+                        if constexpr (R == 8) {
+                            sts128(to + p_swap, make_uint4(w[0][0], w[0][1], w[1][0], w[1][1]));
+                            sts128(to + (p_swap ^ 16u), make_uint4(w[2][0], w[2][1], 0u, 0u));
+                        } else {
+#pragma unroll
+                            for (int t = 0; t < 3; ++t) {
+                                const uint32_t n = (uint32_t)(t * R + r0);
+                                sts128(to + n / 32 * (BN * 32) + (p_swap ^ (n & 16u)), make_uint4(w[t][0], w[t][1], w[t][RH / 4 - 2], w[t][RH / 4 - 1]));
+                            }
+                        }
+                    }
                     if constexpr (HALVES == 2)
 #pragma unroll
                         for (int r = 0; r < RH; ++r) {
@@ -553,7 +615,7 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
                         for (int r = 0; r < RW; ++r) {
                             // (every O: 128 for a weight of one)
                             const float top = fmaxf(one ? refs[r0 + r].m : kNoRef, two ? refs[32 + r0 + r].m : kNoRef);
-                            const float f = exp2_hw(refs[x * 32 + r0 + r].n - top - (t == 0 ? 7.0f : t == 1 ? 11.0f : 15.0f));
+                            const float f = exp2_hw(refs[x * 32 + r0 + r].n - top - (t == 0 ? 7.0f : t == 1 ? 12.0f : 17.0f));
                             o[r] = fmaf(__uint_as_float(v[r]), f, o[r]);
                         }
                     }
