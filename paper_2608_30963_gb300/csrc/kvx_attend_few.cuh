@@ -99,6 +99,12 @@ struct __align__(16) FewRef {
     float f, m, n;
 };
 constexpr float kNoRef = -3.0e38f;
+// The end of a row.
+struct FewEnd {
+    long long to;          // element of the output
+    float a, b;            // factors of both warpgroups' O
+    float lse2, sum;
+};
 constexpr float kAhead = 4.0f;   // references are taken so far above the largest, so that they last (a tile with new ones costs 1200 clocks)
 __device__ __forceinline__ float warp_max(float x)
 {
@@ -349,6 +355,7 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
         float2* red = reinterpret_cast<float2*>(smem + C::RED) + wg * 4 * 32;    // [warp][32]
         float* sums = reinterpret_cast<float*>(smem + C::SUM);                   // [warpgroup][warp][32]
         uint32_t* bad = reinterpret_cast<uint32_t*>(smem + C::BAD);              // [warp]
+        FewEnd* ends = reinterpret_cast<FewEnd*>(smem + C::RED);                 // [32] (when no maxima are exchanged)
         // where this thread's slot of P lies: 32 bytes in each block of 32 columns, their 16-byte halves exchanged every fourth slot
         const uint32_t p_row = sP + wg * C::PB + (uint32_t)slot * 32, p_swap = (uint32_t)(slot >> 2 & 1) << 4;
         uint32_t tiles = 0, done = 0;                    // tiles of the items before; products of this warpgroup waited for
@@ -576,68 +583,77 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
                 ++done;
             }
             tiles += (uint32_t)g.n;
-            // the rows' sums over the warpgroup's threads
+            // the rows' sums over a warp's lanes: halves of the rows change places with a lane each, until a lane has one row
+            {
+                float v[R];
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
-                float s = l[r / RH][r % RH];
+                for (int r = 0; r < R; ++r) v[r] = l[r / RH][r % RH];
+                int row = 0;
 #pragma unroll
-                for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-                if (lane == 0) sums[(wg * 4 + quad) * 32 + r] = s;
+                for (int w = R / 2, o = 16; w; w >>= 1, o >>= 1) {
+                    const bool up = lane & o;
+#pragma unroll
+                    for (int i = 0; i < w; ++i) {
+                        const float other = __shfl_xor_sync(0xffffffffu, up ? v[i] : v[i + w], o);
+                        v[i] = (up ? v[i + w] : v[i]) + other;
+                    }
+                    row += up ? w : 0;
+                }
+#pragma unroll
+                for (int o = 16 / R; o; o >>= 1) v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
+                if (R == 32 || lane % (32 / R) == 0) sums[(wg * 4 + quad) * 32 + row] = v[0];
             }
             group_sync(3, 256);
             tc_fence_after();
-            // heads of 128: half the rows a warpgroup, heads of 256: half the channels
             const bool whole = g.whole(), one = g.n > (int)((tiles - g.n) & 1), two = g.n > (int)((tiles - g.n + 1) & 1);   // warpgroups that had tiles
-            constexpr int RW = DB == 1 ? R / 2 : R;
-            const int r0 = DB == 1 ? wg * RW : 0, k = DB == 1 ? 0 : wg;
-            // reference and sum of a row over both warpgroups
-            auto joined = [&](int row, float& sum) {
+            // a row's end, by a thread: its reference and sum over both warpgroups, what each O is multiplied by (128 for a weight
+            // of one), and where it goes
+            if (sw * 32 + lane < rows) {
+                const int row = sw * 32 + lane;
                 const float ma = one ? refs[row].m : kNoRef, mb = two ? refs[32 + row].m : kNoRef, top = fmaxf(ma, mb);
-                sum = 0.0f;
+                float sum = 0.0f;
                 if (one) sum += (sums[row] + sums[32 + row] + sums[64 + row] + sums[96 + row]) * exp2_hw(ma - top);
                 if (two) sum += (sums[128 + row] + sums[160 + row] + sums[192 + row] + sums[224 + row]) * exp2_hw(mb - top);
-                return top;
-            };
+                const RowId id = row_id(P, g.s, g.h, g.rt * P.tile_rows + row);
+                const float inv = !whole ? 1.0f : sum > 0.0f ? 1.0f / sum : sum;       // (nothing seen: zeros; NaN stays)
+                FewEnd e;
+                e.to = (long long)(g.s.t0 + id.t) * P.o_t + (long long)id.head * P.o_h;
+                e.a = one ? exp2_hw(refs[row].n - top - 7.0f) * inv : 0.0f;
+                e.b = two ? exp2_hw(refs[32 + row].n - top - 7.0f) * inv : 0.0f;
+                e.lse2 = sum == 0.0f ? -INFINITY : top + log2f(sum);
+                e.sum = sum;
+                ends[row] = e;
+                if (whole && P.lse) P.lse[(long long)(g.s.t0 + id.t) * P.Hq + id.head] = e.lse2 * kLn2;
+                if (!whole) __stcg(P.part_ml + (size_t)(2 * blockIdx.x + (g.first ? 0 : 1)) * R + row, make_float2(sum == 0.0f ? -INFINITY : top, sum));
+            }
+            group_sync(3, 256);
+            // heads of 128: half the rows a warpgroup, heads of 256: half the channels
+            constexpr int RW = DB == 1 ? R / 2 : R;
+            const int first_row = DB == 1 ? wg * RW : 0, block = DB == 1 ? 0 : wg, channel = block * 128 + slot;
+            float* part = P.part_o + (size_t)(2 * blockIdx.x + (g.first ? 0 : 1)) * R * D + channel;
             uint32_t not_fine = 0;
-            if (ok) {
-                float o[RW];
+#pragma unroll 1                                             // short code: a cold instruction cache costs small calls most
+            for (int r0 = first_row; ok && r0 < min(first_row + RW, rows); r0 += 4) {
+                uint32_t v[2][3][4];
 #pragma unroll
-                for (int r = 0; r < RW; ++r) o[r] = 0.0f;
+                for (int x = 0; x < 2; ++x)
 #pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    if (!(x ? two : one)) continue;
+                    for (int t = 0; t < 3; ++t) tmem_load<4>(lanes + C::O_COL + (x * DB + block) * C::NP + t * R + r0, v[x][t]);
+                tmem_ld_wait();
 #pragma unroll
-                    for (int t = 0; t < 3; ++t) {
-                        uint32_t v[RW];
-                        tmem_load<RW>(lanes + C::O_COL + (x * DB + k) * C::NP + t * R + r0, v);
-                        tmem_ld_wait();
-#pragma unroll
-                        for (int r = 0; r < RW; ++r) {
-                            // (every O: 128 for a weight of one)
-                            const float top = fmaxf(one ? refs[r0 + r].m : kNoRef, two ? refs[32 + r0 + r].m : kNoRef);
-                            const float f = exp2_hw(refs[x * 32 + r0 + r].n - top - (t == 0 ? 7.0f : t == 1 ? 12.0f : 17.0f));
-                            o[r] = fmaf(__uint_as_float(v[r]), f, o[r]);
-                        }
-                    }
-                }
-                const size_t part = (size_t)(2 * blockIdx.x + (g.first ? 0 : 1)) * R;
-#pragma unroll
-                for (int r = 0; r < RW; ++r) {
-                    const int row = r0 + r;
-                    if (row >= rows) continue;
-                    float sum;
-                    const float top = joined(row, sum);
-                    const int channel = k * 128 + slot;
+                for (int r = 0; r < 4; ++r) {
+                    if (r0 + r >= rows) break;
+                    const FewEnd e = ends[r0 + r];
+                    auto joined = [&](int x) {
+                        return fmaf(__uint_as_float(v[x][2][r]), 0x1p-10f, fmaf(__uint_as_float(v[x][1][r]), 0x1p-5f, __uint_as_float(v[x][0][r])));
+                    };
+                    float y = (one ? joined(0) * e.a : 0.0f) + (two ? joined(1) * e.b : 0.0f);
                     if (whole) {
-                        const float inv = sum > 0.0f ? 1.0f / sum : (sum == 0.0f ? 0.0f : sum);
-                        const float y = sum == 0.0f ? 0.0f : o[r] * inv;
-                        const RowId id = row_id(P, g.s, g.h, g.rt * P.tile_rows + row);
-                        ((__nv_bfloat16*)P.out)[(long long)(g.s.t0 + id.t) * P.o_t + (long long)id.head * P.o_h + channel] = __float2bfloat16_rn(y);
-                        if (!(fabsf(y) <= 3.0e38f) && sum == sum) not_fine |= 1u << row;
-                        if (P.lse && slot == 0 && k == 0) P.lse[(long long)(g.s.t0 + id.t) * P.Hq + id.head] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * kLn2;
+                        if (e.sum == 0.0f) y = 0.0f;
+                        ((__nv_bfloat16*)P.out)[e.to + channel] = __float2bfloat16_rn(y);
+                        if (!(fabsf(y) <= 3.0e38f) && e.sum == e.sum) not_fine |= 1u << (r0 + r);
                     } else {
-                        __stcg(P.part_o + (part + row) * D + channel, o[r]);
-                        if (slot == 0 && k == 0) __stcg(P.part_ml + part + row, make_float2(sum == 0.0f ? -INFINITY : top, sum));
+                        __stcg(part + (size_t)(r0 + r) * D, y);
                     }
                 }
             }
@@ -651,12 +667,9 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
                 for (int x = 0; x < 8; ++x) all_bad |= bad[x];
                 for (int row = sw; row < rows; row += 8) {
                     if (!(all_bad >> row & 1u)) continue;
-                    float sum;
-                    const float top = joined(row, sum);
                     float o[D / 32];
-                    resum_row<__nv_bfloat16, D>(P, g.s, g.b, g.h, g.rt * P.tile_rows + row, top + log2f(sum), o, beat);
-                    const RowId id = row_id(P, g.s, g.h, g.rt * P.tile_rows + row);
-                    store_f32<__nv_bfloat16, D / 32>((__nv_bfloat16*)P.out + (long long)(g.s.t0 + id.t) * P.o_t + (long long)id.head * P.o_h + lane * (D / 32), o);
+                    resum_row<__nv_bfloat16, D>(P, g.s, g.b, g.h, g.rt * P.tile_rows + row, ends[row].lse2, o, beat);
+                    store_f32<__nv_bfloat16, D / 32>((__nv_bfloat16*)P.out + ends[row].to + lane * (D / 32), o);
                 }
             }
             group_sync(3, 256);                          // the tables and the sums are the next item's
