@@ -79,9 +79,7 @@ template <int N> __device__ __forceinline__ void tmem_store(uint32_t at, const u
 __device__ __forceinline__ uint32_t take_term(float2& y, float by)
 {
     const uint32_t t = to_codes(y.x, y.y);
-    const float2 f = codes_f32((unsigned short)t);
-    y.x = (y.x - f.x) * by;
-    y.y = (y.y - f.y) * by;
+    y = fma2(codes_f32((unsigned short)t), make_float2(-by, -by), mul2(y, make_float2(by, by)));     // (exact)
     return t;
 }
 // MN-major operand in blocks of 32 bytes a row, 32-byte-swizzled: lbo between the blocks, 256 bytes between 8-row groups.
@@ -419,17 +417,18 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
             // rows are taken 16 at a time, so that a thread's scores and sums stay in registers; with 32 the halves of the sums
             // change places after each half
             constexpr int RH = R < 16 ? R : 16, HALVES = R / RH;
-            float l[HALVES][RH];
+            float2 l[HALVES][RH / 2];
 #pragma unroll
-            for (int r = 0; r < R; ++r) l[r / RH][r % RH] = 0.0f;
-            float f[RH], m[RH], n[RH];                   // their factors and references
+            for (int r = 0; r < R / 2; ++r) l[2 * r / RH][r % (RH / 2)] = make_float2(0.0f, 0.0f);
+            // their factors, and their references with the other sign, in pairs; a weight is 128 where z is its reference
+            float2 f[RH / 2], m[RH / 2], n[RH / 2];
             auto load_refs = [&](int r0) {
 #pragma unroll
-                for (int r = 0; r < RH; ++r) {
-                    const FewRef v = ref[r0 + r];
-                    f[r] = v.f;
-                    m[r] = v.m;
-                    n[r] = v.n;
+                for (int r = 0; r < RH; r += 2) {
+                    const FewRef v = ref[r0 + r], w = ref[r0 + r + 1];
+                    f[r / 2] = make_float2(v.f, w.f);
+                    m[r / 2] = make_float2(-v.m, -w.m);
+                    n[r / 2] = make_float2(7.0f - v.n, 7.0f - w.n);
                 }
             };
             load_refs(0);
@@ -457,7 +456,7 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
                 }
 #pragma unroll 1
                 for (int r0 = 0; r0 < R; r0 += RH) {
-                    float x[HB][RH];
+                    float2 x[HB][RH / 2];
 #pragma unroll
                     for (int h = 0; h < HB; ++h) {
                         uint32_t hi[RH], lo[RH];
@@ -465,7 +464,9 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
                         tmem_load<RH>(lanes + (wg * HB + h) * C::NQ + R + r0, lo);
                         tmem_ld_wait();
 #pragma unroll
-                        for (int r = 0; r < RH; ++r) x[h][r] = fmaf(__uint_as_float(lo[r]), 0.0625f, __uint_as_float(hi[r]));
+                        for (int r = 0; r < RH; r += 2)
+                            x[h][r / 2] = fma2(make_float2(__uint_as_float(lo[r]), __uint_as_float(lo[r + 1])), make_float2(0.0625f, 0.0625f),
+                                               make_float2(__uint_as_float(hi[r]), __uint_as_float(hi[r + 1])));
                     }
                     if (r0 + RH == R) {
                         tc_fence_before();
@@ -476,9 +477,12 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
 #pragma unroll
                     for (int h = 0; h < HB; ++h)
 #pragma unroll
-                        for (int r = 0; r < RH; ++r) {
-                            float y = x[h][r] * f[r] * kf[h];
-                            if constexpr (CAP) y = capped(y, P.cap, inv_cap) * kLog2e;
+                        for (int r = 0; r < RH / 2; ++r) {
+                            float2 y = mul2(mul2(x[h][r], f[r]), make_float2(kf[h], kf[h]));
+                            if constexpr (CAP) {
+                                y.x = capped(y.x, P.cap, inv_cap) * kLog2e;
+                                y.y = capped(y.y, P.cap, inv_cap) * kLog2e;
+                            }
                             x[h][r] = y;
                         }
                     if (!all) {
@@ -487,21 +491,27 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
                             const FewSees v = sees_of[r0 + r];
 #pragma unroll
                             for (int h = 0; h < HB; ++h)
-                                if (!((j + h * 128 >= v.lo && j + h * 128 < v.hi) || j + h * 128 < v.pre)) x[h][r] = -INFINITY;
+                                if (!((j + h * 128 >= v.lo && j + h * 128 < v.hi) || j + h * 128 < v.pre)) (r & 1 ? x[h][r / 2].y : x[h][r / 2].x) = -INFINITY;
                         }
                     }
-                    float ahead = -INFINITY;             // by how much a score is beyond its reference
+                    float ahead = -INFINITY, ahead_z = -INFINITY;   // by how much a score is beyond its references
 #pragma unroll
                     for (int h = 0; h < HB; ++h)
 #pragma unroll
-                        for (int r = 0; r < RH; ++r) ahead = max3(ahead, x[h][r] - m[r], x[h][r] + vz[h] - n[r]);
-                    if (group_any(1 + wg, 128, ahead > 1.0f && ok)) {
+                        for (int r = 0; r < RH / 2; ++r) {
+                            const float2 a = add2(x[h][r], m[r]), b = add2(add2(x[h][r], make_float2(vz[h], vz[h])), n[r]);
+                            ahead = max3(ahead, a.x, a.y);
+                            ahead_z = max3(ahead_z, b.x, b.y);
+                        }
+                    if (group_any(1 + wg, 128, (ahead > 1.0f || ahead_z > 8.0f) && ok)) {
 #pragma unroll
                         for (int r = 0; r < RH; ++r) {
-                            float a = x[0][r], b = x[0][r] + vz[0];
-                            if constexpr (HB == 2) {
-                                a = fmaxf(a, x[HB - 1][r]);
-                                b = fmaxf(b, x[HB - 1][r] + vz[HB - 1]);
+                            float a = -INFINITY, b = -INFINITY;
+#pragma unroll
+                            for (int h = 0; h < HB; ++h) {
+                                const float y = r & 1 ? x[h][r / 2].y : x[h][r / 2].x;
+                                a = fmaxf(a, y);
+                                b = fmaxf(b, y + vz[h]);
                             }
                             a = warp_max(a);
                             b = warp_max(b);
@@ -519,7 +529,7 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
                         group_sync(1 + wg, 128);
                         load_refs(r0);
 #pragma unroll
-                        for (int r = 0; r < RH; ++r) l[0][r] *= less[r].x;
+                        for (int r = 0; r < RH / 2; ++r) l[0][r] = mul2(l[0][r], make_float2(less[2 * r].x, less[2 * r + 1].x));
                         if (u > u0) {
 #pragma unroll 1
                             for (int k = 0; k < 3 * DB; ++k) {
@@ -539,9 +549,10 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
                     for (int h = 0; h < HB; ++h) {
                         float2 y[RH / 2];
 #pragma unroll
-                        for (int r = 0; r < RH; ++r) {
-                            l[0][r] += exp2_hw(x[h][r] - m[r]);
-                            (r & 1 ? y[r / 2].y : y[r / 2].x) = exp2_hw(x[h][r] + vz[h] - n[r] + 7.0f);
+                        for (int r = 0; r < RH / 2; ++r) {
+                            const float2 a = add2(x[h][r], m[r]), b = add2(add2(x[h][r], make_float2(vz[h], vz[h])), n[r]);
+                            l[0][r] = add2(l[0][r], make_float2(exp2_hw(a.x), exp2_hw(a.y)));
+                            y[r] = make_float2(exp2_hw(b.x), exp2_hw(b.y));
                         }
                         uint32_t w[3][RH / 4];
 #pragma unroll
@@ -567,8 +578,8 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
                     }
                     if constexpr (HALVES == 2)
 #pragma unroll
-                        for (int r = 0; r < RH; ++r) {
-                            const float t = l[0][r];
+                        for (int r = 0; r < RH / 2; ++r) {
+                            const float2 t = l[0][r];
                             l[0][r] = l[1][r];
                             l[1][r] = t;
                         }
@@ -587,7 +598,7 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
             {
                 float v[R];
 #pragma unroll
-                for (int r = 0; r < R; ++r) v[r] = l[r / RH][r % RH];
+                for (int r = 0; r < R; ++r) v[r] = r & 1 ? l[r / RH][r % RH / 2].y : l[r / RH][r % RH / 2].x;
                 int row = 0;
 #pragma unroll
                 for (int w = R / 2, o = 16; w; w >>= 1, o >>= 1) {
