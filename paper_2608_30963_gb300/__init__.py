@@ -507,7 +507,7 @@ _PACK_TOKENS = struct.Struct("@iiPPP").pack          # kvx_new_tokens
 _PACK_OPTS = struct.Struct("@iPPPq").pack            # kvx_attend_opts
 _PACK_PLAN = struct.Struct("@iiPPqiiiPPPq").pack     # kvx_evict_plan
 _PACK_CACHE = struct.Struct("@PPiiqqqPiii4x").pack   # kvx_dst_kv
-_PACK_SCALES = struct.Struct("@PPqq").pack           # the end of kvx_quantised_kv, behind its kvx_dst_kv
+_PACK_QUANTISED = struct.Struct("@PPiiqqqPiii4xPPqq").pack   # kvx_quantised_kv
 
 
 def _rows(t) -> bytes:
@@ -601,41 +601,73 @@ class Decoder:
         raise ValueError(f"caches must be alike, [B, {H}, S, {d}] or pools [pages, {page_size}, {H}, {d}] with an int32 page table, of "
                          f"{self._type}, got {tuple(ks)} and {tuple(v.shape)} of {k.dtype} and {v.dtype}")
 
+    def _code_cache(self, k, s, layers: int, at: int, batch: int, page_table, page_size: int, num_pages: int):
+        """An 8-bit cache whose layers are like codes k and scales s, their pointers at `at`, as kvx_quantised_kv; None if it does not fit."""
+        shape, many = k.shape, s.shape
+        if len(shape) != 4 or len(many) != 3 or shape[3] != self._dim:
+            return None
+        n = 8 * layers
+        if page_table is None:
+            b, h, slots, _ = shape
+            (sb, sh, ss, sc), (zb, zh, zs) = k.stride(), s.stride()
+            if h != self._heads or b < batch or sc != 1 or many[0] != b or many[1] != h or many[2] != slots or (zs != 1 and slots > 1):
+                return None
+            return _PACK_QUANTISED(at, at + n, 0, slots, sb, sh, ss, 0, 0, 0, 0, at + 2 * n, at + 3 * n, zb, zh)
+        pages, size, h, _ = shape
+        if page_size >= 1 and not (size == page_size and h == self._heads and many[0] == pages and many[1] == h and many[2] == size and k.is_contiguous()
+                                   and s.is_contiguous() and page_table.dtype == self._i32 and page_table.shape[0] >= batch
+                                   and page_table.is_contiguous()):       # (the library refuses page sizes below 1)
+            return None
+        return _PACK_QUANTISED(at, at + n, 1, 0, 0, 0, 0, page_table.data_ptr(), page_table.shape[1], page_size, num_pages or pages, at + 2 * n, at + 3 * n,
+                               1, 1)
+
+    def _code_layer(self, k, v, ks, vs, batch: int, page_table, page_size: int, num_pages: int):
+        """One layer of an 8-bit cache as kvx_quantised_kv (and what has to live as long), checked: as _layer, codes and scales of K and V
+        alike."""
+        codes, scales = self._code_types, self._scale_types
+        if (k.shape == v.shape and ks.shape == vs.shape and k.dtype in codes and v.dtype in codes and ks.dtype in scales and vs.dtype in scales
+                and k.stride() == v.stride() and ks.stride() == vs.stride()):
+            ptrs = array.array("Q", (k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr()))
+            cache = self._code_cache(k, ks, 1, ptrs.buffer_info()[0], batch, page_table, page_size, num_pages)
+            if cache is not None:
+                return cache, ptrs
+        raise self._not_codes(k, ks, page_size)
+
     def _code_layers(self, k: Sequence, v: Sequence, k_scale: Sequence, v_scale: Sequence, batch: int, page_table, page_size: int,
                      num_pages: int):
-        """Layers of an 8-bit cache as kvx_quantised_kv (and what has to live as long), checked: as _layer, codes and scales alike in
-        every layer."""
-        H, d, k0, s0 = self._heads, self._dim, k[0], k_scale[0]
-        ks, st, ss, sst = k0.shape, k0.stride(), s0.shape, s0.stride()
-        n = len(k)
+        """Layers of an 8-bit cache, all alike, as _code_layer."""
+        k0, s0, n = k[0], k_scale[0], len(k)
         ok = len(v) == len(k_scale) == len(v_scale) == n
-        for some, shape, stride, types in ((k, ks, st, self._code_types), (v, ks, st, self._code_types), (k_scale, ss, sst, self._scale_types),
-                                           (v_scale, ss, sst, self._scale_types)):
-            for t in some:
-                ok = ok and t.shape == shape and t.dtype in types and (t.stride() == stride)
-        ptrs = array.array("Q", [t.data_ptr() for some in (k, v, k_scale, v_scale) for t in some])
-        at = ptrs.buffer_info()[0]
-        if page_table is None:
-            if (ok and len(ks) == 4 and ks[0] >= batch and ks[1] == H and ks[3] == d and st[3] == 1
-                    and ss == ks[:3] and (ss[2] <= 1 or sst[2] == 1)):
-                return (_PACK_CACHE(at, at + 8 * n, 0, ks[2], st[0], st[1], st[2], 0, 0, 0, 0)
-                        + _PACK_SCALES(at + 16 * n, at + 24 * n, sst[0], sst[1])), ptrs
-        else:
-            ts = page_table.shape
-            if page_size < 1 or (ok and ks[1:] == (page_size, H, d) and k0.is_contiguous() and ss == (ks[0], H, page_size)
-                                 and s0.is_contiguous() and ts[0] >= batch and page_table.dtype == self._i32 and page_table.is_contiguous()):
-                return (_PACK_CACHE(at, at + 8 * n, 1, 0, 0, 0, 0, page_table.data_ptr(), ts[1], page_size, num_pages or ks[0])
-                        + _PACK_SCALES(at + 16 * n, at + 24 * n, 1, 1)), ptrs
-        raise ValueError(f"8-bit caches must be alike: codes [B, {H}, S, {d}] of float8_e4m3fn or uint8 with scales [B, {H}, S] of float8_e8m0fnu or "
-                         f"uint8, or pools [pages, {page_size}, {H}, {d}] with scales [pages, {H}, {page_size}] and an int32 page table, got "
-                         f"{tuple(ks)} of {k0.dtype} with {tuple(ss)} of {s0.dtype}")
+        ptrs = array.array("Q")
+        for like, types, both in ((k0, self._code_types, (k, v)), (s0, self._scale_types, (k_scale, v_scale))):
+            shape, stride, plain = like.shape, like.stride(), like.is_contiguous()
+            for some in both:
+                for t in some:
+                    if t.shape != shape or t.dtype not in types or not (t.is_contiguous() if plain else t.stride() == stride):
+                        ok = False
+                ptrs.extend([t.data_ptr() for t in some])
+        cache = self._code_cache(k0, s0, n, ptrs.buffer_info()[0], batch, page_table, page_size, num_pages) if ok else None
+        if cache is None:
+            raise self._not_codes(k0, s0, page_size)
+        return cache, ptrs
+
+    def _not_codes(self, k, s, page_size: int):
+        H, d = self._heads, self._dim
+        return ValueError(f"8-bit caches must be alike: codes [B, {H}, S, {d}] of float8_e4m3fn or uint8 with scales [B, {H}, S] of float8_e8m0fnu or "
+                          f"uint8, or pools [pages, {page_size}, {H}, {d}] with scales [pages, {H}, {page_size}] and an int32 page table, got "
+                          f"{tuple(k.shape)} of {k.dtype} with {tuple(s.shape)} of {s.dtype}")
 
     def _full_layers(self, k: Sequence, v: Sequence, batch: int, page_table, page_size: int, num_pages: int):
         """Layers of a cache of the decoder's type as kvx_dst_kv, checked alike."""
         self._layer(k[0], v[0], batch, page_table, page_size, num_pages)
-        shape, stride = k[0].shape, k[0].stride()
-        if len(v) != len(k) or any(t.shape != shape or t.dtype != self._type or t.stride() != stride for some in (k, v) for t in some):
-            raise ValueError(f"the layers of a cache must be alike, of {self._type}: {tuple(shape)} with strides {stride}")
+        shape, stride, plain = k[0].shape, k[0].stride(), k[0].is_contiguous()
+        ok, dtype = len(v) == len(k), self._type
+        for some in (k, v):
+            for t in some:
+                if t.shape != shape or t.dtype != dtype or not (t.is_contiguous() if plain else t.stride() == stride):
+                    ok = False
+        if not ok:
+            raise ValueError(f"the layers of a cache must be alike, of {dtype}: {tuple(shape)} with strides {stride}")
         return _cache(k, v, page_table, page_size, num_pages)
 
     def append(self, q, k, v, seq_off, kv_len, cache_k, cache_v, q_out, *, pos=None, page_table=None, page_size: int = 16,
@@ -729,7 +761,7 @@ class Decoder:
         if not (self._index(seq_off, 1) and self._index(kv_len, B) and (pos is None or (self._index(pos, T) and pos.shape[0] == T))):
             raise ValueError("seq_off [B + 1], kv_len [B] and pos [tokens] must be contiguous int32")
         tok = _PACK_TOKENS(B, T, seq_off.data_ptr(), kv_len.data_ptr(), 0 if pos is None else pos.data_ptr())
-        cache, _keep = self._code_layers((cache_k,), (cache_v,), (k_scale,), (v_scale,), B, page_table, page_size, num_pages)
+        cache, _keep = self._code_layer(cache_k, cache_v, k_scale, v_scale, B, page_table, page_size, num_pages)
         st = lib().kvx_append_quantised(self.handle, tok, _rows(q), _rows(k), _rows(v), _rows(q_out), cache, 0, _raw_stream(stream))
         if st:
             _check(st)
@@ -746,8 +778,7 @@ class Decoder:
             raise ValueError("seq_off [B + 1], kv_len [B] and prefix_len [B] must be contiguous int32")
         tok = _PACK_TOKENS(B, T, seq_off.data_ptr(), kv_len.data_ptr(), 0)
         opts = _PACK_OPTS(window, 0 if prefix_len is None else prefix_len.data_ptr(), 0 if lse is None else lse.data_ptr(), 0, 0)
-        cache, _keep = self._code_layers((cache_k,), (cache_v,), (k_scale,), (v_scale,), B if B <= KVX_MAX_ATTEND_BATCH else 0, page_table,
-                                         page_size, num_pages)
+        cache, _keep = self._code_layer(cache_k, cache_v, k_scale, v_scale, B if B <= KVX_MAX_ATTEND_BATCH else 0, page_table, page_size, num_pages)
         st = lib().kvx_attend_quantised(self.handle, tok, _rows(q), cache, 0, opts, _rows(out), _raw_stream(stream))
         if st:
             _check(st)

@@ -56,9 +56,20 @@ __device__ __forceinline__ void unpack_codes(uint2 w, float scale, float (&x)[8]
     }
 }
 
-// A row's LANES lanes (consecutive, aligned) hold 16 of its values each: their codes and the row's scale.  Values that are not
-// finite have no say in the scale and become NaN; magnitudes are taken as at most 1.875 * 2^127 (the next code, 2^128, is
-// no number in 32 bits).  Whole warps call it.
+// Infinities become NaN, magnitudes at most 1.875 * 2^127 (the next code, 2^128, is no number in 32 bits).
+__device__ __forceinline__ float tame(float x)
+{
+    return fabsf(x) <= 3.402823466e38f ? copysignf(fminf(fabsf(x), 1.875f * 0x1p127f), x) : __uint_as_float(0x7fffffffu);
+}
+// The scale of a row from its lanes' largest magnitudes (LANES lanes, consecutive, aligned).  Whole warps call it.
+template <int LANES> __device__ __forceinline__ unsigned row_scale(float top)
+{
+#pragma unroll
+    for (int o = LANES / 2; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    return scale_for(top);
+}
+// A row's LANES lanes hold 16 of its values each: their codes and the row's scale.  Values that are not finite have no say in
+// the scale and become NaN.
 template <int LANES> __device__ __forceinline__ unsigned quantise_row(float (&a)[8], float (&b)[8], uint2& lo, uint2& hi)
 {
     auto largest = [&] {
@@ -68,8 +79,7 @@ template <int LANES> __device__ __forceinline__ unsigned quantise_row(float (&a)
         return top;
     };
     float top = largest();              // (a NaN does not count)
-    if (top > 3.0e38f) {                // rare: infinities are taken out
-        auto tame = [](float x) { return fabsf(x) <= 3.402823466e38f ? copysignf(fminf(fabsf(x), 1.875f * 0x1p127f), x) : __uint_as_float(0x7fffffffu); };
+    if (top > 3.0e38f) {                // rare
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             a[i] = tame(a[i]);
@@ -77,9 +87,7 @@ template <int LANES> __device__ __forceinline__ unsigned quantise_row(float (&a)
         }
         top = largest();
     }
-#pragma unroll
-    for (int o = LANES / 2; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    const unsigned s = scale_for(top);
+    const unsigned s = row_scale<LANES>(top);
     const float f = inv_scale(s);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {

@@ -14,106 +14,168 @@ namespace {
 
 constexpr int kConvertThreads = 256, kAppendThreads = 128;
 
+// Sixteen of a row's values as they came from memory: eight of its first half, eight of its second.
+template <typename T> struct RowPart {
+    uint4 w[sizeof(T)];                              // 16 bytes each
+    __device__ __forceinline__ void load(const T* p, int half)
+    {
+        constexpr int N = 16 / (int)sizeof(T), M = (int)sizeof(T) / 2;
+#pragma unroll
+        for (int i = 0; i < M; ++i) {
+            w[i] = __ldcs(reinterpret_cast<const uint4*>(p + i * N));
+            w[M + i] = __ldcs(reinterpret_cast<const uint4*>(p + half + i * N));
+        }
+    }
+    // values 8 half .. 8 half + 7
+    __device__ __forceinline__ void get(int half, float (&x)[8]) const
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint4 v = sizeof(T) == 2 ? w[half] : w[half * 2 + i / 4];
+            const int e = sizeof(T) == 2 ? i / 2 : i % 4;
+            const uint32_t u = e == 0 ? v.x : e == 1 ? v.y : e == 2 ? v.z : v.w;
+            x[i] = sizeof(T) == 4 ? __uint_as_float(u) : __uint_as_float(i & 1 ? u & 0xffff0000u : u << 16);
+        }
+    }
+};
+
 // Each warp takes 32 rows of one (layer, K or V, sequence) at a time: its lanes find a row each, then all of them convert
-// the rows, U at a time for each of the warp's 32 / LANES places.
+// the rows, U at a time for each of the warp's 32 / LANES places.  The next 32 rows' pages are read before.  What is loaded stays
+// packed until it is used: 64 registers, 32 warps an SM (with floats 115 registers and 604 us for 28 layers of 53385 slots of 2
+// heads of 128).
 template <typename T, int D, bool TO_CODES>
-__global__ void __launch_bounds__(kConvertThreads) convert_kernel(const __grid_constant__ ConvertParams P)
+__global__ void __launch_bounds__(kConvertThreads, TO_CODES ? 4 : 3) convert_kernel(const __grid_constant__ ConvertParams P)
 {
-    constexpr int LANES = D / 16, ROWS = 32 / LANES, U = sizeof(T) == 2 ? 4 : 2;
+    constexpr int LANES = D / 16, ROWS = 32 / LANES, U = !TO_CODES ? 4 : sizeof(T) == 2 ? 2 : 1;
     extern __shared__ long long first[];             // groups of 32 rows before each sequence's
     const int tid = threadIdx.x, lane = tid & 31, sub = lane / LANES, c = lane % LANES * 8;
-    for (int b = tid; b < P.batch; b += kConvertThreads) {
-        const int most = min(P.full.capacity, P.codes.capacity), n = seq_slots(P.kv_len, most, b, P.status);
-        first[b + 1] = ((long long)n * P.H + 31) / 32;
-    }
+    const int most = min(P.full.capacity, P.codes.capacity);
+    for (int b = tid; b < P.batch; b += kConvertThreads) first[b + 1] = ((long long)seq_slots(P.kv_len, most, b, P.status) * P.H + 31) / 32;
     if (tid == 0) first[0] = 0;
     __syncthreads();
     if (tid == 0)
         for (int b = 0; b < P.batch; ++b) first[b + 1] += first[b];
     __syncthreads();
     const long long groups = first[P.batch], total = groups * 2 * P.L, warps = (long long)gridDim.x * (kConvertThreads / 32);
-    for (long long i = (long long)blockIdx.x * (kConvertThreads / 32) + (tid >> 5); i < total; i += warps) {
-        const long long unit = i / groups, g = i - unit * groups;
-        const int l = (int)(unit >> 1);
-        const bool key = !(unit & 1);
+    // a lane's row of group i: its slot (-1: none) and head, and the pages that hold it
+    struct Row {
+        int b, s, h, full, code;
+    };
+    auto page_of = [](const CacheView& C, int b, int s) {
+        if (!C.paged) return 0;
+        const int pi = C.page_shift >= 0 ? s >> C.page_shift : s / C.page_size;
+        return pi < C.max_pages ? C.page_table[(size_t)b * C.max_pages + pi] : -1;
+    };
+    auto row_of = [&](long long i) {
+        Row r = {0, -1, 0, -1, -1};
+        if (i >= total) return r;
+        const long long g = i % groups;
         int lo = 0, hi = P.batch - 1;                // the sequence of group g
         while (lo < hi) {
             const int m = (lo + hi + 1) >> 1;
             if (first[m] <= g) lo = m; else hi = m - 1;
         }
-        const int b = lo, n = min(max(P.kv_len[b], 0), min(P.full.capacity, P.codes.capacity));
+        const int n = min(max(P.kv_len[lo], 0), most);
+        const long long k = (g - first[lo]) * 32 + lane;
+        if (k >= (long long)n * P.H) return r;
         // rows in the order that the wider cache has them in
-        const long long r = (g - first[b]) * 32 + lane;
+        r.b = lo;
+        if (k >> 31) {
+            r.s = (int)(P.full.paged ? k / P.H : k % n);
+            r.h = (int)(P.full.paged ? k % P.H : k / n);
+        } else {
+            const unsigned by = (unsigned)(P.full.paged ? P.H : n), q = (unsigned)k / by, rest = (unsigned)k - q * by;
+            r.s = (int)(P.full.paged ? q : rest);
+            r.h = (int)(P.full.paged ? rest : q);
+        }
+        r.full = page_of(P.full, r.b, r.s);
+        r.code = page_of(P.codes, r.b, r.s);
+        return r;
+    };
+    auto place = [](const CacheView& C, int b, int s, int page, int& in) -> long long {
+        if (!C.paged) return (long long)b * C.sb + (long long)s * C.st;
+        if (page < 0 || page >= C.num_pages) return -1;
+        in = C.page_shift >= 0 ? s & (C.page_size - 1) : s % C.page_size;
+        return ((long long)page * C.page_size + in) * ((long long)C.H * D);
+    };
+    long long i = (long long)blockIdx.x * (kConvertThreads / 32) + (tid >> 5);
+    Row next = row_of(i);
+    for (; i < total; i += warps) {
+        const Row r = next;
+        next = row_of(i + warps);
+        const long long unit = i / groups;
+        const int l = (int)(unit >> 1);
+        const bool key = !(unit & 1);
         long long full = -1, code = -1, scale = 0;
-        if (r < (long long)n * P.H) {
-            const int s = P.full.paged ? (int)(r / P.H) : (int)(r % n), h = P.full.paged ? (int)(r % P.H) : (int)(r / n);
-            full = cache_row(P.full, b, s);
-            const CodePlace at = code_place(P.codes, P.scales, b, s);
-            code = at.row;
+        if (r.s >= 0) {
+            int in = 0;
+            full = place(P.full, r.b, r.s, r.full, in);
+            code = place(P.codes, r.b, r.s, r.code, in);
             if (full < 0 || code < 0) {
                 set_status(P.status, KVX_DEV_PAGE_INVALID);
                 full = code = -1;
             } else {
-                full += cache_head(P.full) * h;
-                code += cache_head(P.codes) * h;
-                scale = at.scale + scale_head(P.codes, P.scales) * h;
+                full += cache_head(P.full) * r.h;
+                code += cache_head(P.codes) * r.h;
+                scale = (P.codes.paged ? (long long)r.code * P.H * P.codes.page_size + in : (long long)r.b * P.scales.sb + r.s) +
+                        scale_head(P.codes, P.scales) * r.h;
             }
         }
         T* fp = (T*)(key ? P.full_k[l] : P.full_v[l]);
         uint8_t* cp = (uint8_t*)(key ? P.code_k[l] : P.code_v[l]);
         uint8_t* sp = key ? P.k_scale[l] : P.v_scale[l];
+        unsigned mine = 0;                           // the lane's row's scale byte
+        if (!TO_CODES && full >= 0) mine = sp[scale];
 #pragma unroll 1
         for (int k0 = 0; k0 < 32; k0 += U * ROWS) {
-            long long f[U], w[U], z[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                f[u] = __shfl_sync(0xffffffffu, full, k0 + u * ROWS + sub);
-                w[u] = __shfl_sync(0xffffffffu, code, k0 + u * ROWS + sub);
-                z[u] = __shfl_sync(0xffffffffu, scale, k0 + u * ROWS + sub);
-            }
             if constexpr (TO_CODES) {
-                float a[U][8], e[U][8];
+                RowPart<T> x[U];
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
-                    if (f[u] >= 0) {
-                        load8<T>(fp + f[u] + c, a[u]);
-                        load8<T>(fp + f[u] + D / 2 + c, e[u]);
-                    } else {
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) a[u][k] = e[u][k] = 0.0f;
-                    }
+                    const long long f = __shfl_sync(0xffffffffu, full, k0 + u * ROWS + sub);
+                    if (f >= 0) x[u].load(fp + f + c, D / 2);
+                    else x[u] = {};
                 }
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
-                    uint2 x, y;
-                    const unsigned s = quantise_row<LANES>(a[u], e[u], x, y);
-                    if (w[u] >= 0) {
-                        __stcs(reinterpret_cast<uint2*>(cp + w[u] + c), x);
-                        __stcs(reinterpret_cast<uint2*>(cp + w[u] + D / 2 + c), y);
-                        if (c == 0) sp[z[u]] = (uint8_t)s;
+                    const long long w = __shfl_sync(0xffffffffu, code, k0 + u * ROWS + sub);
+                    float a[8], b[8];
+                    x[u].get(0, a);
+                    x[u].get(1, b);
+                    uint2 lo, hi;
+                    const unsigned s = quantise_row<LANES>(a, b, lo, hi), from = __shfl_sync(0xffffffffu, s, (lane - k0 - u * ROWS) * LANES & 31);
+                    if (lane >= k0 + u * ROWS && lane < k0 + (u + 1) * ROWS) mine = from;
+                    if (w >= 0) {
+                        __stcs(reinterpret_cast<uint2*>(cp + w + c), lo);
+                        __stcs(reinterpret_cast<uint2*>(cp + w + D / 2 + c), hi);
                     }
                 }
             } else {
                 uint2 x[U], y[U];
-                unsigned s[U];
 #pragma unroll
-                for (int u = 0; u < U; ++u)
-                    if (w[u] >= 0) {
-                        x[u] = __ldcs(reinterpret_cast<const uint2*>(cp + w[u] + c));
-                        y[u] = __ldcs(reinterpret_cast<const uint2*>(cp + w[u] + D / 2 + c));
-                        s[u] = sp[z[u]];
+                for (int u = 0; u < U; ++u) {
+                    const long long w = __shfl_sync(0xffffffffu, code, k0 + u * ROWS + sub);
+                    x[u] = y[u] = make_uint2(0u, 0u);
+                    if (w >= 0) {
+                        x[u] = __ldcs(reinterpret_cast<const uint2*>(cp + w + c));
+                        y[u] = __ldcs(reinterpret_cast<const uint2*>(cp + w + D / 2 + c));
                     }
+                }
 #pragma unroll
-                for (int u = 0; u < U; ++u)
-                    if (f[u] >= 0) {
+                for (int u = 0; u < U; ++u) {
+                    const long long f = __shfl_sync(0xffffffffu, full, k0 + u * ROWS + sub);
+                    const float z = scale_of(__shfl_sync(0xffffffffu, mine, k0 + u * ROWS + sub));
+                    if (f >= 0) {
                         float a[8], e[8];
-                        unpack_codes(x[u], scale_of(s[u]), a);
-                        unpack_codes(y[u], scale_of(s[u]), e);
-                        store8<T>(fp + f[u] + c, a);
-                        store8<T>(fp + f[u] + D / 2 + c, e);
+                        unpack_codes(x[u], z, a);
+                        unpack_codes(y[u], z, e);
+                        store8<T>(fp + f + c, a);
+                        store8<T>(fp + f + D / 2 + c, e);
                     }
+                }
             }
         }
+        if (TO_CODES && full >= 0) sp[scale] = (uint8_t)mine;   // neighbouring slots' side by side
     }
 }
 
@@ -123,82 +185,82 @@ __global__ void __launch_bounds__(kConvertThreads) convert_kernel(const __grid_c
 template <int D>
 __global__ void __launch_bounds__(kConvertThreads) expand_kernel(const __grid_constant__ AttendParams P, __nv_bfloat16* to_k, __nv_bfloat16* to_v)
 {
-    constexpr int LANES = D / 16, ROWS = 32 / LANES, U = 4;
-    extern __shared__ long long first[];             // groups of 32 slots before each sequence's
+    constexpr int LANES = D / 16, ROWS = 32 / LANES, U = 2;
+    extern __shared__ int4 ranges[];                 // slots [0, x) and [y, z) of a sequence; w: groups of 32 slots before its first
     const int tid = threadIdx.x, lane = tid & 31, sub = lane / LANES, c = lane % LANES * 8;
     grid_dependency_wait();
     grid_launch_dependents();
-    // slots [0, a) and [z, L) of a sequence, in tiles
-    auto range = [&](int b, int& a, int& z, int& L) {
-        const Seq s = load_seq(P, b);
-        L = s.L;
-        a = min((s.pre + 127) / 128 * 128, L);
-        z = max(max(window_lo(P, s.slot(0)), 0) / 128 * 128, a);
-        if (s.n == 0) a = z = L = 0;
-    };
     for (int b = tid; b < P.batch; b += kConvertThreads) {
-        int a, z, L;
-        range(b, a, z, L);
-        first[b + 1] = (a + 31) / 32 + (max(L - z, 0) + 31) / 32;
+        const Seq s = load_seq(P, b);
+        const int L = s.n ? s.L : 0, a = min((s.pre + 127) / 128 * 128, L);
+        ranges[b] = make_int4(a, max(max(window_lo(P, s.slot(0)), 0) / 128 * 128, a), L, 0);
     }
-    if (tid == 0) first[0] = 0;
     __syncthreads();
-    if (tid == 0)
-        for (int b = 0; b < P.batch; ++b) first[b + 1] += first[b];
+    if (tid == 0) {
+        int run = 0;
+        for (int b = 0; b < P.batch; ++b) {
+            ranges[b].w = run;
+            run += (ranges[b].x + 31) / 32 + (max(ranges[b].z - ranges[b].y, 0) + 31) / 32;
+        }
+        ranges[P.batch].w = run;
+    }
     __syncthreads();
-    const long long groups = first[P.batch], total = groups * 2 * P.H, warps = (long long)gridDim.x * (kConvertThreads / 32);
-    for (long long i = (long long)blockIdx.x * (kConvertThreads / 32) + (tid >> 5); i < total; i += warps) {
-        // heads one after the other: a token's lie side by side in a pool
-        const long long g = i / (2 * P.H);
-        const int hk = (int)(i - g * (2 * P.H)), h = hk >> 1;
-        const bool key = !(hk & 1);
+    const int groups = ranges[P.batch].w;            // (the workspace holds 2^18 slots)
+    const int total = groups * P.H, warps = gridDim.x * (kConvertThreads / 32);
+    for (int i = blockIdx.x * (kConvertThreads / 32) + (tid >> 5); i < total; i += warps) {
+        // heads one after the other: a slot's lie side by side in a pool
+        const int g = i / P.H, h = i - g * P.H;
         int lo = 0, hi = P.batch - 1;                // the sequence of group g
         while (lo < hi) {
             const int m = (lo + hi + 1) >> 1;
-            if (first[m] <= g) lo = m; else hi = m - 1;
+            if (ranges[m].w <= g) lo = m; else hi = m - 1;
         }
         const int b = lo;
-        int a, z, L;
-        range(b, a, z, L);
-        const int k = (int)(g - first[b]), s0 = k < (a + 31) / 32 ? k * 32 : z + (k - (a + 31) / 32) * 32, s = s0 + lane;
+        const int4 of = ranges[b];
+        const int k = g - of.w, s0 = k < (of.x + 31) / 32 ? k * 32 : of.y + (k - (of.x + 31) / 32) * 32, s = s0 + lane, L = of.z;
         long long code = -1;
-        float scale = 0.0f;
+        float scale[2] = {};
         if (s < L) {
             const CodePlace at = code_place(P.cache, P.scales, b, s);
             if (at.row < 0) {
                 set_status(P.status, KVX_DEV_PAGE_INVALID);
             } else {
+                const long long z = at.scale + scale_head(P.cache, P.scales) * h;
                 code = at.row + cache_head(P.cache) * h;
-                scale = scale_of((key ? P.k_scale : P.v_scale)[at.scale + scale_head(P.cache, P.scales) * h]);
+                scale[0] = scale_of(P.k_scale[z]);
+                scale[1] = scale_of(P.v_scale[z]);
             }
         }
-        const uint8_t* cp = (const uint8_t*)(key ? P.ck : P.cv);
-        __nv_bfloat16* out = (key ? to_k : to_v) + (((long long)b * P.H + h) * P.cache.capacity + s0) * D;
+        const long long to = (((long long)b * P.H + h) * P.cache.capacity + s0) * D + c;
 #pragma unroll 1
         for (int k0 = 0; k0 < 32; k0 += U * ROWS) {
-            uint2 x[U], y[U];
+            uint2 x[U][2], y[U][2];                  // of K and V
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const long long w = __shfl_sync(0xffffffffu, code, k0 + u * ROWS + sub);
-                x[u] = y[u] = make_uint2(0u, 0u);
-                if (w >= 0) {
-                    x[u] = *reinterpret_cast<const uint2*>(cp + w + c);
-                    y[u] = *reinterpret_cast<const uint2*>(cp + w + D / 2 + c);
+#pragma unroll
+                for (int v = 0; v < 2; ++v) {
+                    const uint8_t* from = (const uint8_t*)(v ? P.cv : P.ck) + w + c;
+                    x[u][v] = y[u][v] = make_uint2(0u, 0u);
+                    if (w >= 0) {
+                        x[u][v] = *reinterpret_cast<const uint2*>(from);
+                        y[u][v] = *reinterpret_cast<const uint2*>(from + D / 2);
+                    }
                 }
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int r = k0 + u * ROWS + sub;
-                const float f = __shfl_sync(0xffffffffu, scale, r);
-                if (s0 + r < L) {
+#pragma unroll
+                for (int v = 0; v < 2; ++v) {
+                    const float f = __shfl_sync(0xffffffffu, scale[v], r);
+                    if (s0 + r >= L) continue;
                     float p[8], q[8];
-                    unpack_codes(x[u], f, p);
-                    unpack_codes(y[u], f, q);
-                    uint4 v;
-                    v = make_uint4(pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3]), pack_bf16(p[4], p[5]), pack_bf16(p[6], p[7]));
-                    *reinterpret_cast<uint4*>(out + (long long)r * D + c) = v;
-                    v = make_uint4(pack_bf16(q[0], q[1]), pack_bf16(q[2], q[3]), pack_bf16(q[4], q[5]), pack_bf16(q[6], q[7]));
-                    *reinterpret_cast<uint4*>(out + (long long)r * D + D / 2 + c) = v;
+                    unpack_codes(x[u][v], f, p);
+                    unpack_codes(y[u][v], f, q);
+                    __nv_bfloat16* out = (v ? to_v : to_k) + to + (long long)r * D;
+                    *reinterpret_cast<uint4*>(out) = make_uint4(pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3]), pack_bf16(p[4], p[5]), pack_bf16(p[6], p[7]));
+                    *reinterpret_cast<uint4*>(out + D / 2) = make_uint4(pack_bf16(q[0], q[1]), pack_bf16(q[2], q[3]), pack_bf16(q[4], q[5]), pack_bf16(q[6], q[7]));
                 }
             }
         }
@@ -285,11 +347,11 @@ template <typename T, bool TO_CODES> cudaError_t run_convert(const ConvertParams
 }
 template <int D> cudaError_t run_expand(const AttendParams& P, void* to_k, void* to_v, int num_sms, cudaStream_t stream)
 {
-    const long long groups = ((long long)P.cache.capacity + 63) / 32 * P.batch * P.H * 2;
+    const long long groups = ((long long)P.cache.capacity + 63) / 32 * P.batch * P.H;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)min((groups + kConvertThreads / 32 - 1) / (kConvertThreads / 32), (long long)num_sms * 8));
     cfg.blockDim = dim3(kConvertThreads);
-    cfg.dynamicSmemBytes = (P.batch + 1) * sizeof(long long);
+    cfg.dynamicSmemBytes = (P.batch + 1) * sizeof(int4);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

@@ -21,7 +21,7 @@ def test_null_arguments(lib):
 
 
 def test_the_bytes_that_the_binding_packs_are_the_structs():
-    cache = kvx._PACK_CACHE(1, 2, 1, 3, 4, 5, 6, 7, 8, 9, 10) + kvx._PACK_SCALES(11, 12, 13, 14)
+    cache = kvx._PACK_QUANTISED(1, 2, 1, 3, 4, 5, 6, 7, 8, 9, 10, 11, 12, 13, 14)
     assert len(cache) == ctypes.sizeof(kvx.kvx_quantised_kv)
     s = kvx.kvx_quantised_kv.from_buffer_copy(cache)
     assert (s.codes.paged, s.codes.stride_t, s.codes.num_pages, s.k_scale, s.v_scale, s.scale_stride_b, s.scale_stride_h) == (1, 6, 10, 11, 12, 13, 14)
