@@ -18,16 +18,21 @@ template <typename T, bool CAP> cudaError_t run_codes(const AttendParams& P, int
 
 // Prompts: every row tile of a (sequence, KV head) reads its slots again, so from some row tiles on the slots become bf16
 // once, in the workspace (64 MiB, where the call's cache may fit it), and the kernels of bf16 caches take them from there.
-// (One sequence, us so and with the codes converted by each tile: 7 query heads on each of 4 KV heads of 128 over 16384 slots,
-// 896 rows 62 and 57, 1792 rows 82 and 84, 7168 rows 212 and 247; heads of 256, whose tiles have 128 rows, 512 rows 58 and 56, 1024
-// rows 70 and 79; 4096 tokens over 32768 slots 1171 and 1568.)
+// (One sequence, us so and with the codes converted by each row tile: 7 query heads on each of 4 KV heads of 128 over 16384
+// slots, 896 rows 58 and 55, 1792 rows 79 and 83, 7168 rows 207 and 247; heads of 256, whose tiles have 128 rows, 512 rows 55 and 54,
+// 1024 rows 67 and 76; heads of 64, 4096 rows 36 and 35, 8192 rows 46 and 47; 4096 tokens over 32768 slots 1166 and 1568.
+// Capped scores: heads of 128, 1792 rows 382 and 221, 7168 rows 1040 and 677, so not there; heads of 256, 1024 rows 79 and 86.)
 bool expands(const AttendParams& P)
 {
     const int tile = P.d == 256 ? 128 : 256;
+    if (P.cap > 0.0f && P.d == 128) return false;
     // (batch <= 1024, capacity <= 2^30: no product wraps)
     return (long long)P.T * P.G > 6ll * tile * P.batch && (long long)P.batch * P.cache.capacity <= kAttendScores / ((long long)P.H * P.d);
 }
-// Few rows: the tile's rows (8, 16 or 32) that take the call's mean a sequence and KV head in whole tokens, or 0.
+// Few rows: the rows of a tile (8, 16 or 32) that hold the call's mean a sequence and KV head, in whole tokens, or 0.  (Four
+// sequences of 16384 slots, us so and with the codes converted: 7 rows on each of 4 KV heads of 128 23 and 48, 28 rows 47 and 56, on 8
+// KV heads 32 rows 70 and 84; heads of 256 over 8192 slots, 2 rows 22 and 40, 32 rows 45 and 50; one sequence of 2000 slots, 32
+// rows 18.5 and 18.0.  A head of 64 fills half of a 128-byte block: not taken.)
 int few_rows(const AttendParams& P)
 {
     if (P.d == 64) return 0;
