@@ -5,7 +5,7 @@
 // With few rows (query heads of a token) the products have room to spare, and what costs is bringing K and V: so the
 // cache's codes are the operands, straight from memory, and the other side is split into e4m3 terms that make up for its
 // 4 bits.  A query row is scaled by a power of two and split in two (bf16's 8 bits exactly, down to 2^-14 of the row's largest
-// value, below that to 2^-22 of it), a weight in three (to 2^-12 of itself, 2^-23 of the row's largest).  Terms lie side by
+// value, below that to 2^-22 of it), a weight in three (to 2^-12 of itself, 2^-22 of the row's largest).  Terms lie side by
 // side as columns of one product; sums are fp32.  Slots are the rows of S^T and channels those of O^T, so the rows of a tile
 // are its columns: 256 slots by 8, 16 or 32 rows.
 //   copying warps (7)   128-byte blocks of K and V rows into 128-byte-swizzled tiles, every seventh each

@@ -241,6 +241,8 @@ kvx_status convert(kvx_decoder* dec, const char* who, int batch, int L, const in
     P.kv_len = kv_len;
     P.status = dec->status;
     for (int l = 0; l < L; ++l) {
+        if (full->k[l] == codes->codes.k[l] || full->v[l] == codes->codes.v[l])
+            return fail(KVX_ERR_INVALID_ARG, "%s: the caches are the same memory (layer %d)", who, l);
         P.full_k[l] = full->k[l]; P.full_v[l] = full->v[l];
         P.code_k[l] = codes->codes.k[l]; P.code_v[l] = codes->codes.v[l];
         P.k_scale[l] = codes->k_scale[l]; P.v_scale[l] = codes->v_scale[l];

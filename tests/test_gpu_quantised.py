@@ -633,6 +633,12 @@ def test_refusals():
         with pytest.raises(kvx.KvxError) as e:
             p.dec.attend_quantised(q, off, L, c, c, flat, flat, out)
         assert e.value.status == kvx.KVX_ERR_INVALID_ARG
+    # a cache over itself
+    same = torch.zeros((1, 2, 64, 128), dtype=torch.bfloat16, device="cuda")
+    small = same.view(torch.uint8).view(-1)[:2 * 64 * 128].view(1, 2, 64, 128)
+    with pytest.raises(kvx.KvxError) as e:
+        p.dec.quantise(L, [same], [full[1]], [small], [small.clone()], [flat], [flat])
+    assert e.value.status == kvx.KVX_ERR_INVALID_ARG
     # weight sums: not over 8 bits
     import ctypes
     opts = kvx.kvx_attend_opts(0, None, 1, 1, 64)
