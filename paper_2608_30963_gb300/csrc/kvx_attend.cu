@@ -111,7 +111,7 @@ template <int D, bool CAP> cudaError_t run_fp32(const AttendParams& P, int num_s
     // Few rows for each sequence and head: 16-row tiles waste less of the arithmetic (eight sequences of 4096 slots, heads of
     // 128: 12 rows 79.5 us in tiles of 16 and 89.8 of 64, 18 rows 96.9 and 90.8; heads of 256: 93.9 and 99.0, 162 and 102)
     const bool few = (long long)P.T * P.G <= 16ll * P.batch;
-    return few ? run_simt<float, D, 16, CAP, false>(P, num_sms, stream) : run_simt<float, D, D == 256 ? 32 : 64, CAP, false>(P, num_sms, stream);
+    return few ? run_simt<D, 16, CAP, false>(P, num_sms, stream) : run_simt<D, D == 256 ? 32 : 64, CAP, false>(P, num_sms, stream);
 }
 template <bool CAP> cudaError_t attend_fp32(const AttendParams& P, int num_sms, cudaStream_t stream)
 {

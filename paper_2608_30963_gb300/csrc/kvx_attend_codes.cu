@@ -4,16 +4,16 @@
 namespace kvx {
 namespace {
 
-template <typename T, int D, bool CAP> cudaError_t run_codes(const AttendParams& P, int num_sms, cudaStream_t stream)
+// fp32 queries: on the CUDA cores
+template <int D, bool CAP> cudaError_t run_fp32(const AttendParams& P, int num_sms, cudaStream_t stream)
 {
     // few rows: 16-row tiles, as over fp32 caches
     const bool few = (long long)P.T * P.G <= 16ll * P.batch;
-    return few ? run_simt<T, D, 16, CAP, true>(P, num_sms, stream) : run_simt<T, D, D == 256 ? 32 : 64, CAP, true>(P, num_sms, stream);
+    return few ? run_simt<D, 16, CAP, true>(P, num_sms, stream) : run_simt<D, D == 256 ? 32 : 64, CAP, true>(P, num_sms, stream);
 }
-template <typename T, bool CAP> cudaError_t run_codes(const AttendParams& P, int num_sms, cudaStream_t stream)
+template <bool CAP> cudaError_t attend_fp32(const AttendParams& P, int num_sms, cudaStream_t stream)
 {
-    return P.d == 64 ? run_codes<T, 64, CAP>(P, num_sms, stream) : P.d == 128 ? run_codes<T, 128, CAP>(P, num_sms, stream)
-                                                                             : run_codes<T, 256, CAP>(P, num_sms, stream);
+    return P.d == 64 ? run_fp32<64, CAP>(P, num_sms, stream) : P.d == 128 ? run_fp32<128, CAP>(P, num_sms, stream) : run_fp32<256, CAP>(P, num_sms, stream);
 }
 
 // Prompts: every row tile of a (sequence, KV head) reads its slots again, so from some row tiles on the slots become bf16
@@ -65,16 +65,14 @@ cudaError_t launch_attend_codes(const AttendParams& call, int dtype, int num_sms
     *launches = 0;
     if (call.T == 0) return cudaSuccess;
     AttendParams P = call;
-    *launches = 2;
-    if (dtype == KVX_BF16 && expands(P)) {
-        *launches = 3;
-        return attend_expanded(P, num_sms, stream);
-    }
     P.scores = nullptr;                          // no weight sums
-    if (const int rows = dtype == KVX_BF16 ? few_rows(P) : 0)
-        return P.cap > 0.0f ? launch_attend_few_capped(P, rows, num_sms, stream) : launch_attend_few(P, rows, num_sms, stream);
-    if (dtype == KVX_BF16) return P.cap > 0.0f ? launch_attend_tc_codes_capped(P, num_sms, stream) : launch_attend_tc_codes(P, num_sms, stream);
-    return P.cap > 0.0f ? run_codes<float, true>(P, num_sms, stream) : run_codes<float, false>(P, num_sms, stream);
+    const bool cap = P.cap > 0.0f;
+    *launches = 2;
+    if (dtype != KVX_BF16) return cap ? attend_fp32<true>(P, num_sms, stream) : attend_fp32<false>(P, num_sms, stream);
+    if (const int rows = few_rows(P)) return cap ? launch_attend_few_capped(P, rows, num_sms, stream) : launch_attend_few(P, rows, num_sms, stream);
+    if (!expands(P)) return cap ? launch_attend_tc_codes_capped(P, num_sms, stream) : launch_attend_tc_codes(P, num_sms, stream);
+    *launches = 3;
+    return attend_expanded(call, num_sms, stream);
 }
 
 }  // namespace kvx

@@ -12,9 +12,9 @@
 //   MMA warp            tile i: S(i + 2) into S(i)'s place once that has been read; O of warpgroup i mod 2 += V P(i) when P(i) is there
 //   softmax warps (8)   two warpgroups, every other tile each; a thread has a slot.  A score x takes its K row's scale; a weight
 //                       takes its V row's, in its exponent, z = x + log2 of it, and a reference n of its own beside the sums'
-//                       reference m, so that far scales do not leave e4m3's range.  A row takes new references when x or z
-//                       has grown by more than 1 (a factor of two) beyond them; each warpgroup has its own references, sums
-//                       and O, joined at the end.
+//                       reference m, so that far scales do not leave e4m3's range.  A row takes new references when z has grown by
+//                       more than 1 (a factor of two) beyond n, or x by 64 beyond m (sums in fp32 have room); each warpgroup has
+//                       its own references, sums and O, joined at the end.
 // The last rows of the split work are joined as those of the other attention kernels.
 #pragma once
 
@@ -503,7 +503,7 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
                             ahead = max3(ahead, a.x, a.y);
                             ahead_z = max3(ahead_z, b.x, b.y);
                         }
-                    if (group_any(1 + wg, 128, (ahead > 1.0f || ahead_z > 8.0f) && ok)) {
+                    if (group_any(1 + wg, 128, (ahead > 64.0f || ahead_z > 8.0f) && ok)) {
 #pragma unroll
                         for (int r = 0; r < RH; ++r) {
                             float a = -INFINITY, b = -INFINITY;
@@ -544,7 +544,7 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
                             tmem_st_wait();
                         }
                     }
-                    // weights, 128 for the largest (at most 256: the reference may stay behind by a factor of two)
+                    // weights, 128 for the largest, at most 256 (so that 32 times what a term leaves is at most 256, too)
 #pragma unroll
                     for (int h = 0; h < HB; ++h) {
                         float2 y[RH / 2];

@@ -12,7 +12,6 @@
 #pragma once
 
 #include <atomic>
-#include <type_traits>
 
 #include "kvx_attend_rows.cuh"
 #include "kvx_kernels.h"
@@ -143,7 +142,7 @@ template <int D, int BM> constexpr int simt_smem()
 
 // 128 threads on a tile of BM rows and 32 slots; K of the next tile is copied while V is multiplied, V
 // while the scores are.
-template <typename T, int D, int BM, bool CAP, bool CODES>
+template <int D, int BM, bool CAP, bool CODES>
 __global__ void __launch_bounds__(kThreads) attend_simt_kernel(const __grid_constant__ AttendParams P)
 {
     constexpr int RM = BM / kTR, CN = D / 32;   // rows of a thread; its float4 column groups 4 tc + 32 n
@@ -183,17 +182,7 @@ __global__ void __launch_bounds__(kThreads) attend_simt_kernel(const __grid_cons
             const RowId id = row_id(P, g.s, g.h, g.rt * BM + r);
             return (long long)(g.s.t0 + id.t) * P.q_t + (long long)id.head * P.q_h;
         };
-        if constexpr (std::is_same_v<T, float>) {
-            load_tile<D, BM, kThreads>(sQ, (const float*)P.q, query);
-        } else {
-            for (int x = tid; x < BM * (D / 8); x += kThreads) {
-                const long long at = query(x / (D / 8));
-                float v[8] = {};
-                if (at >= 0) load8<T>((const T*)P.q + at + x % (D / 8) * 8, v);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) sQ[x / (D / 8) * (D + 4) + x % (D / 8) * 8 + e] = v[e];
-            }
-        }
+        load_tile<D, BM, kThreads>(sQ, (const float*)P.q, query);
         // (8 bits: a tile is fetched where its copies would begin, and put where they would be waited for)
         CodeTile<D> codes;
         auto begin = [&](float* dst, const void* src, const unsigned char* scales, int tile) {
@@ -315,7 +304,7 @@ __global__ void __launch_bounds__(kThreads) attend_simt_kernel(const __grid_cons
 #pragma unroll
                 for (int c = 0; c < D / 32; ++c) y[c] = sQ[r * (D + 4) + lane * (D / 32) + c];
                 const RowId id = row_id(P, g.s, g.h, g.rt * BM + r);
-                finish_row<T, D>(P, g.b, g.h, g.rt * BM + r, g.s.t0 + id.t, id.head, sP[r * (kBN + 4)], sP[r * (kBN + 4) + 1], y);
+                finish_row<float, D>(P, g.b, g.h, g.rt * BM + r, g.s.t0 + id.t, id.head, sP[r * (kBN + 4)], sP[r * (kBN + 4) + 1], y);
             }
         } else {
             const size_t at = (size_t)(2 * blockIdx.x + (g.first ? 0 : 1)) * BM;
@@ -346,16 +335,16 @@ template <auto Kernel> int ctas_per_sm(int smem, int threads)
     return n;
 }
 
-template <typename T, int D, int BM, bool CAP, bool CODES> cudaError_t run_simt(const AttendParams& call, int num_sms, cudaStream_t stream)
+template <int D, int BM, bool CAP, bool CODES> cudaError_t run_simt(const AttendParams& call, int num_sms, cudaStream_t stream)
 {
     AttendParams P = call;
     P.tile_rows = BM;
     constexpr int smem = simt_smem<D, BM>();
-    if (cudaError_t e = smem_opt_in<attend_simt_kernel<T, D, BM, CAP, CODES>>(smem); e != cudaSuccess) return e;
-    const int grid = min(num_sms * ctas_per_sm<attend_simt_kernel<T, D, BM, CAP, CODES>>(smem, kThreads), kAttendMaxRows / BM / 2);
-    attend_simt_kernel<T, D, BM, CAP, CODES><<<grid, kThreads, smem, stream>>>(P);
+    if (cudaError_t e = smem_opt_in<attend_simt_kernel<D, BM, CAP, CODES>>(smem); e != cudaSuccess) return e;
+    const int grid = min(num_sms * ctas_per_sm<attend_simt_kernel<D, BM, CAP, CODES>>(smem, kThreads), kAttendMaxRows / BM / 2);
+    attend_simt_kernel<D, BM, CAP, CODES><<<grid, kThreads, smem, stream>>>(P);
     if (cudaError_t e = cudaGetLastError(); e != cudaSuccess) return e;
-    return run_join<T, D, BM>(P, grid, stream);
+    return run_join<float, D, BM>(P, grid, stream);
 }
 
 }  // namespace

@@ -111,7 +111,8 @@ template <int D, int NT> __device__ __forceinline__ bool two_terms(const AttendP
 
 // How K and V tiles are brought: row by row (any page size), or in groups of 8 rows a fixed stride apart (contiguous caches
 // and page sizes that are multiples of 8: 4096 tokens over 32768 slots 1.13 ms against 1.35).  (Tensor copies, a box a page,
-// were slower: with pages of 16, 32 and 64 slots 2.06, 1.29 and 1.18 ms.)
+// were slower: with pages of 16, 32 and 64 slots 2.06, 1.29 and 1.18 ms.)  kCodes: an 8-bit cache, row by row, by warps that copy
+// codes and warps that convert them; 4 more warps, registers for it from the softmax warps' 208 (now 200).
 enum Source { kRows, kGroups, kCodes };
 
 template <int D, int NT, Source SRC, bool CAP>
