@@ -208,3 +208,15 @@ def test_steps_in_a_graph():
         assert all(torch.equal(a[p, o], b[p, o]) for a, b in zip(back, want[3:]))
         assert torch.allclose(one.float(), out[-1:].float(), rtol=2.0 ** -6, atol=2.0 ** -6 * float(out.float().abs().max()))
     assert dec.device_status() == 0
+
+
+def test_example_goes_on_in_8_bits():
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "continue_in_8_bits.py")
+    spec = importlib.util.spec_from_file_location("continue_in_8_bits", path)
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    outs, length, share = m.main(context=300, question=20, answer=3, layers=2)
+    assert len(outs) == 4 and all(bool(torch.isfinite(x).all()) for x in outs) and int(length) == 323
+    assert share == (128 + 1) / 256
