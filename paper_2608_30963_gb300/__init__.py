@@ -626,7 +626,8 @@ class Decoder:
         alike."""
         codes, scales = self._code_types, self._scale_types
         if (k.shape == v.shape and ks.shape == vs.shape and k.dtype in codes and v.dtype in codes and ks.dtype in scales and vs.dtype in scales
-                and k.stride() == v.stride() and ks.stride() == vs.stride()):
+                and ((v.is_contiguous() and vs.is_contiguous() and k.is_contiguous() and ks.is_contiguous())
+                     or (k.stride() == v.stride() and ks.stride() == vs.stride()))):
             ptrs = array.array("Q", (k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr()))
             cache = self._code_cache(k, ks, 1, ptrs.buffer_info()[0], batch, page_table, page_size, num_pages)
             if cache is not None:
@@ -638,6 +639,8 @@ class Decoder:
         """Layers of an 8-bit cache, all alike, as _code_layer."""
         k0, s0, n = k[0], k_scale[0], len(k)
         ok = len(v) == len(k_scale) == len(v_scale) == n
+        if ok and n == 1:
+            return self._code_layer(k0, v[0], s0, v_scale[0], batch, page_table, page_size, num_pages)
         ptrs = array.array("Q")
         for like, types, both in ((k0, self._code_types, (k, v)), (s0, self._scale_types, (k_scale, v_scale))):
             shape, stride, plain = like.shape, like.stride(), like.is_contiguous()
@@ -659,7 +662,9 @@ class Decoder:
 
     def _full_layers(self, k: Sequence, v: Sequence, batch: int, page_table, page_size: int, num_pages: int):
         """Layers of a cache of the decoder's type as kvx_dst_kv, checked alike."""
-        self._layer(k[0], v[0], batch, page_table, page_size, num_pages)
+        first, ptrs = self._layer(k[0], v[0], batch, page_table, page_size, num_pages)
+        if len(k) == len(v) == 1:
+            return first, ptrs
         shape, stride, plain = k[0].shape, k[0].stride(), k[0].is_contiguous()
         ok, dtype = len(v) == len(k), self._type
         for some in (k, v):
@@ -805,9 +810,11 @@ class Decoder:
         if L < 1 or len(dst[0]) != L:
             raise ValueError("the caches must have as many layers as one another, one or more")
         least = B if B <= KVX_MAX_ATTEND_BATCH else 0
-        of = {2: self._full_layers, 4: self._code_layers}
-        (a, _keep_a), (b, _keep_b) = (of[len(x)](*x, least, t, page_size, n) for x, t, n in ((src, table, pages), (dst, dst_table, dst_pages)))
-        _check(getattr(lib(), call)(self.handle, B, L, kv_len.data_ptr(), a, b, _raw_stream(stream)))
+        a, _keep_a = (self._full_layers if len(src) == 2 else self._code_layers)(*src, least, table, page_size, pages)
+        b, _keep_b = (self._full_layers if len(dst) == 2 else self._code_layers)(*dst, least, dst_table, page_size, dst_pages)
+        st = getattr(lib(), call)(self.handle, B, L, kv_len.data_ptr(), a, b, _raw_stream(stream))
+        if st:
+            _check(st)
 
     def device_status(self, stream=None, clear: bool = True) -> int:
         bits = ctypes.c_uint32(0)
