@@ -136,6 +136,25 @@ def test_quantise_and_back(dtype, H, d, lens, page, dst_page, layout):
 
 
 @pytest.mark.parametrize("dtype", sorted(TYPES))
+def test_as_many_layers_as_a_call_takes(dtype):
+    tdt, kdt = TYPES[dtype]
+    L, H, d, lens, S = kvx.KVX_MAX_TARGET_LAYERS, 1, 64, [19, 33], 40
+    dec = kvx.Decoder(synth.ModelGeom(L, H, d, 1e4), H, dtype=kdt)
+    full = [torch.randn((L, 2, H, S, d), generator=torch.Generator().manual_seed(i)).to(tdt).cuda() for i in range(2)]
+    codes = [torch.zeros((L, 2, H, S, d), dtype=torch.uint8, device="cuda") for _ in "kv"]
+    scales = [torch.zeros((L, 2, H, S), dtype=torch.uint8, device="cuda") for _ in "kv"]
+    back = [torch.zeros_like(x) for x in full]
+    dec.quantise(i32(lens), *map(list, full), *map(list, codes), *map(list, scales))
+    dec.dequantise(i32(lens), *map(list, codes), *map(list, scales), *map(list, back))
+    assert dec.device_status() == 0
+    live = (torch.arange(S) < torch.tensor(lens)[:, None])[None, :, None].expand(L, 2, H, S)
+    for x, c, s, b in zip(full, codes, scales, back):
+        wc, ws = held(x.cpu().double())
+        assert torch.equal(c.cpu()[live], wc[live]) and torch.equal(s.cpu()[live], ws[live]) and not c.cpu()[~live].any()
+        assert torch.equal(b.cpu()[live], value(wc, ws).to(tdt)[live]) and not b.cpu()[~live].any()
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
 def test_every_code_and_scale(dtype):
     """All 256 codes under scale bytes of every kind, those that are never written too: 0 stands for 0, 255 for infinity."""
     tdt, kdt = TYPES[dtype]
