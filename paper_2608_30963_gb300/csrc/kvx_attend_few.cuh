@@ -20,7 +20,7 @@
 // What bounds it.  8 rows: the reading of K and V, about 8000 clocks behind it the first time: a token of each of eight sequences over up
 // to 32768 slots, 7 query heads on each of 4 KV heads of 128, 207 MB, 47 us, 4.4 TB/s (the loop runs at a copy's rate; 5 us are the plan and the
 // first reads, 4 the join).  16 and 32 rows: the softmax warps' arithmetic (two exponentials and three terms a weight): 4
-// tokens of 8 query heads on each of 8 KV heads over up to 16384 slots of four sequences, 111 MB, 61 us.  Short calls: latency,
+// tokens of 8 query heads on each of 8 KV heads over up to 16384 slots of four sequences, 111 MB, 57 us.  Short calls: latency,
 // 12 us from launch to end.  (The first case with 128 slots a tile and the scales read by the softmax threads, whose reads take as long
 // as the copies on their way, 54 us; with P stored byte by byte, 57; with the rows' ends unrolled, a code that is always
 // cold, 52.)
@@ -69,19 +69,15 @@ __device__ __forceinline__ void umma_e4m3(uint32_t d_tmem, uint64_t adesc, uint6
 // N columns of the warp's lanes
 template <int N> __device__ __forceinline__ void tmem_load(uint32_t at, uint32_t (&v)[N])
 {
-    if constexpr (N == 32) tmem_ld32(at, v);
-    else if constexpr (N == 16) tmem_ld16(at, v);
-    else if constexpr (N == 8) tmem_ld8(at, v);
+    static_assert(N == 4 || N == 8);
+    if constexpr (N == 8) tmem_ld8(at, v);
     else asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(at));
 }
-template <int N> __device__ __forceinline__ void tmem_store(uint32_t at, const uint32_t (&v)[N])
+__device__ __forceinline__ void tmem_store(uint32_t at, const uint32_t (&v)[8])
 {
-    if constexpr (N == 32) tmem_st32(at, v);
-    else if constexpr (N == 16) tmem_st16(at, v);
-    else
-        asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(at), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]),
-                     "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
-                     : "memory");
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(at), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]),
+                 "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+                 : "memory");
 }
 // Two values rounded to e4m3, and `by` times what that leaves of them.
 __device__ __forceinline__ uint32_t take_term(float2& y, float by)
@@ -100,9 +96,11 @@ __device__ __forceinline__ uint64_t mn32_desc(uint32_t saddr, uint32_t lbo)
 struct __align__(16) FewSees {
     int lo, hi, pre;
 };
-// The factor of its scores, and a warpgroup's references of x and z (log2 units; not infinite, so that differences are numbers).
+// The factor of its scores, and a warpgroup's references (log2 units): m of x, and d = 7 + m - n, so that a weight is exp2((x - m) +
+// (log2 of V's scale + d)): its exponent is a sum of small numbers however large the scores are.  What x has not been seen yet has
+// kNoRef (not an infinity, so that differences are numbers).
 struct __align__(16) FewRef {
-    float f, m, n;
+    float f, m, d;
 };
 constexpr float kNoRef = -3.0e38f;
 // The end of a row.
@@ -412,7 +410,7 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
                     const int own = g.s.slot(id.t);
                     const bool real = r < rows;
                     sees_of[r] = {real ? max(window_lo(P, own), 0) : 0, real ? min(own + 1, g.s.L) : 0, real ? g.s.pre : 0};
-                    refs[r] = refs[32 + r] = {real ? scale_of(s) * P.scale * (CAP ? 1.0f : kLog2e) : 0.0f, kNoRef, kNoRef};
+                    refs[r] = refs[32 + r] = {real ? scale_of(s) * (P.scale * (CAP ? inv_cap : kLog2e)) : 0.0f, kNoRef, -kNoRef};
                 }
             }
             fence_proxy_async();
@@ -422,21 +420,22 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
             const int tb = min(g.s.n, ta + P.tile_rows / P.G) - 1;             // slots that every row sees: [all_lo, all_hi), [0, pre)
             const int all_lo = max(window_lo(P, g.s.slot(tb)), 0), all_hi = min(g.s.slot(ta) + 1, g.s.L);
 
-            // rows are taken 16 at a time, so that a thread's scores and sums stay in registers; with 32 the halves of the sums
-            // change places after each half
-            constexpr int RH = R < 16 ? R : 16, HALVES = R / RH;
-            float2 l[HALVES][RH / 2];
+            // Rows are taken 8 at a time, by the same instructions each time (4 tokens of 8 query heads on each of 8 KV heads over up to
+            // 16384 slots of four sequences 57 us, 16 at a time 62: the code of two warpgroups, copies and products shares one
+            // cache); their sums take each other's place after each part, so that a thread keeps them all in registers.
+            constexpr int RH = 8, PARTS = R / RH;
+            float2 l[PARTS][RH / 2];
 #pragma unroll
             for (int r = 0; r < R / 2; ++r) l[2 * r / RH][r % (RH / 2)] = make_float2(0.0f, 0.0f);
-            // their factors, and their references with the other sign, in pairs; a weight is 128 where z is its reference
-            float2 f[RH / 2], m[RH / 2], n[RH / 2];
+            // their factors, their references (m with the other sign), in pairs; a weight is 128 where z is its reference
+            float2 f[RH / 2], m[RH / 2], d[RH / 2];
             auto load_refs = [&](int r0) {
 #pragma unroll
                 for (int r = 0; r < RH; r += 2) {
                     const FewRef v = ref[r0 + r], w = ref[r0 + r + 1];
                     f[r / 2] = make_float2(v.f, w.f);
                     m[r / 2] = make_float2(-v.m, -w.m);
-                    n[r / 2] = make_float2(7.0f - v.n, 7.0f - w.n);
+                    d[r / 2] = make_float2(v.d, w.d);
                 }
             };
             load_refs(0);
@@ -481,15 +480,16 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
                         __syncwarp();
                         if (lane == 0) mbar_arrive(bar(kFree + wg));
                     }
-                    if (HALVES == 2) load_refs(r0);
+                    if (PARTS > 1) load_refs(r0);
 #pragma unroll
                     for (int h = 0; h < HB; ++h)
 #pragma unroll
                         for (int r = 0; r < RH / 2; ++r) {
                             float2 y = mul2(mul2(x[h][r], f[r]), make_float2(kf[h], kf[h]));
                             if constexpr (CAP) {
-                                y.x = capped(y.x, P.cap, inv_cap) * kLog2e;
-                                y.y = capped(y.y, P.cap, inv_cap) * kLog2e;
+                                const float c = P.cap * kLog2e;
+                                y.x = c * (fabsf(y.x) < 0.5f ? tanh_series(y.x) : tanh_far(y.x));
+                                y.y = c * (fabsf(y.y) < 0.5f ? tanh_series(y.y) : tanh_far(y.y));
                             }
                             x[h][r] = y;
                         }
@@ -507,32 +507,36 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
                     for (int h = 0; h < HB; ++h)
 #pragma unroll
                         for (int r = 0; r < RH / 2; ++r) {
-                            const float2 a = add2(x[h][r], m[r]), b = add2(add2(x[h][r], make_float2(vz[h], vz[h])), n[r]);
+                            const float2 a = add2(x[h][r], m[r]), b = add2(a, add2(d[r], make_float2(vz[h], vz[h])));
                             ahead = max3(ahead, a.x, a.y);
                             ahead_z = max3(ahead_z, b.x, b.y);
                         }
                     if (group_any(1 + wg, 128, (ahead > 64.0f || ahead_z > 8.0f) && ok)) {
 #pragma unroll
                         for (int r = 0; r < RH; ++r) {
-                            float a = -INFINITY, b = -INFINITY;
+                            float a = -INFINITY, b = -INFINITY;      // the warp's largest x, and by how much z is beyond that
 #pragma unroll
-                            for (int h = 0; h < HB; ++h) {
-                                const float y = r & 1 ? x[h][r / 2].y : x[h][r / 2].x;
-                                a = fmaxf(a, y);
-                                b = fmaxf(b, y + vz[h]);
-                            }
+                            for (int h = 0; h < HB; ++h) a = fmaxf(a, r & 1 ? x[h][r / 2].y : x[h][r / 2].x);
                             a = warp_max(a);
+#pragma unroll
+                            for (int h = 0; h < HB; ++h) b = fmaxf(b, ((r & 1 ? x[h][r / 2].y : x[h][r / 2].x) - a) + vz[h]);
                             b = warp_max(b);
                             if (lane == 0) red[quad * 32 + r] = make_float2(a, b);
                         }
                         group_sync(1 + wg, 128);
                         if (slot < RH) {
-                            const float2 a = red[slot], b = red[32 + slot], c = red[64 + slot], d = red[96 + slot];
                             const FewRef old = ref[r0 + slot];
-                            const float m1 = fmaxf(old.m, fmaxf(fmaxf(a.x, b.x), fmaxf(c.x, d.x)) + kAhead), n1 = fmaxf(old.n, fmaxf(fmaxf(a.y, b.y), fmaxf(c.y, d.y)) + kAhead);
+                            float m1 = -INFINITY, n1 = -INFINITY;    // n1: beyond m1
+#pragma unroll
+                            for (int w = 0; w < 4; ++w) m1 = fmaxf(m1, red[w * 32 + slot].x);
+                            m1 = fmaxf(old.m, m1 + kAhead);
+#pragma unroll
+                            for (int w = 0; w < 4; ++w) n1 = fmaxf(n1, red[w * 32 + slot].y + (red[w * 32 + slot].x - m1));
+                            n1 = fmaxf((old.m - m1) + (7.0f - old.d), n1 + kAhead);
+                            const float d1 = fminf(7.0f - n1, -kNoRef);
                             ref[r0 + slot].m = m1;
-                            ref[r0 + slot].n = n1;
-                            less[slot] = make_float2(exp2_hw(old.m - m1), exp2_hw(old.n - n1));
+                            ref[r0 + slot].d = d1;
+                            less[slot] = make_float2(exp2_hw(old.m - m1), exp2_hw((old.m - m1) + (d1 - old.d)));
                         }
                         group_sync(1 + wg, 128);
                         load_refs(r0);
@@ -547,7 +551,7 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
                                 tmem_ld_wait();
 #pragma unroll
                                 for (int r = 0; r < RH; ++r) o[r] = __float_as_uint(__uint_as_float(o[r]) * less[r].y);
-                                tmem_store<RH>(at, o);
+                                tmem_store(at, o);
                             }
                             tmem_st_wait();
                         }
@@ -558,7 +562,7 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
                         float2 y[RH / 2];
 #pragma unroll
                         for (int r = 0; r < RH / 2; ++r) {
-                            const float2 a = add2(x[h][r], m[r]), b = add2(add2(x[h][r], make_float2(vz[h], vz[h])), n[r]);
+                            const float2 a = add2(x[h][r], m[r]), b = add2(a, add2(d[r], make_float2(vz[h], vz[h])));
                             l[0][r] = add2(l[0][r], make_float2(exp2_hw(a.x), exp2_hw(a.y)));
                             y[r] = make_float2(exp2_hw(b.x), exp2_hw(b.y));
                         }
@@ -571,7 +575,7 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
                                 const uint32_t b = t < 2 ? take_term(y[r / 2 + 1], 32.0f) : to_codes(y[r / 2 + 1].x, y[r / 2 + 1].y);
                                 w[t][r / 4] = a | b << 16;
                             }
-                        // column t R + r: 16 columns a store
+                        // column t R + r
                         const uint32_t to = p_row + h * 4096;
                         if constexpr (R == 8) {
                             sts128(to + p_swap, make_uint4(w[0][0], w[0][1], w[1][0], w[1][1]));
@@ -580,16 +584,17 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
 #pragma unroll
                             for (int t = 0; t < 3; ++t) {
                                 const uint32_t n = (uint32_t)(t * R + r0);
-                                sts128(to + n / 32 * (BN * 32) + (p_swap ^ (n & 16u)), make_uint4(w[t][0], w[t][1], w[t][RH / 4 - 2], w[t][RH / 4 - 1]));
+                                sts64(to + n / 32 * (BN * 32) + (p_swap ^ (n & 16u)) + (n & 8u), w[t][0], w[t][1]);
                             }
                         }
                     }
-                    if constexpr (HALVES == 2)
+                    if constexpr (PARTS > 1)
 #pragma unroll
                         for (int r = 0; r < RH / 2; ++r) {
                             const float2 t = l[0][r];
-                            l[0][r] = l[1][r];
-                            l[1][r] = t;
+#pragma unroll
+                            for (int i = 1; i < PARTS; ++i) l[i - 1][r] = l[i][r];
+                            l[PARTS - 1][r] = t;
                         }
                 }
                 fence_proxy_async();
@@ -637,8 +642,8 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
                 const float inv = !whole ? 1.0f : sum > 0.0f ? 1.0f / sum : sum;       // (nothing seen: zeros; NaN stays)
                 FewEnd e;
                 e.to = (long long)(g.s.t0 + id.t) * P.o_t + (long long)id.head * P.o_h;
-                e.a = one ? exp2_hw(refs[row].n - top - 7.0f) * inv : 0.0f;
-                e.b = two ? exp2_hw(refs[32 + row].n - top - 7.0f) * inv : 0.0f;
+                e.a = one ? exp2_hw((ma - top) - refs[row].d) * inv : 0.0f;
+                e.b = two ? exp2_hw((mb - top) - refs[32 + row].d) * inv : 0.0f;
                 e.lse2 = sum == 0.0f ? -INFINITY : top + log2f(sum);
                 e.sum = sum;
                 ends[row] = e;

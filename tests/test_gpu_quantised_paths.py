@@ -86,6 +86,31 @@ def test_few_rows_one_bf16_term_would_show(d):
     assert abs(planted - float(eo[0, 0, 0])) > 2 * float(to[0, 0, 0])
 
 
+@pytest.mark.parametrize("d,G,new,gain", [(*s, g) for s in [(128, 7, 1), (128, 4, 4), (256, 2, 3), (256, 8, 4), (128, 16, 1)] for g in (1e4, 1e6, 1e9, 1e20)] +
+                         [(*s, g) for s in [(64, 4, 1), (128, 4, 100), (256, 2, 700)] for g in (1e4, 1e6)])
+def test_scores_far_from_zero(d, G, new, gain):
+    """A row whose largest score is beyond all others by far is that slot's row of V (to the bit where weights are more than one term):
+    an error of the score is no error of its weight."""
+    p = Problem(2, G, d, [900], [new], "bf16", 16, seed=17, q_gain=gain)
+    out, lse = p.attend()
+    K, V = (value(c, s).double()[0] for c, s in zip(p.code, p.byte))
+    L, alone = p.L[0], 0
+    for head in range(2 * G):
+        x = p.q[:, head].double() @ K[head // G, :L].T * p.scale
+        x = x.masked_fill(torch.arange(L) > torch.arange(L - new, L)[:, None], -math.inf)
+        (a, b), (at, _) = (y.unbind(1) for y in x.topk(2, 1))
+        mag = (p.q[:, head].double().abs() @ K[head // G, :L].abs().T * p.scale).amax(1)
+        # both scores within 6 sqrt(d) roundings of the sum of magnitudes; weights of e^-110 are zero in 32 bits
+        one = a - b > 110 + 2 * 6 * math.sqrt(d) * 2.0 ** -24 * mag
+        alone += int(one.sum())
+        got, want = out[one, head].double(), V[head // G, at[one]]
+        # In many rows a weight is one bf16 number over a reference that may lie behind the row's largest score: it is rounded, by 2^-8 of
+        # itself at most, and the sum that divides it is not; the result is rounded once more, (1 + 2^-8)^2 - 1 = 2^-7 + 2^-16.
+        assert bool(((got - want).abs() <= (2.0 ** -7 + 2.0 ** -16) * want.abs()).all()) if new > 32 else torch.equal(got, want)
+        assert bool(((lse[one, head].double() - a[one]).abs() <= (6 * math.sqrt(d) * 2.0 ** -24 * mag + 2.0 ** -22 * a.abs())[one]).all())
+    assert alone > new * G and p.dec.device_status() == 0
+
+
 @pytest.mark.parametrize("d", [128, 256])
 def test_few_rows_a_flat_tail(d):
     """One score far above 30000 equal ones that weigh as much together: their terms' roundings all go one way."""
