@@ -30,8 +30,8 @@ bool expands(const AttendParams& P)
     return (long long)P.T * P.G > 6ll * tile * P.batch && (long long)P.batch * P.cache.capacity <= kAttendScores / ((long long)P.H * P.d);
 }
 // Few rows: the rows of a tile (8, 16 or 32) that hold the call's mean a sequence and KV head, in whole tokens, or 0.  (Four
-// sequences of 16384 slots, us so and with the codes converted: 7 rows on each of 4 KV heads of 128 23 and 48, 28 rows 47 and 56, on 8
-// KV heads 32 rows 70 and 84; heads of 256 over 8192 slots, 2 rows 22 and 40, 32 rows 45 and 50; one sequence of 2000 slots, 32
+// sequences of 16384 slots, us so and with the codes converted: 7 rows on each of 4 KV heads of 128 23 and 48, 28 rows 46 and 56, on 8
+// KV heads 32 rows 63 and 84; heads of 256 over 8192 slots, 2 rows 22 and 40, 32 rows 45 and 50; one sequence of 2000 slots, 32
 // rows 18.5 and 18.0.  A head of 64 fills half of a 128-byte block: not taken.)
 int few_rows(const AttendParams& P)
 {

@@ -191,6 +191,25 @@ def test_the_workspace_is_shared_by_calls_in_order():
         assert torch.equal(w, first) and torch.equal(outs[0].cpu(), base) and torch.equal(outs[1].cpu(), base1)
 
 
+def test_two_decoders_on_two_streams():
+    """Each has a workspace of its own: calls side by side give the bits that they give one after the other."""
+    sizes = [(dict(H=2, G=7, d=128, ctx=[5000, 300], new=[1, 1]), dict(H=2, G=4, d=128, ctx=[900, 3], new=[400, 400])),
+             (dict(H=2, G=2, d=256, ctx=[3000], new=[6]), dict(H=1, G=4, d=64, ctx=[2000], new=[90]))]
+    for pair in sizes:
+        ps = [Problem(**kw, seed=29 + i) for i, kw in enumerate(pair)]
+        alone = [p.attend()[0] for p in ps]
+        args = [(p.q.cuda(), i32(p.off), i32(p.L), *p.cache()) for p in ps]
+        outs = [[torch.zeros_like(a[0]) for _ in range(8)] for a in args]
+        streams = [torch.cuda.Stream() for _ in ps]
+        torch.cuda.synchronize()
+        for n in range(8):
+            for p, a, o, st in zip(ps, args, outs, streams):
+                p.dec.attend_quantised(*a, o[n], stream=st, **p.place.kw())
+        torch.cuda.synchronize()
+        for p, want, o in zip(ps, alone, outs):
+            assert p.dec.device_status() == 0 and all(torch.equal(x.cpu(), want) for x in o)
+
+
 def test_steps_in_a_graph():
     """Quantise, append, attend (a prompt and a token) and read back as one captured graph, replayed with other lengths."""
     H, G, d, page, pages = 2, 4, 128, 16, 64
