@@ -187,8 +187,9 @@ __global__ void __launch_bounds__(kConvertThreads, TO_CODES ? 4 : 3) convert_ker
 template <int D>
 __global__ void __launch_bounds__(kConvertThreads) expand_kernel(const __grid_constant__ AttendParams P, __nv_bfloat16* to_k, __nv_bfloat16* to_v)
 {
-    constexpr int LANES = D / 16, ROWS = 32 / LANES, U = 4;
-    extern __shared__ int4 ranges[];                 // slots [0, x) and [y, z) of a sequence; w: groups of 32 slots before its first
+    // a warp's slots: as many as it has on their way at once
+    constexpr int LANES = D / 16, ROWS = 32 / LANES, U = 4, GROUP = U * ROWS;
+    extern __shared__ int4 ranges[];                 // slots [0, x) and [y, z) of a sequence; w: groups of slots before its first
     const int tid = threadIdx.x, lane = tid & 31, sub = lane / LANES, c = lane % LANES * 8;
     grid_dependency_wait();
     grid_launch_dependents();
@@ -202,7 +203,7 @@ __global__ void __launch_bounds__(kConvertThreads) expand_kernel(const __grid_co
         int run = 0;
         for (int b = 0; b < P.batch; ++b) {
             ranges[b].w = run;
-            run += (ranges[b].x + 31) / 32 + (max(ranges[b].z - ranges[b].y, 0) + 31) / 32;
+            run += (ranges[b].x + GROUP - 1) / GROUP + (max(ranges[b].z - ranges[b].y, 0) + GROUP - 1) / GROUP;
         }
         ranges[P.batch].w = run;
     }
@@ -220,10 +221,10 @@ __global__ void __launch_bounds__(kConvertThreads) expand_kernel(const __grid_co
         }
         const int b = lo;
         const int4 of = ranges[b];
-        const int k = g - of.w, s0 = k < (of.x + 31) / 32 ? k * 32 : of.y + (k - (of.x + 31) / 32) * 32, s = s0 + lane, L = of.z;
+        const int k = g - of.w, a = (of.x + GROUP - 1) / GROUP, s0 = k < a ? k * GROUP : of.y + (k - a) * GROUP, s = s0 + lane, L = of.z;
         long long code = -1;
         float scale = 0.0f;
-        if (s < L) {
+        if (lane < GROUP && s < L) {
             const CodePlace at = code_place(P.cache, P.scales, b, s);
             if (at.row < 0) {
                 set_status(P.status, KVX_DEV_PAGE_INVALID);
@@ -234,30 +235,27 @@ __global__ void __launch_bounds__(kConvertThreads) expand_kernel(const __grid_co
         }
         const uint8_t* from = (const uint8_t*)(key ? P.ck : P.cv) + c;
         __nv_bfloat16* to = (key ? to_k : to_v) + (((long long)b * P.H + h) * P.cache.capacity + s0) * D + c;
-#pragma unroll 1
-        for (int k0 = 0; k0 < 32; k0 += U * ROWS) {
-            uint2 x[U], y[U];
+        uint2 x[U], y[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const long long w = __shfl_sync(0xffffffffu, code, k0 + u * ROWS + sub);
-                x[u] = y[u] = make_uint2(0u, 0u);
-                if (w >= 0) {
-                    x[u] = *reinterpret_cast<const uint2*>(from + w);
-                    y[u] = *reinterpret_cast<const uint2*>(from + w + D / 2);
-                }
+        for (int u = 0; u < U; ++u) {
+            const long long w = __shfl_sync(0xffffffffu, code, u * ROWS + sub);
+            x[u] = y[u] = make_uint2(0u, 0u);
+            if (w >= 0) {
+                x[u] = *reinterpret_cast<const uint2*>(from + w);
+                y[u] = *reinterpret_cast<const uint2*>(from + w + D / 2);
             }
+        }
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int r = k0 + u * ROWS + sub;
-                const float f = __shfl_sync(0xffffffffu, scale, r);
-                if (s0 + r >= L) continue;
-                float p[8], q[8];
-                unpack_codes(x[u], f, p);
-                unpack_codes(y[u], f, q);
-                __nv_bfloat16* out = to + r * D;
-                *reinterpret_cast<uint4*>(out) = make_uint4(pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3]), pack_bf16(p[4], p[5]), pack_bf16(p[6], p[7]));
-                *reinterpret_cast<uint4*>(out + D / 2) = make_uint4(pack_bf16(q[0], q[1]), pack_bf16(q[2], q[3]), pack_bf16(q[4], q[5]), pack_bf16(q[6], q[7]));
-            }
+        for (int u = 0; u < U; ++u) {
+            const int r = u * ROWS + sub;
+            const float f = __shfl_sync(0xffffffffu, scale, r);
+            if (s0 + r >= L) continue;
+            float p[8], q[8];
+            unpack_codes(x[u], f, p);
+            unpack_codes(y[u], f, q);
+            __nv_bfloat16* out = to + r * D;
+            *reinterpret_cast<uint4*>(out) = make_uint4(pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3]), pack_bf16(p[4], p[5]), pack_bf16(p[6], p[7]));
+            *reinterpret_cast<uint4*>(out + D / 2) = make_uint4(pack_bf16(q[0], q[1]), pack_bf16(q[2], q[3]), pack_bf16(q[4], q[5]), pack_bf16(q[6], q[7]));
         }
     }
 }
@@ -342,7 +340,8 @@ template <typename T, bool TO_CODES> cudaError_t run_convert(const ConvertParams
 }
 template <int D> cudaError_t run_expand(const AttendParams& P, void* to_k, void* to_v, int num_sms, cudaStream_t stream)
 {
-    const long long groups = ((long long)P.cache.capacity + 63) / 32 * P.batch * P.H * 2;
+    constexpr int group = 4 * (512 / D);                 // (expand_kernel's)
+    const long long groups = ((long long)P.cache.capacity + 2 * group - 1) / group * P.batch * P.H * 2;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)min((groups + kConvertThreads / 32 - 1) / (kConvertThreads / 32), (long long)num_sms * 8));
     cfg.blockDim = dim3(kConvertThreads);
