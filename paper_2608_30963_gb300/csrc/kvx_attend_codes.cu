@@ -16,18 +16,19 @@ template <bool CAP> cudaError_t attend_fp32(const AttendParams& P, int num_sms, 
     return P.d == 64 ? run_fp32<64, CAP>(P, num_sms, stream) : P.d == 128 ? run_fp32<128, CAP>(P, num_sms, stream) : run_fp32<256, CAP>(P, num_sms, stream);
 }
 
-// Prompts: every row tile of a (sequence, KV head) reads its slots again, so from some row tiles on the slots become bf16
+// Prompts: every row tile of a (sequence, KV head) reads its slots again, so from some rows on the slots become bf16
 // once, in the workspace (64 MiB, where the call's cache may fit it), and the kernels of bf16 caches take them from there.
 // (One sequence, us so and with the codes converted by each row tile: 7 query heads on each of 4 KV heads of 128 over 16384
-// slots, 896 rows 58 and 55, 1792 rows 79 and 83, 7168 rows 207 and 247; heads of 256, whose tiles have 128 rows, 512 rows 55 and 54,
-// 1024 rows 67 and 76; heads of 64, 4096 rows 36 and 35, 8192 rows 46 and 47; 4096 tokens over 32768 slots 1166 and 1568.
-// Capped scores: heads of 128, 1792 rows 382 and 221, 7168 rows 1040 and 677, so not there; heads of 256, 1024 rows 79 and 86.)
+// slots, 896 rows 58 and 55, 1344 rows 72 and 71, 1792 rows 80 and 82, 7168 rows 207 and 247; heads of 256, whose tiles have 128
+// rows, over 8192 slots, 384 rows 50 and 48, 512 rows 52 and 54, 768 rows 56 and 64, over 2000 slots 768 rows 37 and 36, 1024 rows 39
+// and 39; heads of 64, 4096 rows 36 and 35, 8192 rows 46 and 47; 4096 tokens over 32768 slots 1166 and 1568.
+// Capped scores: heads of 128, 1792 rows 382 and 221, 7168 rows 1040 and 677, so not there; heads of 256, 1024 rows 75 and 86.)
 bool expands(const AttendParams& P)
 {
-    const int tile = P.d == 256 ? 128 : 256;
+    const int rows = P.d == 256 ? 512 : 1536;
     if (P.cap > 0.0f && P.d == 128) return false;
     // (batch <= 1024, capacity <= 2^30: no product wraps)
-    return (long long)P.T * P.G > 6ll * tile * P.batch && (long long)P.batch * P.cache.capacity <= kAttendScores / ((long long)P.H * P.d);
+    return (long long)P.T * P.G > (long long)rows * P.batch && (long long)P.batch * P.cache.capacity <= kAttendScores / ((long long)P.H * P.d);
 }
 // Few rows: the rows of a tile (8, 16 or 32) that hold the call's mean a sequence and KV head, in whole tokens, or 0.  (Four
 // sequences of 16384 slots, us so and with the codes converted: 7 rows on each of 4 KV heads of 128 23 and 48, 28 rows 46 and 56, on 8

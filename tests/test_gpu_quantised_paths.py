@@ -130,7 +130,7 @@ def test_few_rows_a_flat_tail(d):
 
 
 # rows a (sequence, KV head): up to 128 one row tile, up to six of them converted in place, more of them from the workspace
-@pytest.mark.parametrize("d,G,new", [(128, 3, 42), (128, 3, 43), (128, 4, 384), (128, 4, 385), (64, 4, 384), (64, 4, 400), (256, 2, 384), (256, 2, 390), (64, 2, 12),
+@pytest.mark.parametrize("d,G,new", [(128, 3, 42), (128, 3, 43), (128, 4, 384), (128, 4, 385), (64, 4, 384), (64, 4, 400), (256, 2, 256), (256, 2, 257), (256, 2, 384), (256, 2, 390), (64, 2, 12),
                                      (128, 33, 4), (128, 5, 7), (64, 64, 3)])
 @pytest.mark.parametrize("opt", ["plain", "window_prefix", "capped"])
 def test_many_rows(d, G, new, opt):
