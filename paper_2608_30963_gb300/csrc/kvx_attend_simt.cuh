@@ -212,7 +212,7 @@ __global__ void __launch_bounds__(kThreads) attend_simt_kernel(const __grid_cons
             const int tile = g.kv.at(g.i0 + it);
             if constexpr (CODES) codes.put(sK);
             begin(sV, P.cv, P.v_scale, tile);
-            if constexpr (CODES) async_wait<0>();          // (the queries)
+            if constexpr (CODES) cp_async_wait_all();      // the queries: the only copies here, and in no group yet
             else async_wait<1>();
             __syncthreads();
             float x[RM][kKN];
@@ -283,7 +283,7 @@ __global__ void __launch_bounds__(kThreads) attend_simt_kernel(const __grid_cons
             }
             __syncthreads();
         }
-        async_wait<0>();
+        if constexpr (!CODES) async_wait<0>();
         if (g.whole()) {
             // through shared memory (the queries' place), so that a warp has a whole row
 #pragma unroll
