@@ -425,9 +425,12 @@ __device__ __forceinline__ float tanh_series(float x)
     p = fmaf(p, y, -1.0f / 3.0f);
     return fmaf(p * y, x, x);
 }
+// (NaN stays NaN: a score that is none must not count as one at the cap.)
 __device__ __forceinline__ float tanh_far(float x)
 {
-    const float e = exp2_hw(fminf(fabsf(x), 20.0f) * -2.885390081777927f);   // e^(-2|x|)
+    float a;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(a) : "f"(fabsf(x)), "f"(20.0f));
+    const float e = exp2_hw(a * -2.885390081777927f);                        // e^(-2|x|)
     return copysignf(__fdividef(1.0f - e, 1.0f + e), x);
 }
 __device__ __forceinline__ float capped(float s, float cap, float inv_cap)
