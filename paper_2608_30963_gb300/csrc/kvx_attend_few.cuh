@@ -381,7 +381,7 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
                 float top = 0.0f;
 #pragma unroll
                 for (int c = 0; c < CH; ++c) {
-                    if (!(fabsf(q[c]) <= 3.402823466e38f)) q[c] = __uint_as_float(0x7fffffffu);   // (an infinity makes its scores NaN)
+                    if (!(fabsf(q[c]) <= 3.402823466e38f)) q[c] = __uint_as_float(0x7fffffffu);   // (scores of NaN; infinities: at the row's end)
                     top = fmaxf(top, fabsf(q[c]));
                 }
 #pragma unroll
@@ -693,10 +693,18 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
 #pragma unroll
                 for (int x = 0; x < 8; ++x) all_bad |= bad[x];
                 for (int row = sw; row < rows; row += 8) {
-                    if (!(all_bad >> row & 1u)) continue;
-                    float o[D / 32];
-                    resum_row<__nv_bfloat16, D>(P, g.s, g.b, g.h, g.rt * P.tile_rows + row, ends[row].lse2, o, beat);
-                    store_f32<__nv_bfloat16, D / 32>((__nv_bfloat16*)P.out + ends[row].to + lane * (D / 32), o);
+                    const FewEnd e = ends[row];
+                    float o[D / 32], lse2;
+                    if (e.sum != e.sum) {
+                        if (!infinite_row<__nv_bfloat16, D>(P, g.s, g.b, g.h, g.rt * P.tile_rows + row, lse2, o, beat)) continue;
+                        const RowId id = row_id(P, g.s, g.h, g.rt * P.tile_rows + row);
+                        if (P.lse && lane == 0) P.lse[(long long)(g.s.t0 + id.t) * P.Hq + id.head] = lse2 * kLn2;
+                    } else if (all_bad >> row & 1u) {
+                        resum_row<__nv_bfloat16, D>(P, g.s, g.b, g.h, g.rt * P.tile_rows + row, e.lse2, o, beat);
+                    } else {
+                        continue;
+                    }
+                    store_f32<__nv_bfloat16, D / 32>((__nv_bfloat16*)P.out + e.to + lane * (D / 32), o);
                 }
             }
             group_sync(3, 256);                          // the tables and the sums are the next item's
