@@ -112,6 +112,63 @@ struct FewEnd {
     float a, b;            // factors of both warpgroups' O
     float lse2, sum;
 };
+// Row `row` of an item whose query holds an infinity and no NaN: e4m3 has no infinity, so its scores came out NaN, but they are
+// infinite, or numbers where they are capped.  One warp takes its maximum, sum and output along the segment's slots in fp32 (up
+// to the first score that is NaN; 0.3 us a slot) and writes it, or its part of a split row's.
+template <int D, int BN>
+__device__ __noinline__ void infinite_row(const AttendParams& P, const Segment& g, int row, size_t part, volatile int* beat)
+{
+    constexpr int C = D / 32;
+    const int lane = threadIdx.x & 31;
+    const RowId id = row_id(P, g.s, g.h, g.rt * P.tile_rows + row);
+    const long long token = g.s.t0 + id.t;
+    float q[C], x[C], o[C], m = -INFINITY, l = 0.0f;
+    load_f32<__nv_bfloat16, C>((const __nv_bfloat16*)P.q + token * P.q_t + (long long)id.head * P.q_h + lane * C, q);
+#pragma unroll
+    for (int c = 0; c < C; ++c) o[c] = 0.0f;
+    const int i = g.s.slot(id.t);
+    const float inv_cap = P.cap > 0.0f ? 1.0f / P.cap : 0.0f;
+    for (int t = 0; t < g.n && l == l; ++t) {
+        if ((t & 7) == 0 && lane == 0) *beat = *beat + 1;          // waits elsewhere in the CTA go on
+        const int j0 = g.kv.at(g.i0 + t) * BN;
+        for (int j = j0; j < min(j0 + BN, g.s.L) && l == l; ++j) {
+            if (!sees(P, g.s, i, j)) continue;
+            const CodePlace at = code_place(P.cache, P.scales, g.b, j);
+            const long long off = at.row + cache_head(P.cache) * g.h + lane * C, scale = at.scale + scale_head(P.cache, P.scales) * g.h;
+            auto load = [&](const void* rows, const unsigned char* scales) {
+#pragma unroll
+                for (int c = 0; c < C; ++c) x[c] = 0.0f;           // (pages that are not in the pool)
+                if (at.row >= 0) load_codes<C>((const uint8_t*)rows + off, scale_of(scales[scale]), x);
+            };
+            load(P.ck, P.k_scale);
+            float dot = 0.0f;
+#pragma unroll
+            for (int c = 0; c < C; ++c) dot = fmaf(q[c], x[c], dot);
+#pragma unroll
+            for (int k = 16; k; k >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, k);
+            float v = dot * P.scale;
+            if (P.cap > 0.0f) v = capped(v, P.cap, inv_cap);
+            v *= kLog2e;
+            const float next = fmaxf(m, v), base = next == -INFINITY ? 0.0f : next, w = exp2_hw(m - base), p = exp2_hw(v - base);
+            m = next;
+            l = fmaf(l, w, p);
+            load(P.cv, P.v_scale);
+#pragma unroll
+            for (int c = 0; c < C; ++c) o[c] = fmaf(p, x[c], o[c] * w);
+        }
+    }
+    if (g.whole()) {
+        const float inv = l > 0.0f ? 1.0f / l : l;                 // (NaN stays)
+#pragma unroll
+        for (int c = 0; c < C; ++c) o[c] = l == 0.0f ? 0.0f : o[c] * inv;
+        store_f32<__nv_bfloat16, C>((__nv_bfloat16*)P.out + token * P.o_t + (long long)id.head * P.o_h + lane * C, o);
+        if (P.lse && lane == 0) P.lse[token * P.Hq + id.head] = l == 0.0f ? -INFINITY : (m + log2f(l)) * kLn2;
+    } else {
+#pragma unroll
+        for (int c = 0; c < C; ++c) __stcg(P.part_o + part * D + lane * C + c, o[c]);
+        if (lane == 0) __stcg(P.part_ml + part, make_float2(m, l));
+    }
+}
 constexpr float kAhead = 4.0f;   // references are taken so far above the largest, so that they last (a tile with new ones costs 1200 clocks)
 __device__ __forceinline__ float warp_max(float x)
 {
@@ -371,6 +428,7 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
             have = true;
             const int ta = g.rt * (P.tile_rows / P.G), rows = min(P.tile_rows, (g.s.n - ta) * P.G);
             // the queries' terms, a row a warp, and what the rows see
+            uint32_t odd_rows = 0;                       // this warp's whose queries hold infinities
             for (int r = sw; r < R; r += 8) {
                 constexpr int CH = D / 32;               // channels of a lane
                 float q[CH];
@@ -379,11 +437,15 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
                 for (int c = 0; c < CH; ++c) q[c] = 0.0f;
                 if (r < rows) load_f32<__nv_bfloat16, CH>((const __nv_bfloat16*)P.q + (long long)(g.s.t0 + id.t) * P.q_t + (long long)id.head * P.q_h + lane * CH, q);
                 float top = 0.0f;
+                bool infinite = false, none = false;
 #pragma unroll
                 for (int c = 0; c < CH; ++c) {
-                    if (!(fabsf(q[c]) <= 3.402823466e38f)) q[c] = __uint_as_float(0x7fffffffu);   // (scores of NaN; infinities: at the row's end)
+                    infinite = infinite || fabsf(q[c]) == INFINITY;
+                    none = none || q[c] != q[c];
+                    if (!(fabsf(q[c]) <= 3.402823466e38f)) q[c] = __uint_as_float(0x7fffffffu);   // (its scores are NaN; infinities: infinite_row)
                     top = fmaxf(top, fabsf(q[c]));
                 }
+                if (__any_sync(0xffffffffu, infinite) && !__any_sync(0xffffffffu, none)) odd_rows |= 1u << r;
 #pragma unroll
                 for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
                 const unsigned s = scale_for(top);
@@ -693,21 +755,18 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
 #pragma unroll
                 for (int x = 0; x < 8; ++x) all_bad |= bad[x];
                 for (int row = sw; row < rows; row += 8) {
-                    const FewEnd e = ends[row];
-                    float o[D / 32], lse2;
-                    if (e.sum != e.sum) {
-                        if (!infinite_row<__nv_bfloat16, D>(P, g.s, g.b, g.h, g.rt * P.tile_rows + row, lse2, o, beat)) continue;
-                        const RowId id = row_id(P, g.s, g.h, g.rt * P.tile_rows + row);
-                        if (P.lse && lane == 0) P.lse[(long long)(g.s.t0 + id.t) * P.Hq + id.head] = lse2 * kLn2;
-                    } else if (all_bad >> row & 1u) {
-                        resum_row<__nv_bfloat16, D>(P, g.s, g.b, g.h, g.rt * P.tile_rows + row, e.lse2, o, beat);
-                    } else {
-                        continue;
-                    }
-                    store_f32<__nv_bfloat16, D / 32>((__nv_bfloat16*)P.out + e.to + lane * (D / 32), o);
+                    if (!(all_bad >> row & 1u)) continue;
+                    float o[D / 32];
+                    resum_row<__nv_bfloat16, D>(P, g.s, g.b, g.h, g.rt * P.tile_rows + row, ends[row].lse2, o, beat);
+                    store_f32<__nv_bfloat16, D / 32>((__nv_bfloat16*)P.out + ends[row].to + lane * (D / 32), o);
                 }
             }
             group_sync(3, 256);                          // the tables and the sums are the next item's
+            if (odd_rows) {
+                const Segment item = g;
+                for (int row = sw; row < rows; row += 8)
+                    if (odd_rows >> row & 1u) infinite_row<D, BN>(P, item, row, (size_t)(2 * blockIdx.x + (g.first ? 0 : 1)) * R + row, beat);
+            }
         }
         if (threadIdx.x == 128) leave_split(P, *plan, g, have);
     }

@@ -99,63 +99,6 @@ __device__ __noinline__ void resum_row(const AttendParams& P, const Seq& s, int 
     for (int c = 0; c < C; ++c) o[c] = acc[c];
 }
 
-// One row whose query holds an infinity (and no NaN), taken alone by one warp: a maximum, sum and output that run along the slots it
-// sees, in fp32.  e4m3 has no infinity, so where queries are split into such terms the row's scores came out NaN; here they are
-// what they are: capped they are numbers, and without a cap they may all be -inf.  False (nothing done) if the query is not such a one.
-template <typename T, int D>
-__device__ __noinline__ bool infinite_row(const AttendParams& P, const Seq& s, int b, int h, int row, float& lse2, float (&o)[D / 32],
-                                          volatile int* beat = nullptr)
-{
-    constexpr int C = D / 32;
-    const int lane = threadIdx.x & 31;
-    const RowId id = row_id(P, s, h, row);
-    float q[C], x[C];
-    load_f32<T, C>((const T*)P.q + (long long)(s.t0 + id.t) * P.q_t + (long long)id.head * P.q_h + lane * C, q);
-    bool infinite = false, none = false;
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-        infinite = infinite || fabsf(q[c]) == INFINITY;
-        none = none || q[c] != q[c];
-    }
-    if (!__any_sync(0xffffffffu, infinite) || __any_sync(0xffffffffu, none)) return false;
-    float m = -INFINITY, l = 0.0f;
-#pragma unroll
-    for (int c = 0; c < C; ++c) o[c] = 0.0f;
-    const int i = s.slot(id.t), hi = min(i + 1, s.L), lo = max(window_lo(P, i), 0);
-    const float inv_cap = P.cap > 0.0f ? 1.0f / P.cap : 0.0f;
-    for (int j = s.pre > 0 ? 0 : lo; j < max(hi, s.pre); ++j) {
-        if (beat && (j & 4095) == 0 && lane == 0) *beat = *beat + 1;
-        if (!sees(P, s, i, j)) continue;
-        // (rows of pages that are not in the pool are zeros)
-        const CodePlace at = code_place(P.cache, P.scales, b, j);
-        const long long off = at.row + cache_head(P.cache) * h + lane * C, scale = at.scale + scale_head(P.cache, P.scales) * h;
-#pragma unroll
-        for (int c = 0; c < C; ++c) x[c] = 0.0f;
-        if (at.row >= 0) load_codes<C>((const uint8_t*)P.ck + off, scale_of(P.k_scale[scale]), x);
-        float dot = 0.0f;
-#pragma unroll
-        for (int c = 0; c < C; ++c) dot = fmaf(q[c], x[c], dot);
-#pragma unroll
-        for (int k = 16; k; k >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, k);
-        float v = dot * P.scale;
-        if (P.cap > 0.0f) v = capped(v, P.cap, inv_cap);
-        v *= kLog2e;
-        const float next = fmaxf(m, v), base = next == -INFINITY ? 0.0f : next, w = exp2_hw(m - base), p = exp2_hw(v - base);
-        m = next;
-        l = fmaf(l, w, p);
-        if (__any_sync(0xffffffffu, l != l)) break;      // every output is NaN
-#pragma unroll
-        for (int c = 0; c < C; ++c) x[c] = 0.0f;
-        if (at.row >= 0) load_codes<C>((const uint8_t*)P.cv + off, scale_of(P.v_scale[scale]), x);
-#pragma unroll
-        for (int c = 0; c < C; ++c) o[c] = fmaf(p, x[c], o[c] * w);
-    }
-#pragma unroll
-    for (int c = 0; c < C; ++c) o[c] = l == 0.0f ? 0.0f : l == l ? o[c] / l : l;
-    lse2 = l == 0.0f ? -INFINITY : m + log2f(l);
-    return true;
-}
-
 // Write one row from its unnormalised sums (lane holds C channels), its running maximum m (log2 units) and sum l; the
 // row is row `row` of (sequence b, KV head h), its output that of packed token `token` and query head `head`.  Whole
 // warps call it.
@@ -172,11 +115,9 @@ __device__ __forceinline__ void finish_row(const AttendParams& P, int b, int h, 
         o[c] *= inv;
         fine = fine && fabsf(o[c]) <= 3.0e38f;
     }
-    float lse2 = l == 0.0f ? -INFINITY : m + log2f(l);
+    const float lse2 = l == 0.0f ? -INFINITY : m + log2f(l);
     if (!__all_sync(0xffffffffu, fine)) {
-        if (sizeof(T) == 2 && P.k_scale && l != l) {
-            infinite_row<T, D>(P, load_seq(P, b), b, h, row, lse2, o);
-        } else if (l == 0.0f) {
+        if (l == 0.0f) {
 #pragma unroll
             for (int c = 0; c < C; ++c) o[c] = 0.0f;
         } else if (l == l) {
