@@ -5,7 +5,7 @@
 // With few rows (query heads of a token) the products have room to spare, and what costs is bringing K and V: so the
 // cache's codes are the operands, straight from memory, and the other side is split into e4m3 terms that make up for its
 // 4 bits.  A query row is scaled by a power of two and split in two (bf16's 8 bits exactly, down to 2^-14 of the row's largest
-// value, below that to 2^-22 of it), a weight in three (to 2^-12 of itself, 2^-22 of the row's largest).  Terms lie side by
+// value, below that to 2^-22 of it), a weight in three (to 2^-12 of itself, 2^-23 of the largest of some thousand slots).  Terms lie side by
 // side as columns of one product; sums are fp32.  Slots are the rows of S^T and channels those of O^T, so the rows of a tile
 // are its columns: 256 slots by 8, 16 or 32 rows.
 //   copying warps (7)   128-byte blocks of K and V rows into 128-byte-swizzled tiles, every seventh each
@@ -13,8 +13,8 @@
 //   softmax warps (8)   two warpgroups, every other tile each; a thread has a slot.  A score x takes its K row's scale; a weight
 //                       takes its V row's, in its exponent, z = x + log2 of it, and a reference n of its own beside the sums'
 //                       reference m, so that far scales do not leave e4m3's range.  A row takes new references when z has grown by
-//                       more than 1 (a factor of two) beyond n, or x by 64 beyond m (sums in fp32 have room); each warpgroup has
-//                       its own references, sums and O, joined at the end.
+//                       more than 1 (a factor of two) beyond n, or x by 64 beyond m (sums in fp32 have room), and every 32 tiles
+//                       of the warpgroup, down as well as up; each has its own references, sums and O, joined at the end.
 // The last rows of the split work are joined as those of the other attention kernels.
 //
 // What bounds it.  8 rows: the reading of K and V, about 8000 clocks behind it the first time: a token of each of eight sequences over up
@@ -102,9 +102,18 @@ struct __align__(16) FewSees {
 // The factor of its scores, and a warpgroup's references (log2 units): m of x, and d = 7 + m - n, so that a weight is exp2((x - m) +
 // (log2 of V's scale + d)): its exponent is a sum of small numbers however large the scores are.  What x has not been seen yet has
 // kNoRef (not an infinity, so that differences are numbers).
+// n follows the weights up at once, and down every kLower tiles of a warpgroup: the third term of a weight ends at 2^-23 of the
+// largest that n was taken for, and without a way down a long tail of smaller ones behind it would be lost (of 524288 slots of
+// 2^-23.6 each all that this warpgroup has).  O is fp32 and has room for weights that are small beside what it holds, so n may lie up
+// to kLowest below the largest it has been (`low` says how much; not below kDeepest beside m: 2^-d has to be a normal number).
+// What a row loses to the terms' end is then at most the slots of kLower tiles (8192) times 2^-23 of the largest contribution that
+// their reference was taken for, 2^-10 of that, however many slots follow.  (4 tokens of 8 query heads on each of 8 KV heads over
+// 32000 slots of 19 sequences, us with a way down every 16 and 32 tiles and without one: 260, 256 and 251.)
 struct __align__(16) FewRef {
-    float f, m, d;
+    float f, m, d, low;
 };
+constexpr int kLower = 32;
+constexpr float kLowest = 24.0f, kDeepest = -100.0f;
 constexpr float kNoRef = -3.0e38f;
 // The end of a row.
 struct FewEnd {
@@ -114,7 +123,7 @@ struct FewEnd {
 };
 // Row `row` of an item whose query holds an infinity and no NaN: e4m3 has no infinity, so its scores came out NaN, but they are
 // infinite, or numbers where they are capped.  One warp takes its maximum, sum and output along the segment's slots in fp32 (up
-// to the first score that is NaN; 0.3 us a slot) and writes it, or its part of a split row's.
+// to the first score that is NaN; about 1 us a slot) and writes it, or its part of a split row's.
 template <int D, int BN>
 __device__ __noinline__ void infinite_row(const AttendParams& P, const Segment& g, int row, size_t part, volatile int* beat)
 {
@@ -475,7 +484,7 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
                     const int own = g.s.slot(id.t);
                     const bool real = r < rows;
                     sees_of[r] = {real ? max(window_lo(P, own), 0) : 0, real ? min(own + 1, g.s.L) : 0, real ? g.s.pre : 0};
-                    refs[r] = refs[32 + r] = {real ? scale_of(s) * (P.scale * (CAP ? inv_cap : kLog2e)) : 0.0f, kNoRef, -kNoRef};
+                    refs[r] = refs[32 + r] = {real ? scale_of(s) * (P.scale * (CAP ? inv_cap : kLog2e)) : 0.0f, kNoRef, -kNoRef, 0.0f};
                 }
             }
             fence_proxy_async();
@@ -520,6 +529,7 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
                 }
                 const int j0 = g.kv.at(g.i0 + u) * BN, j = j0 + slot;
                 const bool all = (j0 >= all_lo && j0 + BN <= all_hi) || j0 + BN <= g.s.pre;
+                const bool lower = ((u - u0) & (2 * kLower - 1)) == 2 * kLower - 2;
                 // the product that last added to this O, and read P, is complete
                 if (u > u0) {
                     wait(kO + wg, done & 1);
@@ -576,7 +586,7 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
                             ahead = max3(ahead, a.x, a.y);
                             ahead_z = max3(ahead_z, b.x, b.y);
                         }
-                    if (group_any(1 + wg, 128, (ahead > 64.0f || ahead_z > 8.0f) && ok)) {
+                    if (group_any(1 + wg, 128, (ahead > 64.0f || ahead_z > 8.0f || lower) && ok)) {
 #pragma unroll
                         for (int r = 0; r < RH; ++r) {
                             float a = -INFINITY, b = -INFINITY;      // the warp's largest x, and by how much z is beyond that
@@ -597,10 +607,12 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
                             m1 = fmaxf(old.m, m1 + kAhead);
 #pragma unroll
                             for (int w = 0; w < 4; ++w) n1 = fmaxf(n1, red[w * 32 + slot].y + (red[w * 32 + slot].x - m1));
-                            n1 = fmaxf((old.m - m1) + (7.0f - old.d), n1 + kAhead);
+                            const float n0 = (old.m - m1) + (7.0f - old.d);
+                            n1 = fmaxf(lower ? fmaxf(n0 - (kLowest - old.low), fminf(n0, kDeepest)) : n0, n1 + kAhead);
                             const float d1 = fminf(7.0f - n1, -kNoRef);
                             ref[r0 + slot].m = m1;
                             ref[r0 + slot].d = d1;
+                            ref[r0 + slot].low = fmaxf(old.low - (n1 - n0), 0.0f);     // (no references before: 0)
                             less[slot] = make_float2(exp2_hw(old.m - m1), exp2_hw((old.m - m1) + (d1 - old.d)));
                         }
                         group_sync(1 + wg, 128);
