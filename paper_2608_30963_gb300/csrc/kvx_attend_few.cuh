@@ -194,6 +194,7 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
     extern __shared__ __align__(1024) uint8_t smem[];
     const uint32_t s0 = smem_u32(smem);
     constexpr int kFull = 0, kEmpty = C::STAGES, kS = 2 * C::STAGES, kP = kS + 2, kO = kP + 2, kFree = kO + 2, kScale = kFree + 2, kQ = kScale + C::TURNS, kDone = kQ + 1;
+    static_assert(8 * (kDone + 1) <= 512);
     auto bar = [&](int i) { return s0 + (uint32_t)i * 8; };
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + 512);
     int* abort = reinterpret_cast<int*>(smem + 516);

@@ -121,6 +121,8 @@ __global__ void __launch_bounds__(TcShape<D, NT, SRC == kCodes>::THREADS, 1)
 {
     using C = TcShape<D, NT, SRC == kCodes>;
     using B = Bars<C::STAGES>;
+    // the barriers end before the scales of an 8-bit cache's units, or the flags at 512
+    static_assert(8 * B::count <= (SRC == kCodes && C::COLS ? C::SCALES : 512));
     constexpr int BM = C::BM, BN = C::BN;
     extern __shared__ __align__(1024) uint8_t smem[];
     const uint32_t s0 = smem_u32(smem);
@@ -184,8 +186,7 @@ __global__ void __launch_bounds__(TcShape<D, NT, SRC == kCodes>::THREADS, 1)
             constexpr int CPR = D / 16, RPI = 32 / CPR, UNITS = C::UNITS;      // 16-code chunks of a row; rows of an instruction
             const int sub = lane / CPR, chunk = lane % CPR;
             const uint32_t sRaw = sT + C::STAGES * C::TILE;
-            static_assert(C::COLS ? 8 * (2 * C::STAGES + 19) <= C::SCALES && C::SCALES + C::RAW_STAGES * C::RU <= 512
-                                  : C::SCALES + C::RAW_STAGES * C::RU <= C::CTRL);
+            static_assert(C::SCALES + C::RAW_STAGES * C::RU <= (C::COLS ? 512 : C::CTRL));
             uint32_t pos = 0, items = 0;                 // units and items begun
             bool ok = true;
             auto wait = [&](int b, uint32_t parity) { ok = __all_sync(0xffffffffu, ok && W.wait(bar(b), parity)); };

@@ -151,7 +151,8 @@ __device__ __forceinline__ float2 mul2(float2 a, float2 b)
 // Barriers (8 bytes each) in the control block.
 template <int STAGES> struct Bars {
     static constexpr int full = 0, empty = STAGES, sfull = 2 * STAGES, pfull = sfull + 2, ofull = pfull + 2, qfull = ofull + 2,
-                         qempty = qfull + 1, done = qempty + 1, mlfull = done + 1, mlempty = mlfull + 1, added = mlempty + 1, raw_full = added + 1, raw_empty = raw_full + 4;
+                         qempty = qfull + 1, done = qempty + 1, mlfull = done + 1, mlempty = mlfull + 1, added = mlempty + 1, raw_full = added + 1, raw_empty = raw_full + 4,
+                         count = raw_empty + 4;
 };
 // Tensor copy of a box, completing on an mbarrier.
 __device__ __forceinline__ void tma_box3(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t mbar)
