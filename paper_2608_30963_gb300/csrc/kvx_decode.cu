@@ -222,6 +222,25 @@ kvx_status attend(kvx_decoder* dec, const char* who, const kvx_new_tokens* tok, 
     return KVX_OK;
 }
 
+// Whether a pointer of one cache's first L layers is one of the other's: what the host sees of caches that overlap (views may lie
+// between one another, so their extents say nothing).
+bool share_a_pointer(const kvx_dst_kv* full, const kvx_quantised_kv* codes, int L)
+{
+    constexpr unsigned SIZE = 4 * KVX_MAX_TARGET_LAYERS;     // at most half of it is taken
+    const void* table[SIZE] = {};
+    auto place = [&](const void* p) {
+        unsigned i = (unsigned)(((uint64_t)(uintptr_t)p * 0x9e3779b97f4a7c15ull) >> 32) % SIZE;
+        while (table[i] && table[i] != p) i = (i + 1) % SIZE;
+        return i;
+    };
+    for (int l = 0; l < L; ++l)
+        for (const void* p : {(const void*)full->k[l], (const void*)full->v[l]}) table[place(p)] = p;
+    for (int l = 0; l < L; ++l)
+        for (const void* p : {(const void*)codes->codes.k[l], (const void*)codes->codes.v[l], (const void*)codes->k_scale[l], (const void*)codes->v_scale[l]})
+            if (table[place(p)]) return true;
+    return false;
+}
+
 // kvx_quantise and kvx_dequantise.
 kvx_status convert(kvx_decoder* dec, const char* who, int batch, int L, const int32_t* kv_len, const kvx_dst_kv* full, const char* full_name,
                    const kvx_quantised_kv* codes, const char* codes_name, bool to_codes, void* stream)
@@ -237,12 +256,11 @@ kvx_status convert(kvx_decoder* dec, const char* who, int batch, int L, const in
     kvx_status st;
     if ((st = make_view(dec, who, full_name, full, 0, L, P.full)) || (st = make_code_view(dec, who, codes_name, codes, 0, L, P.codes, P.scales)))
         return st;
+    if (share_a_pointer(full, codes, L)) return fail(KVX_ERR_INVALID_ARG, "%s: the caches have a pointer in common", who);
     P.L = L; P.batch = batch; P.H = dec->desc.model.num_kv_heads; P.d = dec->desc.model.head_dim;
     P.kv_len = kv_len;
     P.status = dec->status;
     for (int l = 0; l < L; ++l) {
-        if (full->k[l] == codes->codes.k[l] || full->v[l] == codes->codes.v[l])
-            return fail(KVX_ERR_INVALID_ARG, "%s: the caches are the same memory (layer %d)", who, l);
         P.full_k[l] = full->k[l]; P.full_v[l] = full->v[l];
         P.code_k[l] = codes->codes.k[l]; P.code_v[l] = codes->codes.v[l];
         P.k_scale[l] = codes->k_scale[l]; P.v_scale[l] = codes->v_scale[l];
