@@ -807,8 +807,8 @@ class Decoder:
         B, L = kv_len.shape[0], len(src[0])
         if not self._index(kv_len, B):
             raise ValueError("kv_len must be contiguous int32 [B]")
-        if L < 1 or len(dst[0]) != L:
-            raise ValueError("the caches must have as many layers as one another, one or more")
+        if L < 1 or any(len(x) != L for x in (*src, *dst)):
+            raise ValueError("the caches must have as many layers as one another, one or more, in every list")
         least = B if B <= KVX_MAX_ATTEND_BATCH else 0
         a, _keep_a = (self._full_layers if len(src) == 2 else self._code_layers)(*src, least, table, page_size, pages)
         b, _keep_b = (self._full_layers if len(dst) == 2 else self._code_layers)(*dst, least, dst_table, page_size, dst_pages)

@@ -1,4 +1,4 @@
-"""Conversions into one's own memory are refused, whichever of a cache's pointers is in both."""
+"""Conversions refuse one's own memory, whichever of a cache's pointers is in both, and lists of other lengths."""
 import pytest
 import torch
 
@@ -35,3 +35,20 @@ def test_caches_that_share_memory(L):
                         call()
                     assert e.value.status == kvx.KVX_ERR_INVALID_ARG and "in common" in str(e.value) and dec.launches() == 0
     assert dec.device_status() == 0 and all(bool((x == 1).all()) for y in full for x in y)
+
+
+def test_lists_of_other_lengths():
+    full, held = caches(2)
+    dec = kvx.Decoder(synth.ModelGeom(2, 2, 128, 1e4), 4)
+    n = i32([64])
+    for which in range(6):
+        for short in (0, 1):
+            lists = [*full, *held]
+            lists[which] = lists[which][:short]
+            with pytest.raises(ValueError):
+                dec.quantise(n, *lists)
+            with pytest.raises(ValueError):
+                dec.dequantise(n, *lists[2:], *lists[:2])
+    with pytest.raises(ValueError):
+        dec.quantise(n, *([] for _ in range(6)))
+    assert dec.device_status() == 0
