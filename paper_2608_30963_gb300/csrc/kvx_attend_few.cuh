@@ -524,8 +524,10 @@ __global__ void __launch_bounds__(512, 1) attend_few_kernel(const __grid_constan
 #pragma unroll
                 for (int h = 0; h < HB; ++h) {
                     const uint8_t* from = smem + C::SMEM - C::SCALES + (gu % C::TURNS) * 2 * BN + h * 128 + slot;
-                    const unsigned vs = from[BN];
-                    kf[h] = scale_of(from[0]);
+                    const unsigned ks = from[0], vs = from[BN];
+                    // (an infinite scale: a product of either sign and an infinity is among the sum's, or 0 times one, so the score
+                    // is NaN; the codes' sum alone would give it a sign)
+                    kf[h] = __uint_as_float(ks == 255u ? 0x7fffffffu : ks << 23);
                     vz[h] = vs == 0u ? -INFINITY : vs == 255u ? INFINITY : (float)((int)vs - 127);
                 }
                 const int j0 = g.kv.at(g.i0 + u) * BN, j = j0 + slot;
