@@ -1,8 +1,11 @@
 """Where prompts over an 8-bit cache change kernels: from more than 1536 rows a sequence and KV head on (heads of 256: 512) the slots become
 bf16 in the workspace first, a launch more, if the cache may fit there; capped scores of heads of 128 never do."""
-import pytest
+import math
 
-from test_gpu_quantised import Problem
+import pytest
+import torch
+
+from test_gpu_quantised import Problem, check, check_lse, value
 from test_gpu_quantised_paths import run, wide
 
 pytestmark = pytest.mark.gpu
@@ -27,6 +30,27 @@ def test_a_table_one_page_too_wide(d, G, new):
         assert p.dec.launches() == launches
 
 
+def floor(p, window, prefix):
+    """What few rows' weights may be off by besides their relative bound, in the outputs' channels.  The last of a weight's three
+    terms ends at 2^-23 of the largest weight times its V row's scale, c; so each slot that is seen may be off by 2^-23 c times its code.
+    Codes are at most 448 and a row's largest code is above 224, so c times a code is at most twice the largest contribution (weight
+    times the V row's largest): 2^-22 of that for every slot seen.  It shows in channels where the row that has nearly all the weight is nearly zero."""
+    K, V = (value(c, s).double() for c, s in zip(p.code, p.byte))
+    out = torch.zeros(p.T, p.H * p.G, 1, dtype=torch.float64)
+    for b, n in enumerate(p.new):
+        L = p.L[b]
+        i, j = torch.arange(L - n, L)[:, None], torch.arange(L)
+        seen = (j <= i) & ((i - j < window) if window else True)
+        if prefix is not None:
+            seen = seen | (j < prefix[b])
+        for head in range(p.H * p.G if n else 0):
+            x = p.q[p.off[b]:p.off[b + 1], head].double() @ K[b, head // p.G, :L].T * p.scale
+            x = p.cap * torch.tanh(x / p.cap) if p.cap else x
+            w = torch.softmax(x.masked_fill(~seen, -math.inf), -1)
+            out[p.off[b]:p.off[b + 1], head, 0] = 2.0 ** -22 * seen.sum(1) * (w * V[b, head // p.G, :L].abs().amax(-1)).amax(1)
+    return out
+
+
 @pytest.mark.parametrize("d,G,long,singles", [(128, 4, 300, 60), (128, 2, 200, 40), (256, 4, 300, 60), (256, 2, 100, 33), (128, 7, 25, 50), (64, 4, 200, 30)])
 @pytest.mark.parametrize("opt", ["plain", "window_prefix", "capped"])
 def test_a_prompt_among_single_tokens(d, G, long, singles, opt):
@@ -35,5 +59,10 @@ def test_a_prompt_among_single_tokens(d, G, long, singles, opt):
     ctx = [900, 5, 0] + [37 * i % 700 for i in range(singles)]
     new = [0, long, 0] + [1] * singles
     p = Problem(2, G, d, ctx, new, "bf16", 16, seed=d + long, cap=20.0 if opt == "capped" else 0.0)
-    run(p, *((90, [3 * i % 130 for i in range(len(new))]) if opt == "window_prefix" else (0, None)))
-    assert p.dec.launches() == 2
+    window, prefix = (90, [3 * i % 130 for i in range(len(new))]) if opt == "window_prefix" else (0, None)
+    out, lse = p.attend(window, prefix)
+    assert p.dec.launches() == 2 and p.dec.device_status() == 0
+    eo, el, to, tl = p.exact(window, prefix)
+    check(out, eo, to + (floor(p, window, prefix) if d > 64 else 0.0), "out")
+    check_lse(lse, el, tl)
+    assert torch.equal(p.attend(window, prefix, lse=False)[0], out), "equal calls give equal bits"
