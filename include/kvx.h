@@ -411,8 +411,8 @@ typedef struct {
 } kvx_decoder_desc;
 
 /* Checks the description and allocates what the calls below need on the current device: rotation
- * frequencies, a status word and the workspace of kvx_attend (partial results of split rows, kept
- * scores: 88, 108 or 147 MB for heads of 64, 128 or 256, whatever the lengths).  Synchronous.  On success *out owns device memory until kvx_decoder_destroy. */
+ * frequencies, a status word and the workspace of kvx_attend and kvx_attend_quantised (partial results of split rows; kept
+ * scores, or a prompt's 8-bit slots as bf16: 88, 108 or 147 MB for heads of 64, 128 or 256, whatever the lengths).  Synchronous.  On success *out owns device memory until kvx_decoder_destroy. */
 KVX_API kvx_status kvx_decoder_create(const kvx_decoder_desc* desc, kvx_decoder** out);
 
 /* Free the decoder's device memory.  Synchronises the device first.  NULL is accepted. */
@@ -511,7 +511,8 @@ KVX_API kvx_status kvx_evict(kvx_decoder* dec, const kvx_evict_plan* plan, const
  * a power of two:  value = code * 2^(s - 127)  (s = 0 stands for a scale of 0, 255 for infinity, so that memory filled with
  * zeros reads as zeros).  A row x is quantised as
  *   s = the smallest scale in [10, 247] with max |x| <= 448 * 2^(s - 127),  code = x / 2^(s - 127) to nearest even
- * which leaves each value within 2^-4 of itself (2^-16 of the row's largest near zero).  Every value such a row stands for is
+ * which leaves each value within 2^-4 of itself or 2^-17 of the row's largest, whichever is more (rows whose largest is below
+ * 224 * 2^-117, where the scale ends: 2^-4 of itself or 2^-127).  Every value such a row stands for is
  * exact in bf16 and fp32.  Values that are not finite have no say in the scale and become NaN; magnitudes above
  * 1.875 * 2^127 are taken as that. */
 typedef struct {
@@ -528,7 +529,10 @@ KVX_API kvx_status kvx_append_quantised(kvx_decoder* dec, const kvx_new_tokens* 
                                         void* stream);
 
 /* As kvx_attend, over a cache held in 8 bits: K_h[j] and V_h[j] are the values that its rows stand for.  No weight sums: opts'
- * key_weight must be NULL (KVX_ERR_UNSUPPORTED). */
+ * key_weight must be NULL (KVX_ERR_UNSUPPORTED).  (bf16 queries: attention weights are rounded as over a bf16 cache; in calls of up to
+ * 32 rows, tokens times query heads a KV head, in the sequences' mean, of heads of 128 and 256, the cache's codes are multiplied as they
+ * are: by queries in two e4m3 terms, which hold a channel's 8 bits down to 2^-14 of the row's largest, and by weights in three, within
+ * 2^-12 of themselves or 2^-23 of the largest weight, V's scales taken into them.) */
 KVX_API kvx_status kvx_attend_quantised(kvx_decoder* dec, const kvx_new_tokens* tok, const kvx_rows* q, const kvx_quantised_kv* cache,
                                         int32_t layer, const kvx_attend_opts* opts, const kvx_rows* out, void* stream);
 

@@ -17,12 +17,13 @@
 //                       of the warpgroup, down as well as up; each has its own references, sums and O, joined at the end.
 // The last rows of the split work are joined as those of the other attention kernels.
 //
-// What bounds it.  8 rows: the reading of K and V, about 8000 clocks behind it the first time: a token of each of eight sequences over up
-// to 32768 slots, 7 query heads on each of 4 KV heads of 128, 207 MB, 47 us, 4.4 TB/s (the loop runs at a copy's rate; 5 us are the plan and the
-// first reads, 4 the join).  16 and 32 rows: the softmax warps (two exponentials
-// and three terms a weight): 4 tokens of 8 query heads on each of 8 KV heads over up to 16384 slots of four sequences, 111 MB, 56 us;
-// 44% of the schedulers' slots are used, and for each instruction issued a warp waits 1.4 at barriers and 1.0 for code to
-// arrive.  (32 rows, four sequences of 16384 slots, 63 us: with four softmax warpgroups, two on a tile's rows, 69; with references agreed on
+// What bounds it.  8 rows: the reading of K and V.  Long ranges run at a copy's rate (a token of each of 38 sequences over 65001 slots, 7
+// query heads on each of 4 KV heads of 128, 2.55 GB, 378 us, 6.7 TB/s); where a CTA has some twenty tiles what comes before and
+// after them shows (eight sequences of up to 32768 slots, 207 MB, 47 us, 4.4 TB/s: 31 us at that rate, 16 the plan, the first reads,
+// the ends and the join).  16 and 32 rows: the softmax warps (two exponentials
+// and three terms a weight): 4 tokens of 8 query heads on each of 8 KV heads over up to 16384 slots of four sequences, 111 MB, 56 us, over
+// 32000 slots of 19, 1.26 GB, 256 us, 4.9 TB/s; the schedulers issue in 34% of a launch's clocks, and for each instruction issued a
+// warp waits 1.4 at barriers and 1.0 for code to arrive.  (32 rows, four sequences of 16384 slots, 63 us: with four softmax warpgroups, two on a tile's rows, 69; with references agreed on
 // while the weights are taken, 79; with one exponential, times a factor, for the two, no less.)  Short calls: latency,
 // 12 us from launch to end.  (The first case with 128 slots a tile and the scales read by the softmax threads, whose reads take as long
 // as the copies on their way, 54 us; with P stored byte by byte, 57; with the rows' ends unrolled, a code that is always

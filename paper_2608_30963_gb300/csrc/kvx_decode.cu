@@ -20,7 +20,7 @@ struct kvx_decoder {
     float* part_o = nullptr;               // partial results of split attention rows (kvx_decode.cuh)
     float2* part_ml = nullptr;
     SplitItem* split = nullptr;
-    float* scores = nullptr;               // scores kept for the weight sums
+    float* scores = nullptr;               // scores kept for the weight sums, or a prompt's 8-bit slots as bf16
 };
 
 namespace {

@@ -118,7 +118,8 @@ struct AttendParams {
     float* part_o;        // [2 * grid][BM][d]
     float2* part_ml;      // [2 * grid][BM]: running maximum (log2 units) and sum
     SplitItem* split;     // [grid]
-    // scores of few rows, kept for the weight sums (log2 units): [T][Hq][scores_stride], or NULL
+    // scores of few rows, kept for the weight sums (log2 units): [T][Hq][scores_stride], or NULL.  The same memory holds a prompt's
+    // slots of an 8-bit cache as bf16 rows (launch_attend_codes; no weight sums there).
     float* scores;
     long long scores_stride;
     // an 8-bit cache's scales; NULL: ck and cv are of the decoder's type
@@ -145,7 +146,8 @@ cudaError_t launch_evict(const EvictParams& P, int dtype, int num_sms, cudaStrea
 
 // Workspace of split rows: rows of partial results (2 x grid x BM, so grids stay within it) and split items.
 constexpr int kAttendMaxRows = 2 * 152 * 4 * 64;
-constexpr long long kAttendScores = 16ll << 20;   // floats of kept scores: eight sequences of 64K, 32 query heads
+// Floats of kept scores: eight sequences of 64K, 32 query heads; or 64 MiB of an 8-bit cache's slots as bf16.
+constexpr long long kAttendScores = 16ll << 20;
 constexpr int kAttendMaxCtas = kAttendMaxRows / 2 / 16;
 cudaError_t launch_sum_scores(const AttendParams& P, cudaStream_t stream);
 cudaError_t launch_key_weight(const AttendParams& P, int num_sms, cudaStream_t stream);
@@ -404,7 +406,7 @@ __device__ __forceinline__ Parts item_parts(const Plan& p, const Segment& g)
 }
 
 // Base-2 exponential of the hardware (2 ulp).  The argument is at most 0, but for the weights of the tensor-core attention:
-// there a row's maximum may stay behind by up to 8.
+// there a row's maximum may stay behind by up to 8, and over 8-bit caches a few rows' by up to 64.
 __device__ __forceinline__ float exp2_hw(float x)
 {
     float y;
