@@ -58,3 +58,34 @@ def test_infinite_queries(d, G, ctx, new, cap, dtype, kind):
     assert bool(out[bad].isnan().all()) and bool((lse[bad].isnan()).all())
     check(out[~bad], eo[~bad], to[~bad], "out")
     check_lse(lse[~bad], el[~bad], tl[~bad])
+
+
+@pytest.mark.parametrize("d,G,ctx,new,page", [(128, 4, [6000], [2], 16), (256, 2, [3000, 40], [3, 2], 7), (128, 8, [700, 5, 0], [4, 2, 3], 0), (64, 4, [900], [60], 16)])
+@pytest.mark.parametrize("window,prefix", [(500, None), (300, 900), (0, 70), (1, 0)])
+def test_infinite_queries_masks(d, G, ctx, new, page, window, prefix):
+    """Each slot that a mask leaves counts once, in whole rows and split ones; tokens that see nothing give zeros.  Capped."""
+    cap, blind = 20.0, 1 if prefix is None else 0
+    L = [c + n for c, n in zip(ctx, new)]
+    L[-1] = max(0, new[-1] - 1) if blind and ctx[-1] == 0 else L[-1]
+    p = Problem(2, G, d, ctx, new, "bf16", page, seed=d + window, cap=cap, kv_len=L)
+    p.q[:, 1, 5] = math.inf
+    p.code[0][..., 5] = 0x3b | (torch.randint(0, 2, p.code[0].shape[:-1], generator=torch.Generator().manual_seed(2)) << 7).to(torch.uint8)
+    p.byte[0].clamp_(max=160)
+    pre = None if prefix is None else [prefix] * len(new)
+    eo, el, to, tl = p.exact(window, pre)
+    K, V = (value(c, s).double() for c, s in zip(p.code, p.byte))
+    for b, n in enumerate(new):
+        r, i, j = slice(int(p.off[b]), int(p.off[b + 1])), torch.arange(L[b] - n, L[b])[:, None], torch.arange(L[b])
+        seen = (j <= i) & ((i - j < window) if window else True)
+        seen = seen | (j < prefix) if prefix is not None else seen
+        x = (cap * torch.sign(p.q[r, 1, 5].double()[:, None] * K[b, 0, :L[b], 5])).masked_fill(~seen, -math.inf)
+        w = torch.exp(x - cap)
+        share, v, e = w / w.sum(1, keepdim=True).clamp(min=1e-300), V[b, 0, :L[b]], 24 * U * cap
+        eo[r, 1] = share @ v
+        to[r, 1] = 1.05 * (2 * e + 2.0 ** -20 + 2.0 ** -8 + 6 * math.sqrt(max(L[b], 1)) * U) * (share @ v.abs()) + 2.0 ** -8 * 1.01 * eo[r, 1].abs() + 1e-30
+        el[r, 1] = torch.logsumexp(x, 1) if L[b] else -math.inf
+        tl[r, 1] = e + 2.0 ** -20 + 2.0 ** -22 * el[r, 1].abs()
+    out, lse = p.attend(window, pre)
+    check(out, eo, to, "out")
+    check_lse(lse, el, tl)
+    assert p.dec.device_status() == 0

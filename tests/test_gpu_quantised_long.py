@@ -87,3 +87,23 @@ def test_long_ranges(d, G, new, kind):
     floor = (2.0 ** -23 * 2 * part.topk(-(-n // 8192), -1)[0].sum(-1) * 8192).cpu()
     check(out.cpu(), eo, to + floor[..., None], "out")
     check_lse(lse.cpu(), el, tl)
+
+
+@pytest.mark.parametrize("d,G,new", [(128, 7, 1), (256, 8, 4)])
+@pytest.mark.parametrize("byte", [10, 24, 30, 60, 200, 240])
+def test_a_tail_under_far_scales(d, G, new, byte):
+    """As above, V's rows under scales from 2^-117 to 2^113: references have to stay where their powers are numbers.  Below 2^-100 they do not
+    follow the weights down, and the tail may be lost; the large weight's row never is."""
+    n = 200000
+    code = [torch.zeros((n, d), dtype=torch.uint8, device="cuda"), torch.full((n, d), 0x38, dtype=torch.uint8, device="cuda")]
+    scales = [torch.full((n,), x, dtype=torch.uint8, device="cuda") for x in (127, byte)]
+    code[0][5] = 0x38
+    dec = kvx.Decoder(synth.ModelGeom(1, 1, d, 1e4), G)
+    q = torch.full((new, G, d), 23.6 * math.log(2.0) / math.sqrt(d), device="cuda").bfloat16()
+    out, lse = attend(dec, q, code, scales, n)
+    one = 2.0 ** (byte - 127)
+    score = float(q[0, 0].double().sum()) / math.sqrt(d)
+    share = math.exp(score) / (math.exp(score) + n)
+    tol = 2.0 ** -8 + 2.0 ** -12 + 2 * 2.0 ** -10 * share + (1 - share if byte < 31 else 0.0)
+    assert float((out.double() / one - 1.0).abs().max()) <= tol
+    assert float((lse.double() - math.log(math.exp(score) + n - new)).abs().max()) <= 1e-4
